@@ -513,6 +513,162 @@ int32_t wg_decode_step_host(wg_ctx *ctx, const int32_t *gid, int32_t *sid, int32
                             int64_t mask_stride_words, int32_t *token_dev, int32_t *token_host,
                             int32_t *status, uint32_t flags, void *stream);
 
+/* ---- constrained beam search -------------------------------------------------------- *
+ * The paper masks logits before a token is chosen (Sections 1 and 2); its evaluation decodes one
+ * hypothesis per request.  These calls choose the hypotheses of a beam search under the same
+ * masks.  Row i = r * n_beam + b is beam b of request r, everywhere.
+ *
+ * Selection.  With x the row's logits, A its allowed tokens and `score` the row's running score:
+ *   lse        = log sum of exp(x[t]) over t in A          (WG_BEAM_NORM_ALLOWED)
+ *                log sum of exp(x[t]) over the vocabulary  (WG_BEAM_NORM_FULL)
+ *                0, the logits are log-probabilities       (WG_BEAM_NORM_NONE)
+ *   s(b, t)    = score + (x[t] - lse), t in A, in fp32 (the sum of the exponentials too)
+ * A finished row offers one candidate, its EOS token at its score as it stands.  Candidates are
+ * those with s > -inf (NaN is none: a NaN among the logits that lse covers, or a +inf, leaves the row
+ * without candidates).  Per request the n_out best candidates are returned, best first; equal
+ * scores (-0.0 equals 0.0) go to the lower b * V + t.  Where there are fewer, the rest is
+ * score -inf, parent -1, token -1. */
+enum { WG_BEAM_NORM_ALLOWED = 0, WG_BEAM_NORM_FULL = 1, WG_BEAM_NORM_NONE = 2 };
+#define WG_BEAM_MAX_BEAMS 32
+#define WG_BEAM_MAX_OUT 64
+
+/* Scratch of the selection (about 4 bytes per 256 tokens and row), on the current device.  Calls
+ * that share a wg_beam are issued like calls that share a wg_ctx: one at a time, on one stream or on
+ * streams ordered by events.
+ *   V             vocabulary size of every call
+ *   max_requests  1 <= max_requests, max_requests * max_beams <= WG_MAX_ROWS
+ *   max_beams     1 .. WG_BEAM_MAX_BEAMS;  V * max_beams < 2^32
+ *   max_out       1 .. WG_BEAM_MAX_OUT
+ * Errors: WG_ERR_ARG, WG_ERR_CUDA. */
+typedef struct wg_beam wg_beam;
+int32_t wg_beam_create(int32_t V, int32_t max_requests, int32_t max_beams, int32_t max_out,
+                       wg_beam **out);
+void wg_beam_free(wg_beam *beam);
+
+/* One selection.
+ *   logits      device, n_req * n_beam rows as in wg_apply_mask; read only
+ *   bitmask     device, packed masks as written by wg_build_masks, or NULL: everything is allowed.
+ *               Bits at and beyond V are ignored.
+ *   score       device, n_req * n_beam running scores; -inf marks a row without a hypothesis
+ *               (it is not read further: the beams of a first step but one)
+ *   finished    device, n_req * n_beam, non-zero = finished, or NULL: none is
+ *   eos_id      0 <= eos_id < V (not looked at when finished is NULL)
+ *   n_out       1 .. max_out, the same for all requests
+ *   score_out, parent_out, token_out   device, n_req rows of n_out entries.  parent_out is the beam
+ *               within the request.  score_out may be `score` itself when n_out == n_beam.
+ * Any alignment of rows is taken at full speed. */
+int32_t wg_beam_select(wg_beam *beam, const void *logits, int32_t dtype, int64_t row_stride_elems,
+                       const uint32_t *bitmask, int64_t mask_stride_words, const float *score,
+                       const int32_t *finished, int32_t eos_id, int32_t n_req, int32_t n_beam,
+                       int32_t n_out, int32_t norm, float *score_out, int32_t *parent_out,
+                       int32_t *token_out, void *stream);
+
+/* One whole decode step of a beam search under grammars: the masks of the rows' states from the
+ * cache (missing ones are built and inserted, as in wg_decode_step), the selection with
+ * n_out = n_beam, and the states after it: row j of a request takes its parent's grammar and the
+ * state its parent reaches on the chosen token.  A row in the DONE state is a finished one.  The
+ * logits are not written.
+ *   gid, sid, score   device, n_req * n_beam, updated in place
+ *   bitmask     device, n_req * n_beam rows of W words: where masks go that the cache has no room
+ *               for; its contents are not defined afterwards
+ *   parent_out, token_out  device, n_req * n_beam (-1 for a row without a candidate: its grammar
+ *               and state stay what they were, its score is -inf)
+ *   status      device, n_req * n_beam, or NULL: WG_OK, WG_ERR_EMPTY_MASK (no candidate was left
+ *               for the row; counted in empty_masks)
+ *   flags       WG_USE_CACHE or WG_NO_CACHE
+ * The wg_beam's V must be the vocabulary's, and n_req * n_beam at most the context's max_batch.
+ * Not after a wg_decode_step_shard on a slice (see there). */
+int32_t wg_beam_step(wg_beam *beam, wg_ctx *ctx, int32_t *gid, int32_t *sid, float *score,
+                     int32_t n_req, int32_t n_beam, const void *logits, int32_t dtype,
+                     int64_t row_stride_elems, uint32_t *bitmask, int64_t mask_stride_words,
+                     int32_t norm, int32_t *parent_out, int32_t *token_out, int32_t *status,
+                     uint32_t flags, void *stream);
+
+/* The hypotheses of a search read back: out[r, j, :] is the token sequence of final beam j, found
+ * by following the parents from the last step to the first.
+ *   token, parent  device, n_steps x n_req x n_beam, as the steps returned them
+ *   out            device, n_req x n_beam x n_steps
+ * A beam whose way back meets a parent outside 0 .. n_beam - 1 has no sequence: its row is -1.
+ * n_req <= WG_MAX_ROWS, n_beam <= WG_BEAM_MAX_BEAMS; n_steps = 0 does nothing. */
+int32_t wg_beam_backtrack(const int32_t *token, const int32_t *parent, int32_t n_steps,
+                          int32_t n_req, int32_t n_beam, int32_t *out, void *stream);
+
+/* ---- block tables of a paged cache -------------------------------------------------- *
+ * What moves beside the automaton states when hypotheses are kept, shared and dropped: the
+ * model's key / value cache, held in blocks of `block_size` tokens.  Sequence s has a length len[s] and
+ * a row of block ids; token p of it lives in slot table[s, p / block_size] * block_size +
+ * p % block_size.  Entries from ceil(len[s] / block_size) on are -1.  Blocks are counted: a block
+ * that no row names is free.  Whenever blocks are taken, the lowest-numbered free ones are
+ * taken, for the lowest sequences first, so results do not depend on the order in which the GPU runs.
+ *
+ * A wg_kv_pool holds the counts and scratch for calls with up to max_seqs sequences.  Calls on one
+ * pool must be issued from one thread at a time and on one stream at a time (or on streams ordered
+ * by events).  All blocks are free at first.  Errors: WG_ERR_ARG (n_blocks < 1, block_size < 1,
+ * max_seqs < 1 or > WG_MAX_ROWS), WG_ERR_CUDA. */
+typedef struct wg_kv_pool wg_kv_pool;
+int32_t wg_kv_pool_create(int32_t n_blocks, int32_t block_size, int32_t max_seqs, wg_kv_pool **out);
+void wg_kv_pool_free(wg_kv_pool *pool);
+
+/* Device array of n_blocks counts: how many table rows name the block.  Read only. */
+const int32_t *wg_kv_pool_refs(const wg_kv_pool *pool);
+/* Sets the counts (device, n_blocks, >= 0; negative ones count as 0), e.g. from a saved state. */
+int32_t wg_kv_pool_load(wg_kv_pool *pool, const int32_t *refs, void *stream);
+/* The number of free blocks.  Synchronises `stream`. */
+int32_t wg_kv_pool_n_free(wg_kv_pool *pool, int32_t *n_free, void *stream);
+
+/* Room for new tokens: sequence s goes from len[s] to len[s] + n_new[s] tokens.
+ *   table       device, n_seq rows of max_blocks entries, table_stride apart; updated in place
+ *   len         device, n_seq, updated in place
+ *   n_new       device, n_seq, >= 0
+ *   cu          device, n_seq + 1: where each sequence's tokens begin in the arrays below
+ *   slot, pos, seq  device, n_tokens entries each: the slot, the position within its sequence and the
+ *               sequence of every token; -1 from cu[n_seq] on
+ *   status      device, n_seq, or NULL: WG_OK; WG_ERR_ARG: n_new < 0, or len outside the table, or
+ *               the sequence would outgrow it (taken as n_new = 0); WG_ERR_CAPACITY: not enough
+ *               free blocks or not enough room in `slot`
+ * Blocks are granted in order: a sequence that needs some is refused when those wanted up to and
+ * including it are more than there are.  A refused sequence keeps its length and table; its tokens
+ * keep their places, with slot -1.  cu is cut off at n_tokens. */
+int32_t wg_kv_extend(wg_kv_pool *pool, int32_t *table, int64_t table_stride, int32_t max_blocks,
+                     int32_t *len, const int32_t *n_new, int32_t n_seq, int32_t *cu, int64_t *slot,
+                     int32_t *pos, int32_t *seq, int32_t n_tokens, int32_t *status, void *stream);
+
+/* Gives tokens back: sequence s is cut to keep[s] tokens (0: it is over; drafted tokens that were
+ * not accepted; ...).  Blocks beyond are counted down, and free when nobody names them any more.
+ * status (or NULL): WG_OK, or WG_ERR_ARG for keep[s] outside 0 .. len[s] or len[s] outside the table
+ * (nothing is changed).  Cutting into a block that other sequences share leaves it shared: such a sequence
+ * must not be extended. */
+int32_t wg_kv_shrink(wg_kv_pool *pool, int32_t *table, int64_t table_stride, int32_t max_blocks,
+                     int32_t *len, const int32_t *keep, int32_t n_seq, int32_t *status,
+                     void *stream);
+
+/* One array of cache data: block b, token i of it at base + (b * block_size + i) * token_bytes.
+ * base and token_bytes are best multiples of 16; others are copied byte by byte. */
+typedef struct wg_kv_plane {
+    void *base;           /* device */
+    int64_t token_bytes;
+} wg_kv_plane;
+
+/* The cache follows a selection: sequence r * n_beam + j becomes a copy of r * n_beam + parent[j].
+ * Full blocks are shared between the children of a parent.  A partly filled last block goes to the
+ * parent's first child; every further child gets a block of its own, into which the filled tokens
+ * are copied in all planes.  Blocks that nobody names any more are free (and may be taken for
+ * those copies).
+ *   parent      device, n_req * n_beam: beam within the request; anything outside 0 .. n_beam - 1
+ *               ends the sequence (length 0)
+ *   table, len  as above, n_seq = n_req * n_beam rows, updated in place
+ *   planes      device array of n_planes entries, or NULL with n_planes = 0 (tables only)
+ *   copy_src, copy_dst  device, n_req * n_beam, or NULL: the block that sequence was copied from /
+ *               to, -1 where nothing was copied
+ *   status      device, n_req * n_beam, or NULL: WG_OK, WG_ERR_CAPACITY (no block left for the copy:
+ *               the sequence keeps its full blocks and its length is cut to them), WG_ERR_ARG (the
+ *               parent's len lay outside the table: the sequence is ended)
+ * n_beam <= WG_BEAM_MAX_BEAMS, n_req * n_beam <= max_seqs. */
+int32_t wg_kv_reorder(wg_kv_pool *pool, int32_t *table, int64_t table_stride, int32_t max_blocks,
+                      int32_t *len, const int32_t *parent, int32_t n_req, int32_t n_beam,
+                      const wg_kv_plane *planes, int32_t n_planes, int32_t *copy_src,
+                      int32_t *copy_dst, int32_t *status, void *stream);
+
 /* ---- diagnostics ------------------------------------------------------------------- */
 
 /* Per-kernel timing for benchmarks.  While enabled, wg_decode_step records CUDA events on the

@@ -32,6 +32,11 @@ WG_NO_CACHE = 1
 WG_RESTART_ON_DONE = 2
 WG_CACHE_DENSE = 0
 WG_CACHE_COMPACT = 1
+WG_BEAM_NORM_ALLOWED = 0
+WG_BEAM_NORM_FULL = 1
+WG_BEAM_NORM_NONE = 2
+WG_BEAM_MAX_BEAMS = 32
+WG_BEAM_MAX_OUT = 64
 WG_ENTRY_ALLOWS = 0
 WG_ENTRY_DENIES = 1
 
@@ -104,6 +109,21 @@ _SIGNATURES = {
     "wg_step_graph_free": (None, [_vp]),
     "wg_decode_step_host": (_i32, [_vp, _vp, _vp, _i32, _vp, _vp, _i32, _i64, _vp, _i64, _vp, _vp,
                                    _vp, _u32, _vp]),
+    "wg_beam_create": (_i32, [_i32, _i32, _i32, _i32, C.POINTER(_vp)]),
+    "wg_beam_free": (None, [_vp]),
+    "wg_beam_select": (_i32, [_vp, _vp, _i32, _i64, _vp, _i64, _vp, _vp, _i32, _i32, _i32, _i32, _i32,
+                              _vp, _vp, _vp, _vp]),
+    "wg_beam_step": (_i32, [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _i32, _i64, _vp, _i64, _i32, _vp,
+                            _vp, _vp, _u32, _vp]),
+    "wg_beam_backtrack": (_i32, [_vp, _vp, _i32, _i32, _i32, _vp, _vp]),
+    "wg_kv_pool_create": (_i32, [_i32, _i32, _i32, C.POINTER(_vp)]),
+    "wg_kv_pool_free": (None, [_vp]),
+    "wg_kv_pool_refs": (_vp, [_vp]),
+    "wg_kv_pool_load": (_i32, [_vp, _vp, _vp]),
+    "wg_kv_pool_n_free": (_i32, [_vp, C.POINTER(_i32), _vp]),
+    "wg_kv_extend": (_i32, [_vp, _vp, _i64, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _i32, _vp, _vp]),
+    "wg_kv_shrink": (_i32, [_vp, _vp, _i64, _i32, _vp, _vp, _i32, _vp, _vp]),
+    "wg_kv_reorder": (_i32, [_vp, _vp, _i64, _i32, _vp, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _vp]),
     "wg_ctx_set_timing": (_i32, [_vp, _i32]),
     "wg_ctx_get_timing": (_i32, [_vp, C.POINTER(C.c_double), C.POINTER(C.c_double),
                                  C.POINTER(_i64)]),
@@ -686,3 +706,279 @@ def wg_decode_step_host(ctx: Context, gid, sid, logits_host, logits_dev, bitmask
         ctx.handle, g, s, B, C.c_void_p(logits_host.data_ptr()), lp, dtype, stride, mp, mstride,
         tok, C.c_void_p(token_host.data_ptr()), st, int(flags), _stream_ptr(stream)),
         "wg_decode_step_host")
+
+
+# ---- constrained beam search ---------------------------------------------------------------------
+class Beam:
+    """wg_beam: scratch of the selection for up to ``max_requests`` requests of ``max_beams`` beams."""
+
+    def __init__(self, V: int, max_requests: int, max_beams: int, max_out: Optional[int] = None):
+        import torch
+        self.V, self.max_requests, self.max_beams = int(V), int(max_requests), int(max_beams)
+        self.max_out = int(max_beams if max_out is None else max_out)
+        self.device = torch.cuda.current_device()
+        h = _vp()
+        _check(_lib.wg_beam_create(self.V, self.max_requests, self.max_beams, self.max_out, C.byref(h)),
+               "wg_beam_create")
+        self.handle = h
+
+    def close(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.wg_beam_free(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        self.close()
+
+
+def _beam_rows(n_beam: int, rows: int):
+    n_beam = int(n_beam)
+    if n_beam < 1 or rows < 1 or rows % n_beam:
+        raise ValueError(f"{rows} rows are no whole number of requests of {n_beam} beams")
+    return rows // n_beam, n_beam
+
+
+def _beam_out(t, n_req: int, dtype, what: str, device):
+    """(pointer, entries per request) of a contiguous [n_req, n_out] output."""
+    p = _dev_ptr(t, dtype, what, device)
+    if t.dim() != 2 or not t.is_contiguous() or t.shape[0] != n_req:
+        raise ValueError(f"{what} must be a contiguous tensor of {n_req} rows")
+    return p, int(t.shape[1])
+
+
+class BeamPlan:
+    """A wg_beam_select call with everything but the logits marshalled once (see ``StepPlan``).
+
+    ``score`` (and ``finished``) hold one entry per row, ``score_out``, ``parent_out`` and ``token_out``
+    are ``[n_req, n_out]``; the arrays are kept and read or written by every call.  Without ``stream``
+    a call goes to the stream that is current when it is made.
+    """
+
+    def __init__(self, beam: Beam, n_beam: int, score, score_out, parent_out, token_out, bitmask=None,
+                 finished=None, eos_id: int = 0, norm: int = WG_BEAM_NORM_ALLOWED, stream=None):
+        import torch
+        self._keep = (beam, score, score_out, parent_out, token_out, bitmask, finished)
+        dev = beam.device
+        rows = int(score.numel())
+        self.n_req, self.n_beam = _beam_rows(n_beam, rows)
+        self.rows, self._V, self._device = rows, beam.V, dev
+        so, n_out = _beam_out(score_out, self.n_req, torch.float32, "score_out", dev)
+        po, n_p = _beam_out(parent_out, self.n_req, torch.int32, "parent_out", dev)
+        to, n_t = _beam_out(token_out, self.n_req, torch.int32, "token_out", dev)
+        if not n_out == n_p == n_t:
+            raise ValueError("score_out, parent_out and token_out disagree on the candidates per request")
+        mask, mstride = (None, 0) if bitmask is None else \
+            _mat(bitmask, rows, (beam.V + 31) // 32, (torch.int32, torch.uint32), "bitmask", dev)
+        if finished is not None and not 0 <= int(eos_id) < beam.V:
+            raise ValueError(f"eos_id {eos_id} is not in the vocabulary")
+        self._head = beam.handle
+        self._tail = (mask, mstride, _vec(score, rows, torch.float32, "score", dev),
+                      _vec(finished, rows, torch.int32, "finished", dev), int(eos_id), self.n_req,
+                      self.n_beam, n_out, int(norm), so, po, to)
+        self._stream = None if stream is None else _stream_ptr(stream)
+        self._dtypes = {torch.bfloat16: WG_DTYPE_BF16, torch.float32: WG_DTYPE_FP32}
+        self._fn = _lib.wg_beam_select
+
+    def __call__(self, logits) -> None:
+        if logits.dim() != 2 or logits.shape[0] != self.rows or logits.shape[1] < self._V \
+                or logits.stride(1) != 1 or not logits.is_cuda or logits.device.index != self._device:
+            raise ValueError("logits must be a tensor [rows, V] with unit inner stride on the beam's device")
+        if logits.dtype not in self._dtypes:
+            raise TypeError(f"logits must be bfloat16 or float32, not {logits.dtype}")
+        rc = self._fn(self._head, logits.data_ptr(), self._dtypes[logits.dtype], logits.stride(0), *self._tail,
+                      self._stream or _stream_ptr(None))
+        if rc != WG_OK:
+            raise WgError(rc, "wg_beam_select")
+
+
+def wg_beam_select(beam: Beam, n_beam: int, logits, score, score_out, parent_out, token_out, bitmask=None,
+                   finished=None, eos_id: int = 0, norm: int = WG_BEAM_NORM_ALLOWED, stream=None) -> None:
+    """One selection: the best candidates of every request over its beams and the vocabulary."""
+    BeamPlan(beam, n_beam, score, score_out, parent_out, token_out, bitmask, finished, eos_id, norm, stream)(logits)
+
+
+def wg_beam_step(beam: Beam, ctx: Context, n_beam: int, gid, sid, score, logits, bitmask, parent_out, token_out,
+                 status=None, norm: int = WG_BEAM_NORM_ALLOWED, flags: int = WG_USE_CACHE, stream=None) -> None:
+    """One decode step of a beam search under grammars: masks, selection, and the rows' grammars, states
+    and scores after it (in place)."""
+    import torch
+    g, s, rows, lp, dtype, stride, mp, mstride, tok, st = _step_args(
+        ctx, gid, sid, logits, ctx.vocab.V, bitmask, token_out, status)
+    if tok is None or parent_out is None:
+        raise ValueError("parent_out and token_out are required")
+    n_req, n_beam = _beam_rows(n_beam, rows)
+    dev = _device_of(ctx)
+    _check(_lib.wg_beam_step(beam.handle, ctx.handle, g, s, _vec(score, rows, torch.float32, "score", dev), n_req,
+                             n_beam, lp, dtype, stride, mp, mstride, int(norm),
+                             _vec(parent_out, rows, torch.int32, "parent_out", dev), tok, st, int(flags),
+                             _stream_ptr(stream)), "wg_beam_step")
+
+
+def wg_beam_backtrack(token, parent, out, stream=None) -> None:
+    """``token``, ``parent``: [n_steps, n_req, n_beam] as the steps returned them; ``out``:
+    [n_req, n_beam, n_steps], the sequence of every final beam."""
+    import torch
+    if token.dim() != 3 or tuple(parent.shape) != tuple(token.shape):
+        raise ValueError("token and parent must be [n_steps, n_req, n_beam]")
+    T, R, K = (int(n) for n in token.shape)
+    dev = token.device.index if token.is_cuda else None
+    if tuple(out.shape) != (R, K, T):
+        raise ValueError(f"out must be [{R}, {K}, {T}]")
+    ptr = []
+    for t, what in ((token, "token"), (parent, "parent"), (out, "out")):
+        ptr.append(_dev_ptr(t, torch.int32, what, dev))
+        if not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous")
+    _check(_lib.wg_beam_backtrack(ptr[0], ptr[1], T, R, K, ptr[2], _stream_ptr(stream)), "wg_beam_backtrack")
+
+
+# ---- block tables of a paged cache ---------------------------------------------------------------
+class _DeviceArray:
+    """A library-owned int32 array for ``torch.as_tensor`` (which makes a view, not a copy)."""
+
+    def __init__(self, ptr: int, n: int):
+        self.__cuda_array_interface__ = {"data": (ptr, False), "shape": (n,), "typestr": "<i4", "version": 2}
+
+
+class KvPool:
+    """wg_kv_pool: the blocks of a paged cache, counted by the table rows that name them."""
+
+    def __init__(self, n_blocks: int, block_size: int, max_seqs: int):
+        import torch
+        self.n_blocks, self.block_size, self.max_seqs = int(n_blocks), int(block_size), int(max_seqs)
+        self.device = torch.cuda.current_device()
+        h = _vp()
+        _check(_lib.wg_kv_pool_create(self.n_blocks, self.block_size, self.max_seqs, C.byref(h)),
+               "wg_kv_pool_create")
+        self.handle = h
+        self._ref = None
+
+    @property
+    def ref(self):
+        """int32 [n_blocks] view of the counts, to be read only; it must not outlive the pool."""
+        if self._ref is None:
+            import torch
+            self._ref = torch.as_tensor(_DeviceArray(_lib.wg_kv_pool_refs(self.handle), self.n_blocks),
+                                        device=f"cuda:{self.device}")
+        return self._ref
+
+    def load(self, ref, stream=None) -> None:
+        """Sets the counts from an int32 device tensor (a saved ``ref``)."""
+        import torch
+        _check(_lib.wg_kv_pool_load(self.handle, _vec(ref, self.n_blocks, torch.int32, "ref", self.device),
+                                    _stream_ptr(stream)), "wg_kv_pool_load")
+
+    def n_free(self, stream=None) -> int:
+        n = _i32()
+        _check(_lib.wg_kv_pool_n_free(self.handle, C.byref(n), _stream_ptr(stream)), "wg_kv_pool_n_free")
+        return n.value
+
+    def close(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            self._ref = None
+            _lib.wg_kv_pool_free(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        self.close()
+
+
+class SlotMap:
+    """Where a step's tokens go: ``cu`` [n_seq + 1], and per token ``slot`` (int64), ``pos`` and ``seq``."""
+
+    def __init__(self, n_seq: int, n_tokens: int, device=None):
+        import torch
+        dev = torch.device("cuda", torch.cuda.current_device() if device is None else int(device))
+        self.n_seq, self.n_tokens, self.device = int(n_seq), int(n_tokens), dev.index
+        self.cu = torch.zeros(self.n_seq + 1, dtype=torch.int32, device=dev)
+        self.slot = torch.full((self.n_tokens,), -1, dtype=torch.int64, device=dev)
+        self.pos = torch.full((self.n_tokens,), -1, dtype=torch.int32, device=dev)
+        self.seq = torch.full((self.n_tokens,), -1, dtype=torch.int32, device=dev)
+        self._args = tuple(C.c_void_p(t.data_ptr()) for t in (self.cu, self.slot, self.pos, self.seq)) \
+            + (self.n_tokens,)
+
+
+class KvPlanes:
+    """The cache arrays that follow a reorder: CUDA tensors ``[n_blocks, block_size, ...]``, contiguous
+    (e.g. the keys and the values of every layer, and their scales)."""
+
+    def __init__(self, planes, block_size: int):
+        import torch
+        self.planes = list(planes)
+        self.block_size = int(block_size)
+        if not self.planes:
+            raise ValueError("no planes")
+        self.device = self.planes[0].device.index
+        self.n_blocks = int(self.planes[0].shape[0])
+        rows = []
+        for i, t in enumerate(self.planes):
+            if not t.is_cuda or t.device.index != self.device:
+                raise ValueError(f"plane {i} is not on cuda:{self.device}")
+            if t.dim() < 2 or not t.is_contiguous() or t.shape[0] != self.n_blocks \
+                    or t.shape[1] != self.block_size:
+                raise ValueError(f"plane {i} must be contiguous [n_blocks, block_size, ...]")
+            rows.append([t.data_ptr(), t.numel() // (self.n_blocks * self.block_size) * t.element_size()])
+        self._table = torch.tensor(rows, dtype=torch.int64).to(f"cuda:{self.device}")
+        self._args = (C.c_void_p(self._table.data_ptr()), len(rows))
+
+
+class KvTables:
+    """Block tables ``table`` [n_seq, max_blocks] and lengths ``lens`` [n_seq] (int32, updated in place)
+    over a pool; ``status`` [n_seq] gets the calls' per-sequence results.  Pointers are taken once: the
+    tensors must stay where they are."""
+
+    def __init__(self, pool: KvPool, table, lens, status=None):
+        import torch
+        dev = pool.device
+        self._keep = (pool, table, lens, status)
+        self.pool, self.table, self.lens, self.status, self.device = pool, table, lens, status, dev
+        self.n_seq = int(table.shape[0])
+        if self.n_seq > pool.max_seqs:
+            raise ValueError(f"{self.n_seq} sequences, the pool takes {pool.max_seqs}")
+        tp, stride = _mat(table, self.n_seq, 1, torch.int32, "table", dev)
+        self._head = (pool.handle, tp, stride, int(table.shape[1]),
+                      _vec(lens, self.n_seq, torch.int32, "lens", dev))
+        self._status = _vec(status, self.n_seq, torch.int32, "status", dev)
+
+    def _rows(self, t, what):
+        import torch
+        if not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != self.n_seq \
+                or t.device.index != self.device:
+            raise ValueError(f"{what} must be a contiguous int32 tensor of {self.n_seq} entries on "
+                             f"cuda:{self.device}")
+        return t.data_ptr()
+
+    def extend(self, n_new, slots: SlotMap, stream=None) -> None:
+        """wg_kv_extend: room for ``n_new`` [n_seq] more tokens; ``slots`` says where they go."""
+        if slots.n_seq != self.n_seq or slots.device != self.device:
+            raise ValueError("slots were made for another batch or device")
+        rc = _lib.wg_kv_extend(*self._head, self._rows(n_new, "n_new"), self.n_seq, *slots._args, self._status,
+                               _stream_ptr(stream))
+        if rc != WG_OK:
+            raise WgError(rc, "wg_kv_extend")
+
+    def shrink(self, keep, status=None, stream=None) -> None:
+        """wg_kv_shrink: cuts the sequences to ``keep`` [n_seq] tokens.  ``status``, where given, gets
+        WG_ERR_ARG for a ``keep`` outside 0 .. the sequence's length (which is then left alone)."""
+        st = self._rows(status, "status") if status is not None else None
+        rc = _lib.wg_kv_shrink(*self._head, self._rows(keep, "keep"), self.n_seq, st, _stream_ptr(stream))
+        if rc != WG_OK:
+            raise WgError(rc, "wg_kv_shrink")
+
+    def reorder(self, parent, planes: Optional[KvPlanes] = None, copy_src=None, copy_dst=None,
+                stream=None) -> None:
+        """wg_kv_reorder: ``parent`` [n_req, n_beam] as a selection returned it."""
+        import torch
+        if parent.dim() != 2:
+            raise ValueError("parent must be [n_req, n_beam]")
+        if planes is not None and (planes.block_size != self.pool.block_size or planes.n_blocks < self.pool.n_blocks
+                                   or planes.device != self.device):
+            raise ValueError("planes were made for another pool")
+        n_req, n_beam = (int(n) for n in parent.shape)
+        rc = _lib.wg_kv_reorder(*self._head, self._rows(parent, "parent"), n_req, n_beam,
+                                *((None, 0) if planes is None else planes._args),
+                                _vec(copy_src, self.n_seq, torch.int32, "copy_src", self.device),
+                                _vec(copy_dst, self.n_seq, torch.int32, "copy_dst", self.device), self._status,
+                                _stream_ptr(stream))
+        if rc != WG_OK:
+            raise WgError(rc, "wg_kv_reorder")

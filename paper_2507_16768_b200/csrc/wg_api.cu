@@ -1,4 +1,5 @@
 // Host side of the C ABI declared in wg.h: object lifetimes, uploads and kernel launches.
+#include <algorithm>
 #include <cstdio>
 #include <cstring>
 #include <mutex>
@@ -6,6 +7,7 @@
 #include <vector>
 
 #include "wg_host.h"
+#include "wg_beam.cuh"
 #include "wg_kernels.cuh"
 
 struct wg_vocab {
@@ -1387,3 +1389,5 @@ int32_t wg_cache_prewarm(wg_ctx *c, int32_t grammar_id, void *stream) {
 }
 
 }  // extern "C"
+
+#include "wg_beam_api.inl"

@@ -1,0 +1,183 @@
+// Host side of constrained beam search (wg_beam_* of wg.h).  Part of wg_api.cu's translation unit:
+// the step launches that file's lookup and build kernels on the context.
+
+struct wg_beam {
+    int32_t V = 0, max_requests = 0, max_beams = 0, max_out = 0;
+    int32_t chunk_stride = 0, max_parts = 0;
+    float *chunk_max = nullptr;
+    float2 *parts = nullptr;
+};
+
+namespace {
+
+// Spans per row, for the worst alignment of a row (it may begin up to 7 elements into a piece).
+int32_t beam_spans(int32_t V) { return (V + 7 + 1023) / 1024; }
+
+template <typename E, int NORM, bool CTX>
+cudaError_t launch_beam_scan(const BeamArgs &a, const CtxDev &ctx, dim3 grid, cudaStream_t st) {
+    return launch_pdl(beam_scan_kernel<E, NORM, CTX>, grid, dim3(BEAM_THREADS), st, a, ctx);
+}
+
+template <typename E, bool CTX>
+int32_t launch_beam(const BeamArgs &a, const CtxDev &ctx, const VocabDev &v, const BeamStepArgs &step,
+                    int32_t n_req, dim3 grid, float *score_out, int32_t *parent_out, int32_t *token_out,
+                    cudaStream_t st) {
+    if (a.norm == WG_BEAM_NORM_ALLOWED)
+        WG_CUDA((launch_beam_scan<E, WG_BEAM_NORM_ALLOWED, CTX>(a, ctx, grid, st)));
+    else if (a.norm == WG_BEAM_NORM_FULL)
+        WG_CUDA((launch_beam_scan<E, WG_BEAM_NORM_FULL, CTX>(a, ctx, grid, st)));
+    else
+        WG_CUDA((launch_beam_scan<E, WG_BEAM_NORM_NONE, CTX>(a, ctx, grid, st)));
+    WG_LAUNCHED();
+    WG_CUDA(launch_pdl(beam_pick_kernel<E, CTX>, dim3((unsigned)n_req), dim3(PICK_THREADS), st, a, ctx, v,
+                       step, score_out, parent_out, token_out));
+    WG_LAUNCHED();
+    return WG_OK;
+}
+
+// The scan's grid, (blocks per row, rows): as few spans per warp as it takes to fill the GPU about
+// four times over, at most BEAM_SPANS_PER_WARP (as apply_grid).
+dim3 beam_grid(BeamArgs &a, int32_t rows) {
+    const int n_spans = beam_spans(a.V);
+    int per_warp = BEAM_SPANS_PER_WARP;
+    while (per_warp > 1 && (long long)rows * ((n_spans + BEAM_WARPS * per_warp - 1) / (BEAM_WARPS * per_warp)) <
+                               16LL * sm_count())
+        per_warp >>= 1;
+    a.spans_per_block = BEAM_WARPS * per_warp;
+    const int blocks = (n_spans + a.spans_per_block - 1) / a.spans_per_block;
+    a.n_parts = blocks * BEAM_WARPS;
+    return dim3((unsigned)blocks, (unsigned)rows);
+}
+
+bool beam_sizes_ok(const wg_beam *beam, int32_t n_req, int32_t n_beam, int32_t n_out, int32_t norm) {
+    return beam && n_req >= 1 && n_req <= beam->max_requests && n_beam >= 1 && n_beam <= beam->max_beams &&
+           n_out >= 1 && n_out <= beam->max_out && norm >= WG_BEAM_NORM_ALLOWED && norm <= WG_BEAM_NORM_NONE;
+}
+
+bool elem_aligned(const void *p, int32_t dtype) {
+    return (uintptr_t)p % (dtype == WG_DTYPE_BF16 ? 2 : 4) == 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t wg_beam_create(int32_t V, int32_t max_requests, int32_t max_beams, int32_t max_out, wg_beam **out) {
+    NvtxRange nvtx_range("wg_beam_create");
+    if (!out) return WG_ERR_ARG;
+    *out = nullptr;
+    if (V < 1 || V > INT32_MAX - 2048 || max_requests < 1 || max_beams < 1 || max_beams > WG_BEAM_MAX_BEAMS ||
+        max_out < 1 || max_out > WG_BEAM_MAX_OUT || (int64_t)max_requests * max_beams > WG_MAX_ROWS ||
+        (int64_t)V * max_beams >= (1LL << 32))
+        return WG_ERR_ARG;
+    wg_beam *b = new (std::nothrow) wg_beam();
+    if (!b) return WG_ERR_ARG;
+    b->V = V;
+    b->max_requests = max_requests;
+    b->max_beams = max_beams;
+    b->max_out = max_out;
+    b->chunk_stride = beam_spans(V) * 4;
+    b->max_parts = (beam_spans(V) + BEAM_WARPS - 1) / BEAM_WARPS * BEAM_WARPS;   // one span per warp
+    const size_t rows = (size_t)max_requests * max_beams;
+    int32_t rc = dev_alloc(&b->chunk_max, rows * b->chunk_stride);
+    if (rc == WG_OK) rc = dev_alloc(&b->parts, rows * b->max_parts);
+    if (rc != WG_OK) {
+        wg_beam_free(b);
+        return rc;
+    }
+    *out = b;
+    return WG_OK;
+}
+
+void wg_beam_free(wg_beam *b) {
+    if (!b) return;
+    cudaFree(b->chunk_max);   // (waits for queued work)
+    cudaFree(b->parts);
+    delete b;
+}
+
+int32_t wg_beam_select(wg_beam *beam, const void *logits, int32_t dtype, int64_t row_stride_elems,
+                       const uint32_t *bitmask, int64_t mask_stride_words, const float *score,
+                       const int32_t *finished, int32_t eos_id, int32_t n_req, int32_t n_beam,
+                       int32_t n_out, int32_t norm, float *score_out, int32_t *parent_out,
+                       int32_t *token_out, void *stream) {
+    NvtxRange nvtx_range("wg_beam_select");
+    if (!beam_sizes_ok(beam, n_req, n_beam, n_out, norm) || !logits || !score || !score_out || !parent_out ||
+        !token_out)
+        return WG_ERR_ARG;
+    if (dtype != WG_DTYPE_BF16 && dtype != WG_DTYPE_FP32) return WG_ERR_ARG;
+    const int32_t V = beam->V, W = (V + 31) / 32;
+    if (row_stride_elems < V || !elem_aligned(logits, dtype) || (bitmask && mask_stride_words < W))
+        return WG_ERR_ARG;
+    if (finished && (eos_id < 0 || eos_id >= V)) return WG_ERR_ARG;
+    if (score_out == score && n_out != n_beam) return WG_ERR_ARG;
+    BeamArgs a{logits, row_stride_elems, bitmask, mask_stride_words, score, finished, nullptr, nullptr,
+               n_beam, V, W, n_out, eos_id, norm, 0, 0, beam->chunk_stride, beam->chunk_max, beam->parts};
+    const dim3 grid = beam_grid(a, n_req * n_beam);
+    const CtxDev none{};
+    const VocabDev no_vocab{};
+    const BeamStepArgs no_step{};
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return dtype == WG_DTYPE_BF16
+        ? launch_beam<uint16_t, false>(a, none, no_vocab, no_step, n_req, grid, score_out, parent_out, token_out, st)
+        : launch_beam<uint32_t, false>(a, none, no_vocab, no_step, n_req, grid, score_out, parent_out, token_out, st);
+}
+
+int32_t wg_beam_step(wg_beam *beam, wg_ctx *c, int32_t *gid, int32_t *sid, float *score, int32_t n_req,
+                     int32_t n_beam, const void *logits, int32_t dtype, int64_t row_stride_elems,
+                     uint32_t *bitmask, int64_t mask_stride_words, int32_t norm, int32_t *parent_out,
+                     int32_t *token_out, int32_t *status, uint32_t flags, void *stream) {
+    NvtxRange nvtx_range("wg_beam_step");
+    if (!beam_sizes_ok(beam, n_req, n_beam, n_beam, norm) || !c || !gid || !sid || !score || !logits ||
+        !bitmask || !parent_out || !token_out)
+        return WG_ERR_ARG;
+    if (dtype != WG_DTYPE_BF16 && dtype != WG_DTYPE_FP32) return WG_ERR_ARG;
+    if (flags & ~(uint32_t)WG_NO_CACHE) return WG_ERR_ARG;
+    const VocabDev &v = c->vocab->dev;
+    const int32_t rows = n_req * n_beam;
+    if (beam->V != v.V || !batch_ok(c, rows)) return WG_ERR_ARG;
+    if (row_stride_elems < v.V || !elem_aligned(logits, dtype) || mask_stride_words < v.W) return WG_ERR_ARG;
+    const bool no_cache = (flags & WG_NO_CACHE) != 0;
+    if (!no_cache && c->part_end != 0) return WG_ERR_ARG;  // cached masks are partial: see wg_decode_step_shard
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    // the rows' masks, as the first launches of a decode step
+    BuildWork work{};
+    if (no_cache) {
+        WG_CUDA(launch_pdl(reset_rows_kernel, dim3((rows + 255) / 256), dim3(256), st, c->dev, rows));
+        work = BuildWork{gid, sid, nullptr, bitmask, mask_stride_words, nullptr, rows, 0, 0, 0};
+    } else {
+        WG_CUDA(launch_pdl(cache_lookup_insert_kernel, dim3(1), dim3(1024), st, c->dev, gid, sid, rows,
+                           bitmask, mask_stride_words));
+        work = BuildWork{c->dev.bl_gid, c->dev.bl_sid, c->dev.bl_dst, nullptr, 0, c->dev.bl_count, 0, 0, 0, 0};
+    }
+    WG_LAUNCHED();
+    const int32_t rc = launch_build(c, work, rows, st, true);
+    if (rc != WG_OK) return rc;
+    BeamArgs a{logits, row_stride_elems, bitmask, mask_stride_words, score, nullptr, gid, sid,
+               n_beam, v.V, v.W, n_beam, v.eos_id, norm, 0, 0, beam->chunk_stride, beam->chunk_max, beam->parts};
+    const dim3 grid = beam_grid(a, rows);
+    const BeamStepArgs step{gid, sid, status};
+    return dtype == WG_DTYPE_BF16
+        ? launch_beam<uint16_t, true>(a, c->dev, v, step, n_req, grid, score, parent_out, token_out, st)
+        : launch_beam<uint32_t, true>(a, c->dev, v, step, n_req, grid, score, parent_out, token_out, st);
+}
+
+int32_t wg_beam_backtrack(const int32_t *token, const int32_t *parent, int32_t n_steps, int32_t n_req,
+                          int32_t n_beam, int32_t *out, void *stream) {
+    NvtxRange nvtx_range("wg_beam_backtrack");
+    if (n_steps < 0 || n_req < 1 || n_req > WG_MAX_ROWS || n_beam < 1 || n_beam > WG_BEAM_MAX_BEAMS)
+        return WG_ERR_ARG;
+    if (n_steps == 0) return WG_OK;
+    if (!token || !parent || !out) return WG_ERR_ARG;
+    // 32 KB for the parents of a tile of steps and as much for the way back
+    const int tile = std::min(n_steps, 32768 / n_beam);
+    const size_t smem = (size_t)tile * n_beam * 2;
+    if (smem > 32 * 1024)
+        WG_CUDA(cudaFuncSetAttribute(beam_backtrack_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 65536));
+    WG_CUDA(launch_pdl_smem(beam_backtrack_kernel, dim3((unsigned)n_req), dim3(BACK_THREADS), smem,
+                            static_cast<cudaStream_t>(stream), token, parent, n_steps, n_req, n_beam, tile, out));
+    WG_LAUNCHED();
+    return WG_OK;
+}
+
+}  // extern "C"

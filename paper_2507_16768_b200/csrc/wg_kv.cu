@@ -1,0 +1,676 @@
+// Block tables of a paged cache (wg_kv_* of wg.h): room for new tokens, tokens given back, and tables that
+// follow a beam search's selection.
+//
+// State of a pool: ref[b] = how many table rows name block b, and one bit per block that is set while
+// ref[b] == 0.  "The k-th free block" is then a prefix sum over the bits' population counts, and what
+// is taken does not depend on the order in which blocks came free: whatever order the atomics of a
+// call ran in, the counts and bits after it are the same.
+#include <new>
+
+#include "wg_host.h"
+
+namespace {
+
+constexpr int PLAN_THREADS = 1024;      // one block: plans of a whole batch
+constexpr int FILL_THREADS = 256;
+constexpr int MOVE_THREADS = 128;       // columns of a table per block
+constexpr int COPY_THREADS = 256;
+constexpr int WORDS_PER_THREAD = 8;     // words of free bits a thread counts per round
+
+struct PoolDev {
+    int32_t *ref;         // [n_blocks]
+    uint32_t *free_bits;  // [n_words], padded with zero words to a whole round of a thread
+    int32_t *n_free;
+    int32_t n_blocks, n_words, block_size;
+    // per-call scratch
+    int32_t *taken;       // [n_blocks] blocks handed out by the call, in order
+    int32_t *first;       // [max_seqs] where a sequence's blocks begin in `taken`, or -1: refused
+    int32_t *old_len;     // [max_seqs] lengths before the call
+    int32_t *new_len;     // [max_seqs]
+    int32_t *src, *dst, *filled;  // [max_seqs] copies of a reorder
+    int32_t *n_copies;
+    int32_t *arrived;     // blocks of the reorder's first kernel that have finished; zero between calls
+};
+
+__device__ __forceinline__ void kv_enter() {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+__device__ __forceinline__ int32_t blocks_of(int32_t len, int32_t block_size) {   // ceil, no overflow
+    return len / block_size + (len % block_size != 0);
+}
+
+// Inclusive prefix sum over the block, and the block's total.  `warps`: shared, blockDim.x / 32.
+template <typename T>
+__device__ __forceinline__ T block_scan(T x, T *warps, T &total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = (int)(blockDim.x >> 5);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const T y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        if (lane >= o) x += y;
+    }
+    if (lane == 31) warps[warp] = x;
+    __syncthreads();
+    if (warp == 0) {
+        T w = lane < n_warps ? warps[lane] : T(0);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const T y = __shfl_up_sync(0xFFFFFFFFu, w, o);
+            if (lane >= o) w += y;
+        }
+        if (lane < n_warps) warps[lane] = w;
+    }
+    __syncthreads();
+    total = warps[n_warps - 1];
+    const T before = warp > 0 ? warps[warp - 1] : T(0);
+    __syncthreads();   // `warps` may be used again
+    return x + before;
+}
+
+__device__ __forceinline__ int nth_set_bit(uint32_t w, int n) {   // position of the n-th set bit (0-based)
+    int at = 0;
+#pragma unroll
+    for (int half = 16; half > 0; half >>= 1) {
+        const int c = __popc((w >> at) & ((1u << half) - 1u));
+        if (n >= c) {
+            n -= c;
+            at += half;
+        }
+    }
+    return at;
+}
+
+// Called by a whole block: takes the `n` lowest free blocks (n <= the number of free ones; the caller has
+// seen to that), in ascending order into pool.taken, with count 1.  Every round a thread counts
+// WORDS_PER_THREAD words; after the scan each of the round's blocks finds its word by bisection.
+struct TakeShared {
+    int32_t upto[PLAN_THREADS];   // free blocks up to and including a thread's words
+    int32_t warps[32];
+};
+
+__device__ __forceinline__ void take_blocks(const PoolDev &pool, TakeShared &sh, int n) {
+    const int threads = (int)blockDim.x;
+    int done = 0;
+    for (int w0 = 0; w0 < pool.n_words && done < n; w0 += threads * WORDS_PER_THREAD) {
+        const int mine = w0 + (int)threadIdx.x * WORDS_PER_THREAD;
+        uint32_t w[WORDS_PER_THREAD];
+        int count = 0;
+#pragma unroll
+        for (int i = 0; i < WORDS_PER_THREAD; i += 4) {
+            uint4 q = make_uint4(0, 0, 0, 0);
+            if (mine + i < pool.n_words) q = __ldcg(reinterpret_cast<const uint4 *>(pool.free_bits + mine + i));
+            w[i] = q.x; w[i + 1] = q.y; w[i + 2] = q.z; w[i + 3] = q.w;
+        }
+#pragma unroll
+        for (int i = 0; i < WORDS_PER_THREAD; ++i) count += __popc(w[i]);
+        int total;
+        const int upto = block_scan(count, sh.warps, total);
+        sh.upto[threadIdx.x] = upto;
+        __syncthreads();
+        const int here = min(total, n - done);
+        for (int k = threadIdx.x; k < here; k += threads) {
+            int lo = 0, hi = threads - 1;             // the first thread whose words reach past k
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (sh.upto[mid] > k) hi = mid; else lo = mid + 1;
+            }
+            int left = k - (lo > 0 ? sh.upto[lo - 1] : 0);
+            int at = w0 + lo * WORDS_PER_THREAD;
+            uint32_t word = __ldcg(&pool.free_bits[at]);
+            for (int c = __popc(word); left >= c; c = __popc(word)) {
+                left -= c;
+                word = __ldcg(&pool.free_bits[++at]);
+            }
+            const int id = at * 32 + nth_set_bit(word, left);
+            pool.taken[done + k] = id;
+            pool.ref[id] = 1;
+        }
+        __syncthreads();                              // everybody has looked the bits up
+        int drop = min(count, here - (upto - count)); // of this thread's blocks, the lowest `drop` are gone
+#pragma unroll
+        for (int i = 0; i < WORDS_PER_THREAD; ++i) {
+            if (drop <= 0) break;
+            const int c = __popc(w[i]);
+            if (c == 0) continue;
+            if (drop >= c) {
+                w[i] = 0u;
+                drop -= c;
+            } else {
+                w[i] &= ~((1u << nth_set_bit(w[i], drop)) - 1u);
+                drop = 0;
+            }
+            pool.free_bits[mine + i] = w[i];
+        }
+        done += here;
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ bool id_ok(const PoolDev &pool, int32_t id) { return id >= 0 && id < pool.n_blocks; }
+
+// `by` fewer (or, negative, more) rows name block `id`; a block nobody names is free.  A call only takes
+// away references that rows hold, so a count reaches zero once, with the last of them.
+__device__ __forceinline__ void drop_refs(const PoolDev &pool, int32_t id, int32_t by, int &freed) {
+    if (atomicSub(&pool.ref[id], by) == by) {
+        atomicOr(&pool.free_bits[id >> 5], 1u << (id & 31));
+        ++freed;
+    }
+}
+
+__device__ __forceinline__ void add_freed(const PoolDev &pool, int freed) {   // called by whole warps
+    freed = __reduce_add_sync(0xFFFFFFFFu, freed);
+    if ((threadIdx.x & 31) == 0 && freed) atomicAdd(pool.n_free, freed);
+}
+
+// ---------------------------------------------------------------------------------------
+// Pool set-up
+// ---------------------------------------------------------------------------------------
+// refs == NULL: all blocks free.  A thread per word of bits.
+__global__ void pool_load_kernel(PoolDev pool, const int32_t *refs) {
+    const int w = blockIdx.x * blockDim.x + threadIdx.x;
+    uint32_t bits = 0;
+    if (w < pool.n_words) {
+        for (int i = 0; i < 32; ++i) {
+            const int id = w * 32 + i;
+            if (id >= pool.n_blocks) break;
+            const int32_t r = refs ? max(refs[id], 0) : 0;
+            pool.ref[id] = r;
+            if (r == 0) bits |= 1u << i;
+        }
+        pool.free_bits[w] = bits;
+    }
+    add_freed(pool, __popc(bits));
+}
+
+// ---------------------------------------------------------------------------------------
+// Extend
+// ---------------------------------------------------------------------------------------
+struct ExtendArgs {
+    int32_t *table;
+    int64_t stride;
+    int32_t max_blocks;
+    int32_t *len;
+    const int32_t *n_new;
+    int32_t n_seq;
+    int32_t *cu;
+    int64_t *slot;
+    int32_t *pos, *seq;
+    int32_t n_tokens;
+    int32_t *status;
+};
+
+// Token t of the call: its sequence by bisection over cu, its block from the table or, for a new
+// block, from the blocks taken.  The token at a block's first position also enters the block into the
+// table (new blocks begin where the old length's last block ends, so each holds exactly one such token).
+__device__ __forceinline__ void extend_token(const PoolDev &pool, const ExtendArgs &a, int t, int n_used) {
+    int64_t slot = -1;
+    int32_t pos = -1, s = -1;
+    if (t < n_used) {
+        int lo = 0, hi = a.n_seq - 1;      // the last sequence that begins at or before t and is not empty
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (a.cu[mid + 1] > t) hi = mid; else lo = mid + 1;
+        }
+        s = lo;
+        const int32_t len = pool.old_len[s];
+        pos = len + (t - a.cu[s]);
+        const int32_t first = pool.first[s];
+        if (first >= 0) {
+            const int32_t held = blocks_of(len, pool.block_size), col = pos / pool.block_size;
+            const int32_t in = pos - col * pool.block_size;
+            int32_t *entry = a.table + (int64_t)s * a.stride + col;
+            int32_t id;
+            if (col < held) {
+                id = *entry;
+            } else {
+                id = pool.taken[first + col - held];
+                if (in == 0) *entry = id;
+            }
+            if (id_ok(pool, id)) slot = (int64_t)id * pool.block_size + in;
+        }
+    }
+    a.slot[t] = slot;
+    a.pos[t] = pos;
+    a.seq[t] = s;
+}
+
+// One block: who gets how many blocks, which ones, and where each sequence's tokens begin.
+// FILL: the same block also writes the tokens' slots (few tokens: one launch less).
+template <bool FILL>
+__global__ void __launch_bounds__(PLAN_THREADS, 1)
+extend_plan_kernel(PoolDev pool, ExtendArgs a) {
+    __shared__ TakeShared take;
+    __shared__ long long warps[32];
+    kv_enter();
+    const int n_free = *pool.n_free;
+    long long want0 = 0, tok0 = 0;       // before this round
+    int granted_blocks = 0;              // the largest granted prefix
+    const int64_t room = (int64_t)a.max_blocks * pool.block_size;
+    for (int s0 = 0; s0 < a.n_seq; s0 += PLAN_THREADS) {
+        const int s = s0 + (int)threadIdx.x;
+        int32_t len = 0, add = 0, need = 0, st = WG_OK;
+        if (s < a.n_seq) {
+            len = a.len[s];
+            add = a.n_new[s];
+            if (len < 0 || len > room || add < 0 || (int64_t)len + add > room) {
+                st = WG_ERR_ARG;
+                add = 0;
+            } else {
+                need = blocks_of(len + add, pool.block_size) - blocks_of(len, pool.block_size);
+            }
+        }
+        long long tokens, wanted;
+        const long long tok = block_scan((long long)add, warps, tokens) + tok0;
+        const long long want = block_scan((long long)need, warps, wanted) + want0;
+        int last = 0;                    // blocks granted up to and including this sequence
+        if (s < a.n_seq) {
+            const bool fits = st == WG_OK &&
+                              (add == 0 || (tok <= a.n_tokens && (need == 0 || want <= n_free)));
+            if (st == WG_OK && !fits) st = WG_ERR_CAPACITY;
+            a.cu[s + 1] = (int32_t)min(tok, (long long)a.n_tokens);
+            pool.old_len[s] = len;
+            pool.first[s] = fits ? (int32_t)min(want - need, (long long)n_free) : -1;
+            if (fits) {
+                a.len[s] = len + add;
+                if (need > 0) last = (int)want;
+            }
+            if (a.status) a.status[s] = st;
+        }
+        granted_blocks = max(granted_blocks, __reduce_max_sync(0xFFFFFFFFu, last));
+        want0 += wanted;
+        tok0 += tokens;
+    }
+    if (threadIdx.x == 0) a.cu[0] = 0;
+    // the warps' largest prefixes
+    if ((threadIdx.x & 31) == 0) take.warps[threadIdx.x >> 5] = granted_blocks;
+    __syncthreads();
+    granted_blocks = __reduce_max_sync(0xFFFFFFFFu, take.warps[threadIdx.x & 31]);
+    __syncthreads();
+    if (granted_blocks > 0) {
+        take_blocks(pool, take, granted_blocks);
+        if (threadIdx.x == 0) *pool.n_free = n_free - granted_blocks;
+    }
+    if (FILL) {
+        __syncthreads();
+        const int n_used = a.n_seq > 0 ? a.cu[a.n_seq] : 0;
+        for (int t = threadIdx.x; t < a.n_tokens; t += PLAN_THREADS) extend_token(pool, a, t, n_used);
+    }
+}
+
+__global__ void __launch_bounds__(FILL_THREADS)
+extend_fill_kernel(PoolDev pool, ExtendArgs a) {
+    kv_enter();
+    const int n_used = a.cu[a.n_seq];
+    const int t = blockIdx.x * FILL_THREADS + (int)threadIdx.x;
+    if (t < a.n_tokens) extend_token(pool, a, t, n_used);
+}
+
+// ---------------------------------------------------------------------------------------
+// Shrink: a warp per sequence.
+// ---------------------------------------------------------------------------------------
+__global__ void __launch_bounds__(FILL_THREADS)
+shrink_kernel(PoolDev pool, int32_t *table, int64_t stride, int32_t max_blocks, int32_t *len,
+              const int32_t *keep, int32_t n_seq, int32_t *status) {
+    kv_enter();
+    const int s = (int)((blockIdx.x * FILL_THREADS + threadIdx.x) >> 5), lane = threadIdx.x & 31;
+    if (s >= n_seq) return;
+    const int32_t have = len[s], want = keep[s];
+    const bool ok = have >= 0 && have <= (int64_t)max_blocks * pool.block_size && want >= 0 && want <= have;
+    if (lane == 0 && status) status[s] = ok ? WG_OK : WG_ERR_ARG;
+    if (!ok) return;
+    const int32_t end = blocks_of(have, pool.block_size);
+    int freed = 0;
+    for (int c = blocks_of(want, pool.block_size) + lane; c < end; c += 32) {
+        int32_t *entry = table + (int64_t)s * stride + c;
+        const int32_t id = *entry;
+        if (id_ok(pool, id)) drop_refs(pool, id, 1, freed);
+        *entry = -1;
+    }
+    add_freed(pool, freed);
+    if (lane == 0) len[s] = want;
+}
+
+// ---------------------------------------------------------------------------------------
+// Reorder
+// ---------------------------------------------------------------------------------------
+struct MoveArgs {
+    int32_t *table;
+    int64_t stride;
+    int32_t max_blocks;
+    int32_t *len;
+    const int32_t *parent;
+    int32_t n_req, n_beam;
+    int32_t *copy_src, *copy_dst, *status;
+};
+
+// What a request's rows become; filled by the block for its request.
+struct MoveShared {
+    int32_t parent[WG_BEAM_MAX_BEAMS];    // -1: the sequence ends
+    int32_t blocks[WG_BEAM_MAX_BEAMS];    // columns in use
+    int32_t partly[WG_BEAM_MAX_BEAMS];    // the column of a partly filled last block, or -1
+    int32_t children[WG_BEAM_MAX_BEAMS];
+    int32_t first[WG_BEAM_MAX_BEAMS];     // first child, or n_beam
+};
+
+// First kernel: grid = (tiles of MOVE_THREADS columns, requests); a thread holds one column of all the
+// request's rows, so the rows move in place with no other thread in the way.  Row b's block of the
+// column was held once and is held by its children afterwards: the count changes by children - 1 (a
+// partly filled last block stays with one child only).  Rows that name the same block are summed
+// first: in the columns of a shared prompt nothing is left to count.  The block that finishes last
+// hands out the blocks for the copies.
+__global__ void __launch_bounds__(MOVE_THREADS)
+move_rows_kernel(PoolDev pool, MoveArgs a) {
+    extern __shared__ int32_t column[];   // [n_beam][MOVE_THREADS]
+    __shared__ MoveShared sh;
+    __shared__ TakeShared take;
+    __shared__ int32_t is_last;
+    kv_enter();
+    const int K = a.n_beam, row0 = blockIdx.y * K, bs = pool.block_size;
+    const int64_t room = (int64_t)a.max_blocks * bs;
+    if ((int)threadIdx.x < K) {
+        const int32_t p = a.parent[row0 + threadIdx.x], l = a.len[row0 + threadIdx.x];
+        sh.parent[threadIdx.x] = p >= 0 && p < K ? p : -1;
+        const int32_t len = l >= 0 && l <= room ? l : 0;
+        sh.blocks[threadIdx.x] = blocks_of(len, bs);
+        sh.partly[threadIdx.x] = len % bs != 0 ? len / bs : -1;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < K) {
+        int n = 0, first = K;
+        for (int j = K - 1; j >= 0; --j)
+            if (sh.parent[j] == (int)threadIdx.x) {
+                ++n;
+                first = j;
+            }
+        sh.children[threadIdx.x] = n;
+        sh.first[threadIdx.x] = first;
+    }
+    __syncthreads();
+    int32_t most = 0;
+    for (int b = 0; b < K; ++b) most = max(most, sh.blocks[b]);
+    int freed = 0;
+    const int c = blockIdx.x * MOVE_THREADS + (int)threadIdx.x;
+    if (c < most) {
+        int32_t *col = a.table + (int64_t)row0 * a.stride + c;
+        int32_t *v = column + threadIdx.x;
+        for (int b = 0; b < K; ++b) {
+            const int32_t id = c < sh.blocks[b] ? col[b * a.stride] : -1;
+            v[b * MOVE_THREADS] = id_ok(pool, id) ? id : -1;
+        }
+        // counts
+        for (int b = 0; b < K; ++b) {
+            const int32_t id = v[b * MOVE_THREADS];
+            if (id < 0) continue;
+            bool seen = false;
+            int32_t change = 0;
+            for (int o = 0; o < K; ++o) {
+                if (v[o * MOVE_THREADS] != id) continue;
+                if (o < b) { seen = true; break; }
+                change += (c == sh.partly[o] ? min(sh.children[o], 1) : sh.children[o]) - 1;
+            }
+            if (!seen && change != 0) drop_refs(pool, id, -change, freed);
+        }
+        // rows
+        for (int j = 0; j < K; ++j) {
+            const int p = sh.parent[j];
+            int32_t id = p >= 0 ? v[p * MOVE_THREADS] : -1;
+            if (p >= 0 && c == sh.partly[p] && j != sh.first[p]) id = -1;   // its own block: later
+            if (id != v[j * MOVE_THREADS]) col[j * a.stride] = id;
+        }
+    }
+    add_freed(pool, freed);
+    // ---- the last block to finish
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        is_last = atomicAdd(pool.arrived, 1) == (int)(gridDim.x * gridDim.y) - 1;
+    }
+    __syncthreads();
+    if (!is_last) return;
+    __threadfence();
+    const int n_rows = a.n_req * K;
+    const int n_free = *(volatile int32_t *)pool.n_free;
+    int done = 0, granted = 0;
+    for (int r0 = 0; r0 < n_rows; r0 += MOVE_THREADS) {
+        const int i = r0 + (int)threadIdx.x;
+        int32_t st = WG_OK, filled = 0, src = -1, full = 0;
+        bool copy = false;
+        if (i < n_rows) {
+            const int first_row = i / K * K, j = i - first_row, p = a.parent[i];
+            int32_t l = 0;
+            if (p >= 0 && p < K) {
+                l = a.len[first_row + p];
+                if (l < 0 || l > room) {
+                    st = WG_ERR_ARG;
+                    l = 0;
+                }
+            }
+            filled = l % bs;
+            full = l - filled;
+            if (filled != 0) {
+                int first = 0;
+                while (a.parent[first_row + first] != p) ++first;    // (it stops at j at the latest)
+                copy = first != j;
+                if (copy) src = __ldcg(&a.table[(int64_t)(first_row + first) * a.stride + l / bs]);
+                if (copy && !id_ok(pool, src)) copy = false;
+            }
+            pool.new_len[i] = l;
+        }
+        int total;
+        const int upto = block_scan(copy ? 1 : 0, take.warps, total);
+        const int rank = done + upto - 1;
+        const bool got = copy && rank < n_free;
+        if (i < n_rows) {
+            if (copy && !got) {
+                st = WG_ERR_CAPACITY;
+                pool.new_len[i] = full;
+            }
+            if (got) {
+                pool.src[rank] = src;
+                pool.dst[rank] = i;       // the row, until its block is known
+                pool.filled[rank] = filled;
+            }
+            if (a.status) a.status[i] = st;
+            if (a.copy_src) a.copy_src[i] = got ? src : -1;
+            if (a.copy_dst && !got) a.copy_dst[i] = -1;
+        }
+        done += total;
+    }
+    granted = min(done, n_free);
+    __syncthreads();
+    take_blocks(pool, take, granted);
+    for (int i = threadIdx.x; i < n_rows; i += MOVE_THREADS) a.len[i] = pool.new_len[i];
+    for (int k = threadIdx.x; k < granted; k += MOVE_THREADS) {
+        const int row = pool.dst[k], id = pool.taken[k];
+        a.table[(int64_t)row * a.stride + pool.new_len[row] / bs] = id;
+        if (a.copy_dst) a.copy_dst[row] = id;
+        pool.dst[k] = id;
+    }
+    if (threadIdx.x == 0) {
+        *pool.n_free = n_free - granted;
+        *pool.n_copies = granted;
+        *pool.arrived = 0;
+    }
+}
+
+// Second kernel: the filled tokens of every copied block, in all planes.  The blocks take (copy, plane)
+// pairs in turn.
+__global__ void __launch_bounds__(COPY_THREADS)
+copy_blocks_kernel(PoolDev pool, const wg_kv_plane *planes, int32_t n_planes) {
+    kv_enter();
+    const int64_t n = (int64_t)*pool.n_copies * n_planes;
+    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+        const int k = (int)(i / n_planes);
+        const wg_kv_plane pl = planes[i - (int64_t)k * n_planes];
+        const int64_t per_block = (int64_t)pool.block_size * pl.token_bytes;
+        const char *src = static_cast<const char *>(pl.base) + (int64_t)pool.src[k] * per_block;
+        char *dst = static_cast<char *>(pl.base) + (int64_t)pool.dst[k] * per_block;
+        const int64_t bytes = (int64_t)pool.filled[k] * pl.token_bytes;
+        if ((((uintptr_t)src | (uintptr_t)dst | (uint64_t)bytes) & 15) == 0) {
+            const uint4 *s = reinterpret_cast<const uint4 *>(src);
+            uint4 *d = reinterpret_cast<uint4 *>(dst);
+            const int64_t m = bytes / 16;
+            int64_t at = threadIdx.x;
+            for (; at + 3 * COPY_THREADS < m; at += 4 * COPY_THREADS) {
+                uint4 x[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) x[u] = __ldcs(s + at + u * COPY_THREADS);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) d[at + u * COPY_THREADS] = x[u];
+            }
+            for (; at < m; at += COPY_THREADS) d[at] = __ldcs(s + at);
+        } else {
+            for (int64_t at = threadIdx.x; at < bytes; at += COPY_THREADS) dst[at] = src[at];
+        }
+    }
+}
+
+}  // namespace
+
+struct wg_kv_pool {
+    PoolDev dev{};
+    int32_t max_seqs = 0;
+};
+
+namespace {
+
+// A batch of tokens up to this many is placed by the planning block itself.
+constexpr int32_t FILL_IN_PLAN = 2048;
+
+bool table_ok(const wg_kv_pool *pool, const int32_t *table, int64_t stride, int32_t max_blocks,
+              const int32_t *len, int32_t n_seq) {
+    return pool && table && len && n_seq >= 1 && n_seq <= pool->max_seqs && max_blocks >= 1 &&
+           stride >= max_blocks;
+}
+
+int32_t pool_load(wg_kv_pool *p, const int32_t *refs, cudaStream_t st) {
+    WG_CUDA(cudaMemsetAsync(p->dev.n_free, 0, sizeof(int32_t), st));
+    pool_load_kernel<<<(p->dev.n_words + 255) / 256, 256, 0, st>>>(p->dev, refs);
+    WG_LAUNCHED();
+    return WG_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t wg_kv_pool_create(int32_t n_blocks, int32_t block_size, int32_t max_seqs, wg_kv_pool **out) {
+    NvtxRange nvtx_range("wg_kv_pool_create");
+    if (!out) return WG_ERR_ARG;
+    *out = nullptr;
+    if (n_blocks < 1 || n_blocks > (1 << 30) || block_size < 1 || max_seqs < 1 || max_seqs > WG_MAX_ROWS)
+        return WG_ERR_ARG;
+    wg_kv_pool *p = new (std::nothrow) wg_kv_pool();
+    if (!p) return WG_ERR_ARG;
+    PoolDev &d = p->dev;
+    p->max_seqs = max_seqs;
+    d.n_blocks = n_blocks;
+    d.block_size = block_size;
+    d.n_words = (n_blocks + 31) / 32;
+    const size_t words = ((size_t)d.n_words + WORDS_PER_THREAD - 1) / WORDS_PER_THREAD * WORDS_PER_THREAD;
+    int32_t rc = dev_alloc(&d.ref, (size_t)n_blocks);
+    if (rc == WG_OK) rc = dev_alloc(&d.free_bits, words);
+    if (rc == WG_OK) rc = dev_alloc(&d.taken, (size_t)n_blocks);
+    if (rc == WG_OK) rc = dev_alloc(&d.n_free, 1);
+    if (rc == WG_OK) rc = dev_alloc(&d.n_copies, 1);
+    if (rc == WG_OK) rc = dev_alloc(&d.arrived, 1);
+    for (int32_t **a : {&d.first, &d.old_len, &d.new_len, &d.src, &d.dst, &d.filled})
+        if (rc == WG_OK) rc = dev_alloc(a, (size_t)max_seqs);
+    if (rc == WG_OK && (cudaMemset(d.free_bits, 0, words * sizeof(uint32_t)) != cudaSuccess ||
+                        cudaMemset(d.arrived, 0, sizeof(int32_t)) != cudaSuccess))
+        rc = WG_ERR_CUDA;
+    if (rc == WG_OK) rc = pool_load(p, nullptr, cudaStreamLegacy);
+    if (rc == WG_OK && cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess) rc = WG_ERR_CUDA;
+    if (rc != WG_OK) {
+        wg_kv_pool_free(p);
+        return rc;
+    }
+    *out = p;
+    return WG_OK;
+}
+
+void wg_kv_pool_free(wg_kv_pool *p) {
+    if (!p) return;
+    const PoolDev &d = p->dev;
+    for (void *q : {(void *)d.ref, (void *)d.free_bits, (void *)d.taken, (void *)d.n_free, (void *)d.n_copies,
+                    (void *)d.arrived, (void *)d.first, (void *)d.old_len, (void *)d.new_len, (void *)d.src,
+                    (void *)d.dst, (void *)d.filled})
+        cudaFree(q);
+    delete p;
+}
+
+const int32_t *wg_kv_pool_refs(const wg_kv_pool *p) { return p ? p->dev.ref : nullptr; }
+
+int32_t wg_kv_pool_load(wg_kv_pool *p, const int32_t *refs, void *stream) {
+    NvtxRange nvtx_range("wg_kv_pool_load");
+    if (!p || !refs) return WG_ERR_ARG;
+    return pool_load(p, refs, static_cast<cudaStream_t>(stream));
+}
+
+int32_t wg_kv_pool_n_free(wg_kv_pool *p, int32_t *n_free, void *stream) {
+    if (!p || !n_free) return WG_ERR_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    WG_CUDA(cudaMemcpyAsync(n_free, p->dev.n_free, sizeof(int32_t), cudaMemcpyDeviceToHost, st));
+    WG_CUDA(cudaStreamSynchronize(st));
+    return WG_OK;
+}
+
+int32_t wg_kv_extend(wg_kv_pool *p, int32_t *table, int64_t table_stride, int32_t max_blocks, int32_t *len,
+                     const int32_t *n_new, int32_t n_seq, int32_t *cu, int64_t *slot, int32_t *pos,
+                     int32_t *seq, int32_t n_tokens, int32_t *status, void *stream) {
+    NvtxRange nvtx_range("wg_kv_extend");
+    if (!table_ok(p, table, table_stride, max_blocks, len, n_seq) || !n_new || !cu || n_tokens < 0 ||
+        (n_tokens > 0 && (!slot || !pos || !seq)))
+        return WG_ERR_ARG;
+    const ExtendArgs a{table, table_stride, max_blocks, len, n_new, n_seq, cu, slot, pos, seq, n_tokens, status};
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (n_tokens <= FILL_IN_PLAN) {
+        WG_CUDA(launch_pdl(extend_plan_kernel<true>, dim3(1), dim3(PLAN_THREADS), st, p->dev, a));
+        WG_LAUNCHED();
+        return WG_OK;
+    }
+    WG_CUDA(launch_pdl(extend_plan_kernel<false>, dim3(1), dim3(PLAN_THREADS), st, p->dev, a));
+    WG_LAUNCHED();
+    WG_CUDA(launch_pdl(extend_fill_kernel, dim3((unsigned)((n_tokens + FILL_THREADS - 1) / FILL_THREADS)),
+                       dim3(FILL_THREADS), st, p->dev, a));
+    WG_LAUNCHED();
+    return WG_OK;
+}
+
+int32_t wg_kv_shrink(wg_kv_pool *p, int32_t *table, int64_t table_stride, int32_t max_blocks, int32_t *len,
+                     const int32_t *keep, int32_t n_seq, int32_t *status, void *stream) {
+    NvtxRange nvtx_range("wg_kv_shrink");
+    if (!table_ok(p, table, table_stride, max_blocks, len, n_seq) || !keep) return WG_ERR_ARG;
+    const unsigned blocks = (unsigned)(((int64_t)n_seq * 32 + FILL_THREADS - 1) / FILL_THREADS);
+    WG_CUDA(launch_pdl(shrink_kernel, dim3(blocks), dim3(FILL_THREADS), static_cast<cudaStream_t>(stream),
+                       p->dev, table, table_stride, max_blocks, len, keep, n_seq, status));
+    WG_LAUNCHED();
+    return WG_OK;
+}
+
+int32_t wg_kv_reorder(wg_kv_pool *p, int32_t *table, int64_t table_stride, int32_t max_blocks, int32_t *len,
+                      const int32_t *parent, int32_t n_req, int32_t n_beam, const wg_kv_plane *planes,
+                      int32_t n_planes, int32_t *copy_src, int32_t *copy_dst, int32_t *status, void *stream) {
+    NvtxRange nvtx_range("wg_kv_reorder");
+    if (n_req < 1 || n_beam < 1 || n_beam > WG_BEAM_MAX_BEAMS || (int64_t)n_req * n_beam > WG_MAX_ROWS ||
+        !table_ok(p, table, table_stride, max_blocks, len, n_req * n_beam) || !parent || n_planes < 0 ||
+        (n_planes > 0 && !planes))
+        return WG_ERR_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const MoveArgs a{table, table_stride, max_blocks, len, parent, n_req, n_beam, copy_src, copy_dst, status};
+    const dim3 grid((unsigned)((max_blocks + MOVE_THREADS - 1) / MOVE_THREADS), (unsigned)n_req);
+    WG_CUDA(launch_pdl_smem(move_rows_kernel, grid, dim3(MOVE_THREADS), (size_t)n_beam * MOVE_THREADS * sizeof(int32_t),
+                            st, p->dev, a));
+    WG_LAUNCHED();
+    if (n_planes == 0) return WG_OK;
+    const int64_t most = (int64_t)n_req * (n_beam - 1) * n_planes;   // copies cannot be more
+    if (most == 0) return WG_OK;
+    const int64_t resident = (int64_t)sm_count() * 8;
+    WG_CUDA(launch_pdl(copy_blocks_kernel, dim3((unsigned)(most < resident ? most : resident)), dim3(COPY_THREADS), st,
+                       p->dev, planes, n_planes));
+    WG_LAUNCHED();
+    return WG_OK;
+}
+
+}  // extern "C"
