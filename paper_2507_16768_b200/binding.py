@@ -833,34 +833,43 @@ def wg_beam_backtrack(token, parent, out, stream=None) -> None:
 
 
 # ---- block tables of a paged cache ---------------------------------------------------------------
-class _DeviceArray:
-    """A library-owned int32 array for ``torch.as_tensor`` (which makes a view, not a copy)."""
+class _PoolHandle:
+    """Owns the library's pool object: freed when neither the pool nor a view of its counts is left."""
 
-    def __init__(self, ptr: int, n: int):
+    def __init__(self, n_blocks: int, block_size: int, max_seqs: int):
+        self.value = None
+        h = _vp()
+        _check(_lib.wg_kv_pool_create(n_blocks, block_size, max_seqs, C.byref(h)), "wg_kv_pool_create")
+        self.value = h
+
+    def __del__(self):
+        if self.value and _lib is not None:
+            _lib.wg_kv_pool_free(self.value)
+            self.value = None
+
+
+class _DeviceArray:
+    """A library-owned int32 array for ``torch.as_tensor``, which makes a view of it and keeps this
+    object, and with it the memory, for as long as the view lives."""
+
+    def __init__(self, owner, ptr: int, n: int):
+        self._owner = owner
         self.__cuda_array_interface__ = {"data": (ptr, False), "shape": (n,), "typestr": "<i4", "version": 2}
 
 
 class KvPool:
-    """wg_kv_pool: the blocks of a paged cache, counted by the table rows that name them."""
+    """wg_kv_pool: the blocks of a paged cache, counted by the table rows that name them.
+
+    ``ref`` is an int32 [n_blocks] view of the counts, to be read only."""
 
     def __init__(self, n_blocks: int, block_size: int, max_seqs: int):
         import torch
         self.n_blocks, self.block_size, self.max_seqs = int(n_blocks), int(block_size), int(max_seqs)
         self.device = torch.cuda.current_device()
-        h = _vp()
-        _check(_lib.wg_kv_pool_create(self.n_blocks, self.block_size, self.max_seqs, C.byref(h)),
-               "wg_kv_pool_create")
-        self.handle = h
-        self._ref = None
-
-    @property
-    def ref(self):
-        """int32 [n_blocks] view of the counts, to be read only; it must not outlive the pool."""
-        if self._ref is None:
-            import torch
-            self._ref = torch.as_tensor(_DeviceArray(_lib.wg_kv_pool_refs(self.handle), self.n_blocks),
-                                        device=f"cuda:{self.device}")
-        return self._ref
+        self._owner = _PoolHandle(self.n_blocks, self.block_size, self.max_seqs)
+        self.handle = self._owner.value
+        self.ref = torch.as_tensor(_DeviceArray(self._owner, _lib.wg_kv_pool_refs(self.handle), self.n_blocks),
+                                   device=f"cuda:{self.device}")
 
     def load(self, ref, stream=None) -> None:
         """Sets the counts from an int32 device tensor (a saved ``ref``)."""
@@ -872,15 +881,6 @@ class KvPool:
         n = _i32()
         _check(_lib.wg_kv_pool_n_free(self.handle, C.byref(n), _stream_ptr(stream)), "wg_kv_pool_n_free")
         return n.value
-
-    def close(self):
-        if getattr(self, "handle", None) and _lib is not None:
-            self._ref = None
-            _lib.wg_kv_pool_free(self.handle)
-            self.handle = None
-
-    def __del__(self):
-        self.close()
 
 
 class SlotMap:

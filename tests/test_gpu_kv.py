@@ -213,6 +213,25 @@ def test_planes_of_odd_sizes_and_long_rows(wg):
     both.reorder([[3, 2, 3, 2]], [wide, odd])
 
 
+def test_counts_outlive_their_pool(wg):
+    """A view of the counts keeps the memory it shows."""
+    import gc
+    pool = wg.KvPool(1000, 4, 2)
+    pool.load(i32(np.arange(1000)))
+    view = pool.ref
+    owner = pool._owner
+    del pool
+    gc.collect()
+    assert owner.value and view.tolist() == list(range(1000))
+    import weakref
+    gone = weakref.ref(owner)
+    del owner
+    assert gone() is not None
+    del view
+    gc.collect()
+    assert gone() is None
+
+
 def test_refusals(wg):
     for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, 1, 65536), (-5, 1, 1)):
         with pytest.raises(wg.WgError):
