@@ -17,6 +17,8 @@ def __getattr__(name):
     if name == "binding":
         return binding
     try:
-        return getattr(binding, name)
+        value = getattr(binding, name)
     except AttributeError:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}") from None
+    globals()[name] = value      # found without this function from now on
+    return value

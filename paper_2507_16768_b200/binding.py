@@ -708,6 +708,15 @@ def wg_decode_step_host(ctx: Context, gid, sid, logits_host, logits_dev, bitmask
         "wg_decode_step_host")
 
 
+def _on_stream(stream, device: int):
+    """The raw stream of a call: the given one, else the current one of the device that the call's arrays
+    are on (asked for by number: making a stream object costs more than a small launch)."""
+    if stream is not None:
+        return stream.cuda_stream
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 # ---- constrained beam search ---------------------------------------------------------------------
 class Beam:
     """wg_beam: scratch of the selection for up to ``max_requests`` requests of ``max_beams`` beams."""
@@ -775,7 +784,7 @@ class BeamPlan:
         self._tail = (mask, mstride, _vec(score, rows, torch.float32, "score", dev),
                       _vec(finished, rows, torch.int32, "finished", dev), int(eos_id), self.n_req,
                       self.n_beam, n_out, int(norm), so, po, to)
-        self._stream = None if stream is None else _stream_ptr(stream)
+        self._stream = stream
         self._dtypes = {torch.bfloat16: WG_DTYPE_BF16, torch.float32: WG_DTYPE_FP32}
         self._fn = _lib.wg_beam_select
 
@@ -786,7 +795,7 @@ class BeamPlan:
         if logits.dtype not in self._dtypes:
             raise TypeError(f"logits must be bfloat16 or float32, not {logits.dtype}")
         rc = self._fn(self._head, logits.data_ptr(), self._dtypes[logits.dtype], logits.stride(0), *self._tail,
-                      self._stream or _stream_ptr(None))
+                      _on_stream(self._stream, self._device))
         if rc != WG_OK:
             raise WgError(rc, "wg_beam_select")
 
@@ -811,25 +820,26 @@ def wg_beam_step(beam: Beam, ctx: Context, n_beam: int, gid, sid, score, logits,
     _check(_lib.wg_beam_step(beam.handle, ctx.handle, g, s, _vec(score, rows, torch.float32, "score", dev), n_req,
                              n_beam, lp, dtype, stride, mp, mstride, int(norm),
                              _vec(parent_out, rows, torch.int32, "parent_out", dev), tok, st, int(flags),
-                             _stream_ptr(stream)), "wg_beam_step")
+                             _on_stream(stream, dev)), "wg_beam_step")
 
 
 def wg_beam_backtrack(token, parent, out, stream=None) -> None:
     """``token``, ``parent``: [n_steps, n_req, n_beam] as the steps returned them; ``out``:
     [n_req, n_beam, n_steps], the sequence of every final beam."""
     import torch
-    if token.dim() != 3 or tuple(parent.shape) != tuple(token.shape):
+    if token.dim() != 3 or parent.shape != token.shape:
         raise ValueError("token and parent must be [n_steps, n_req, n_beam]")
-    T, R, K = (int(n) for n in token.shape)
-    dev = token.device.index if token.is_cuda else None
-    if tuple(out.shape) != (R, K, T):
+    T, R, K = token.shape
+    dev = token.device.index
+    if out.shape != (R, K, T):
         raise ValueError(f"out must be [{R}, {K}, {T}]")
-    ptr = []
     for t, what in ((token, "token"), (parent, "parent"), (out, "out")):
-        ptr.append(_dev_ptr(t, torch.int32, what, dev))
-        if not t.is_contiguous():
-            raise ValueError(f"{what} must be contiguous")
-    _check(_lib.wg_beam_backtrack(ptr[0], ptr[1], T, R, K, ptr[2], _stream_ptr(stream)), "wg_beam_backtrack")
+        if not t.is_cuda or t.dtype != torch.int32:
+            raise TypeError(f"{what} must be an int32 CUDA tensor")
+        if t.device.index != dev or not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous, all on one device")
+    _check(_lib.wg_beam_backtrack(token.data_ptr(), parent.data_ptr(), T, R, K, out.data_ptr(),
+                                  _on_stream(stream, dev)), "wg_beam_backtrack")
 
 
 # ---- block tables of a paged cache ---------------------------------------------------------------
@@ -875,11 +885,11 @@ class KvPool:
         """Sets the counts from an int32 device tensor (a saved ``ref``)."""
         import torch
         _check(_lib.wg_kv_pool_load(self.handle, _vec(ref, self.n_blocks, torch.int32, "ref", self.device),
-                                    _stream_ptr(stream)), "wg_kv_pool_load")
+                                    _on_stream(stream, self.device)), "wg_kv_pool_load")
 
     def n_free(self, stream=None) -> int:
         n = _i32()
-        _check(_lib.wg_kv_pool_n_free(self.handle, C.byref(n), _stream_ptr(stream)), "wg_kv_pool_n_free")
+        _check(_lib.wg_kv_pool_n_free(self.handle, C.byref(n), _on_stream(stream, self.device)), "wg_kv_pool_n_free")
         return n.value
 
 
@@ -930,7 +940,7 @@ class KvTables:
     def __init__(self, pool: KvPool, table, lens, status=None):
         import torch
         dev = pool.device
-        self._keep = (pool, table, lens, status)
+        self._i32 = torch.int32
         self.pool, self.table, self.lens, self.status, self.device = pool, table, lens, status, dev
         self.n_seq = int(table.shape[0])
         if self.n_seq > pool.max_seqs:
@@ -941,8 +951,7 @@ class KvTables:
         self._status = _vec(status, self.n_seq, torch.int32, "status", dev)
 
     def _rows(self, t, what):
-        import torch
-        if not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != self.n_seq \
+        if not t.is_cuda or t.dtype != self._i32 or not t.is_contiguous() or t.numel() != self.n_seq \
                 or t.device.index != self.device:
             raise ValueError(f"{what} must be a contiguous int32 tensor of {self.n_seq} entries on "
                              f"cuda:{self.device}")
@@ -953,7 +962,7 @@ class KvTables:
         if slots.n_seq != self.n_seq or slots.device != self.device:
             raise ValueError("slots were made for another batch or device")
         rc = _lib.wg_kv_extend(*self._head, self._rows(n_new, "n_new"), self.n_seq, *slots._args, self._status,
-                               _stream_ptr(stream))
+                               _on_stream(stream, self.device))
         if rc != WG_OK:
             raise WgError(rc, "wg_kv_extend")
 
@@ -961,24 +970,23 @@ class KvTables:
         """wg_kv_shrink: cuts the sequences to ``keep`` [n_seq] tokens.  ``status``, where given, gets
         WG_ERR_ARG for a ``keep`` outside 0 .. the sequence's length (which is then left alone)."""
         st = self._rows(status, "status") if status is not None else None
-        rc = _lib.wg_kv_shrink(*self._head, self._rows(keep, "keep"), self.n_seq, st, _stream_ptr(stream))
+        rc = _lib.wg_kv_shrink(*self._head, self._rows(keep, "keep"), self.n_seq, st, _on_stream(stream, self.device))
         if rc != WG_OK:
             raise WgError(rc, "wg_kv_shrink")
 
     def reorder(self, parent, planes: Optional[KvPlanes] = None, copy_src=None, copy_dst=None,
                 stream=None) -> None:
         """wg_kv_reorder: ``parent`` [n_req, n_beam] as a selection returned it."""
-        import torch
         if parent.dim() != 2:
             raise ValueError("parent must be [n_req, n_beam]")
         if planes is not None and (planes.block_size != self.pool.block_size or planes.n_blocks < self.pool.n_blocks
                                    or planes.device != self.device):
             raise ValueError("planes were made for another pool")
-        n_req, n_beam = (int(n) for n in parent.shape)
+        n_req, n_beam = parent.shape
         rc = _lib.wg_kv_reorder(*self._head, self._rows(parent, "parent"), n_req, n_beam,
                                 *((None, 0) if planes is None else planes._args),
-                                _vec(copy_src, self.n_seq, torch.int32, "copy_src", self.device),
-                                _vec(copy_dst, self.n_seq, torch.int32, "copy_dst", self.device), self._status,
-                                _stream_ptr(stream))
+                                None if copy_src is None else self._rows(copy_src, "copy_src"),
+                                None if copy_dst is None else self._rows(copy_dst, "copy_dst"), self._status,
+                                _on_stream(stream, self.device))
         if rc != WG_OK:
             raise WgError(rc, "wg_kv_reorder")

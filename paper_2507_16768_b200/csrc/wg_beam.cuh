@@ -18,10 +18,9 @@
 
 constexpr int BEAM_THREADS = 256;           // scan
 constexpr int BEAM_WARPS = BEAM_THREADS / 32;
-constexpr int BEAM_SPANS_PER_WARP = 4;      // a block covers at most 8 * 4 spans of 1024 tokens
 constexpr int BEAM_CHUNK = 256;             // tokens per chunk maximum
 constexpr int PICK_THREADS = 512;
-constexpr int PICK_GROUPS = 128;            // four threads each
+constexpr int PICK_GROUPS = 128;            // at most
 constexpr int PICK_LIST = 512;              // candidates that are ranked against each other
 
 struct BeamArgs {
@@ -33,11 +32,13 @@ struct BeamArgs {
     const int32_t *finished;  // or NULL
     const int32_t *gid, *sid; // with a context: the rows' states (finished = DONE)
     int32_t n_beam, V, W, n_out, eos, norm;
-    int32_t spans_per_block;
-    int32_t n_parts;          // (max, sum) pairs per row: scan blocks per row * BEAM_WARPS
-    int32_t chunk_stride;     // chunk maxima per row (four per span)
+    int32_t per_item, items_per_row;  // steps a warp takes at a time
+    uint32_t n_items;
+    int32_t chunk_stride;     // chunk maxima per row, a multiple of 4
+    int32_t chunk_log2;       // the pick's threads side by side on a row: 32 .. 512
     float *chunk_max;         // [rows][chunk_stride]
-    float2 *parts;            // [rows][n_parts]
+    float2 *parts;            // [n_items] (max, sum) of every item
+    int32_t *next_item;       // items taken beyond the first of every warp; zero between calls
 };
 
 // What a step under grammars does with the selection.
@@ -208,121 +209,124 @@ __device__ __forceinline__ void piece_exp(const uint32_t (&w)[4], float m, float
 }
 
 // ---------------------------------------------------------------------------------------
-// Scan.  grid = (blocks per row, rows); a warp takes spans of 1024 positions, 2 KB (four 16-byte
-// loads per lane) at a time, the next 2 KB requested before the current are worked on.
+// Scan.  A warp works in steps of 2 KB of one row (four 16-byte loads per lane): 1024 bf16 or 512 fp32
+// positions, and takes items of a.per_item consecutive steps of a row from a device counter (rows
+// differ a lot: a finished one costs nothing, a literal state a few sectors, a free-text slot every
+// logit).  Within an item the mask words of two steps and the logits of one are in flight while a
+// step is worked on.
 // ---------------------------------------------------------------------------------------
-template <typename E, int NORM, bool CTX>
-__global__ void __launch_bounds__(BEAM_THREADS)
-beam_scan_kernel(BeamArgs a, CtxDev ctx) {
-    constexpr int EPC = ElemTraits<E>::PER_CHUNK;
-    constexpr int GROUP = 4;                                  // loads per lane and step
-    constexpr int STEPS = 1024 / (32 * EPC * GROUP);          // steps per span: 1 (bf16), 2 (fp32)
-    constexpr int PER_CHUNK = BEAM_CHUNK / (32 * EPC);        // loads per chunk: 1, 2
-    constexpr int CHUNKS = GROUP / PER_CHUNK;                 // chunks per step: 4, 2
-    constexpr uint32_t ALL = (1u << EPC) - 1u;
-    pdl_enter();
-    const int row = blockIdx.y;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (beam_row_kind<CTX>(a, ctx, row, a.score[row]) != BEAM_ROW_LIVE) return;
-    const RowView<E> x(a.logits, a.row_stride, row, a.V);
-    const MaskSource mask = mask_source<CTX>(a, ctx, row);
-    const int n_spans = (a.V + x.off + 1023) / 1024;
-    const int first = blockIdx.x * a.spans_per_block + warp;
-    const int end = min((int)(blockIdx.x + 1) * a.spans_per_block, n_spans);
-    uint32_t words[BEAM_SPANS_PER_WARP];
-#pragma unroll
-    for (int k = 0; k < BEAM_SPANS_PER_WARP; ++k) {
-        const int span = first + k * BEAM_WARPS;
-        words[k] = span < end ? shifted_word(mask, span * 32 + lane, x.off) : 0u;
-    }
-    float *chunk_row = a.chunk_max + (int64_t)row * a.chunk_stride;
-    float m = -INFINITY, s0 = 0.f, s1 = 0.f;   // m is the same in all lanes
+template <typename E>
+struct ScanShape {
+    static constexpr int EPC = ElemTraits<E>::PER_CHUNK;
+    static constexpr int LOADS = 4;                             // per lane and step
+    static constexpr int STEP = LOADS * 32 * EPC;               // positions: 1024, 512
+    static constexpr int CHUNKS = STEP / BEAM_CHUNK;            // 4, 2
+    static constexpr int PER_CHUNK = LOADS / CHUNKS;            // loads per chunk: 1, 2
+};
 
-    uint4 next[GROUP];
-    // requests the loads of step q of the span in slot k
-    auto request = [&](int k, int q) {
-        const int span = first + k * BEAM_WARPS;
+template <typename E, int NORM, bool CTX>
+__global__ void __launch_bounds__(BEAM_THREADS, 4)
+beam_scan_kernel(BeamArgs a, CtxDev ctx) {
+    using S = ScanShape<E>;
+    constexpr uint32_t ALL = (1u << S::EPC) - 1u;
+    pdl_enter();
+    const int lane = threadIdx.x & 31;
+    uint32_t item = blockIdx.x * BEAM_WARPS + (threadIdx.x >> 5);
+    while (item < a.n_items) {
+        uint32_t taken = 0;
+        if (lane == 0) taken = (uint32_t)atomicAdd(a.next_item, 1);
+        const int row = (int)(item / (uint32_t)a.items_per_row);
+        const int part = (int)(item - (uint32_t)row * (uint32_t)a.items_per_row);
+        const RowView<E> x(a.logits, a.row_stride, row, a.V);
+        const MaskSource mask = mask_source<CTX>(a, ctx, row);
+        const int n_steps = (a.V + x.off + S::STEP - 1) / S::STEP;
+        const int first = part * a.per_item, end = min(first + a.per_item, n_steps);
+        // lane l holds the mask word of positions 32 * l .. of the step
+        auto step_word = [&](int s) -> uint32_t {
+            return s < end && lane < S::STEP / 32 ? shifted_word(mask, s * (S::STEP / 32) + lane, x.off) : 0u;
+        };
+        uint32_t word = step_word(first), word1 = step_word(first + 1);
+        if (beam_row_kind<CTX>(a, ctx, row, a.score[row]) == BEAM_ROW_LIVE) {
+            uint4 next[S::LOADS];
+            auto request = [&](int s, uint32_t words) {
 #pragma unroll
-        for (int i = 0; i < GROUP; ++i) {
-            const int c = (q * GROUP + i) * 32 + lane;        // piece within the span
-            const uint32_t word = __shfl_sync(0xFFFFFFFFu, words[k], c * EPC / 32);
-            const uint32_t bits = (word >> (c * EPC % 32)) & ALL;
-            next[i] = make_uint4(0, 0, 0, 0);
-            if (span < end && (NORM == WG_BEAM_NORM_FULL || bits != 0u))
-                next[i] = x.piece(span * 1024 + c * EPC);
-        }
-    };
-    request(0, 0);
-#pragma unroll
-    for (int k = 0; k < BEAM_SPANS_PER_WARP; ++k) {
-        const int span = first + k * BEAM_WARPS;
-#pragma unroll
-        for (int q = 0; q < STEPS; ++q) {
-            uint4 v[GROUP];
-#pragma unroll
-            for (int i = 0; i < GROUP; ++i) v[i] = next[i];
-            if (q + 1 < STEPS) request(k, q + 1);
-            else if (k + 1 < BEAM_SPANS_PER_WARP) request(k + 1, 0);
-            if (span >= end) continue;
-            const bool some = __ballot_sync(0xFFFFFFFFu, words[k] != 0u) != 0u;
-            float best[CHUNKS];
-#pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) best[i] = -INFINITY;
-            if (NORM == WG_BEAM_NORM_FULL || some) {
-                uint32_t w[GROUP][4];
-                float top = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < GROUP; ++i) {
-                    const int c = (q * GROUP + i) * 32 + lane;
-                    const uint32_t word = __shfl_sync(0xFFFFFFFFu, words[k], c * EPC / 32);
-                    const uint32_t bits = (word >> (c * EPC % 32)) & ALL;
-                    uint32_t y[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-                    if (NORM == WG_BEAM_NORM_FULL) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) w[i][j] = y[j];
-                        top = fmaxf(top, piece_max<E>(y));
-                        mask_piece<E>(y, bits);
-                    } else {
-                        mask_piece<E>(y, bits);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) w[i][j] = y[j];
-                    }
-                    best[i / PER_CHUNK] = fmaxf(best[i / PER_CHUNK], piece_max<E>(y));
+                for (int i = 0; i < S::LOADS; ++i) {
+                    const int c = i * 32 + lane;              // piece within the step
+                    const uint32_t bits = __shfl_sync(0xFFFFFFFFu, words, c * S::EPC / 32) >> (c * S::EPC % 32) & ALL;
+                    next[i] = make_uint4(0, 0, 0, 0);
+                    if (NORM == WG_BEAM_NORM_FULL || bits != 0u) next[i] = x.piece(s * S::STEP + c * S::EPC);
                 }
+            };
+            float *chunk_row = a.chunk_max + (int64_t)row * a.chunk_stride;
+            float m = -INFINITY, s0 = 0.f, s1 = 0.f;          // m is the same in all lanes
+            if (first < end) request(first, word);
+            for (int s = first; s < end; ++s) {
+                uint4 v[S::LOADS];
 #pragma unroll
-                for (int i = 0; i < CHUNKS; ++i) best[i] = warp_max(best[i]);
-                if (NORM != WG_BEAM_NORM_NONE) {
-                    float high = m;
-                    if (NORM == WG_BEAM_NORM_FULL) {
-                        high = fmaxf(high, warp_max(top));
-                    } else {
+                for (int i = 0; i < S::LOADS; ++i) v[i] = next[i];
+                const uint32_t words = word;
+                word = word1;
+                word1 = step_word(s + 2);
+                if (s + 1 < end) request(s + 1, word);
+                float best[S::CHUNKS];
 #pragma unroll
-                        for (int i = 0; i < CHUNKS; ++i) high = fmaxf(high, best[i]);
-                    }
-                    if (high > m) {                            // uniform
-                        const float scale = exp2_fast((m - high) * LOG2_E);
-                        s0 *= scale;
-                        s1 *= scale;
-                        m = high;
-                    }
-                    if (m > -INFINITY) {
+                for (int i = 0; i < S::CHUNKS; ++i) best[i] = -INFINITY;
+                if (NORM == WG_BEAM_NORM_FULL || __any_sync(0xFFFFFFFFu, words != 0u)) {
+                    uint32_t w[S::LOADS][4];
+                    float top = -INFINITY;
 #pragma unroll
-                        for (int i = 0; i < GROUP; ++i) piece_exp<E>(w[i], m, s0, s1);
+                    for (int i = 0; i < S::LOADS; ++i) {
+                        const int c = i * 32 + lane;
+                        const uint32_t bits = __shfl_sync(0xFFFFFFFFu, words, c * S::EPC / 32) >> (c * S::EPC % 32) & ALL;
+                        uint32_t y[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                        if (NORM == WG_BEAM_NORM_FULL) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) w[i][j] = y[j];
+                            top = fmaxf(top, piece_max<E>(y));
+                            mask_piece<E>(y, bits);
+                        } else {
+                            mask_piece<E>(y, bits);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) w[i][j] = y[j];
+                        }
+                        best[i / S::PER_CHUNK] = fmaxf(best[i / S::PER_CHUNK], piece_max<E>(y));
                     }
+#pragma unroll
+                    for (int i = 0; i < S::CHUNKS; ++i) best[i] = warp_max(best[i]);
+                    if (NORM != WG_BEAM_NORM_NONE) {
+                        float high = m;
+                        if (NORM == WG_BEAM_NORM_FULL) {
+                            high = fmaxf(high, warp_max(top));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < S::CHUNKS; ++i) high = fmaxf(high, best[i]);
+                        }
+                        if (high > m) {                        // uniform
+                            const float scale = exp2_fast((m - high) * LOG2_E);
+                            s0 *= scale;
+                            s1 *= scale;
+                            m = high;
+                        }
+                        if (m > -INFINITY) {
+#pragma unroll
+                            for (int i = 0; i < S::LOADS; ++i) piece_exp<E>(w[i], m, s0, s1);
+                        }
+                    }
+                }
+                if (lane == 0) {
+                    float *dst = chunk_row + s * S::CHUNKS;
+                    if constexpr (S::CHUNKS == 4) *reinterpret_cast<float4 *>(dst) = make_float4(best[0], best[1], best[2], best[3]);
+                    else *reinterpret_cast<float2 *>(dst) = make_float2(best[0], best[1]);
                 }
             }
-            if (lane == 0) {
-                float *dst = chunk_row + span * 4 + q * CHUNKS;
-                if (CHUNKS == 4) *reinterpret_cast<float4 *>(dst) = make_float4(best[0], best[1], best[2 % CHUNKS], best[3 % CHUNKS]);
-                else *reinterpret_cast<float2 *>(dst) = make_float2(best[0], best[1]);
+            if (NORM != WG_BEAM_NORM_NONE) {
+                float s = s0 + s1;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+                if (lane == 0) a.parts[item] = make_float2(m, s);
             }
         }
-    }
-    if (NORM != WG_BEAM_NORM_NONE) {
-        float s = s0 + s1;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-        if (lane == 0) a.parts[(int64_t)row * a.n_parts + blockIdx.x * BEAM_WARPS + warp] = make_float2(m, s);
+        item = gridDim.x * BEAM_WARPS + __shfl_sync(0xFFFFFFFFu, taken, 0);
     }
 }
 
@@ -342,15 +346,17 @@ __device__ __forceinline__ unsigned long long pack_key(uint32_t key, uint32_t id
 }
 
 struct PickShared {
-    unsigned long long list[PICK_LIST];
-    uint32_t group[PICK_GROUPS];
-    uint32_t chunk[WG_BEAM_MAX_OUT];       // the chosen chunks, best first
+    // two lists of candidates (chunks, then elements), zero behind the last one
+    alignas(16) unsigned long long list[2][PICK_LIST];
+    alignas(16) uint32_t group[PICK_GROUPS];
+    uint32_t chunk[WG_BEAM_MAX_OUT];       // the chosen chunks
     int32_t parent[WG_BEAM_MAX_OUT], token[WG_BEAM_MAX_OUT];
     float score[WG_BEAM_MAX_BEAMS], lse[WG_BEAM_MAX_BEAMS];
     int32_t kind[WG_BEAM_MAX_BEAMS];
-    int32_t n_written[WG_BEAM_MAX_BEAMS];  // chunk maxima the scan wrote for the row
+    int32_t n_written[WG_BEAM_MAX_BEAMS];  // chunk maxima the scan wrote for the row (0: not live)
+    MaskSource mask[WG_BEAM_MAX_BEAMS];
     uint32_t bound;                        // key that n_out candidates reach
-    int32_t n;
+    int32_t n[2];
     int32_t count[PICK_THREADS / 32];
 };
 
@@ -366,23 +372,20 @@ __device__ __forceinline__ int block_sum(PickShared &sh, int v) {
     return total;
 }
 
-// Puts the candidates that `each` enumerates into sh.list: all that reach `bound`, or, where
-// those are more than the list holds (many equal scores), exactly the n_out largest, found by
-// bisection over the packed keys.  `each(f)` calls f(packed key) for the calling thread's share; packed
-// keys are unlike one another.  Returns how many are listed.
+// Puts the candidates that `each` enumerates into the (empty) list: all that reach `bound`, or, where
+// those are more than it holds (many equal scores), exactly the n_out largest, found by bisection
+// over the packed keys.  `each(f)` calls f(packed key) for the calling thread's share; packed keys
+// are unlike one another.  Returns how many are listed.
 template <typename Each>
-__device__ __forceinline__ int collect(PickShared &sh, uint32_t bound, int n_out, const Each &each) {
-    if (threadIdx.x == 0) sh.n = 0;
-    __syncthreads();
+__device__ __forceinline__ int collect(PickShared &sh, int which, uint32_t bound, int n_out, const Each &each) {
+    const auto push = [&](unsigned long long k) {
+        const int at = atomicAdd(&sh.n[which], 1);
+        if (at < PICK_LIST) sh.list[which][at] = k;
+    };
     const unsigned long long low = (unsigned long long)bound << 32;
-    each([&](unsigned long long k) {
-        if (k >= low) {
-            const int at = atomicAdd(&sh.n, 1);
-            if (at < PICK_LIST) sh.list[at] = k;
-        }
-    });
+    each([&](unsigned long long k) { if (k >= low) push(k); });
     __syncthreads();
-    const int n = sh.n;
+    const int n = sh.n[which];
     if (n <= PICK_LIST) return n;
     unsigned long long cut = 0ull;         // the largest value that n_out keys reach
     for (int bit = 63; bit >= 0; --bit) {
@@ -391,51 +394,84 @@ __device__ __forceinline__ int collect(PickShared &sh, uint32_t bound, int n_out
         each([&](unsigned long long k) { mine += k >= trial; });
         if (block_sum(sh, mine) >= n_out) cut = trial;
     }
-    if (threadIdx.x == 0) sh.n = 0;
+    if (threadIdx.x == 0) sh.n[which] = 0;
+    sh.list[which][threadIdx.x] = 0ull;
     __syncthreads();
-    each([&](unsigned long long k) {
-        if (k >= cut) {
-            const int at = atomicAdd(&sh.n, 1);
-            if (at < PICK_LIST) sh.list[at] = k;
-        }
-    });
+    each([&](unsigned long long k) { if (k >= cut) push(k); });
     __syncthreads();
-    return min(sh.n, PICK_LIST);
+    return sh.n[which];
 }
 
 // Calls f(rank, packed key) for the listed candidates of rank below n_out (0 = the largest).
 template <typename F>
-__device__ __forceinline__ void ranked(const PickShared &sh, int n, int n_out, const F &f) {
-    for (int i = threadIdx.x; i < n; i += PICK_THREADS) {
-        const unsigned long long mine = sh.list[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += sh.list[j] > mine;
-        if (rank < n_out) f(rank, mine);
+__device__ __forceinline__ void ranked(const PickShared &sh, int which, int n, int n_out, const F &f) {
+    if ((int)threadIdx.x >= n) return;
+    const unsigned long long mine = sh.list[which][threadIdx.x];
+    int rank = 0;
+    for (int j = 0; j < n; j += 8) {       // (the list is a multiple of 8 long, zeros at its end)
+#pragma unroll
+        for (int u = 0; u < 8; u += 2) {
+            const ulonglong2 two = *reinterpret_cast<const ulonglong2 *>(&sh.list[which][j + u]);
+            rank += (two.x > mine) + (two.y > mine);
+        }
     }
+    if (rank < n_out) f(rank, mine);
 }
+static_assert(PICK_LIST == PICK_THREADS, "a thread per listed candidate");
 
+// The block's n_out best candidates, listed in sh.list[1]; returns how many there are (they may be
+// more: rank them).
 template <typename E, bool CTX>
-__device__ __forceinline__ void beam_pick(PickShared &sh, const BeamArgs &a, const CtxDev &ctx, int req) {
+__device__ __forceinline__ int beam_pick(PickShared &sh, const BeamArgs &a, const CtxDev &ctx, int req) {
     constexpr int EPC = ElemTraits<E>::PER_CHUNK;
     constexpr int PER_CHUNK = BEAM_CHUNK / (32 * EPC);
+    constexpr int HELD = 8;                // chunk maxima a thread keeps in registers
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int K = a.n_beam, row0 = req * K;
     const int n_chunks = a.chunk_stride;
-    // ---- the rows' log-sum-exp from the warps' pairs
+    // A thread's chunks: column c0, c0 + width, .. of beam b0, b0 + side, ..  They are asked for before
+    // anything else is known, so that their latency passes together with that of the rows' facts.
+    const int width = 1 << a.chunk_log2, side = PICK_THREADS >> a.chunk_log2;
+    const int c0 = threadIdx.x & (width - 1), b0 = threadIdx.x >> a.chunk_log2;
+    const float *maxima = a.chunk_max + (int64_t)row0 * n_chunks;
+    const auto onward = [&](int &b, int &c) {
+        c += width;
+        if (c >= n_chunks) {
+            c = c0;
+            b += side;
+        }
+    };
+    const int start_b = c0 < n_chunks ? b0 : K;
+    float held[HELD];
+    {
+        int b = start_b, c = c0;
+#pragma unroll
+        for (int j = 0; j < HELD; ++j) {
+            held[j] = 0.f;
+            if (b < K) held[j] = maxima[(int64_t)b * n_chunks + c];
+            onward(b, c);
+        }
+    }
+    sh.list[0][threadIdx.x] = sh.list[1][threadIdx.x] = 0ull;
+    if (threadIdx.x < 2) sh.n[threadIdx.x] = 0;
+    if (threadIdx.x == 2) sh.bound = 1u;
+    // ---- the rows: their log-sum-exp from the items' pairs
     for (int b = warp; b < K; b += PICK_THREADS / 32) {
         const int row = row0 + b;
         const float score = a.score[row];
-        const int kind = beam_row_kind<CTX>(a, ctx, row, score);
-        float lse = 0.f;
-        if (kind == BEAM_ROW_LIVE && a.norm != WG_BEAM_NORM_NONE) {
-            float m = -INFINITY, s = 0.f;
-            for (int i = lane; i < a.n_parts; i += 32) {
-                const float2 p = a.parts[(int64_t)row * a.n_parts + i];
+        float m = -INFINITY, s = 0.f, lse = 0.f;
+        if (a.norm != WG_BEAM_NORM_NONE) {     // (for a row that is not live the pairs are left over: not used)
+#pragma unroll 4
+            for (int i = lane; i < a.items_per_row; i += 32) {
+                const float2 p = a.parts[(int64_t)row * a.items_per_row + i];
                 const float high = fmaxf(m, p.x);
-                if (high > -INFINITY)      // (a pair that saw nothing is (-inf, 0))
+                if (high > -INFINITY)          // (a pair that saw nothing is (-inf, 0))
                     s = s * exp2_fast((m - high) * LOG2_E) + p.y * exp2_fast((p.x - high) * LOG2_E);
                 m = high;
             }
+        }
+        const int kind = beam_row_kind<CTX>(a, ctx, row, score);
+        if (a.norm != WG_BEAM_NORM_NONE) {
             const float high = warp_max(m);
             s = high > -INFINITY ? s * exp2_fast((m - high) * LOG2_E) : 0.f;
 #pragma unroll
@@ -443,73 +479,97 @@ __device__ __forceinline__ void beam_pick(PickShared &sh, const BeamArgs &a, con
             lse = high + logf(s);
         }
         if (lane == 0) {
+            const RowView<E> x(a.logits, a.row_stride, row, a.V);
             sh.score[b] = score;
             sh.lse[b] = lse;
             sh.kind[b] = kind;
-            const RowView<E> x(a.logits, a.row_stride, row, a.V);
             sh.n_written[b] = kind == BEAM_ROW_LIVE ? (a.V + x.off + BEAM_CHUNK - 1) / BEAM_CHUNK : 0;
+            sh.mask[b] = mask_source<CTX>(a, ctx, row);
         }
     }
     __syncthreads();
     // ---- the n_out best chunks
-    const int n_keys = K * n_chunks;
-    auto chunk_key = [&](int i) -> uint32_t {
-        const int b = i / n_chunks;
-        const int c = i - b * n_chunks;
-        if (c >= sh.n_written[b]) return 0u;
-        return score_key(sh.score[b] + (a.chunk_max[(int64_t)(row0 + b) * n_chunks + c] - sh.lse[b]));
+    const auto chunk_key = [&](int b, int c, float maximum) -> uint32_t {
+        return c < sh.n_written[b] ? score_key(sh.score[b] + (maximum - sh.lse[b])) : 0u;
     };
-    // a lower bound for the n_out-th largest: that of the maxima of 128 groups of threads
-    uint32_t top = 0;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < n_keys; i += PICK_THREADS) top = max(top, chunk_key(i));
-    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-    if ((lane & 3) == 0) sh.group[threadIdx.x >> 2] = top;
+    uint32_t key[HELD], top = 0;
+    int rest_b = start_b, rest_c = c0;         // the first chunk that is not held
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) {
+        key[j] = rest_b < K ? chunk_key(rest_b, rest_c, held[j]) : 0u;
+        top = max(top, key[j]);
+        onward(rest_b, rest_c);
+    }
+    const auto each_chunk = [&](auto f) {
+        int b = start_b, c = c0;
+#pragma unroll
+        for (int j = 0; j < HELD; ++j) {
+            f(pack_key(key[j], (uint32_t)(b * n_chunks + c)));
+            onward(b, c);
+        }
+        while (b < K) {
+            f(pack_key(chunk_key(b, c, maxima[(int64_t)b * n_chunks + c]), (uint32_t)(b * n_chunks + c)));
+            onward(b, c);
+        }
+    };
+    for (int b = rest_b, c = rest_c; b < K; onward(b, c))
+        top = max(top, chunk_key(b, c, maxima[(int64_t)b * n_chunks + c]));
+    // A lower bound for the n_out-th largest: that of the maxima of some groups of threads, at least
+    // twice as many groups as are wanted (few of the best then share a group, and few keys more than
+    // n_out reach the bound).
+    const int n_groups = a.n_out <= 16 ? 32 : a.n_out <= 32 ? 64 : 128;
+    for (int o = 1; o < PICK_THREADS / n_groups; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    if ((threadIdx.x & (PICK_THREADS / n_groups - 1)) == 0) sh.group[threadIdx.x / (PICK_THREADS / n_groups)] = top;
     __syncthreads();
-    if (threadIdx.x < PICK_GROUPS) {
+    if ((int)threadIdx.x < n_groups) {
         const uint32_t mine = sh.group[threadIdx.x];
         int rank = 0;
 #pragma unroll 8
-        for (int j = 0; j < PICK_GROUPS; ++j)
-            rank += sh.group[j] > mine || (sh.group[j] == mine && j < (int)threadIdx.x);
-        if (rank == a.n_out - 1) sh.bound = max(mine, 1u);
+        for (int j = 0; j < n_groups; j += 4) {
+            const uint4 g = *reinterpret_cast<const uint4 *>(&sh.group[j]);
+            const int t = (int)threadIdx.x - j;
+            rank += (g.x > mine || (g.x == mine && 0 < t)) + (g.y > mine || (g.y == mine && 1 < t)) +
+                    (g.z > mine || (g.z == mine && 2 < t)) + (g.w > mine || (g.w == mine && 3 < t));
+        }
+        if (rank == a.n_out - 1 && mine > 0u) sh.bound = mine;
     }
     __syncthreads();
-    const uint32_t chunk_bound = sh.bound;
-    int n = collect(sh, chunk_bound, a.n_out, [&](auto f) {
-#pragma unroll 4
-        for (int i = threadIdx.x; i < n_keys; i += PICK_THREADS) f(pack_key(chunk_key(i), (uint32_t)i));
-    });
+    int n = collect(sh, 0, sh.bound, a.n_out, each_chunk);
+    // (sh.bound has been read by everybody: collect ends with a barrier)
     if (threadIdx.x == 0) sh.bound = 1u;
     __syncthreads();
-    ranked(sh, n, a.n_out, [&](int rank, unsigned long long k) {
+    ranked(sh, 0, n, a.n_out, [&](int rank, unsigned long long k) {
         sh.chunk[rank] = 0xFFFFFFFFu - (uint32_t)k;
         if (rank == a.n_out - 1) sh.bound = (uint32_t)(k >> 32);   // n_out elements reach this
     });
     __syncthreads();
     // ---- the n_out best elements of those chunks, and the finished rows' candidates
     const int n_sel = min(n, a.n_out);
-    const uint32_t elem_bound = sh.bound;
-    n = collect(sh, elem_bound, a.n_out, [&](auto f) {
+    return collect(sh, 1, sh.bound, a.n_out, [&](auto f) {
         for (int i = warp; i < n_sel; i += PICK_THREADS / 32) {
             const int at = (int)sh.chunk[i];
             const int b = at / n_chunks, p0 = (at - b * n_chunks) * BEAM_CHUNK;
             const RowView<E> x(a.logits, a.row_stride, row0 + b, a.V);
-            const MaskSource mask = mask_source<CTX>(a, ctx, row0 + b);
+            const MaskSource mask = sh.mask[b];
             const float score = sh.score[b], lse = sh.lse[b];
+            uint4 v[PER_CHUNK];
+            uint32_t bits[PER_CHUNK];
 #pragma unroll
             for (int q = 0; q < PER_CHUNK; ++q) {
                 const int p = p0 + (q * 32 + lane) * EPC;
-                const uint32_t bits = shifted_word(mask, p >> 5, x.off) >> (p & 31);
-                const uint4 v = x.piece(p);
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                v[q] = x.piece(p);
+                bits[q] = shifted_word(mask, p >> 5, x.off) >> (p & 31);
+            }
+#pragma unroll
+            for (int q = 0; q < PER_CHUNK; ++q) {
+                const int p = p0 + (q * 32 + lane) * EPC;
+                const uint32_t w[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
 #pragma unroll
                 for (int j = 0; j < EPC; ++j) {
                     const uint32_t e = sizeof(E) == 2
                         ? ((j & 1) ? (w[j >> 1] & 0xFFFF0000u) : (w[j >> 1] << 16)) : w[j];
-                    const uint32_t key = ((bits >> j) & 1u) ? score_key(score + (__uint_as_float(e) - lse)) : 0u;
-                    f(pack_key(key, (uint32_t)b * (uint32_t)a.V + (uint32_t)(p + j - x.off)));
+                    const uint32_t k = ((bits[q] >> j) & 1u) ? score_key(score + (__uint_as_float(e) - lse)) : 0u;
+                    f(pack_key(k, (uint32_t)b * (uint32_t)a.V + (uint32_t)(p + j - x.off)));
                 }
             }
         }
@@ -525,8 +585,8 @@ beam_pick_kernel(BeamArgs a, CtxDev ctx, VocabDev v, BeamStepArgs st, float *sco
     __shared__ PickShared sh;
     pdl_enter();
     const int req = blockIdx.x;
-    beam_pick<E, CTX>(sh, a, ctx, req);
-    const int n = min(sh.n, PICK_LIST);
+    if (req == 0 && threadIdx.x == 0) *a.next_item = 0;
+    const int n = beam_pick<E, CTX>(sh, a, ctx, req);
     // ---- out, best first
     const int64_t out0 = (int64_t)req * a.n_out;
     if ((int)threadIdx.x < a.n_out && (int)threadIdx.x >= n) {
@@ -534,7 +594,7 @@ beam_pick_kernel(BeamArgs a, CtxDev ctx, VocabDev v, BeamStepArgs st, float *sco
         parent_out[out0 + threadIdx.x] = sh.parent[threadIdx.x] = -1;
         token_out[out0 + threadIdx.x] = sh.token[threadIdx.x] = -1;
     }
-    ranked(sh, n, a.n_out, [&](int rank, unsigned long long k) {
+    ranked(sh, 1, n, a.n_out, [&](int rank, unsigned long long k) {
         const uint32_t flat = 0xFFFFFFFFu - (uint32_t)k;
         const uint32_t b = flat / (uint32_t)a.V;
         score_out[out0 + rank] = key_score((uint32_t)(k >> 32));
@@ -579,14 +639,14 @@ beam_pick_kernel(BeamArgs a, CtxDev ctx, VocabDev v, BeamStepArgs st, float *sco
 // ---------------------------------------------------------------------------------------
 // Back-track.  One block per request walks its parents from the last step to the first.  The walk is
 // a chain of dependent look-ups, so the steps are cut into segments: every segment is first walked
-// from all beams at once (a map from its last beams to its first), the maps are chained, and
-// then every segment is walked again from the beam that the final hypothesis really comes by.  Parents are
-// staged in shared memory as bytes, a tile of steps at a time.
+// from all beams at once (a map from its last beams to its first), the maps are composed by a
+// logarithmic scan, and then every segment is walked again from the beam that each final beam
+// really comes by.  Parents are staged in shared memory as bytes, a tile of steps at a time.
 // ---------------------------------------------------------------------------------------
-constexpr int BACK_THREADS = 512;
+constexpr int BACK_THREADS = 1024;
 constexpr int BACK_DEAD = 255;
 
-__global__ void __launch_bounds__(BACK_THREADS)
+__global__ void __launch_bounds__(BACK_THREADS, 1)
 beam_backtrack_kernel(const int32_t *__restrict__ token, const int32_t *__restrict__ parent, int T,
                       int n_req, int K, int tile, int32_t *__restrict__ out) {
     extern __shared__ uint8_t back_smem[];
@@ -600,50 +660,56 @@ beam_backtrack_kernel(const int32_t *__restrict__ token, const int32_t *__restri
     const int64_t col = (int64_t)r * K;
     const int n_seg = BACK_THREADS / K;
     const int seg = (int)threadIdx.x / K, j = (int)threadIdx.x - seg * K;
+    const bool works = seg < n_seg;                 // (a few threads are left over unless K divides them)
     if ((int)threadIdx.x < K) at[threadIdx.x] = (uint8_t)threadIdx.x;
     for (int t1 = T; t1 > 0; t1 -= tile) {          // steps [t0, t1)
         const int t0 = max(0, t1 - tile), n = t1 - t0;
         __syncthreads();                            // the previous tile is done with
-        for (int i = threadIdx.x; i < n * K; i += BACK_THREADS) {
-            const int t = i / K;
-            const int p = parent[(int64_t)(t0 + t) * step + col + (i - t * K)];
-            par[i] = p >= 0 && p < K ? (uint8_t)p : (uint8_t)BACK_DEAD;
+        if (works) {
+            const int32_t *from = parent + t0 * step + col + j;
+#pragma unroll 8
+            for (int t = seg; t < n; t += n_seg) {
+                const int p = __ldcs(from + t * step);
+                par[t * K + j] = p >= 0 && p < K ? (uint8_t)p : (uint8_t)BACK_DEAD;
+            }
         }
         __syncthreads();
         const int per = (n + n_seg - 1) / n_seg;
         const int lo = min(n, seg * per), hi = min(n, lo + per);
-        if (seg < n_seg) {
-            int b = j;
+        int b = j;
+        if (works) {
             for (int t = hi - 1; t >= lo; --t)
                 if (b != BACK_DEAD) b = par[t * K + b];
             maps[seg * K + j] = (uint8_t)b;
         }
         __syncthreads();
-        if ((int)threadIdx.x < K) {                 // maps[s][j] becomes where j enters segment s
-            int b = at[threadIdx.x];
-            for (int s = n_seg - 1; s >= 0; --s) {
-                // (a beam's own entry may be needed by its siblings: read by all, then written)
-                const int to = b == BACK_DEAD ? BACK_DEAD : maps[s * K + b];
-                __syncwarp((1ull << K) - 1ull);
-                maps[s * K + threadIdx.x] = (uint8_t)b;
-                b = to;
+        // maps[s] becomes the composition of the maps of all segments from the last down to s
+        for (int d = 1; d < n_seg; d <<= 1) {
+            if (works && seg + d < n_seg) {
+                b = maps[(seg + d) * K + j];
+                if (b != BACK_DEAD) b = maps[seg * K + b];
             }
-            at[threadIdx.x] = (uint8_t)b;
+            __syncthreads();
+            if (works) maps[seg * K + j] = (uint8_t)b;
+            __syncthreads();
         }
-        __syncthreads();
-        if (seg < n_seg) {
-            int b = maps[seg * K + j];
+        if (works) {
+            b = at[j];
+            if (seg + 1 < n_seg && b != BACK_DEAD) b = maps[(seg + 1) * K + b];
             for (int t = hi - 1; t >= lo; --t) {
                 path[t * K + j] = (uint8_t)b;
                 if (b != BACK_DEAD) b = par[t * K + b];
             }
         }
         __syncthreads();
+        if ((int)threadIdx.x < K && at[threadIdx.x] != BACK_DEAD) at[threadIdx.x] = maps[at[threadIdx.x]];
         for (int t = threadIdx.x; t < n; t += BACK_THREADS) {
-            const int32_t *row = token + (int64_t)(t0 + t) * step + col;
+            const int32_t *row = token + (t0 + t) * step + col;
+            int32_t *to = out + col * T + t0 + t;
+#pragma unroll 8
             for (int jj = 0; jj < K; ++jj) {
-                const int b = path[t * K + jj];
-                out[(col + jj) * T + t0 + t] = b == BACK_DEAD ? -1 : row[b];
+                const int from = path[t * K + jj];
+                to[(int64_t)jj * T] = from == BACK_DEAD ? -1 : __ldg(row + from);
             }
         }
     }

@@ -3,15 +3,18 @@
 
 struct wg_beam {
     int32_t V = 0, max_requests = 0, max_beams = 0, max_out = 0;
-    int32_t chunk_stride = 0, max_parts = 0;
+    int32_t chunk_stride = 0;
     float *chunk_max = nullptr;
     float2 *parts = nullptr;
+    int32_t *next_item = nullptr;
 };
 
 namespace {
 
-// Spans per row, for the worst alignment of a row (it may begin up to 7 elements into a piece).
+// Spans of 1024 positions per row, for the worst alignment of a row (it may begin up to 7 elements into
+// a piece).
 int32_t beam_spans(int32_t V) { return (V + 7 + 1023) / 1024; }
+constexpr int BEAM_MAX_STEPS = 8;
 
 template <typename E, int NORM, bool CTX>
 cudaError_t launch_beam_scan(const BeamArgs &a, const CtxDev &ctx, dim3 grid, cudaStream_t st) {
@@ -35,18 +38,21 @@ int32_t launch_beam(const BeamArgs &a, const CtxDev &ctx, const VocabDev &v, con
     return WG_OK;
 }
 
-// The scan's grid, (blocks per row, rows): as few spans per warp as it takes to fill the GPU about
-// four times over, at most BEAM_SPANS_PER_WARP (as apply_grid).
-dim3 beam_grid(BeamArgs &a, int32_t rows) {
-    const int n_spans = beam_spans(a.V);
-    int per_warp = BEAM_SPANS_PER_WARP;
-    while (per_warp > 1 && (long long)rows * ((n_spans + BEAM_WARPS * per_warp - 1) / (BEAM_WARPS * per_warp)) <
-                               16LL * sm_count())
-        per_warp >>= 1;
-    a.spans_per_block = BEAM_WARPS * per_warp;
-    const int blocks = (n_spans + a.spans_per_block - 1) / a.spans_per_block;
-    a.n_parts = blocks * BEAM_WARPS;
-    return dim3((unsigned)blocks, (unsigned)rows);
+// How the scan is dealt out: items of several steps once there is work for every resident warp a few
+// times over, single steps below that.
+dim3 beam_grid(BeamArgs &a, int32_t rows, int32_t dtype) {
+    const int step = dtype == WG_DTYPE_BF16 ? ScanShape<uint16_t>::STEP : ScanShape<uint32_t>::STEP;
+    const long long steps = (a.V + 7 + step - 1) / step;
+    const long long resident = (long long)sm_count() * 4 * BEAM_WARPS;
+    long long per = rows * steps / (resident * 3);
+    per = per < 1 ? 1 : per > BEAM_MAX_STEPS ? BEAM_MAX_STEPS : per;
+    a.per_item = (int32_t)per;
+    a.items_per_row = (int32_t)((steps + per - 1) / per);
+    a.n_items = (uint32_t)((long long)rows * a.items_per_row);
+    a.chunk_log2 = 5;
+    while (a.chunk_log2 < 9 && (1 << a.chunk_log2) < a.chunk_stride) ++a.chunk_log2;
+    const long long blocks = ((long long)a.n_items + BEAM_WARPS - 1) / BEAM_WARPS;
+    return dim3((unsigned)std::min(blocks, resident / BEAM_WARPS));
 }
 
 bool beam_sizes_ok(const wg_beam *beam, int32_t n_req, int32_t n_beam, int32_t n_out, int32_t norm) {
@@ -68,7 +74,8 @@ int32_t wg_beam_create(int32_t V, int32_t max_requests, int32_t max_beams, int32
     *out = nullptr;
     if (V < 1 || V > INT32_MAX - 2048 || max_requests < 1 || max_beams < 1 || max_beams > WG_BEAM_MAX_BEAMS ||
         max_out < 1 || max_out > WG_BEAM_MAX_OUT || (int64_t)max_requests * max_beams > WG_MAX_ROWS ||
-        (int64_t)V * max_beams >= (1LL << 32))
+        (int64_t)V * max_beams >= (1LL << 32) ||
+        (int64_t)max_requests * max_beams * beam_spans(V) * 2 >= (1LL << 31))   // items have 32-bit numbers
         return WG_ERR_ARG;
     wg_beam *b = new (std::nothrow) wg_beam();
     if (!b) return WG_ERR_ARG;
@@ -77,10 +84,11 @@ int32_t wg_beam_create(int32_t V, int32_t max_requests, int32_t max_beams, int32
     b->max_beams = max_beams;
     b->max_out = max_out;
     b->chunk_stride = beam_spans(V) * 4;
-    b->max_parts = (beam_spans(V) + BEAM_WARPS - 1) / BEAM_WARPS * BEAM_WARPS;   // one span per warp
     const size_t rows = (size_t)max_requests * max_beams;
     int32_t rc = dev_alloc(&b->chunk_max, rows * b->chunk_stride);
-    if (rc == WG_OK) rc = dev_alloc(&b->parts, rows * b->max_parts);
+    if (rc == WG_OK) rc = dev_alloc(&b->parts, rows * beam_spans(V) * 2);   // (an fp32 span is two steps)
+    if (rc == WG_OK) rc = dev_alloc(&b->next_item, 1);
+    if (rc == WG_OK && cudaMemset(b->next_item, 0, sizeof(int32_t)) != cudaSuccess) rc = WG_ERR_CUDA;
     if (rc != WG_OK) {
         wg_beam_free(b);
         return rc;
@@ -93,6 +101,7 @@ void wg_beam_free(wg_beam *b) {
     if (!b) return;
     cudaFree(b->chunk_max);   // (waits for queued work)
     cudaFree(b->parts);
+    cudaFree(b->next_item);
     delete b;
 }
 
@@ -112,8 +121,9 @@ int32_t wg_beam_select(wg_beam *beam, const void *logits, int32_t dtype, int64_t
     if (finished && (eos_id < 0 || eos_id >= V)) return WG_ERR_ARG;
     if (score_out == score && n_out != n_beam) return WG_ERR_ARG;
     BeamArgs a{logits, row_stride_elems, bitmask, mask_stride_words, score, finished, nullptr, nullptr,
-               n_beam, V, W, n_out, eos_id, norm, 0, 0, beam->chunk_stride, beam->chunk_max, beam->parts};
-    const dim3 grid = beam_grid(a, n_req * n_beam);
+               n_beam, V, W, n_out, eos_id, norm, 0, 0, 0u, beam->chunk_stride, 0, beam->chunk_max, beam->parts,
+               beam->next_item};
+    const dim3 grid = beam_grid(a, n_req * n_beam, dtype);
     const CtxDev none{};
     const VocabDev no_vocab{};
     const BeamStepArgs no_step{};
@@ -154,8 +164,9 @@ int32_t wg_beam_step(wg_beam *beam, wg_ctx *c, int32_t *gid, int32_t *sid, float
     const int32_t rc = launch_build(c, work, rows, st, true);
     if (rc != WG_OK) return rc;
     BeamArgs a{logits, row_stride_elems, bitmask, mask_stride_words, score, nullptr, gid, sid,
-               n_beam, v.V, v.W, n_beam, v.eos_id, norm, 0, 0, beam->chunk_stride, beam->chunk_max, beam->parts};
-    const dim3 grid = beam_grid(a, rows);
+               n_beam, v.V, v.W, n_beam, v.eos_id, norm, 0, 0, 0u, beam->chunk_stride, 0, beam->chunk_max, beam->parts,
+               beam->next_item};
+    const dim3 grid = beam_grid(a, rows, dtype);
     const BeamStepArgs step{gid, sid, status};
     return dtype == WG_DTYPE_BF16
         ? launch_beam<uint16_t, true>(a, c->dev, v, step, n_req, grid, score, parent_out, token_out, st)

@@ -14,8 +14,9 @@ namespace {
 constexpr int PLAN_THREADS = 1024;      // one block: plans of a whole batch
 constexpr int FILL_THREADS = 256;
 constexpr int MOVE_THREADS = 128;       // columns of a table per block
+constexpr int SHRINK_THREADS = 128;
 constexpr int COPY_THREADS = 256;
-constexpr int WORDS_PER_THREAD = 8;     // words of free bits a thread counts per round
+constexpr int WORDS_PER_THREAD = 4;     // words of free bits a thread counts per round
 
 struct PoolDev {
     int32_t *ref;         // [n_blocks]
@@ -27,7 +28,8 @@ struct PoolDev {
     int32_t *first;       // [max_seqs] where a sequence's blocks begin in `taken`, or -1: refused
     int32_t *old_len;     // [max_seqs] lengths before the call
     int32_t *new_len;     // [max_seqs]
-    int32_t *src, *dst, *filled;  // [max_seqs] copies of a reorder
+    int32_t *src;         // [max_seqs] a reorder's rows: the block to copy, or -1
+    int32_t *from, *dst, *filled;  // [max_seqs] its copies, one after the other
     int32_t *n_copies;
     int32_t *arrived;     // blocks of the reorder's first kernel that have finished; zero between calls
 };
@@ -41,29 +43,31 @@ __device__ __forceinline__ int32_t blocks_of(int32_t len, int32_t block_size) { 
     return len / block_size + (len % block_size != 0);
 }
 
-// Inclusive prefix sum over the block, and the block's total.  `warps`: shared, blockDim.x / 32.
+__device__ __forceinline__ int up(int x, int o) { return __shfl_up_sync(0xFFFFFFFFu, x, o); }
+
+// Inclusive prefix sum over the block, and the block's total.  `warps`: shared, 32 entries.
 template <typename T>
 __device__ __forceinline__ T block_scan(T x, T *warps, T &total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = (int)(blockDim.x >> 5);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const T y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        const T y = up(x, o);
         if (lane >= o) x += y;
     }
     if (lane == 31) warps[warp] = x;
     __syncthreads();
     if (warp == 0) {
-        T w = lane < n_warps ? warps[lane] : T(0);
+        T w = lane < n_warps ? warps[lane] : T{};
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const T y = __shfl_up_sync(0xFFFFFFFFu, w, o);
+            const T y = up(w, o);
             if (lane >= o) w += y;
         }
         if (lane < n_warps) warps[lane] = w;
     }
     __syncthreads();
     total = warps[n_warps - 1];
-    const T before = warp > 0 ? warps[warp - 1] : T(0);
+    const T before = warp > 0 ? warps[warp - 1] : T{};
     __syncthreads();   // `warps` may be used again
     return x + before;
 }
@@ -82,69 +86,65 @@ __device__ __forceinline__ int nth_set_bit(uint32_t w, int n) {   // position of
 }
 
 // Called by a whole block: takes the `n` lowest free blocks (n <= the number of free ones; the caller has
-// seen to that), in ascending order into pool.taken, with count 1.  Every round a thread counts
-// WORDS_PER_THREAD words; after the scan each of the round's blocks finds its word by bisection.
+// seen to that) with count 1 and calls got(k, id) for the k-th of them.  Every round a thread counts
+// four words of free bits; after the scan each of the round's blocks finds its word by bisection.
+// `w`: the thread's words of the first round, asked for early.
+template <int THREADS>
 struct TakeShared {
-    int32_t upto[PLAN_THREADS];   // free blocks up to and including a thread's words
+    uint32_t words[THREADS * WORDS_PER_THREAD];
+    int32_t upto[THREADS];        // free blocks up to and including a thread's words
     int32_t warps[32];
 };
 
-__device__ __forceinline__ void take_blocks(const PoolDev &pool, TakeShared &sh, int n) {
-    const int threads = (int)blockDim.x;
+__device__ __forceinline__ uint4 free_words(const PoolDev &pool, int at) {
+    return at < pool.n_words ? __ldcg(reinterpret_cast<const uint4 *>(pool.free_bits + at)) : make_uint4(0, 0, 0, 0);
+}
+
+template <int THREADS, typename Got>
+__device__ __forceinline__ void take_blocks(const PoolDev &pool, TakeShared<THREADS> &sh, int n, uint4 w, const Got &got) {
     int done = 0;
-    for (int w0 = 0; w0 < pool.n_words && done < n; w0 += threads * WORDS_PER_THREAD) {
+    for (int w0 = 0; done < n && w0 < pool.n_words; w0 += THREADS * WORDS_PER_THREAD) {
         const int mine = w0 + (int)threadIdx.x * WORDS_PER_THREAD;
-        uint32_t w[WORDS_PER_THREAD];
-        int count = 0;
-#pragma unroll
-        for (int i = 0; i < WORDS_PER_THREAD; i += 4) {
-            uint4 q = make_uint4(0, 0, 0, 0);
-            if (mine + i < pool.n_words) q = __ldcg(reinterpret_cast<const uint4 *>(pool.free_bits + mine + i));
-            w[i] = q.x; w[i + 1] = q.y; w[i + 2] = q.z; w[i + 3] = q.w;
-        }
-#pragma unroll
-        for (int i = 0; i < WORDS_PER_THREAD; ++i) count += __popc(w[i]);
+        if (w0 > 0) w = free_words(pool, mine);
+        *reinterpret_cast<uint4 *>(&sh.words[threadIdx.x * WORDS_PER_THREAD]) = w;
+        const int count = __popc(w.x) + __popc(w.y) + __popc(w.z) + __popc(w.w);
         int total;
         const int upto = block_scan(count, sh.warps, total);
         sh.upto[threadIdx.x] = upto;
         __syncthreads();
         const int here = min(total, n - done);
-        for (int k = threadIdx.x; k < here; k += threads) {
-            int lo = 0, hi = threads - 1;             // the first thread whose words reach past k
+        for (int k = threadIdx.x; k < here; k += THREADS) {
+            int lo = 0, hi = THREADS - 1;             // the first thread whose words reach past k
             while (lo < hi) {
                 const int mid = (lo + hi) >> 1;
                 if (sh.upto[mid] > k) hi = mid; else lo = mid + 1;
             }
             int left = k - (lo > 0 ? sh.upto[lo - 1] : 0);
-            int at = w0 + lo * WORDS_PER_THREAD;
-            uint32_t word = __ldcg(&pool.free_bits[at]);
+            int at = lo * WORDS_PER_THREAD;
+            uint32_t word = sh.words[at];
             for (int c = __popc(word); left >= c; c = __popc(word)) {
                 left -= c;
-                word = __ldcg(&pool.free_bits[++at]);
+                word = sh.words[++at];
             }
-            const int id = at * 32 + nth_set_bit(word, left);
-            pool.taken[done + k] = id;
+            const int id = (w0 + at) * 32 + nth_set_bit(word, left);
             pool.ref[id] = 1;
+            got(done + k, id);
         }
-        __syncthreads();                              // everybody has looked the bits up
         int drop = min(count, here - (upto - count)); // of this thread's blocks, the lowest `drop` are gone
+        if (drop > 0) {
+            uint32_t v[WORDS_PER_THREAD] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int i = 0; i < WORDS_PER_THREAD; ++i) {
-            if (drop <= 0) break;
-            const int c = __popc(w[i]);
-            if (c == 0) continue;
-            if (drop >= c) {
-                w[i] = 0u;
+            for (int i = 0; i < WORDS_PER_THREAD; ++i) {
+                const int c = __popc(v[i]);
+                if (drop >= c) v[i] = 0u;
+                else if (drop > 0) v[i] &= ~((1u << nth_set_bit(v[i], drop)) - 1u);
                 drop -= c;
-            } else {
-                w[i] &= ~((1u << nth_set_bit(w[i], drop)) - 1u);
-                drop = 0;
             }
-            pool.free_bits[mine + i] = w[i];
+            *reinterpret_cast<uint4 *>(pool.free_bits + mine) = make_uint4(v[0], v[1], v[2], v[3]);
         }
         done += here;
+        __syncthreads();                              // the shared words are free for the next round
     }
-    __syncthreads();
 }
 
 __device__ __forceinline__ bool id_ok(const PoolDev &pool, int32_t id) { return id >= 0 && id < pool.n_blocks; }
@@ -203,20 +203,21 @@ struct ExtendArgs {
 // Token t of the call: its sequence by bisection over cu, its block from the table or, for a new
 // block, from the blocks taken.  The token at a block's first position also enters the block into the
 // table (new blocks begin where the old length's last block ends, so each holds exactly one such token).
-__device__ __forceinline__ void extend_token(const PoolDev &pool, const ExtendArgs &a, int t, int n_used) {
+__device__ __forceinline__ void extend_token(const PoolDev &pool, const ExtendArgs &a, int t, int n_used,
+                                             const int32_t *cu, const int32_t *old_len, const int32_t *first,
+                                             const int32_t *taken) {
     int64_t slot = -1;
     int32_t pos = -1, s = -1;
     if (t < n_used) {
-        int lo = 0, hi = a.n_seq - 1;      // the last sequence that begins at or before t and is not empty
+        int lo = 0, hi = a.n_seq - 1;      // the sequence that begins at or before t and ends after it
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
-            if (a.cu[mid + 1] > t) hi = mid; else lo = mid + 1;
+            if (cu[mid + 1] > t) hi = mid; else lo = mid + 1;
         }
         s = lo;
-        const int32_t len = pool.old_len[s];
-        pos = len + (t - a.cu[s]);
-        const int32_t first = pool.first[s];
-        if (first >= 0) {
+        const int32_t len = old_len[s];
+        pos = len + (t - cu[s]);
+        if (first[s] >= 0) {
             const int32_t held = blocks_of(len, pool.block_size), col = pos / pool.block_size;
             const int32_t in = pos - col * pool.block_size;
             int32_t *entry = a.table + (int64_t)s * a.stride + col;
@@ -224,7 +225,7 @@ __device__ __forceinline__ void extend_token(const PoolDev &pool, const ExtendAr
             if (col < held) {
                 id = *entry;
             } else {
-                id = pool.taken[first + col - held];
+                id = taken[first[s] + col - held];
                 if (in == 0) *entry = id;
             }
             if (id_ok(pool, id)) slot = (int64_t)id * pool.block_size + in;
@@ -235,17 +236,32 @@ __device__ __forceinline__ void extend_token(const PoolDev &pool, const ExtendAr
     a.seq[t] = s;
 }
 
+// A batch of up to this many tokens in at most PLAN_THREADS sequences is placed by the planning block
+// itself, everything it needs for that in shared memory (one launch less).
+constexpr int32_t FILL_IN_PLAN = 2048;
+
+struct PlanSums {
+    long long tokens, wanted;
+    __device__ __forceinline__ PlanSums operator+(const PlanSums &o) const { return {tokens + o.tokens, wanted + o.wanted}; }
+    __device__ __forceinline__ PlanSums &operator+=(const PlanSums &o) { return *this = *this + o; }
+};
+__device__ __forceinline__ PlanSums up(const PlanSums &x, int o) {
+    return {__shfl_up_sync(0xFFFFFFFFu, x.tokens, o), __shfl_up_sync(0xFFFFFFFFu, x.wanted, o)};
+}
+
 // One block: who gets how many blocks, which ones, and where each sequence's tokens begin.
-// FILL: the same block also writes the tokens' slots (few tokens: one launch less).
 template <bool FILL>
 __global__ void __launch_bounds__(PLAN_THREADS, 1)
 extend_plan_kernel(PoolDev pool, ExtendArgs a) {
-    __shared__ TakeShared take;
-    __shared__ long long warps[32];
+    __shared__ TakeShared<PLAN_THREADS> take;
+    __shared__ PlanSums warps[32];
+    __shared__ int32_t sh_cu[FILL ? PLAN_THREADS + 1 : 1], sh_len[FILL ? PLAN_THREADS : 1];
+    __shared__ int32_t sh_first[FILL ? PLAN_THREADS : 1], sh_taken[FILL ? FILL_IN_PLAN : 1];
     kv_enter();
+    const uint4 free0 = free_words(pool, (int)threadIdx.x * WORDS_PER_THREAD);
     const int n_free = *pool.n_free;
-    long long want0 = 0, tok0 = 0;       // before this round
-    int granted_blocks = 0;              // the largest granted prefix
+    PlanSums before{0, 0};               // of the rounds done
+    int granted = 0;                     // blocks granted: the largest prefix that is
     const int64_t room = (int64_t)a.max_blocks * pool.block_size;
     for (int s0 = 0; s0 < a.n_seq; s0 += PLAN_THREADS) {
         const int s = s0 + (int)threadIdx.x;
@@ -260,41 +276,53 @@ extend_plan_kernel(PoolDev pool, ExtendArgs a) {
                 need = blocks_of(len + add, pool.block_size) - blocks_of(len, pool.block_size);
             }
         }
-        long long tokens, wanted;
-        const long long tok = block_scan((long long)add, warps, tokens) + tok0;
-        const long long want = block_scan((long long)need, warps, wanted) + want0;
+        PlanSums total;
+        const PlanSums upto = block_scan(PlanSums{add, need}, warps, total) + before;
         int last = 0;                    // blocks granted up to and including this sequence
         if (s < a.n_seq) {
             const bool fits = st == WG_OK &&
-                              (add == 0 || (tok <= a.n_tokens && (need == 0 || want <= n_free)));
+                              (add == 0 || (upto.tokens <= a.n_tokens && (need == 0 || upto.wanted <= n_free)));
             if (st == WG_OK && !fits) st = WG_ERR_CAPACITY;
-            a.cu[s + 1] = (int32_t)min(tok, (long long)a.n_tokens);
-            pool.old_len[s] = len;
-            pool.first[s] = fits ? (int32_t)min(want - need, (long long)n_free) : -1;
+            const int32_t cu = (int32_t)min(upto.tokens, (long long)a.n_tokens);
+            const int32_t first = fits ? (int32_t)min(upto.wanted - need, (long long)n_free) : -1;
+            a.cu[s + 1] = cu;
+            if (FILL) {
+                sh_cu[s + 1] = cu;
+                sh_len[s] = len;
+                sh_first[s] = first;
+            } else {
+                pool.old_len[s] = len;
+                pool.first[s] = first;
+            }
             if (fits) {
                 a.len[s] = len + add;
-                if (need > 0) last = (int)want;
+                if (need > 0) last = (int)upto.wanted;
             }
             if (a.status) a.status[s] = st;
         }
-        granted_blocks = max(granted_blocks, __reduce_max_sync(0xFFFFFFFFu, last));
-        want0 += wanted;
-        tok0 += tokens;
+        granted = max(granted, __reduce_max_sync(0xFFFFFFFFu, last));
+        before += total;
     }
-    if (threadIdx.x == 0) a.cu[0] = 0;
-    // the warps' largest prefixes
-    if ((threadIdx.x & 31) == 0) take.warps[threadIdx.x >> 5] = granted_blocks;
+    if (threadIdx.x == 0) {
+        a.cu[0] = 0;
+        if (FILL) sh_cu[0] = 0;
+    }
+    if ((threadIdx.x & 31) == 0) take.warps[threadIdx.x >> 5] = granted;
     __syncthreads();
-    granted_blocks = __reduce_max_sync(0xFFFFFFFFu, take.warps[threadIdx.x & 31]);
+    granted = __reduce_max_sync(0xFFFFFFFFu, take.warps[threadIdx.x & 31]);
     __syncthreads();
-    if (granted_blocks > 0) {
-        take_blocks(pool, take, granted_blocks);
-        if (threadIdx.x == 0) *pool.n_free = n_free - granted_blocks;
+    if (granted > 0) {
+        take_blocks(pool, take, granted, free0, [&](int k, int id) {
+            if (FILL) sh_taken[k] = id;
+            else pool.taken[k] = id;
+        });
+        if (threadIdx.x == 0) *pool.n_free = n_free - granted;
     }
     if (FILL) {
         __syncthreads();
-        const int n_used = a.n_seq > 0 ? a.cu[a.n_seq] : 0;
-        for (int t = threadIdx.x; t < a.n_tokens; t += PLAN_THREADS) extend_token(pool, a, t, n_used);
+        const int n_used = sh_cu[a.n_seq];
+        for (int t = threadIdx.x; t < a.n_tokens; t += PLAN_THREADS)
+            extend_token(pool, a, t, n_used, sh_cu, sh_len, sh_first, sh_taken);
     }
 }
 
@@ -303,32 +331,46 @@ extend_fill_kernel(PoolDev pool, ExtendArgs a) {
     kv_enter();
     const int n_used = a.cu[a.n_seq];
     const int t = blockIdx.x * FILL_THREADS + (int)threadIdx.x;
-    if (t < a.n_tokens) extend_token(pool, a, t, n_used);
+    if (t < a.n_tokens) extend_token(pool, a, t, n_used, a.cu, pool.old_len, pool.first, pool.taken);
 }
 
 // ---------------------------------------------------------------------------------------
-// Shrink: a warp per sequence.
+// Shrink: a block per sequence.
 // ---------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(FILL_THREADS)
+__global__ void __launch_bounds__(SHRINK_THREADS)
 shrink_kernel(PoolDev pool, int32_t *table, int64_t stride, int32_t max_blocks, int32_t *len,
-              const int32_t *keep, int32_t n_seq, int32_t *status) {
+              const int32_t *keep, int32_t *status) {
     kv_enter();
-    const int s = (int)((blockIdx.x * FILL_THREADS + threadIdx.x) >> 5), lane = threadIdx.x & 31;
-    if (s >= n_seq) return;
+    const int s = blockIdx.x;
     const int32_t have = len[s], want = keep[s];
     const bool ok = have >= 0 && have <= (int64_t)max_blocks * pool.block_size && want >= 0 && want <= have;
-    if (lane == 0 && status) status[s] = ok ? WG_OK : WG_ERR_ARG;
+    if (threadIdx.x == 0 && status) status[s] = ok ? WG_OK : WG_ERR_ARG;
     if (!ok) return;
     const int32_t end = blocks_of(have, pool.block_size);
+    int32_t *row = table + (int64_t)s * stride;
     int freed = 0;
-    for (int c = blocks_of(want, pool.block_size) + lane; c < end; c += 32) {
-        int32_t *entry = table + (int64_t)s * stride + c;
-        const int32_t id = *entry;
-        if (id_ok(pool, id)) drop_refs(pool, id, 1, freed);
-        *entry = -1;
+    constexpr int AT_ONCE = 4;
+    for (int c0 = blocks_of(want, pool.block_size) + (int)threadIdx.x; c0 < end; c0 += AT_ONCE * SHRINK_THREADS) {
+        int32_t id[AT_ONCE], left[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int c = c0 + u * SHRINK_THREADS;
+            id[u] = c < end ? row[c] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) left[u] = id_ok(pool, id[u]) ? atomicSub(&pool.ref[id[u]], 1) - 1 : -1;
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            if (c0 + u * SHRINK_THREADS < end) row[c0 + u * SHRINK_THREADS] = -1;
+            if (left[u] == 0) {
+                atomicOr(&pool.free_bits[id[u] >> 5], 1u << (id[u] & 31));
+                ++freed;
+            }
+        }
     }
     add_freed(pool, freed);
-    if (lane == 0) len[s] = want;
+    __syncthreads();                       // everybody has read the length
+    if (threadIdx.x == 0) len[s] = want;
 }
 
 // ---------------------------------------------------------------------------------------
@@ -347,11 +389,15 @@ struct MoveArgs {
 // What a request's rows become; filled by the block for its request.
 struct MoveShared {
     int32_t parent[WG_BEAM_MAX_BEAMS];    // -1: the sequence ends
+    int32_t len[WG_BEAM_MAX_BEAMS];       // old lengths, 0 where they lie outside the table
     int32_t blocks[WG_BEAM_MAX_BEAMS];    // columns in use
     int32_t partly[WG_BEAM_MAX_BEAMS];    // the column of a partly filled last block, or -1
     int32_t children[WG_BEAM_MAX_BEAMS];
     int32_t first[WG_BEAM_MAX_BEAMS];     // first child, or n_beam
+    int32_t bad[WG_BEAM_MAX_BEAMS];       // the length lay outside
 };
+
+constexpr int MOVE_ROWS = 4;              // rows a thread of the last block takes per round
 
 // First kernel: grid = (tiles of MOVE_THREADS columns, requests); a thread holds one column of all the
 // request's rows, so the rows move in place with no other thread in the way.  Row b's block of the
@@ -363,15 +409,17 @@ __global__ void __launch_bounds__(MOVE_THREADS)
 move_rows_kernel(PoolDev pool, MoveArgs a) {
     extern __shared__ int32_t column[];   // [n_beam][MOVE_THREADS]
     __shared__ MoveShared sh;
-    __shared__ TakeShared take;
+    __shared__ TakeShared<MOVE_THREADS> take;
     __shared__ int32_t is_last;
     kv_enter();
     const int K = a.n_beam, row0 = blockIdx.y * K, bs = pool.block_size;
     const int64_t room = (int64_t)a.max_blocks * bs;
     if ((int)threadIdx.x < K) {
         const int32_t p = a.parent[row0 + threadIdx.x], l = a.len[row0 + threadIdx.x];
-        sh.parent[threadIdx.x] = p >= 0 && p < K ? p : -1;
         const int32_t len = l >= 0 && l <= room ? l : 0;
+        sh.parent[threadIdx.x] = p >= 0 && p < K ? p : -1;
+        sh.len[threadIdx.x] = len;
+        sh.bad[threadIdx.x] = len != l;
         sh.blocks[threadIdx.x] = blocks_of(len, bs);
         sh.partly[threadIdx.x] = len % bs != 0 ? len / bs : -1;
     }
@@ -386,107 +434,121 @@ move_rows_kernel(PoolDev pool, MoveArgs a) {
         sh.children[threadIdx.x] = n;
         sh.first[threadIdx.x] = first;
     }
-    __syncthreads();
     int32_t most = 0;
     for (int b = 0; b < K; ++b) most = max(most, sh.blocks[b]);
+    __syncthreads();
+    // what the last block needs of a row: its length, and that there is nothing to copy (where there is,
+    // the thread that holds the column says so below)
+    if (blockIdx.x == 0 && (int)threadIdx.x < K) {
+        const int j = threadIdx.x, p = sh.parent[j];
+        pool.new_len[row0 + j] = p >= 0 ? sh.len[p] : 0;
+        if (a.status) a.status[row0 + j] = p >= 0 && sh.bad[p] ? WG_ERR_ARG : WG_OK;
+        if (p < 0 || sh.partly[p] < 0 || sh.first[p] == j) pool.src[row0 + j] = -1;
+    }
     int freed = 0;
     const int c = blockIdx.x * MOVE_THREADS + (int)threadIdx.x;
     if (c < most) {
         int32_t *col = a.table + (int64_t)row0 * a.stride + c;
         int32_t *v = column + threadIdx.x;
-        for (int b = 0; b < K; ++b) {
-            const int32_t id = c < sh.blocks[b] ? col[b * a.stride] : -1;
-            v[b * MOVE_THREADS] = id_ok(pool, id) ? id : -1;
+        bool same = true, plain = true;   // all rows name one block; no row's partly filled one
+        int32_t id0 = -1;
+        for (int b0 = 0; b0 < K; b0 += 8) {
+            int32_t id[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) id[u] = b0 + u < K && c < sh.blocks[b0 + u] ? col[(b0 + u) * a.stride] : -1;
+            if (b0 == 0) id0 = id[0];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (b0 + u < K) {
+                    v[(b0 + u) * MOVE_THREADS] = id_ok(pool, id[u]) ? id[u] : -1;
+                    same = same && id[u] == id0;
+                    plain = plain && c != sh.partly[b0 + u];
+                }
         }
         // counts
-        for (int b = 0; b < K; ++b) {
-            const int32_t id = v[b * MOVE_THREADS];
-            if (id < 0) continue;
-            bool seen = false;
-            int32_t change = 0;
-            for (int o = 0; o < K; ++o) {
-                if (v[o * MOVE_THREADS] != id) continue;
-                if (o < b) { seen = true; break; }
-                change += (c == sh.partly[o] ? min(sh.children[o], 1) : sh.children[o]) - 1;
+        int alive = 0;
+        for (int j = 0; j < K; ++j) alive += sh.parent[j] >= 0;
+        if (same && plain && id_ok(pool, id0)) {
+            if (alive != K) drop_refs(pool, id0, K - alive, freed);
+        } else {
+            for (int b = 0; b < K; ++b) {
+                const int32_t id = v[b * MOVE_THREADS];
+                if (id < 0) continue;
+                bool seen = false;
+                int32_t change = 0;
+                for (int o = 0; o < K; ++o) {
+                    if (v[o * MOVE_THREADS] != id) continue;
+                    if (o < b) { seen = true; break; }
+                    change += (c == sh.partly[o] ? min(sh.children[o], 1) : sh.children[o]) - 1;
+                }
+                if (!seen && change != 0) drop_refs(pool, id, -change, freed);
             }
-            if (!seen && change != 0) drop_refs(pool, id, -change, freed);
         }
         // rows
-        for (int j = 0; j < K; ++j) {
-            const int p = sh.parent[j];
-            int32_t id = p >= 0 ? v[p * MOVE_THREADS] : -1;
-            if (p >= 0 && c == sh.partly[p] && j != sh.first[p]) id = -1;   // its own block: later
-            if (id != v[j * MOVE_THREADS]) col[j * a.stride] = id;
+        if (!(same && plain && alive == K)) {
+            for (int j = 0; j < K; ++j) {
+                const int p = sh.parent[j];
+                int32_t id = p >= 0 ? v[p * MOVE_THREADS] : -1;
+                if (p >= 0 && c == sh.partly[p] && j != sh.first[p]) {
+                    pool.src[row0 + j] = id;                             // its own block: later
+                    id = -1;
+                }
+                if (id != v[j * MOVE_THREADS]) col[j * a.stride] = id;
+            }
         }
     }
     add_freed(pool, freed);
     // ---- the last block to finish
+    __threadfence();
     __syncthreads();
-    if (threadIdx.x == 0) {
-        __threadfence();
-        is_last = atomicAdd(pool.arrived, 1) == (int)(gridDim.x * gridDim.y) - 1;
-    }
+    if (threadIdx.x == 0) is_last = atomicAdd(pool.arrived, 1) == (int)(gridDim.x * gridDim.y) - 1;
     __syncthreads();
     if (!is_last) return;
     __threadfence();
+    const uint4 free0 = free_words(pool, (int)threadIdx.x * WORDS_PER_THREAD);
     const int n_rows = a.n_req * K;
-    const int n_free = *(volatile int32_t *)pool.n_free;
-    int done = 0, granted = 0;
-    for (int r0 = 0; r0 < n_rows; r0 += MOVE_THREADS) {
-        const int i = r0 + (int)threadIdx.x;
-        int32_t st = WG_OK, filled = 0, src = -1, full = 0;
-        bool copy = false;
-        if (i < n_rows) {
-            const int first_row = i / K * K, j = i - first_row, p = a.parent[i];
-            int32_t l = 0;
-            if (p >= 0 && p < K) {
-                l = a.len[first_row + p];
-                if (l < 0 || l > room) {
-                    st = WG_ERR_ARG;
-                    l = 0;
-                }
-            }
-            filled = l % bs;
-            full = l - filled;
-            if (filled != 0) {
-                int first = 0;
-                while (a.parent[first_row + first] != p) ++first;    // (it stops at j at the latest)
-                copy = first != j;
-                if (copy) src = __ldcg(&a.table[(int64_t)(first_row + first) * a.stride + l / bs]);
-                if (copy && !id_ok(pool, src)) copy = false;
-            }
-            pool.new_len[i] = l;
+    const int n_free = __ldcg(pool.n_free);
+    int done = 0;
+    for (int r0 = 0; r0 < n_rows; r0 += MOVE_THREADS * MOVE_ROWS) {
+        const int i0 = r0 + (int)threadIdx.x * MOVE_ROWS;
+        int32_t src[MOVE_ROWS], len[MOVE_ROWS];
+        int mine = 0, total;
+#pragma unroll
+        for (int u = 0; u < MOVE_ROWS; ++u) {
+            src[u] = i0 + u < n_rows ? __ldcg(&pool.src[i0 + u]) : -1;
+            len[u] = i0 + u < n_rows ? __ldcg(&pool.new_len[i0 + u]) : 0;
         }
-        int total;
-        const int upto = block_scan(copy ? 1 : 0, take.warps, total);
-        const int rank = done + upto - 1;
-        const bool got = copy && rank < n_free;
-        if (i < n_rows) {
-            if (copy && !got) {
-                st = WG_ERR_CAPACITY;
-                pool.new_len[i] = full;
-            }
+#pragma unroll
+        for (int u = 0; u < MOVE_ROWS; ++u) mine += src[u] >= 0;
+        int rank = done + block_scan(mine, take.warps, total) - mine;
+#pragma unroll
+        for (int u = 0; u < MOVE_ROWS; ++u) {
+            const int i = i0 + u;
+            if (i >= n_rows) break;
+            const bool got = src[u] >= 0 && rank < n_free;
             if (got) {
-                pool.src[rank] = src;
-                pool.dst[rank] = i;       // the row, until its block is known
-                pool.filled[rank] = filled;
+                pool.dst[rank] = i;               // the row, until its block is known
+                pool.from[rank] = src[u];
+                pool.filled[rank] = len[u] % bs;
+            } else if (src[u] >= 0) {
+                len[u] -= len[u] % bs;
+                if (a.status) a.status[i] = WG_ERR_CAPACITY;
             }
-            if (a.status) a.status[i] = st;
-            if (a.copy_src) a.copy_src[i] = got ? src : -1;
+            rank += src[u] >= 0;
+            a.len[i] = len[u];
+            if (a.copy_src) a.copy_src[i] = got ? src[u] : -1;
             if (a.copy_dst && !got) a.copy_dst[i] = -1;
         }
         done += total;
     }
-    granted = min(done, n_free);
+    const int granted = min(done, n_free);
     __syncthreads();
-    take_blocks(pool, take, granted);
-    for (int i = threadIdx.x; i < n_rows; i += MOVE_THREADS) a.len[i] = pool.new_len[i];
-    for (int k = threadIdx.x; k < granted; k += MOVE_THREADS) {
-        const int row = pool.dst[k], id = pool.taken[k];
-        a.table[(int64_t)row * a.stride + pool.new_len[row] / bs] = id;
+    take_blocks(pool, take, granted, free0, [&](int k, int id) {
+        const int row = pool.dst[k];
+        a.table[(int64_t)row * a.stride + a.len[row] / bs] = id;
         if (a.copy_dst) a.copy_dst[row] = id;
         pool.dst[k] = id;
-    }
+    });
     if (threadIdx.x == 0) {
         *pool.n_free = n_free - granted;
         *pool.n_copies = granted;
@@ -504,7 +566,7 @@ copy_blocks_kernel(PoolDev pool, const wg_kv_plane *planes, int32_t n_planes) {
         const int k = (int)(i / n_planes);
         const wg_kv_plane pl = planes[i - (int64_t)k * n_planes];
         const int64_t per_block = (int64_t)pool.block_size * pl.token_bytes;
-        const char *src = static_cast<const char *>(pl.base) + (int64_t)pool.src[k] * per_block;
+        const char *src = static_cast<const char *>(pl.base) + (int64_t)pool.from[k] * per_block;
         char *dst = static_cast<char *>(pl.base) + (int64_t)pool.dst[k] * per_block;
         const int64_t bytes = (int64_t)pool.filled[k] * pl.token_bytes;
         if ((((uintptr_t)src | (uintptr_t)dst | (uint64_t)bytes) & 15) == 0) {
@@ -534,9 +596,6 @@ struct wg_kv_pool {
 };
 
 namespace {
-
-// A batch of tokens up to this many is placed by the planning block itself.
-constexpr int32_t FILL_IN_PLAN = 2048;
 
 bool table_ok(const wg_kv_pool *pool, const int32_t *table, int64_t stride, int32_t max_blocks,
               const int32_t *len, int32_t n_seq) {
@@ -575,7 +634,7 @@ int32_t wg_kv_pool_create(int32_t n_blocks, int32_t block_size, int32_t max_seqs
     if (rc == WG_OK) rc = dev_alloc(&d.n_free, 1);
     if (rc == WG_OK) rc = dev_alloc(&d.n_copies, 1);
     if (rc == WG_OK) rc = dev_alloc(&d.arrived, 1);
-    for (int32_t **a : {&d.first, &d.old_len, &d.new_len, &d.src, &d.dst, &d.filled})
+    for (int32_t **a : {&d.first, &d.old_len, &d.new_len, &d.src, &d.from, &d.dst, &d.filled})
         if (rc == WG_OK) rc = dev_alloc(a, (size_t)max_seqs);
     if (rc == WG_OK && (cudaMemset(d.free_bits, 0, words * sizeof(uint32_t)) != cudaSuccess ||
                         cudaMemset(d.arrived, 0, sizeof(int32_t)) != cudaSuccess))
@@ -595,7 +654,7 @@ void wg_kv_pool_free(wg_kv_pool *p) {
     const PoolDev &d = p->dev;
     for (void *q : {(void *)d.ref, (void *)d.free_bits, (void *)d.taken, (void *)d.n_free, (void *)d.n_copies,
                     (void *)d.arrived, (void *)d.first, (void *)d.old_len, (void *)d.new_len, (void *)d.src,
-                    (void *)d.dst, (void *)d.filled})
+                    (void *)d.from, (void *)d.dst, (void *)d.filled})
         cudaFree(q);
     delete p;
 }
@@ -625,7 +684,7 @@ int32_t wg_kv_extend(wg_kv_pool *p, int32_t *table, int64_t table_stride, int32_
         return WG_ERR_ARG;
     const ExtendArgs a{table, table_stride, max_blocks, len, n_new, n_seq, cu, slot, pos, seq, n_tokens, status};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (n_tokens <= FILL_IN_PLAN) {
+    if (n_tokens <= FILL_IN_PLAN && n_seq <= PLAN_THREADS) {
         WG_CUDA(launch_pdl(extend_plan_kernel<true>, dim3(1), dim3(PLAN_THREADS), st, p->dev, a));
         WG_LAUNCHED();
         return WG_OK;
@@ -642,9 +701,8 @@ int32_t wg_kv_shrink(wg_kv_pool *p, int32_t *table, int64_t table_stride, int32_
                      const int32_t *keep, int32_t n_seq, int32_t *status, void *stream) {
     NvtxRange nvtx_range("wg_kv_shrink");
     if (!table_ok(p, table, table_stride, max_blocks, len, n_seq) || !keep) return WG_ERR_ARG;
-    const unsigned blocks = (unsigned)(((int64_t)n_seq * 32 + FILL_THREADS - 1) / FILL_THREADS);
-    WG_CUDA(launch_pdl(shrink_kernel, dim3(blocks), dim3(FILL_THREADS), static_cast<cudaStream_t>(stream),
-                       p->dev, table, table_stride, max_blocks, len, keep, n_seq, status));
+    WG_CUDA(launch_pdl(shrink_kernel, dim3((unsigned)n_seq), dim3(SHRINK_THREADS), static_cast<cudaStream_t>(stream),
+                       p->dev, table, table_stride, max_blocks, len, keep, status));
     WG_LAUNCHED();
     return WG_OK;
 }
