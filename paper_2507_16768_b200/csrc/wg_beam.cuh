@@ -4,21 +4,21 @@
 // With m = max of x over the tokens in the denominator and s = sum of exp(x - m), lse = m + log s,
 // and a candidate's score is c + (x[t] - lse).  The n_out best of a request are found without ever
 // writing scores out:
-//   * the scan reads every logit once and keeps, per chunk of 256 tokens, the largest allowed logit,
+//   * the scan reads every logit once and keeps, per chunk of 512 tokens, the largest allowed logit,
 //     and per warp (m, s) with the running-maximum rescaling of an online softmax;
 //   * a score is a non-decreasing function of the logit within a row (two fp32 roundings, both
 //     monotonic), so a chunk's best score is the score of its largest logit.  Rank the chunks of all
 //     beams by (best score, then the lower chunk number).  An element outside the first n_out
 //     chunks is beaten by the best element of each of them: by score, or at equal scores by index,
 //     since a chunk before it holds lower indices only.  So the n_out best elements lie in the first
-//     n_out chunks, and those 256 * n_out elements are all that the pick reads again.
+//     n_out chunks, and those 512 * n_out elements are all that the pick reads again.
 #pragma once
 
 #include "wg_kernels.cuh"
 
 constexpr int BEAM_THREADS = 256;           // scan
 constexpr int BEAM_WARPS = BEAM_THREADS / 32;
-constexpr int BEAM_CHUNK = 256;             // tokens per chunk maximum
+constexpr int BEAM_CHUNK = 512;             // positions per chunk maximum
 constexpr int PICK_THREADS = 512;
 constexpr int PICK_GROUPS = 128;            // at most
 constexpr int PICK_LIST = 512;              // candidates that are ranked against each other
@@ -142,37 +142,58 @@ __device__ __forceinline__ uint32_t shifted_word(const MaskSource &m, int w, int
     return __funnelshift_l(m.word(w - 1), m.word(w), off);
 }
 
-// Disallowed elements of a piece become -inf.  bit i of `bits` belongs to element i.
-template <typename E>
-__device__ __forceinline__ void mask_piece(uint32_t (&w)[4], uint32_t bits) {
-    if (sizeof(E) == 2) {
-        // bit i of a group of four to the top of byte i (the partial products do not overlap), then
-        // a byte permute that spreads that top bit over the element's two bytes
+// Disallowed elements become -inf, in all pieces of a step.  Byte i of `bits` (fp32: its low nibble)
+// belongs to piece i.  bf16: with bit j of every byte moved to the byte's top, one byte permute spreads
+// the top bits of two such words over the two elements of a word (its sign-spreading mode, which the
+// intrinsic does not know), so a pair costs a permute and a select.
+template <int SEL>
+__device__ __forceinline__ uint32_t permute(uint32_t lo, uint32_t hi) {
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(lo), "r"(hi), "n"(SEL));
+    return r;
+}
+
+template <typename E, int N>
+__device__ __forceinline__ void mask_pieces(uint32_t (&w)[N][4], uint32_t bits) {
+    if constexpr (sizeof(E) == 2) {
+        static_assert(N == 4, "a byte of bits per piece");
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t t = ((bits >> (4 * h)) & 0xFu) * 0x10204080u;
-            uint32_t lo, hi;    // (the intrinsic knows no sign spreading)
-            asm("prmt.b32 %0, %1, 0, 0x9988;" : "=r"(lo) : "r"(t));
-            asm("prmt.b32 %0, %1, 0, 0xBBAA;" : "=r"(hi) : "r"(t));
-            w[2 * h] = (w[2 * h] & lo) | (NEG_INF_BF16X2 & ~lo);
-            w[2 * h + 1] = (w[2 * h + 1] & hi) | (NEG_INF_BF16X2 & ~hi);
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t lo = bits << (7 - 2 * j), hi = bits << (6 - 2 * j);
+            const uint32_t keep[4] = {permute<0xCC88>(lo, hi), permute<0xDD99>(lo, hi), permute<0xEEAA>(lo, hi),
+                                      permute<0xFFBB>(lo, hi)};
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i][j] = (w[i][j] & keep[i]) | (NEG_INF_BF16X2 & ~keep[i]);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = ((bits >> i) & 1u) ? w[i] : NEG_INF_F32;
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[i][j] = ((bits >> (8 * i + j)) & 1u) ? w[i][j] : NEG_INF_F32;
     }
 }
 
-// Largest element of a piece (NaN elements are passed over unless there is nothing else).
-template <typename E>
-__device__ __forceinline__ float piece_max(const uint32_t (&w)[4]) {
-    if (sizeof(E) == 2) {
-        const uint32_t u = bf162_bits(__hmax2(__hmax2(as_bf162(w[0]), as_bf162(w[1])),
-                                              __hmax2(as_bf162(w[2]), as_bf162(w[3]))));
+// Largest element of N pieces (NaN elements are passed over).
+template <typename E, int N>
+__device__ __forceinline__ float pieces_max(const uint32_t (&w)[N][4], int first, int end) {
+    if constexpr (sizeof(E) == 2) {
+        __nv_bfloat162 m = as_bf162(NEG_INF_BF16X2);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i >= first && i < end)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) m = __hmax2(m, as_bf162(w[i][j]));
+        const uint32_t u = bf162_bits(m);
         return fmaxf(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
+    } else {
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i >= first && i < end)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) m = fmaxf(m, __uint_as_float(w[i][j]));
+        return m;
     }
-    return fmaxf(fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1])),
-                 fmaxf(__uint_as_float(w[2]), __uint_as_float(w[3])));
 }
 
 __device__ __forceinline__ float warp_max(float x) {
@@ -191,136 +212,225 @@ __device__ __forceinline__ float exp2_fast(float x) {
 
 constexpr float LOG2_E = 1.4426950408889634f;
 
-// Sum of exp(x - m) over a piece.  The difference is formed before it is scaled: a row whose
-// largest logit is the type's lowest value must still give exp(0) for it.
-template <typename E>
-__device__ __forceinline__ void piece_exp(const uint32_t (&w)[4], float m, float &s0, float &s1) {
+// Where a row's exponentials are measured from: 2^(x * log2 e - reference).  Kept in the logarithm's own
+// base, so that one fused multiply-add makes the exponent and no rounding of m * log2 e is lost.
+// Beyond |m| = 2^100 that product could overflow (masks of the type's lowest value, infinities): the
+// difference x - m is formed first there.
+constexpr float FAR_M = 1.2676506e30f;
+
+__device__ __forceinline__ float reference(float m) { return __fmul_rn(m, LOG2_E); }
+
+// What a sum measured from m is multiplied by to be measured from high >= m (-inf: a sum of nothing).
+__device__ __forceinline__ float moved(float m, float high) {
+    return exp2_fast(fabsf(high) < FAR_M ? reference(m) - reference(high) : (m - high) * LOG2_E);
+}
+
+// Adds exp(x - m) of N pieces to four sums.
+template <typename E, int N>
+__device__ __forceinline__ void pieces_exp(const uint32_t (&w)[N][4], float m, float (&sum)[4]) {
+    const bool near = fabsf(m) < FAR_M;          // uniform
+    const float minus_ref = -reference(m);
+    auto each = [&](auto term) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (sizeof(E) == 2) {
-            s0 += exp2_fast((__uint_as_float(w[i] << 16) - m) * LOG2_E);
-            s1 += exp2_fast((__uint_as_float(w[i] & 0xFFFF0000u) - m) * LOG2_E);
-        } else if (i & 1) {
-            s1 += exp2_fast((__uint_as_float(w[i]) - m) * LOG2_E);
-        } else {
-            s0 += exp2_fast((__uint_as_float(w[i]) - m) * LOG2_E);
-        }
-    }
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (sizeof(E) == 2) {
+                    sum[j] += term(__uint_as_float(w[i][j] << 16));
+                    sum[j] += term(__uint_as_float(w[i][j] & 0xFFFF0000u));
+                } else {
+                    sum[j] += term(__uint_as_float(w[i][j]));
+                }
+            }
+    };
+    if (near) each([&](float x) { return exp2_fast(fmaf(x, LOG2_E, minus_ref)); });
+    else each([&](float x) { return exp2_fast((x - m) * LOG2_E); });
+}
+
+// What (m, s) say of the sum of exp: its logarithm.
+__device__ __forceinline__ float log_sum(float m, float s) {
+    if (fabsf(m) < FAR_M) return (reference(m) + log2f(s)) * 0.6931471805599453f;
+    return m + logf(s);
 }
 
 // ---------------------------------------------------------------------------------------
-// Scan.  A warp works in steps of 2 KB of one row (four 16-byte loads per lane): 1024 bf16 or 512 fp32
-// positions, and takes items of a.per_item consecutive steps of a row from a device counter (rows
-// differ a lot: a finished one costs nothing, a literal state a few sectors, a free-text slot every
-// logit).  Within an item the mask words of two steps and the logits of one are in flight while a
-// step is worked on.
+// Scan.  A warp works in steps of 4 KB of one row (eight 16-byte loads per lane, all in flight
+// together): 2048 bf16 or 1024 fp32 positions, and takes items of a.per_item consecutive steps of a row
+// from a device counter (rows differ a lot: a finished one costs nothing, a literal state a few
+// sectors, a free-text slot every logit).
 // ---------------------------------------------------------------------------------------
 template <typename E>
 struct ScanShape {
     static constexpr int EPC = ElemTraits<E>::PER_CHUNK;
-    static constexpr int LOADS = 4;                             // per lane and step
-    static constexpr int STEP = LOADS * 32 * EPC;               // positions: 1024, 512
+    static constexpr int HALF = 4;                              // loads a mask register covers
+    static constexpr int LOADS = 2 * HALF;                      // per lane and step
+    static constexpr int STEP = LOADS * 32 * EPC;               // positions: 2048, 1024
     static constexpr int CHUNKS = STEP / BEAM_CHUNK;            // 4, 2
-    static constexpr int PER_CHUNK = LOADS / CHUNKS;            // loads per chunk: 1, 2
+    static constexpr int PER_CHUNK = LOADS / CHUNKS;            // loads per chunk: 2, 4
+    static constexpr int WORDS = STEP / 32 / 32;                // mask words per lane and step: 2, 1
 };
+
+// A row as the scan walks it.
+template <typename E, int NORM, bool CTX>
+struct ScanRow {
+    using S = ScanShape<E>;
+    RowView<E> x;
+    MaskSource mask;
+
+    __device__ __forceinline__ ScanRow(const BeamArgs &a, const CtxDev &ctx, int row)
+        : x(a.logits, a.row_stride, row, a.V), mask(mask_source<CTX>(a, ctx, row)) {}
+
+    // whether step s lies wholly inside the row
+    __device__ __forceinline__ bool whole(int s) const {
+        return s * S::STEP >= x.off && (s + 1) * S::STEP <= x.V + x.off;
+    }
+
+    // lane l: the mask bits of positions 32 * l .. of step s, and of those 1024 further on
+    __device__ __forceinline__ void words(uint32_t (&word)[S::WORDS], int s) const {
+        const int w = s * (S::STEP / 32) + (int)(threadIdx.x & 31);
+        if (whole(s) && (!CTX || !mask.hdr)) {
+#pragma unroll
+            for (int i = 0; i < S::WORDS; ++i) {
+                word[i] = mask.words ? __ldg(mask.words + w + 32 * i) : 0xFFFFFFFFu;
+                if (x.off != 0 && mask.words)
+                    word[i] = __funnelshift_l(__ldg(mask.words + max(w + 32 * i - 1, 0)), word[i], x.off);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < S::WORDS; ++i) word[i] = shifted_word(mask, w + 32 * i, x.off);
+        }
+    }
+
+    // The step's words dealt to the lanes that hold the elements: byte i of bits[h] (fp32: its low
+    // nibble) belongs to this lane's piece HALF * h + i.
+    __device__ __forceinline__ static void deal(const uint32_t (&word)[S::WORDS], uint32_t (&bits)[2]) {
+        const int lane = threadIdx.x & 31;
+        const int byte = lane * S::EPC / 8 & 3;
+        const uint32_t pick = byte | (4 + byte) << 4;    // the wanted byte of two words, side by side
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t w[S::HALF];
+#pragma unroll
+            for (int i = 0; i < S::HALF; ++i)
+                w[i] = __shfl_sync(0xFFFFFFFFu, word[S::WORDS == 2 ? h : 0],
+                                   ((S::WORDS == 2 ? i : h * S::HALF + i) * 32 + lane) * S::EPC / 32);
+            bits[h] = __byte_perm(__byte_perm(w[0], w[1], pick), __byte_perm(w[2], w[3], pick), 0x5410);
+            if (sizeof(E) == 4) bits[h] = (bits[h] >> (lane * S::EPC & 4)) & 0x0F0F0F0Fu;
+        }
+    }
+
+    // This lane's pieces of step s.  A piece without an allowed element is not read, unless all are
+    // summed: what is left in v is masked later.
+    __device__ __forceinline__ void load(uint32_t (&v)[2][S::HALF][4], int s, const uint32_t (&bits)[2]) const {
+        const int p = s * S::STEP + (int)(threadIdx.x & 31) * S::EPC;
+        const E *at = x.base + p;
+        const bool inside = whole(s);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < S::HALF; ++i) {
+                const uint32_t want = NORM == WG_BEAM_NORM_FULL ? 1u : bits[h] & (0xFFu << (8 * i));
+                if (inside) {
+                    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t"
+                                 "@p ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                                 : "+r"(v[h][i][0]), "+r"(v[h][i][1]), "+r"(v[h][i][2]), "+r"(v[h][i][3])
+                                 : "l"(at + (h * S::HALF + i) * 32 * S::EPC), "r"(want));
+                } else if (want) {
+                    const uint4 one = x.piece(p + (h * S::HALF + i) * 32 * S::EPC);
+                    v[h][i][0] = one.x; v[h][i][1] = one.y; v[h][i][2] = one.z; v[h][i][3] = one.w;
+                }
+            }
+    }
+};
+
+// m becomes high (if that is more), and the sums are measured from there.
+__device__ __forceinline__ void raise(float high, float &m, float (&sum)[4]) {
+    if (high > m) {
+        const float f = moved(m, high);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] *= f;
+        m = high;
+    }
+}
+
+// One step's share of a row: its chunk maxima out, its exponentials added to (m, sum); m is the same in
+// all lanes.
+template <typename E, int NORM>
+__device__ __forceinline__ void scan_step(uint32_t (&v)[2][ScanShape<E>::HALF][4], const uint32_t (&bits)[2],
+                                          float *chunks, float &m, float (&sum)[4]) {
+    using S = ScanShape<E>;
+    constexpr uint32_t ALL = sizeof(E) == 2 ? 0xFFFFFFFFu : 0x0F0F0F0Fu;
+    constexpr int PER_HALF = S::CHUNKS / 2;
+    float best[S::CHUNKS];
+#pragma unroll
+    for (int i = 0; i < S::CHUNKS; ++i) best[i] = -INFINITY;
+    if (NORM == WG_BEAM_NORM_FULL) {
+        // the whole vocabulary is summed; the maxima are those of what is allowed
+        raise(warp_max(fmaxf(pieces_max<E>(v[0], 0, S::HALF), pieces_max<E>(v[1], 0, S::HALF))), m, sum);
+        if (m > -INFINITY) {
+            pieces_exp<E>(v[0], m, sum);
+            pieces_exp<E>(v[1], m, sum);
+        }
+    }
+    if (__any_sync(0xFFFFFFFFu, (bits[0] | bits[1]) != 0u)) {
+        if (!__all_sync(0xFFFFFFFFu, (bits[0] & bits[1]) == ALL)) {
+            mask_pieces<E>(v[0], bits[0]);
+            mask_pieces<E>(v[1], bits[1]);
+        }
+#pragma unroll
+        for (int i = 0; i < S::CHUNKS; ++i) {
+            const int at = i % PER_HALF * S::PER_CHUNK;
+            best[i] = warp_max(pieces_max<E>(v[i / PER_HALF], at, at + S::PER_CHUNK));
+        }
+        if (NORM == WG_BEAM_NORM_ALLOWED) {
+            float high = best[0];
+#pragma unroll
+            for (int i = 1; i < S::CHUNKS; ++i) high = fmaxf(high, best[i]);
+            raise(high, m, sum);
+            if (m > -INFINITY) {
+                pieces_exp<E>(v[0], m, sum);
+                pieces_exp<E>(v[1], m, sum);
+            }
+        }
+    }
+    if ((threadIdx.x & 31) == 0) {
+        if constexpr (S::CHUNKS == 4) *reinterpret_cast<float4 *>(chunks) = make_float4(best[0], best[1], best[2], best[3]);
+        else *reinterpret_cast<float2 *>(chunks) = make_float2(best[0], best[1]);
+    }
+}
 
 template <typename E, int NORM, bool CTX>
 __global__ void __launch_bounds__(BEAM_THREADS, 4)
 beam_scan_kernel(BeamArgs a, CtxDev ctx) {
     using S = ScanShape<E>;
-    constexpr uint32_t ALL = (1u << S::EPC) - 1u;
+    using Row = ScanRow<E, NORM, CTX>;
     pdl_enter();
     const int lane = threadIdx.x & 31;
     uint32_t item = blockIdx.x * BEAM_WARPS + (threadIdx.x >> 5);
+    uint32_t v[2][S::HALF][4] = {};
     while (item < a.n_items) {
         uint32_t taken = 0;
         if (lane == 0) taken = (uint32_t)atomicAdd(a.next_item, 1);
         const int row = (int)(item / (uint32_t)a.items_per_row);
-        const int part = (int)(item - (uint32_t)row * (uint32_t)a.items_per_row);
-        const RowView<E> x(a.logits, a.row_stride, row, a.V);
-        const MaskSource mask = mask_source<CTX>(a, ctx, row);
-        const int n_steps = (a.V + x.off + S::STEP - 1) / S::STEP;
-        const int first = part * a.per_item, end = min(first + a.per_item, n_steps);
-        // lane l holds the mask word of positions 32 * l .. of the step
-        auto step_word = [&](int s) -> uint32_t {
-            return s < end && lane < S::STEP / 32 ? shifted_word(mask, s * (S::STEP / 32) + lane, x.off) : 0u;
-        };
-        uint32_t word = step_word(first), word1 = step_word(first + 1);
+        const Row r(a, ctx, row);
+        const int first = (int)(item - (uint32_t)row * (uint32_t)a.items_per_row) * a.per_item;
+        const int end = min(first + a.per_item, (a.V + r.x.off + S::STEP - 1) / S::STEP);
+        uint32_t word[S::WORDS];
+        r.words(word, first);
         if (beam_row_kind<CTX>(a, ctx, row, a.score[row]) == BEAM_ROW_LIVE) {
-            uint4 next[S::LOADS];
-            auto request = [&](int s, uint32_t words) {
-#pragma unroll
-                for (int i = 0; i < S::LOADS; ++i) {
-                    const int c = i * 32 + lane;              // piece within the step
-                    const uint32_t bits = __shfl_sync(0xFFFFFFFFu, words, c * S::EPC / 32) >> (c * S::EPC % 32) & ALL;
-                    next[i] = make_uint4(0, 0, 0, 0);
-                    if (NORM == WG_BEAM_NORM_FULL || bits != 0u) next[i] = x.piece(s * S::STEP + c * S::EPC);
-                }
-            };
-            float *chunk_row = a.chunk_max + (int64_t)row * a.chunk_stride;
-            float m = -INFINITY, s0 = 0.f, s1 = 0.f;          // m is the same in all lanes
-            if (first < end) request(first, word);
+            float *chunks = a.chunk_max + (int64_t)row * a.chunk_stride + first * S::CHUNKS;
+            float m = -INFINITY, sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
             for (int s = first; s < end; ++s) {
-                uint4 v[S::LOADS];
-#pragma unroll
-                for (int i = 0; i < S::LOADS; ++i) v[i] = next[i];
-                const uint32_t words = word;
-                word = word1;
-                word1 = step_word(s + 2);
-                if (s + 1 < end) request(s + 1, word);
-                float best[S::CHUNKS];
-#pragma unroll
-                for (int i = 0; i < S::CHUNKS; ++i) best[i] = -INFINITY;
-                if (NORM == WG_BEAM_NORM_FULL || __any_sync(0xFFFFFFFFu, words != 0u)) {
-                    uint32_t w[S::LOADS][4];
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int i = 0; i < S::LOADS; ++i) {
-                        const int c = i * 32 + lane;
-                        const uint32_t bits = __shfl_sync(0xFFFFFFFFu, words, c * S::EPC / 32) >> (c * S::EPC % 32) & ALL;
-                        uint32_t y[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-                        if (NORM == WG_BEAM_NORM_FULL) {
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) w[i][j] = y[j];
-                            top = fmaxf(top, piece_max<E>(y));
-                            mask_piece<E>(y, bits);
-                        } else {
-                            mask_piece<E>(y, bits);
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) w[i][j] = y[j];
-                        }
-                        best[i / S::PER_CHUNK] = fmaxf(best[i / S::PER_CHUNK], piece_max<E>(y));
-                    }
-#pragma unroll
-                    for (int i = 0; i < S::CHUNKS; ++i) best[i] = warp_max(best[i]);
-                    if (NORM != WG_BEAM_NORM_NONE) {
-                        float high = m;
-                        if (NORM == WG_BEAM_NORM_FULL) {
-                            high = fmaxf(high, warp_max(top));
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < S::CHUNKS; ++i) high = fmaxf(high, best[i]);
-                        }
-                        if (high > m) {                        // uniform
-                            const float scale = exp2_fast((m - high) * LOG2_E);
-                            s0 *= scale;
-                            s1 *= scale;
-                            m = high;
-                        }
-                        if (m > -INFINITY) {
-#pragma unroll
-                            for (int i = 0; i < S::LOADS; ++i) piece_exp<E>(w[i], m, s0, s1);
-                        }
-                    }
-                }
-                if (lane == 0) {
-                    float *dst = chunk_row + s * S::CHUNKS;
-                    if constexpr (S::CHUNKS == 4) *reinterpret_cast<float4 *>(dst) = make_float4(best[0], best[1], best[2], best[3]);
-                    else *reinterpret_cast<float2 *>(dst) = make_float2(best[0], best[1]);
-                }
+                uint32_t bits[2];
+                Row::deal(word, bits);
+                r.load(v, s, bits);
+                if (s + 1 < end) r.words(word, s + 1);
+                scan_step<E, NORM>(v, bits, chunks, m, sum);
+                chunks += S::CHUNKS;
             }
             if (NORM != WG_BEAM_NORM_NONE) {
-                float s = s0 + s1;
+                float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
                 if (lane == 0) a.parts[item] = make_float2(m, s);
@@ -466,17 +576,17 @@ __device__ __forceinline__ int beam_pick(PickShared &sh, const BeamArgs &a, cons
                 const float2 p = a.parts[(int64_t)row * a.items_per_row + i];
                 const float high = fmaxf(m, p.x);
                 if (high > -INFINITY)          // (a pair that saw nothing is (-inf, 0))
-                    s = s * exp2_fast((m - high) * LOG2_E) + p.y * exp2_fast((p.x - high) * LOG2_E);
+                    s = s * moved(m, high) + p.y * moved(p.x, high);
                 m = high;
             }
         }
         const int kind = beam_row_kind<CTX>(a, ctx, row, score);
         if (a.norm != WG_BEAM_NORM_NONE) {
             const float high = warp_max(m);
-            s = high > -INFINITY ? s * exp2_fast((m - high) * LOG2_E) : 0.f;
+            s = high > -INFINITY ? s * moved(m, high) : 0.f;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-            lse = high + logf(s);
+            lse = log_sum(high, s);
         }
         if (lane == 0) {
             const RowView<E> x(a.logits, a.row_stride, row, a.V);

@@ -11,10 +11,10 @@ struct wg_beam {
 
 namespace {
 
-// Spans of 1024 positions per row, for the worst alignment of a row (it may begin up to 7 elements into
+// Spans of 2048 positions per row, for the worst alignment of a row (it may begin up to 7 elements into
 // a piece).
-int32_t beam_spans(int32_t V) { return (V + 7 + 1023) / 1024; }
-constexpr int BEAM_MAX_STEPS = 8;
+int32_t beam_spans(int32_t V) { return (V + 7 + 2047) / 2048; }
+constexpr int BEAM_MAX_STEPS = 3;
 
 template <typename E, int NORM, bool CTX>
 cudaError_t launch_beam_scan(const BeamArgs &a, const CtxDev &ctx, dim3 grid, cudaStream_t st) {
@@ -72,7 +72,7 @@ int32_t wg_beam_create(int32_t V, int32_t max_requests, int32_t max_beams, int32
     NvtxRange nvtx_range("wg_beam_create");
     if (!out) return WG_ERR_ARG;
     *out = nullptr;
-    if (V < 1 || V > INT32_MAX - 2048 || max_requests < 1 || max_beams < 1 || max_beams > WG_BEAM_MAX_BEAMS ||
+    if (V < 1 || V > INT32_MAX - 4096 || max_requests < 1 || max_beams < 1 || max_beams > WG_BEAM_MAX_BEAMS ||
         max_out < 1 || max_out > WG_BEAM_MAX_OUT || (int64_t)max_requests * max_beams > WG_MAX_ROWS ||
         (int64_t)V * max_beams >= (1LL << 32) ||
         (int64_t)max_requests * max_beams * beam_spans(V) * 2 >= (1LL << 31))   // items have 32-bit numbers
