@@ -17,6 +17,10 @@
 #include "wg_kernels.cuh"
 
 constexpr int BEAM_THREADS = 256;           // scan
+#ifndef WGB
+#define WGB 4
+#endif
+constexpr int BEAM_BLOCKS = WGB;              // per SM
 constexpr int BEAM_WARPS = BEAM_THREADS / 32;
 constexpr int BEAM_CHUNK = 512;             // positions per chunk maximum
 constexpr int PICK_THREADS = 512;
@@ -32,13 +36,12 @@ struct BeamArgs {
     const int32_t *finished;  // or NULL
     const int32_t *gid, *sid; // with a context: the rows' states (finished = DONE)
     int32_t n_beam, V, W, n_out, eos, norm;
-    int32_t per_item, items_per_row;  // steps a warp takes at a time
-    uint32_t n_items;
+    int32_t n_rows, steps_per_row;
     int32_t chunk_stride;     // chunk maxima per row, a multiple of 4
     int32_t chunk_log2;       // the pick's threads side by side on a row: 32 .. 512
     float *chunk_max;         // [rows][chunk_stride]
-    float2 *parts;            // [n_items] (max, sum) of every item
-    int32_t *next_item;       // items taken beyond the first of every warp; zero between calls
+    float2 *parts;            // [rows][steps_per_row] (max, sum) of every step
+    int32_t *next_item;       // items taken beyond the first two of every block; zero between calls
 };
 
 // What a step under grammars does with the selection.
@@ -225,26 +228,53 @@ __device__ __forceinline__ float moved(float m, float high) {
     return exp2_fast(fabsf(high) < FAR_M ? reference(m) - reference(high) : (m - high) * LOG2_E);
 }
 
-// Adds exp(x - m) of N pieces to four sums.
+// Two fp32 values in one 64-bit register, for the instructions that work on both.
+typedef unsigned long long Pair;
+__device__ __forceinline__ Pair pair(float lo, float hi) {
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 halves(Pair x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ __forceinline__ Pair add2(Pair x, Pair y) {
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(Pair x, Pair y, Pair z) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+    return r;
+}
+
+// Adds exp(x - m) of N pieces to two pairs of sums.
 template <typename E, int N>
-__device__ __forceinline__ void pieces_exp(const uint32_t (&w)[N][4], float m, float (&sum)[4]) {
-    const bool near = fabsf(m) < FAR_M;          // uniform
-    const float minus_ref = -reference(m);
-    auto each = [&](auto term) {
+__device__ __forceinline__ void pieces_exp(const uint32_t (&w)[N][4], float m, Pair (&sum)[2]) {
+    auto each = [&](auto exponent) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (sizeof(E) == 2) {
-                    sum[j] += term(__uint_as_float(w[i][j] << 16));
-                    sum[j] += term(__uint_as_float(w[i][j] & 0xFFFF0000u));
-                } else {
-                    sum[j] += term(__uint_as_float(w[i][j]));
-                }
+            for (int j = 0; j < 4; j += sizeof(E) == 2 ? 1 : 2) {
+                const Pair x = sizeof(E) == 2
+                    ? pair(__uint_as_float(w[i][j] << 16), __uint_as_float(w[i][j] & 0xFFFF0000u))
+                    : pair(__uint_as_float(w[i][j]), __uint_as_float(w[i][(j + 1) & 3]));
+                const float2 e = halves(exponent(x));
+                Pair &to = sum[sizeof(E) == 2 ? j & 1 : j >> 1];
+                to = add2(to, pair(exp2_fast(e.x), exp2_fast(e.y)));
             }
     };
-    if (near) each([&](float x) { return exp2_fast(fmaf(x, LOG2_E, minus_ref)); });
-    else each([&](float x) { return exp2_fast((x - m) * LOG2_E); });
+    const Pair scale = pair(LOG2_E, LOG2_E);
+    if (fabsf(m) < FAR_M) {                      // uniform
+        const Pair minus = pair(-reference(m), -reference(m));
+        each([&](Pair x) { return fma2(x, scale, minus); });
+    } else {
+        const Pair minus = pair(-m, -m), zero = pair(-0.f, -0.f);
+        each([&](Pair x) { return fma2(add2(x, minus), scale, zero); });
+    }
 }
 
 // What (m, s) say of the sum of exp: its logarithm.
@@ -323,32 +353,37 @@ struct ScanRow {
     // summed: what is left in v is masked later.
     __device__ __forceinline__ void load(uint32_t (&v)[2][S::HALF][4], int s, const uint32_t (&bits)[2]) const {
         const int p = s * S::STEP + (int)(threadIdx.x & 31) * S::EPC;
-        const E *at = x.base + p;
-        const bool inside = whole(s);
+        if (whole(s)) {
+            const E *at = x.base + p;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < S::HALF; ++i) {
-                const uint32_t want = NORM == WG_BEAM_NORM_FULL ? 1u : bits[h] & (0xFFu << (8 * i));
-                if (inside) {
+                for (int i = 0; i < S::HALF; ++i)
                     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t"
                                  "@p ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
                                  : "+r"(v[h][i][0]), "+r"(v[h][i][1]), "+r"(v[h][i][2]), "+r"(v[h][i][3])
-                                 : "l"(at + (h * S::HALF + i) * 32 * S::EPC), "r"(want));
-                } else if (want) {
-                    const uint4 one = x.piece(p + (h * S::HALF + i) * 32 * S::EPC);
-                    v[h][i][0] = one.x; v[h][i][1] = one.y; v[h][i][2] = one.z; v[h][i][3] = one.w;
-                }
-            }
+                                 : "l"(at + (h * S::HALF + i) * 32 * S::EPC),
+                                   "r"(NORM == WG_BEAM_NORM_FULL ? 1u : bits[h] & (0xFFu << (8 * i))));
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < S::HALF; ++i)
+                    if (NORM == WG_BEAM_NORM_FULL || (bits[h] & (0xFFu << (8 * i)))) {
+                        const uint4 one = x.piece(p + (h * S::HALF + i) * 32 * S::EPC);
+                        v[h][i][0] = one.x; v[h][i][1] = one.y; v[h][i][2] = one.z; v[h][i][3] = one.w;
+                    }
+        }
     }
 };
 
 // m becomes high (if that is more), and the sums are measured from there.
-__device__ __forceinline__ void raise(float high, float &m, float (&sum)[4]) {
+__device__ __forceinline__ void raise(float high, float &m, Pair (&sum)[2]) {
     if (high > m) {
         const float f = moved(m, high);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sum[j] *= f;
+        const Pair both = pair(f, f), zero = pair(-0.f, -0.f);
+        sum[0] = fma2(sum[0], both, zero);
+        sum[1] = fma2(sum[1], both, zero);
         m = high;
     }
 }
@@ -357,7 +392,7 @@ __device__ __forceinline__ void raise(float high, float &m, float (&sum)[4]) {
 // all lanes.
 template <typename E, int NORM>
 __device__ __forceinline__ void scan_step(uint32_t (&v)[2][ScanShape<E>::HALF][4], const uint32_t (&bits)[2],
-                                          float *chunks, float &m, float (&sum)[4]) {
+                                          float *chunks, float &m, Pair (&sum)[2]) {
     using S = ScanShape<E>;
     constexpr uint32_t ALL = sizeof(E) == 2 ? 0xFFFFFFFFu : 0x0F0F0F0Fu;
     constexpr int PER_HALF = S::CHUNKS / 2;
@@ -399,44 +434,71 @@ __device__ __forceinline__ void scan_step(uint32_t (&v)[2][ScanShape<E>::HALF][4
     }
 }
 
+// What a warp knows of its next step: where it is, and, asked for a turn ahead, its mask words and
+// whether the row counts.
+template <typename E>
+struct ScanNext {
+    int row, s;
+    uint32_t word[ScanShape<E>::WORDS];
+    float score;
+    int32_t finished;
+};
+
 template <typename E, int NORM, bool CTX>
-__global__ void __launch_bounds__(BEAM_THREADS, 4)
+__global__ void __launch_bounds__(BEAM_THREADS, BEAM_BLOCKS)
 beam_scan_kernel(BeamArgs a, CtxDev ctx) {
     using S = ScanShape<E>;
     using Row = ScanRow<E, NORM, CTX>;
+    __shared__ uint32_t published[2];
     pdl_enter();
-    const int lane = threadIdx.x & 31;
-    uint32_t item = blockIdx.x * BEAM_WARPS + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t n_items = ((uint32_t)a.n_rows * (uint32_t)a.steps_per_row + BEAM_WARPS - 1) / BEAM_WARPS;
+    const auto look = [&](uint32_t item) -> ScanNext<E> {
+        ScanNext<E> n;
+        const uint32_t step = item * BEAM_WARPS + warp;
+        n.row = (int)(step / (uint32_t)a.steps_per_row);
+        n.s = (int)(step - (uint32_t)n.row * (uint32_t)a.steps_per_row);
+        if (item >= n_items || n.row >= a.n_rows) {
+            n.row = -1;
+            return n;
+        }
+        n.score = a.score[n.row];
+        n.finished = !CTX && a.finished ? a.finished[n.row] : 0;
+        Row(a, ctx, n.row).words(n.word, n.s);
+        return n;
+    };
+    uint32_t item = blockIdx.x, after = gridDim.x + blockIdx.x;
+    ScanNext<E> n = look(item);
     uint32_t v[2][S::HALF][4] = {};
-    while (item < a.n_items) {
-        uint32_t taken = 0;
-        if (lane == 0) taken = (uint32_t)atomicAdd(a.next_item, 1);
-        const int row = (int)(item / (uint32_t)a.items_per_row);
-        const Row r(a, ctx, row);
-        const int first = (int)(item - (uint32_t)row * (uint32_t)a.items_per_row) * a.per_item;
-        const int end = min(first + a.per_item, (a.V + r.x.off + S::STEP - 1) / S::STEP);
-        uint32_t word[S::WORDS];
-        r.words(word, first);
-        if (beam_row_kind<CTX>(a, ctx, row, a.score[row]) == BEAM_ROW_LIVE) {
-            float *chunks = a.chunk_max + (int64_t)row * a.chunk_stride + first * S::CHUNKS;
-            float m = -INFINITY, sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-            for (int s = first; s < end; ++s) {
-                uint32_t bits[2];
-                Row::deal(word, bits);
-                r.load(v, s, bits);
-                if (s + 1 < end) r.words(word, s + 1);
-                scan_step<E, NORM>(v, bits, chunks, m, sum);
-                chunks += S::CHUNKS;
-            }
+    for (int turn = 0; item < n_items; turn ^= 1) {
+        uint32_t taken = 0;
+        if (threadIdx.x == 0) taken = (uint32_t)atomicAdd(a.next_item, 1);
+        const int row = n.row, s = n.s;
+        const bool live = row >= 0 && (CTX ? beam_row_kind<CTX>(a, ctx, row, n.score) == BEAM_ROW_LIVE
+                                           : n.score > -INFINITY && !n.finished);
+        uint32_t bits[2];
+        if (live) {
+            Row::deal(n.word, bits);
+            Row(a, ctx, row).load(v, s, bits);
+        }
+        n = look(after);
+        if (live) {
+            float m = -INFINITY;
+            Pair sum[2] = {0ull, 0ull};
+            scan_step<E, NORM>(v, bits, a.chunk_max + (int64_t)row * a.chunk_stride + s * S::CHUNKS, m, sum);
             if (NORM != WG_BEAM_NORM_NONE) {
-                float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                const float2 two = halves(add2(sum[0], sum[1]));
+                float total = two.x + two.y;
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-                if (lane == 0) a.parts[item] = make_float2(m, s);
+                for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+                if (lane == 0) a.parts[(int64_t)row * a.steps_per_row + s] = make_float2(m, total);
             }
         }
-        item = gridDim.x * BEAM_WARPS + __shfl_sync(0xFFFFFFFFu, taken, 0);
+        if (threadIdx.x == 0) published[turn] = 2 * gridDim.x + taken;
+        __syncthreads();
+        item = after;
+        after = published[turn];
     }
 }
 
@@ -572,8 +634,8 @@ __device__ __forceinline__ int beam_pick(PickShared &sh, const BeamArgs &a, cons
         float m = -INFINITY, s = 0.f, lse = 0.f;
         if (a.norm != WG_BEAM_NORM_NONE) {     // (for a row that is not live the pairs are left over: not used)
 #pragma unroll 4
-            for (int i = lane; i < a.items_per_row; i += 32) {
-                const float2 p = a.parts[(int64_t)row * a.items_per_row + i];
+            for (int i = lane; i < a.steps_per_row; i += 32) {
+                const float2 p = a.parts[(int64_t)row * a.steps_per_row + i];
                 const float high = fmaxf(m, p.x);
                 if (high > -INFINITY)          // (a pair that saw nothing is (-inf, 0))
                     s = s * moved(m, high) + p.y * moved(p.x, high);

@@ -14,16 +14,15 @@ namespace {
 // Spans of 2048 positions per row, for the worst alignment of a row (it may begin up to 7 elements into
 // a piece).
 int32_t beam_spans(int32_t V) { return (V + 7 + 2047) / 2048; }
-constexpr int BEAM_MAX_STEPS = 3;
 
 template <typename E, int NORM, bool CTX>
-cudaError_t launch_beam_scan(const BeamArgs &a, const CtxDev &ctx, dim3 grid, cudaStream_t st) {
-    return launch_pdl(beam_scan_kernel<E, NORM, CTX>, grid, dim3(BEAM_THREADS), st, a, ctx);
+cudaError_t launch_beam_scan(const BeamArgs &a, const CtxDev &ctx, unsigned grid, cudaStream_t st) {
+    return launch_pdl(beam_scan_kernel<E, NORM, CTX>, dim3(grid), dim3(BEAM_THREADS), st, a, ctx);
 }
 
 template <typename E, bool CTX>
 int32_t launch_beam(const BeamArgs &a, const CtxDev &ctx, const VocabDev &v, const BeamStepArgs &step,
-                    int32_t n_req, dim3 grid, float *score_out, int32_t *parent_out, int32_t *token_out,
+                    int32_t n_req, unsigned grid, float *score_out, int32_t *parent_out, int32_t *token_out,
                     cudaStream_t st) {
     if (a.norm == WG_BEAM_NORM_ALLOWED)
         WG_CUDA((launch_beam_scan<E, WG_BEAM_NORM_ALLOWED, CTX>(a, ctx, grid, st)));
@@ -38,21 +37,15 @@ int32_t launch_beam(const BeamArgs &a, const CtxDev &ctx, const VocabDev &v, con
     return WG_OK;
 }
 
-// How the scan is dealt out: items of several steps once there is work for every resident warp a few
-// times over, single steps below that.
-dim3 beam_grid(BeamArgs &a, int32_t rows, int32_t dtype) {
+// The scan's grid: as many blocks as are resident at once, or a step per warp.
+unsigned beam_grid(BeamArgs &a, int32_t rows, int32_t dtype) {
     const int step = dtype == WG_DTYPE_BF16 ? ScanShape<uint16_t>::STEP : ScanShape<uint32_t>::STEP;
-    const long long steps = (a.V + 7 + step - 1) / step;
-    const long long resident = (long long)sm_count() * 4 * BEAM_WARPS;
-    long long per = rows * steps / (resident * 3);
-    per = per < 1 ? 1 : per > BEAM_MAX_STEPS ? BEAM_MAX_STEPS : per;
-    a.per_item = (int32_t)per;
-    a.items_per_row = (int32_t)((steps + per - 1) / per);
-    a.n_items = (uint32_t)((long long)rows * a.items_per_row);
+    a.n_rows = rows;
+    a.steps_per_row = (int32_t)(((long long)a.V + 7 + step - 1) / step);
     a.chunk_log2 = 5;
     while (a.chunk_log2 < 9 && (1 << a.chunk_log2) < a.chunk_stride) ++a.chunk_log2;
-    const long long blocks = ((long long)a.n_items + BEAM_WARPS - 1) / BEAM_WARPS;
-    return dim3((unsigned)std::min(blocks, resident / BEAM_WARPS));
+    const long long items = ((long long)rows * a.steps_per_row + BEAM_WARPS - 1) / BEAM_WARPS;
+    return (unsigned)std::min(items, (long long)sm_count() * BEAM_BLOCKS);
 }
 
 bool beam_sizes_ok(const wg_beam *beam, int32_t n_req, int32_t n_beam, int32_t n_out, int32_t norm) {
@@ -121,9 +114,9 @@ int32_t wg_beam_select(wg_beam *beam, const void *logits, int32_t dtype, int64_t
     if (finished && (eos_id < 0 || eos_id >= V)) return WG_ERR_ARG;
     if (score_out == score && n_out != n_beam) return WG_ERR_ARG;
     BeamArgs a{logits, row_stride_elems, bitmask, mask_stride_words, score, finished, nullptr, nullptr,
-               n_beam, V, W, n_out, eos_id, norm, 0, 0, 0u, beam->chunk_stride, 0, beam->chunk_max, beam->parts,
+               n_beam, V, W, n_out, eos_id, norm, 0, 0, beam->chunk_stride, 0, beam->chunk_max, beam->parts,
                beam->next_item};
-    const dim3 grid = beam_grid(a, n_req * n_beam, dtype);
+    const unsigned grid = beam_grid(a, n_req * n_beam, dtype);
     const CtxDev none{};
     const VocabDev no_vocab{};
     const BeamStepArgs no_step{};
@@ -164,9 +157,9 @@ int32_t wg_beam_step(wg_beam *beam, wg_ctx *c, int32_t *gid, int32_t *sid, float
     const int32_t rc = launch_build(c, work, rows, st, true);
     if (rc != WG_OK) return rc;
     BeamArgs a{logits, row_stride_elems, bitmask, mask_stride_words, score, nullptr, gid, sid,
-               n_beam, v.V, v.W, n_beam, v.eos_id, norm, 0, 0, 0u, beam->chunk_stride, 0, beam->chunk_max, beam->parts,
+               n_beam, v.V, v.W, n_beam, v.eos_id, norm, 0, 0, beam->chunk_stride, 0, beam->chunk_max, beam->parts,
                beam->next_item};
-    const dim3 grid = beam_grid(a, rows, dtype);
+    const unsigned grid = beam_grid(a, rows, dtype);
     const BeamStepArgs step{gid, sid, status};
     return dtype == WG_DTYPE_BF16
         ? launch_beam<uint16_t, true>(a, c->dev, v, step, n_req, grid, score, parent_out, token_out, st)
