@@ -27,6 +27,19 @@ constexpr int PICK_THREADS = 512;
 constexpr int PICK_GROUPS = 128;            // at most
 constexpr int PICK_LIST = 512;              // candidates that are ranked against each other
 
+// n / d for n < 2^31 by a multiplication: M = ceil(2^(31 + k) / d) with 2^(k - 1) < d <= 2^k fits 32 bits, and
+// n * (M * d - 2^(31 + k)) < 2^31 * 2^k, so the quotient is exact.
+struct Divisor {
+    uint32_t d, mul;
+    int32_t shift;
+    static Divisor of(uint32_t d) {
+        int k = 0;
+        while ((1ull << k) < d) ++k;
+        return {d, (uint32_t)(((1ull << (31 + k)) + d - 1) / d), 31 + k};
+    }
+    __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return (uint32_t)(((uint64_t)n * mul) >> shift); }
+};
+
 struct BeamArgs {
     const void *logits;
     int64_t row_stride;       // elements
@@ -36,11 +49,12 @@ struct BeamArgs {
     const int32_t *finished;  // or NULL
     const int32_t *gid, *sid; // with a context: the rows' states (finished = DONE)
     int32_t n_beam, V, W, n_out, eos, norm;
-    int32_t n_rows, steps_per_row;
+    uint32_t n_steps, n_items;  // steps of all rows, and those eight by eight
+    Divisor per_row;            // steps of a row
     int32_t chunk_stride;     // chunk maxima per row, a multiple of 4
     int32_t chunk_log2;       // the pick's threads side by side on a row: 32 .. 512
     float *chunk_max;         // [rows][chunk_stride]
-    float2 *parts;            // [rows][steps_per_row] (max, sum) of every step
+    float2 *parts;            // [n_steps] (max, sum) of every step
     int32_t *next_item;       // items taken beyond the first two of every block; zero between calls
 };
 
@@ -300,6 +314,9 @@ struct ScanShape {
     static constexpr int WORDS = STEP / 32 / 32;                // mask words per lane and step: 2, 1
 };
 
+// The top bit of every byte of x that is not zero (a byte's low bits carry into it, or it is set).
+__device__ __forceinline__ uint32_t filled(uint32_t x) { return (((x & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | x) & 0x80808080u; }
+
 // A row as the scan walks it.
 template <typename E, int NORM, bool CTX>
 struct ScanRow {
@@ -355,6 +372,16 @@ struct ScanRow {
         const int p = s * S::STEP + (int)(threadIdx.x & 31) * S::EPC;
         if (whole(s)) {
             const E *at = x.base + p;
+            if (NORM == WG_BEAM_NORM_FULL || __all_sync(0xFFFFFFFFu, (filled(bits[0]) & filled(bits[1])) == 0x80808080u)) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < S::HALF; ++i)
+                        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                     : "=r"(v[h][i][0]), "=r"(v[h][i][1]), "=r"(v[h][i][2]), "=r"(v[h][i][3])
+                                     : "l"(at + (h * S::HALF + i) * 32 * S::EPC));
+                return;
+            }
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -452,16 +479,13 @@ beam_scan_kernel(BeamArgs a, CtxDev ctx) {
     __shared__ uint32_t published[2];
     pdl_enter();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t n_items = ((uint32_t)a.n_rows * (uint32_t)a.steps_per_row + BEAM_WARPS - 1) / BEAM_WARPS;
     const auto look = [&](uint32_t item) -> ScanNext<E> {
         ScanNext<E> n;
         const uint32_t step = item * BEAM_WARPS + warp;
-        n.row = (int)(step / (uint32_t)a.steps_per_row);
-        n.s = (int)(step - (uint32_t)n.row * (uint32_t)a.steps_per_row);
-        if (item >= n_items || n.row >= a.n_rows) {
-            n.row = -1;
-            return n;
-        }
+        n.row = -1;
+        if (item >= a.n_items || step >= a.n_steps) return n;
+        n.row = (int)a.per_row.quotient(step);
+        n.s = (int)(step - n.row * a.per_row.d);
         n.score = a.score[n.row];
         n.finished = !CTX && a.finished ? a.finished[n.row] : 0;
         Row(a, ctx, n.row).words(n.word, n.s);
@@ -471,7 +495,7 @@ beam_scan_kernel(BeamArgs a, CtxDev ctx) {
     ScanNext<E> n = look(item);
     uint32_t v[2][S::HALF][4] = {};
 #pragma unroll 1
-    for (int turn = 0; item < n_items; turn ^= 1) {
+    for (int turn = 0; item < a.n_items; turn ^= 1) {
         uint32_t taken = 0;
         if (threadIdx.x == 0) taken = (uint32_t)atomicAdd(a.next_item, 1);
         const int row = n.row, s = n.s;
@@ -492,7 +516,7 @@ beam_scan_kernel(BeamArgs a, CtxDev ctx) {
                 float total = two.x + two.y;
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
-                if (lane == 0) a.parts[(int64_t)row * a.steps_per_row + s] = make_float2(m, total);
+                if (lane == 0) a.parts[(uint32_t)row * a.per_row.d + s] = make_float2(m, total);
             }
         }
         if (threadIdx.x == 0) published[turn] = 2 * gridDim.x + taken;
@@ -634,8 +658,8 @@ __device__ __forceinline__ int beam_pick(PickShared &sh, const BeamArgs &a, cons
         float m = -INFINITY, s = 0.f, lse = 0.f;
         if (a.norm != WG_BEAM_NORM_NONE) {     // (for a row that is not live the pairs are left over: not used)
 #pragma unroll 4
-            for (int i = lane; i < a.steps_per_row; i += 32) {
-                const float2 p = a.parts[(int64_t)row * a.steps_per_row + i];
+            for (int i = lane; i < (int)a.per_row.d; i += 32) {
+                const float2 p = a.parts[(int64_t)row * (int)a.per_row.d + i];
                 const float high = fmaxf(m, p.x);
                 if (high > -INFINITY)          // (a pair that saw nothing is (-inf, 0))
                     s = s * moved(m, high) + p.y * moved(p.x, high);

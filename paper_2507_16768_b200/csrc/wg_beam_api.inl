@@ -40,12 +40,12 @@ int32_t launch_beam(const BeamArgs &a, const CtxDev &ctx, const VocabDev &v, con
 // The scan's grid: as many blocks as are resident at once, or a step per warp.
 unsigned beam_grid(BeamArgs &a, int32_t rows, int32_t dtype) {
     const int step = dtype == WG_DTYPE_BF16 ? ScanShape<uint16_t>::STEP : ScanShape<uint32_t>::STEP;
-    a.n_rows = rows;
-    a.steps_per_row = (int32_t)(((long long)a.V + 7 + step - 1) / step);
+    a.per_row = Divisor::of((uint32_t)(((long long)a.V + 7 + step - 1) / step));
+    a.n_steps = (uint32_t)rows * a.per_row.d;
+    a.n_items = (a.n_steps + BEAM_WARPS - 1) / BEAM_WARPS;
     a.chunk_log2 = 5;
     while (a.chunk_log2 < 9 && (1 << a.chunk_log2) < a.chunk_stride) ++a.chunk_log2;
-    const long long items = ((long long)rows * a.steps_per_row + BEAM_WARPS - 1) / BEAM_WARPS;
-    return (unsigned)std::min(items, (long long)sm_count() * BEAM_BLOCKS);
+    return std::min(a.n_items, (uint32_t)sm_count() * BEAM_BLOCKS);
 }
 
 bool beam_sizes_ok(const wg_beam *beam, int32_t n_req, int32_t n_beam, int32_t n_out, int32_t norm) {
@@ -114,7 +114,7 @@ int32_t wg_beam_select(wg_beam *beam, const void *logits, int32_t dtype, int64_t
     if (finished && (eos_id < 0 || eos_id >= V)) return WG_ERR_ARG;
     if (score_out == score && n_out != n_beam) return WG_ERR_ARG;
     BeamArgs a{logits, row_stride_elems, bitmask, mask_stride_words, score, finished, nullptr, nullptr,
-               n_beam, V, W, n_out, eos_id, norm, 0, 0, beam->chunk_stride, 0, beam->chunk_max, beam->parts,
+               n_beam, V, W, n_out, eos_id, norm, 0u, 0u, Divisor{}, beam->chunk_stride, 0, beam->chunk_max, beam->parts,
                beam->next_item};
     const unsigned grid = beam_grid(a, n_req * n_beam, dtype);
     const CtxDev none{};
@@ -157,7 +157,7 @@ int32_t wg_beam_step(wg_beam *beam, wg_ctx *c, int32_t *gid, int32_t *sid, float
     const int32_t rc = launch_build(c, work, rows, st, true);
     if (rc != WG_OK) return rc;
     BeamArgs a{logits, row_stride_elems, bitmask, mask_stride_words, score, nullptr, gid, sid,
-               n_beam, v.V, v.W, n_beam, v.eos_id, norm, 0, 0, beam->chunk_stride, 0, beam->chunk_max, beam->parts,
+               n_beam, v.V, v.W, n_beam, v.eos_id, norm, 0u, 0u, Divisor{}, beam->chunk_stride, 0, beam->chunk_max, beam->parts,
                beam->next_item};
     const unsigned grid = beam_grid(a, rows, dtype);
     const BeamStepArgs step{gid, sid, status};
