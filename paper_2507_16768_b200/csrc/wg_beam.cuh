@@ -24,6 +24,7 @@ constexpr int BEAM_BLOCKS = WGB;              // per SM
 constexpr int BEAM_WARPS = BEAM_THREADS / 32;
 constexpr int BEAM_CHUNK = 512;             // positions per chunk maximum
 constexpr int PICK_THREADS = 512;
+constexpr int PICK_WARPS = PICK_THREADS / 32;
 constexpr int PICK_GROUPS = 128;            // at most
 constexpr int PICK_LIST = 512;              // candidates that are ranked against each other
 
@@ -69,13 +70,15 @@ enum { BEAM_ROW_DEAD = 0, BEAM_ROW_LIVE = 1, BEAM_ROW_FINISHED = 2 };
 // What a row can offer: nothing (no hypothesis), one candidate (finished), or its tokens.
 template <bool CTX>
 __device__ __forceinline__ int beam_row_kind(const BeamArgs &a, const CtxDev &ctx, int row, float score) {
-    if (!(score > -INFINITY)) return BEAM_ROW_DEAD;     // (NaN too)
+    // (what is asked for does not hang on the score: all of it on its way together)
+    bool finished;
     if (CTX) {
         const int g = a.gid[row], s = a.sid[row];
-        if (g >= 0 && g < ctx.n_grammars && s > 0 && s == ctx.grammars[g].done) return BEAM_ROW_FINISHED;
-        return BEAM_ROW_LIVE;
+        finished = g >= 0 && g < ctx.n_grammars && s > 0 && s == ctx.grammars[g].done;
+    } else {
+        finished = a.finished && a.finished[row];
     }
-    return a.finished && a.finished[row] ? BEAM_ROW_FINISHED : BEAM_ROW_LIVE;
+    return !(score > -INFINITY) ? BEAM_ROW_DEAD : finished ? BEAM_ROW_FINISHED : BEAM_ROW_LIVE;   // (NaN: dead)
 }
 
 // Where a row's packed mask is: a row of words, a compact cache entry, or nowhere (all allowed).
@@ -544,16 +547,16 @@ __device__ __forceinline__ unsigned long long pack_key(uint32_t key, uint32_t id
 struct PickShared {
     // two lists of candidates (chunks, then elements), zero behind the last one
     alignas(16) unsigned long long list[2][PICK_LIST];
-    alignas(16) uint32_t group[PICK_GROUPS];
+    alignas(16) float group[PICK_GROUPS];
     uint32_t chunk[WG_BEAM_MAX_OUT];       // the chosen chunks
     int32_t parent[WG_BEAM_MAX_OUT], token[WG_BEAM_MAX_OUT];
     float score[WG_BEAM_MAX_BEAMS], lse[WG_BEAM_MAX_BEAMS];
     int32_t kind[WG_BEAM_MAX_BEAMS];
     int32_t n_written[WG_BEAM_MAX_BEAMS];  // chunk maxima the scan wrote for the row (0: not live)
     MaskSource mask[WG_BEAM_MAX_BEAMS];
-    uint32_t bound;                        // key that n_out candidates reach
+    float bound[2];                        // scores that n_out candidates reach: chunks, elements
     int32_t n[2];
-    int32_t count[PICK_THREADS / 32];
+    int32_t count[PICK_WARPS];
 };
 
 // Sum of v over the block, in every thread.
@@ -563,37 +566,37 @@ __device__ __forceinline__ int block_sum(PickShared &sh, int v) {
     __syncthreads();
     int total = 0;
 #pragma unroll
-    for (int i = 0; i < PICK_THREADS / 32; ++i) total += sh.count[i];
+    for (int i = 0; i < PICK_WARPS; ++i) total += sh.count[i];
     __syncthreads();
     return total;
 }
 
-// Puts the candidates that `each` enumerates into the (empty) list: all that reach `bound`, or, where
-// those are more than it holds (many equal scores), exactly the n_out largest, found by bisection
-// over the packed keys.  `each(f)` calls f(packed key) for the calling thread's share; packed keys
-// are unlike one another.  Returns how many are listed.
+// Puts the candidates that `each` enumerates into the (empty) list: all whose score reaches `bound` (and
+// is above -inf), or, where those are more than it holds (many equal scores), exactly the n_out
+// largest, found by bisection over the packed keys.  `each(f)` calls f(score, index) for the calling
+// thread's share; no two candidates have an index in common.  Returns how many are listed.
 template <typename Each>
-__device__ __forceinline__ int collect(PickShared &sh, int which, uint32_t bound, int n_out, const Each &each) {
+__device__ __forceinline__ int collect(PickShared &sh, int which, float bound, int n_out, const Each &each) {
     const auto push = [&](unsigned long long k) {
         const int at = atomicAdd(&sh.n[which], 1);
         if (at < PICK_LIST) sh.list[which][at] = k;
     };
-    const unsigned long long low = (unsigned long long)bound << 32;
-    each([&](unsigned long long k) { if (k >= low) push(k); });
+    each([&](float s, uint32_t idx) { if (s >= bound && s > -INFINITY) push(pack_key(score_key(s), idx)); });
     __syncthreads();
     const int n = sh.n[which];
     if (n <= PICK_LIST) return n;
-    unsigned long long cut = 0ull;         // the largest value that n_out keys reach
+    unsigned long long cut = 0ull;         // the largest value that n_out packed keys reach
+#pragma unroll 1
     for (int bit = 63; bit >= 0; --bit) {
         const unsigned long long trial = cut | (1ull << bit);
         int mine = 0;
-        each([&](unsigned long long k) { mine += k >= trial; });
+        each([&](float s, uint32_t idx) { mine += pack_key(score_key(s), idx) >= trial; });
         if (block_sum(sh, mine) >= n_out) cut = trial;
     }
     if (threadIdx.x == 0) sh.n[which] = 0;
     sh.list[which][threadIdx.x] = 0ull;
     __syncthreads();
-    each([&](unsigned long long k) { if (k >= cut) push(k); });
+    each([&](float s, uint32_t idx) { if (pack_key(score_key(s), idx) >= cut) push(pack_key(score_key(s), idx)); });
     __syncthreads();
     return sh.n[which];
 }
@@ -615,13 +618,39 @@ __device__ __forceinline__ void ranked(const PickShared &sh, int which, int n, i
 }
 static_assert(PICK_LIST == PICK_THREADS, "a thread per listed candidate");
 
-// The block's n_out best candidates, listed in sh.list[1]; returns how many there are (they may be
-// more: rank them).
+// sh.bound[0] = the n_out-th largest of the maxima (every thread's `top`) of some groups of threads, a lower
+// bound for the n_out-th largest of all: each group's maximum is one of them.  At least twice as many
+// groups as are wanted: few of the best then share a group, and few more than n_out reach the bound.
+__device__ __forceinline__ void group_bound(PickShared &sh, float top, int n_out) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int per_warp = n_out <= 8 ? 1 : n_out <= 16 ? 2 : n_out <= 32 ? 4 : 8, n_groups = per_warp * PICK_WARPS;
+    if (per_warp == 1) top = warp_max(top);
+    else for (int o = 16 / per_warp; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    if ((lane & (32 / per_warp - 1)) == 0) sh.group[warp * per_warp + lane / (32 / per_warp)] = top;
+    __syncthreads();
+    if ((int)threadIdx.x < n_groups) {
+        const float mine = sh.group[threadIdx.x];
+        int rank = 0;
+#pragma unroll 2
+        for (int j = 0; j < n_groups; j += 4) {
+            const float4 g = *reinterpret_cast<const float4 *>(&sh.group[j]);
+            const int t = (int)threadIdx.x - j;
+            rank += (g.x > mine || (g.x == mine && 0 < t)) + (g.y > mine || (g.y == mine && 1 < t)) +
+                    (g.z > mine || (g.z == mine && 2 < t)) + (g.w > mine || (g.w == mine && 3 < t));
+        }
+        if (rank == n_out - 1) sh.bound[0] = mine;
+    }
+    __syncthreads();
+}
+
+// The request's best candidates, listed in sh.list[1]: the n_out best and possibly more.  Returns how
+// many are listed.
 template <typename E, bool CTX>
 __device__ __forceinline__ int beam_pick(PickShared &sh, const BeamArgs &a, const CtxDev &ctx, int req) {
     constexpr int EPC = ElemTraits<E>::PER_CHUNK;
     constexpr int PER_CHUNK = BEAM_CHUNK / (32 * EPC);
     constexpr int HELD = 8;                // chunk maxima a thread keeps in registers
+    constexpr int PARTS = 4;               // pairs a lane has in flight
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int K = a.n_beam, row0 = req * K;
     const int n_chunks = a.chunk_stride;
@@ -629,50 +658,66 @@ __device__ __forceinline__ int beam_pick(PickShared &sh, const BeamArgs &a, cons
     // anything else is known, so that their latency passes together with that of the rows' facts.
     const int width = 1 << a.chunk_log2, side = PICK_THREADS >> a.chunk_log2;
     const int c0 = threadIdx.x & (width - 1), b0 = threadIdx.x >> a.chunk_log2;
+    const int turns = (n_chunks + width - 1) >> a.chunk_log2;           // columns of a thread on a row
+    const int slots = (K + side - 1) / side * turns;
     const float *maxima = a.chunk_max + (int64_t)row0 * n_chunks;
-    const auto onward = [&](int &b, int &c) {
-        c += width;
-        if (c >= n_chunks) {
-            c = c0;
-            b += side;
+    // calls f(slot, beam, column) for the thread's slots [first, end)
+    const auto visit = [&](int first, int end, auto f) {
+        int b = b0 + first / turns * side, turn = first % turns;
+        for (int j = first; j < end; ++j) {
+            f(j, b, c0 + (turn << a.chunk_log2));
+            if (++turn == turns) {
+                turn = 0;
+                b += side;
+            }
         }
     };
-    const int start_b = c0 < n_chunks ? b0 : K;
     float held[HELD];
     {
-        int b = start_b, c = c0;
+        int b = b0, turn = 0;
 #pragma unroll
         for (int j = 0; j < HELD; ++j) {
-            held[j] = 0.f;
-            if (b < K) held[j] = maxima[(int64_t)b * n_chunks + c];
-            onward(b, c);
+            const int c = c0 + (turn << a.chunk_log2);
+            held[j] = -INFINITY;
+            if (j < slots && b < K && c < n_chunks) held[j] = maxima[b * n_chunks + c];
+            if (++turn == turns) {
+                turn = 0;
+                b += side;
+            }
         }
     }
     sh.list[0][threadIdx.x] = sh.list[1][threadIdx.x] = 0ull;
     if (threadIdx.x < 2) sh.n[threadIdx.x] = 0;
-    if (threadIdx.x == 2) sh.bound = 1u;
-    // ---- the rows: their log-sum-exp from the items' pairs
-    for (int b = warp; b < K; b += PICK_THREADS / 32) {
-        const int row = row0 + b;
+    if (threadIdx.x == 2) sh.bound[0] = sh.bound[1] = -INFINITY;
+    // ---- the rows: whether they count, and their log-sum-exp from the steps' pairs (those of a row that
+    // does not count are left over: read all the same, in one go with the rest, and not used)
+    for (int b = warp; b < K; b += PICK_WARPS) {
+        const int row = row0 + b, n_parts = (int)a.per_row.d;
+        const float2 *parts = a.parts + (int64_t)row * n_parts;
+        const bool sums = a.norm != WG_BEAM_NORM_NONE;
         const float score = a.score[row];
-        float m = -INFINITY, s = 0.f, lse = 0.f;
-        if (a.norm != WG_BEAM_NORM_NONE) {     // (for a row that is not live the pairs are left over: not used)
-#pragma unroll 4
-            for (int i = lane; i < (int)a.per_row.d; i += 32) {
-                const float2 p = a.parts[(int64_t)row * (int)a.per_row.d + i];
-                const float high = fmaxf(m, p.x);
-                if (high > -INFINITY)          // (a pair that saw nothing is (-inf, 0))
-                    s = s * moved(m, high) + p.y * moved(p.x, high);
-                m = high;
-            }
+        float2 p[PARTS];
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) {
+            p[i] = make_float2(-INFINITY, 0.f);
+            if (sums && lane + 32 * i < n_parts) p[i] = parts[lane + 32 * i];
         }
         const int kind = beam_row_kind<CTX>(a, ctx, row, score);
-        if (a.norm != WG_BEAM_NORM_NONE) {
-            const float high = warp_max(m);
-            s = high > -INFINITY ? s * moved(m, high) : 0.f;
+        float lse = 0.f;
+        if (sums) {
+            float m = p[0].x, s = 0.f;
+#pragma unroll
+            for (int i = 1; i < PARTS; ++i) m = fmaxf(m, p[i].x);
+            for (int i = lane + 32 * PARTS; i < n_parts; i += 32) m = fmaxf(m, parts[i].x);
+            m = warp_max(m);
+            if (m > -INFINITY) {           // (a pair that saw nothing is (-inf, 0))
+#pragma unroll
+                for (int i = 0; i < PARTS; ++i) s += p[i].y * moved(p[i].x, m);
+                for (int i = lane + 32 * PARTS; i < n_parts; i += 32) s += parts[i].y * moved(parts[i].x, m);
+            }
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-            lse = log_sum(high, s);
+            lse = log_sum(m, s);
         }
         if (lane == 0) {
             const RowView<E> x(a.logits, a.row_stride, row, a.V);
@@ -685,92 +730,68 @@ __device__ __forceinline__ int beam_pick(PickShared &sh, const BeamArgs &a, cons
     }
     __syncthreads();
     // ---- the n_out best chunks
-    const auto chunk_key = [&](int b, int c, float maximum) -> uint32_t {
-        return c < sh.n_written[b] ? score_key(sh.score[b] + (maximum - sh.lse[b])) : 0u;
+    const auto chunk_score = [&](int b, int c, float maximum) -> float {
+        return b < K && c < sh.n_written[b] ? sh.score[b] + (maximum - sh.lse[b]) : -INFINITY;
     };
-    uint32_t key[HELD], top = 0;
-    int rest_b = start_b, rest_c = c0;         // the first chunk that is not held
-#pragma unroll
-    for (int j = 0; j < HELD; ++j) {
-        key[j] = rest_b < K ? chunk_key(rest_b, rest_c, held[j]) : 0u;
-        top = max(top, key[j]);
-        onward(rest_b, rest_c);
-    }
-    const auto each_chunk = [&](auto f) {
-        int b = start_b, c = c0;
+    float top = -INFINITY;
+    {
+        int b = b0, turn = 0;
 #pragma unroll
         for (int j = 0; j < HELD; ++j) {
-            f(pack_key(key[j], (uint32_t)(b * n_chunks + c)));
-            onward(b, c);
+            if (j >= slots) break;                 // uniform
+            held[j] = chunk_score(b, c0 + (turn << a.chunk_log2), held[j]);
+            top = fmaxf(top, held[j]);
+            if (++turn == turns) {
+                turn = 0;
+                b += side;
+            }
         }
-        while (b < K) {
-            f(pack_key(chunk_key(b, c, maxima[(int64_t)b * n_chunks + c]), (uint32_t)(b * n_chunks + c)));
-            onward(b, c);
-        }
-    };
-    for (int b = rest_b, c = rest_c; b < K; onward(b, c))
-        top = max(top, chunk_key(b, c, maxima[(int64_t)b * n_chunks + c]));
-    // A lower bound for the n_out-th largest: that of the maxima of some groups of threads, at least
-    // twice as many groups as are wanted (few of the best then share a group, and few keys more than
-    // n_out reach the bound).
-    const int n_groups = a.n_out <= 16 ? 32 : a.n_out <= 32 ? 64 : 128;
-    for (int o = 1; o < PICK_THREADS / n_groups; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    if ((threadIdx.x & (PICK_THREADS / n_groups - 1)) == 0) sh.group[threadIdx.x / (PICK_THREADS / n_groups)] = top;
-    __syncthreads();
-    if ((int)threadIdx.x < n_groups) {
-        const uint32_t mine = sh.group[threadIdx.x];
-        int rank = 0;
-#pragma unroll 8
-        for (int j = 0; j < n_groups; j += 4) {
-            const uint4 g = *reinterpret_cast<const uint4 *>(&sh.group[j]);
-            const int t = (int)threadIdx.x - j;
-            rank += (g.x > mine || (g.x == mine && 0 < t)) + (g.y > mine || (g.y == mine && 1 < t)) +
-                    (g.z > mine || (g.z == mine && 2 < t)) + (g.w > mine || (g.w == mine && 3 < t));
-        }
-        if (rank == a.n_out - 1 && mine > 0u) sh.bound = mine;
     }
-    __syncthreads();
-    int n = collect(sh, 0, sh.bound, a.n_out, each_chunk);
-    // (sh.bound has been read by everybody: collect ends with a barrier)
-    if (threadIdx.x == 0) sh.bound = 1u;
-    __syncthreads();
+    const auto beyond = [&](int b, int c) -> float {               // a chunk that is not held
+        return b < K && c < n_chunks ? chunk_score(b, c, maxima[b * n_chunks + c]) : -INFINITY;
+    };
+    visit(HELD, slots, [&](int, int b, int c) { top = fmaxf(top, beyond(b, c)); });
+    group_bound(sh, top, a.n_out);
+    int n = collect(sh, 0, sh.bound[0], a.n_out, [&](auto f) {
+        int b = b0, turn = 0;
+#pragma unroll
+        for (int j = 0; j < HELD; ++j) {
+            if (j >= slots) break;
+            f(held[j], (uint32_t)(b * n_chunks + c0 + (turn << a.chunk_log2)));
+            if (++turn == turns) {
+                turn = 0;
+                b += side;
+            }
+        }
+        visit(HELD, slots, [&](int, int bb, int c) { f(beyond(bb, c), (uint32_t)(bb * n_chunks + c)); });
+    });
     ranked(sh, 0, n, a.n_out, [&](int rank, unsigned long long k) {
         sh.chunk[rank] = 0xFFFFFFFFu - (uint32_t)k;
-        if (rank == a.n_out - 1) sh.bound = (uint32_t)(k >> 32);   // n_out elements reach this
+        if (rank == a.n_out - 1) sh.bound[1] = key_score((uint32_t)(k >> 32));   // n_out elements reach this
     });
     __syncthreads();
     // ---- the n_out best elements of those chunks, and the finished rows' candidates
-    const int n_sel = min(n, a.n_out);
-    return collect(sh, 1, sh.bound, a.n_out, [&](auto f) {
-        for (int i = warp; i < n_sel; i += PICK_THREADS / 32) {
-            const int at = (int)sh.chunk[i];
-            const int b = at / n_chunks, p0 = (at - b * n_chunks) * BEAM_CHUNK;
+    // (a warp takes 32 pieces of a chunk at a time)
+    const int n_sel = min(n, a.n_out) * PER_CHUNK;
+    return collect(sh, 1, sh.bound[1], a.n_out, [&](auto f) {
+        for (int i = warp; i < n_sel; i += PICK_WARPS) {
+            const int at = (int)sh.chunk[i / PER_CHUNK];
+            const int b = at / n_chunks, p = (at - b * n_chunks) * BEAM_CHUNK + (i % PER_CHUNK * 32 + lane) * EPC;
             const RowView<E> x(a.logits, a.row_stride, row0 + b, a.V);
-            const MaskSource mask = sh.mask[b];
+            const uint4 u = x.piece(p);
+            uint32_t bits = shifted_word(sh.mask[b], p >> 5, x.off) >> (p & 31);
             const float score = sh.score[b], lse = sh.lse[b];
-            uint4 v[PER_CHUNK];
-            uint32_t bits[PER_CHUNK];
+            const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+            const uint32_t idx = (uint32_t)b * (uint32_t)a.V + (uint32_t)(p - x.off);
 #pragma unroll
-            for (int q = 0; q < PER_CHUNK; ++q) {
-                const int p = p0 + (q * 32 + lane) * EPC;
-                v[q] = x.piece(p);
-                bits[q] = shifted_word(mask, p >> 5, x.off) >> (p & 31);
-            }
-#pragma unroll
-            for (int q = 0; q < PER_CHUNK; ++q) {
-                const int p = p0 + (q * 32 + lane) * EPC;
-                const uint32_t w[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
-#pragma unroll
-                for (int j = 0; j < EPC; ++j) {
-                    const uint32_t e = sizeof(E) == 2
-                        ? ((j & 1) ? (w[j >> 1] & 0xFFFF0000u) : (w[j >> 1] << 16)) : w[j];
-                    const uint32_t k = ((bits[q] >> j) & 1u) ? score_key(score + (__uint_as_float(e) - lse)) : 0u;
-                    f(pack_key(k, (uint32_t)b * (uint32_t)a.V + (uint32_t)(p + j - x.off)));
-                }
+            for (int j = 0; j < EPC; ++j) {
+                const uint32_t e = sizeof(E) == 2
+                    ? ((j & 1) ? (v[j >> 1] & 0xFFFF0000u) : (v[j >> 1] << 16)) : v[j & 3];
+                f((bits >> j) & 1u ? score + (__uint_as_float(e) - lse) : -INFINITY, idx + j);
             }
         }
         if ((int)threadIdx.x < K && sh.kind[threadIdx.x] == BEAM_ROW_FINISHED)
-            f(pack_key(score_key(sh.score[threadIdx.x]), threadIdx.x * (uint32_t)a.V + (uint32_t)a.eos));
+            f(sh.score[threadIdx.x], threadIdx.x * (uint32_t)a.V + (uint32_t)a.eos);
     });
 }
 
