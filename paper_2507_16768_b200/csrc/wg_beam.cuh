@@ -383,8 +383,7 @@ struct ScanRow {
                         asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
                                      : "=r"(v[h][i][0]), "=r"(v[h][i][1]), "=r"(v[h][i][2]), "=r"(v[h][i][3])
                                      : "l"(at + (h * S::HALF + i) * 32 * S::EPC));
-                return;
-            }
+            } else {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -393,7 +392,8 @@ struct ScanRow {
                                  "@p ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
                                  : "+r"(v[h][i][0]), "+r"(v[h][i][1]), "+r"(v[h][i][2]), "+r"(v[h][i][3])
                                  : "l"(at + (h * S::HALF + i) * 32 * S::EPC),
-                                   "r"(NORM == WG_BEAM_NORM_FULL ? 1u : bits[h] & (0xFFu << (8 * i))));
+                                   "r"(bits[h] & (0xFFu << (8 * i))));
+            }
         } else {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -486,6 +486,8 @@ beam_scan_kernel(BeamArgs a, CtxDev ctx) {
         ScanNext<E> n;
         const uint32_t step = item * BEAM_WARPS + warp;
         n.row = -1;
+#pragma unroll
+        for (int i = 0; i < S::WORDS; ++i) n.word[i] = 0u;
         if (item >= a.n_items || step >= a.n_steps) return n;
         n.row = (int)a.per_row.quotient(step);
         n.s = (int)(step - n.row * a.per_row.d);
@@ -504,13 +506,19 @@ beam_scan_kernel(BeamArgs a, CtxDev ctx) {
         const int row = n.row, s = n.s;
         const bool live = row >= 0 && (CTX ? beam_row_kind<CTX>(a, ctx, row, n.score) == BEAM_ROW_LIVE
                                            : n.score > -INFINITY && !n.finished);
+        // (most steps of a state inside a literal allow nothing)
+        const bool any = NORM == WG_BEAM_NORM_FULL || __any_sync(0xFFFFFFFFu, (n.word[0] | n.word[S::WORDS - 1]) != 0u);
         uint32_t bits[2];
-        if (live) {
+        if (live && any) {
             Row::deal(n.word, bits);
             Row(a, ctx, row).load(v, s, bits);
         }
         n = look(after);
-        if (live) {
+        if (live && !any) {
+            if (lane < S::CHUNKS) a.chunk_max[(int64_t)row * a.chunk_stride + s * S::CHUNKS + lane] = -INFINITY;
+            if (NORM != WG_BEAM_NORM_NONE && lane == 0)
+                a.parts[(uint32_t)row * a.per_row.d + s] = make_float2(-INFINITY, 0.f);
+        } else if (live) {
             float m = -INFINITY;
             Pair sum[2] = {0ull, 0ull};
             scan_step<E, NORM>(v, bits, a.chunk_max + (int64_t)row * a.chunk_stride + s * S::CHUNKS, m, sum);
