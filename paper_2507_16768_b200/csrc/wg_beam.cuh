@@ -14,6 +14,7 @@
 //     n_out chunks, and those 512 * n_out elements are all that the pick reads again.
 #pragma once
 
+#include "wg_divide.cuh"
 #include "wg_kernels.cuh"
 
 constexpr int BEAM_THREADS = 256;           // scan
@@ -27,19 +28,6 @@ constexpr int PICK_THREADS = 512;
 constexpr int PICK_WARPS = PICK_THREADS / 32;
 constexpr int PICK_GROUPS = 128;            // at most
 constexpr int PICK_LIST = 512;              // candidates that are ranked against each other
-
-// n / d for n < 2^31 by a multiplication: M = ceil(2^(31 + k) / d) with 2^(k - 1) < d <= 2^k fits 32 bits, and
-// n * (M * d - 2^(31 + k)) < 2^31 * 2^k, so the quotient is exact.
-struct Divisor {
-    uint32_t d, mul;
-    int32_t shift;
-    static Divisor of(uint32_t d) {
-        int k = 0;
-        while ((1ull << k) < d) ++k;
-        return {d, (uint32_t)(((1ull << (31 + k)) + d - 1) / d), 31 + k};
-    }
-    __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return (uint32_t)(((uint64_t)n * mul) >> shift); }
-};
 
 struct BeamArgs {
     const void *logits;
@@ -862,84 +850,148 @@ beam_pick_kernel(BeamArgs a, CtxDev ctx, VocabDev v, BeamStepArgs st, float *sco
 }
 
 // ---------------------------------------------------------------------------------------
-// Back-track.  One block per request walks its parents from the last step to the first.  The walk is
-// a chain of dependent look-ups, so the steps are cut into segments: every segment is first walked
-// from all beams at once (a map from its last beams to its first), the maps are composed by a
-// logarithmic scan, and then every segment is walked again from the beam that each final beam
-// really comes by.  Parents are staged in shared memory as bytes, a tile of steps at a time.
+// Back-track.  The walk from the last step to the first is a chain of dependent look-ups, so the steps are
+// cut into segments: every segment is first walked from all beams at once (a map from its last beams
+// to its first), the maps are composed, and then every segment is walked again from the beam that each
+// final beam really comes by.  A cluster of up to eight blocks takes a group of neighbouring requests (as many
+// as make up to 32 columns: 128 bytes of every step, read in whole lines) and a tile of steps, a part of the
+// tile for each block; the parts' maps are exchanged through the cluster's shared memory.  Within a
+// block a thread walks one column of one of the part's segments.
 // ---------------------------------------------------------------------------------------
 constexpr int BACK_THREADS = 1024;
+constexpr int BACK_STEPS = 512;         // most steps of a block's part
+constexpr int BACK_CLUSTER = 8;         // most blocks of a cluster
 constexpr int BACK_DEAD = 255;
 
+struct BackShared {
+    int32_t token[BACK_STEPS * 33];     // [step][column], a row padded by one: columns lie in other banks
+    uint8_t parent[BACK_STEPS * 32];    // [step][column]
+    uint8_t path[BACK_STEPS * 32];      // [step][column]: the column of the step that this final one comes by
+    uint8_t maps[2][BACK_THREADS];      // [segment][column]
+    uint8_t part[32];                   // the whole part's map
+    uint8_t at[32], from[32];           // where the final columns stand before the tile; where they enter the part
+};
+
+struct BackArgs {
+    const int32_t *token, *parent;
+    int32_t *out;
+    int32_t T, n_req, K;
+    int32_t group;                      // requests of a block
+    int32_t steps;                      // of a part (at most BACK_STEPS)
+};
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+
+// The byte at `p` of this block's shared memory, in the shared memory of the cluster's block `rank`.
+__device__ __forceinline__ uint32_t cluster_byte(const uint8_t *p, uint32_t rank) {
+    uint32_t at, x;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.u8 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+    return x;
+}
+
 __global__ void __launch_bounds__(BACK_THREADS, 1)
-beam_backtrack_kernel(const int32_t *__restrict__ token, const int32_t *__restrict__ parent, int T,
-                      int n_req, int K, int tile, int32_t *__restrict__ out) {
+beam_backtrack_kernel(BackArgs a) {
     extern __shared__ uint8_t back_smem[];
-    uint8_t *par = back_smem;                       // [tile][K]
-    uint8_t *path = par + tile * K;                 // [tile][K]: beam of step t of final beam j
-    __shared__ uint8_t maps[BACK_THREADS];          // [segment][K]
-    __shared__ uint8_t at[WG_BEAM_MAX_BEAMS];       // where the final beams stand before the tile
+    BackShared &sh = *reinterpret_cast<BackShared *>(back_smem);
     pdl_enter();
-    const int r = blockIdx.x;
-    const int64_t step = (int64_t)n_req * K;        // entries per step
-    const int64_t col = (int64_t)r * K;
-    const int n_seg = BACK_THREADS / K;
-    const int seg = (int)threadIdx.x / K, j = (int)threadIdx.x - seg * K;
-    const bool works = seg < n_seg;                 // (a few threads are left over unless K divides them)
-    if ((int)threadIdx.x < K) at[threadIdx.x] = (uint8_t)threadIdx.x;
-    for (int t1 = T; t1 > 0; t1 -= tile) {          // steps [t0, t1)
-        const int t0 = max(0, t1 - tile), n = t1 - t0;
-        __syncthreads();                            // the previous tile is done with
-        if (works) {
-            const int32_t *from = parent + t0 * step + col + j;
-#pragma unroll 8
-            for (int t = seg; t < n; t += n_seg) {
-                const int p = __ldcs(from + t * step);
-                par[t * K + j] = p >= 0 && p < K ? (uint8_t)p : (uint8_t)BACK_DEAD;
+    const int n_parts = (int)gridDim.x, part = (int)blockIdx.x;      // the cluster is the grid's x extent
+    const int64_t step = (int64_t)a.n_req * a.K;                     // entries per step
+    const int64_t col0 = (int64_t)blockIdx.y * a.group * a.K;
+    const int width = (int)min((int64_t)a.group * a.K, step - col0);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;      // a warp per segment, a lane per column
+    constexpr int SEGMENTS = BACK_THREADS / 32;
+    const bool mine = lane < width;
+    const int base = lane / a.K * a.K;                               // the lane's request's first column
+    const int tile = n_parts * a.steps;
+    if (threadIdx.x < 32) sh.at[threadIdx.x] = (uint8_t)(mine ? lane : BACK_DEAD);
+    for (int t1 = a.T; t1 > 0; t1 -= tile) {                         // tiles from the last to the first
+        const int t0 = t1 - tile + part * a.steps;                   // this block's part: [max(t0, 0), t0 + steps)
+        const int first = max(t0, 0), n = max(0, t0 + a.steps - first);
+        __syncthreads();                                             // the previous tile is done with
+        // ---- in: a warp reads a step's line
+        {
+            const int32_t *parent = a.parent + first * step + col0 + lane, *token = a.token + first * step + col0 + lane;
+            constexpr int LOADS = BACK_STEPS / SEGMENTS;
+            int32_t p[LOADS], x[LOADS];
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int t = warp + i * SEGMENTS;
+                p[i] = x[i] = 0;
+                if (t < n && mine) {
+                    p[i] = __ldcs(parent + t * step);
+                    x[i] = __ldcs(token + t * step);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int t = warp + i * SEGMENTS;
+                if (t < n) {
+                    sh.parent[t * 32 + lane] = mine && p[i] >= 0 && p[i] < a.K ? (uint8_t)(base + p[i]) : (uint8_t)BACK_DEAD;
+                    sh.token[t * 33 + lane] = x[i];
+                }
             }
         }
         __syncthreads();
-        const int per = (n + n_seg - 1) / n_seg;
-        const int lo = min(n, seg * per), hi = min(n, lo + per);
-        int b = j;
-        if (works) {
-            for (int t = hi - 1; t >= lo; --t)
-                if (b != BACK_DEAD) b = par[t * K + b];
-            maps[seg * K + j] = (uint8_t)b;
-        }
+        // ---- the segments' maps
+        const int per = (n + SEGMENTS - 1) / SEGMENTS;
+        const int lo = min(n, warp * per), hi = min(n, lo + per);
+        int b = lane;
+        for (int t = hi - 1; t >= lo; --t)
+            if (b != BACK_DEAD) b = sh.parent[t * 32 + b];
+        sh.maps[0][threadIdx.x] = (uint8_t)b;
         __syncthreads();
         // maps[s] becomes the composition of the maps of all segments from the last down to s
-        for (int d = 1; d < n_seg; d <<= 1) {
-            if (works && seg + d < n_seg) {
-                b = maps[(seg + d) * K + j];
-                if (b != BACK_DEAD) b = maps[seg * K + b];
+        int now = 0;
+#pragma unroll
+        for (int d = 1; d < SEGMENTS; d <<= 1) {
+            if (warp + d < SEGMENTS) {
+                const int far = sh.maps[now][threadIdx.x + d * 32];
+                b = far == BACK_DEAD ? BACK_DEAD : sh.maps[now][warp * 32 + far];
             }
-            __syncthreads();
-            if (works) maps[seg * K + j] = (uint8_t)b;
+            now ^= 1;
+            sh.maps[now][threadIdx.x] = (uint8_t)b;
             __syncthreads();
         }
-        if (works) {
-            b = at[j];
-            if (seg + 1 < n_seg && b != BACK_DEAD) b = maps[(seg + 1) * K + b];
-            for (int t = hi - 1; t >= lo; --t) {
-                path[t * K + j] = (uint8_t)b;
-                if (b != BACK_DEAD) b = par[t * K + b];
+        // ---- the parts: from the last one down to this one, and on to the first
+        if (threadIdx.x < 32) sh.part[threadIdx.x] = sh.maps[now][threadIdx.x];
+        cluster_sync();
+        if (threadIdx.x < 32) {
+            int c = sh.at[threadIdx.x];
+            for (int q = n_parts - 1; q >= 0; --q) {
+                if (q == part) sh.from[threadIdx.x] = (uint8_t)c;
+                if (c != BACK_DEAD) c = (int)cluster_byte(&sh.part[c], (uint32_t)q);
             }
+            sh.at[threadIdx.x] = (uint8_t)c;
+        }
+        cluster_sync();                                              // the maps have been read, and `from` is there
+        // ---- the way
+        b = sh.from[lane];
+        if (warp + 1 < SEGMENTS && b != BACK_DEAD) b = sh.maps[now][(warp + 1) * 32 + b];
+        for (int t = hi - 1; t >= lo; --t) {
+            sh.path[t * 32 + lane] = (uint8_t)b;
+            if (b != BACK_DEAD) b = sh.parent[t * 32 + b];
         }
         __syncthreads();
-        if ((int)threadIdx.x < K && at[threadIdx.x] != BACK_DEAD) at[threadIdx.x] = maps[at[threadIdx.x]];
-        for (int t = threadIdx.x; t < n; t += BACK_THREADS) {
-            const int32_t *row = token + (t0 + t) * step + col;
-            int32_t *to = out + col * T + t0 + t;
-#pragma unroll 8
-            for (int jj = 0; jj < K; ++jj) {
-                const int from = path[t * K + jj];
-                to[(int64_t)jj * T] = from == BACK_DEAD ? -1 : __ldg(row + from);
+        // ---- out: a warp writes 32 steps of a column
+        const int columns = (n + 31) / 32;
+        for (int i = warp; i < columns * width; i += SEGMENTS) {
+            const int c = i / columns, t = (i - c * columns) * 32 + lane;
+            if (t < n) {
+                const int from = sh.path[t * 32 + c];
+                // (a way back that broke off in this tile, or is known to have: no sequence)
+                const bool gone = from == BACK_DEAD || sh.at[c] == BACK_DEAD;
+                a.out[(col0 + c) * a.T + first + t] = gone ? -1 : sh.token[t * 33 + from];
             }
         }
     }
+    // a way back that broke off in a later tile than the first: what was written of it before goes
     __syncthreads();
-    for (int jj = 0; jj < K; ++jj)                  // a way back that broke off: no sequence
-        if (at[jj] == BACK_DEAD)
-            for (int t = threadIdx.x; t < T; t += BACK_THREADS) out[(col + jj) * T + t] = -1;
+    if (a.T > tile)
+        for (int c = 0; c < width; ++c)
+            if (sh.at[c] == BACK_DEAD)
+                for (int t = part * BACK_THREADS + (int)threadIdx.x; t < a.T; t += n_parts * BACK_THREADS)
+                    a.out[(col0 + c) * a.T + t] = -1;
 }

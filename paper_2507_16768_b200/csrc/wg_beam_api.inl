@@ -173,13 +173,25 @@ int32_t wg_beam_backtrack(const int32_t *token, const int32_t *parent, int32_t n
         return WG_ERR_ARG;
     if (n_steps == 0) return WG_OK;
     if (!token || !parent || !out) return WG_ERR_ARG;
-    // 32 KB for the parents of a tile of steps and as much for the way back
-    const int tile = std::min(n_steps, 32768 / n_beam);
-    const size_t smem = (size_t)tile * n_beam * 2;
-    if (smem > 32 * 1024)
-        WG_CUDA(cudaFuncSetAttribute(beam_backtrack_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 65536));
-    WG_CUDA(launch_pdl_smem(beam_backtrack_kernel, dim3((unsigned)n_req), dim3(BACK_THREADS), smem,
-                            static_cast<cudaStream_t>(stream), token, parent, n_steps, n_req, n_beam, tile, out));
+    BackArgs a{token, parent, out, n_steps, n_req, n_beam, 32 / n_beam, 0};
+    int parts = 1;
+    while (parts < BACK_CLUSTER && parts * BACK_STEPS < n_steps) parts <<= 1;
+    a.steps = std::min(BACK_STEPS, (n_steps + parts - 1) / parts);
+    WG_CUDA(cudaFuncSetAttribute(beam_backtrack_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(BackShared)));
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)parts;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)parts, (unsigned)((n_req + a.group - 1) / a.group));
+    cfg.blockDim = dim3(BACK_THREADS);
+    cfg.dynamicSmemBytes = sizeof(BackShared);
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    WG_CUDA(cudaLaunchKernelEx(&cfg, beam_backtrack_kernel, a));
     WG_LAUNCHED();
     return WG_OK;
 }

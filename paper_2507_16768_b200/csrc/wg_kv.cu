@@ -7,6 +7,7 @@
 // call ran in, the counts and bits after it are the same.
 #include <new>
 
+#include "wg_divide.cuh"
 #include "wg_host.h"
 
 namespace {
@@ -22,14 +23,15 @@ struct PoolDev {
     int32_t *ref;         // [n_blocks]
     uint32_t *free_bits;  // [n_words], padded with zero words to a whole round of a thread
     int32_t *n_free;
-    int32_t n_blocks, n_words, block_size;
+    int32_t n_blocks, n_words;
+    Divisor block;        // tokens of a block
     // per-call scratch
     int32_t *taken;       // [n_blocks] blocks handed out by the call, in order
     int32_t *first;       // [max_seqs] where a sequence's blocks begin in `taken`, or -1: refused
     int32_t *old_len;     // [max_seqs] lengths before the call
     int32_t *new_len;     // [max_seqs]
     int32_t *src;         // [max_seqs] a reorder's rows: the block to copy, or -1
-    int32_t *from, *dst, *filled;  // [max_seqs] its copies, one after the other
+    int4 *copy;           // [max_seqs] its copies, one after the other: from, to, tokens, column
     int32_t *n_copies;
     int32_t *arrived;     // blocks of the reorder's first kernel that have finished; zero between calls
 };
@@ -39,9 +41,13 @@ __device__ __forceinline__ void kv_enter() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-__device__ __forceinline__ int32_t blocks_of(int32_t len, int32_t block_size) {   // ceil, no overflow
-    return len / block_size + (len % block_size != 0);
-}
+// A length (>= 0) in whole blocks and the tokens beyond them.
+struct Blocks {
+    int32_t whole, rest;
+    __device__ __forceinline__ Blocks(const PoolDev &pool, int32_t len)
+        : whole((int32_t)pool.block.quotient((uint32_t)len)), rest(len - whole * (int32_t)pool.block.d) {}
+    __device__ __forceinline__ int32_t held() const { return whole + (rest != 0); }
+};
 
 __device__ __forceinline__ int up(int x, int o) { return __shfl_up_sync(0xFFFFFFFFu, x, o); }
 
@@ -87,12 +93,12 @@ __device__ __forceinline__ int nth_set_bit(uint32_t w, int n) {   // position of
 
 // Called by a whole block: takes the `n` lowest free blocks (n <= the number of free ones; the caller has
 // seen to that) with count 1 and calls got(k, id) for the k-th of them.  Every round a thread counts
-// four words of free bits; after the scan each of the round's blocks finds its word by bisection.
+// four words of free bits; after the scan the warps go over the threads' words, a lane per bit.
 // `w`: the thread's words of the first round, asked for early.
 template <int THREADS>
 struct TakeShared {
-    uint32_t words[THREADS * WORDS_PER_THREAD];
-    int32_t upto[THREADS];        // free blocks up to and including a thread's words
+    uint4 words[THREADS];
+    int32_t before[THREADS];      // free blocks before a thread's words
     int32_t warps[32];
 };
 
@@ -102,35 +108,37 @@ __device__ __forceinline__ uint4 free_words(const PoolDev &pool, int at) {
 
 template <int THREADS, typename Got>
 __device__ __forceinline__ void take_blocks(const PoolDev &pool, TakeShared<THREADS> &sh, int n, uint4 w, const Got &got) {
+    const int lane = threadIdx.x & 31;
     int done = 0;
+#pragma unroll 1
     for (int w0 = 0; done < n && w0 < pool.n_words; w0 += THREADS * WORDS_PER_THREAD) {
         const int mine = w0 + (int)threadIdx.x * WORDS_PER_THREAD;
         if (w0 > 0) w = free_words(pool, mine);
-        *reinterpret_cast<uint4 *>(&sh.words[threadIdx.x * WORDS_PER_THREAD]) = w;
+        sh.words[threadIdx.x] = w;
         const int count = __popc(w.x) + __popc(w.y) + __popc(w.z) + __popc(w.w);
         int total;
-        const int upto = block_scan(count, sh.warps, total);
-        sh.upto[threadIdx.x] = upto;
+        const int before = block_scan(count, sh.warps, total) - count;
+        sh.before[threadIdx.x] = before;
         __syncthreads();
         const int here = min(total, n - done);
-        for (int k = threadIdx.x; k < here; k += THREADS) {
-            int lo = 0, hi = THREADS - 1;             // the first thread whose words reach past k
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (sh.upto[mid] > k) hi = mid; else lo = mid + 1;
+#pragma unroll 1
+        for (int g = threadIdx.x >> 5; g < THREADS; g += THREADS / 32) {
+            int k = sh.before[g];
+            if (k >= here) break;
+            const uint32_t *words = reinterpret_cast<const uint32_t *>(&sh.words[g]);
+#pragma unroll 1
+            for (int i = 0; i < WORDS_PER_THREAD; ++i) {
+                const uint32_t word = words[i];
+                const int at = k + __popc(word & ((1u << lane) - 1u));
+                if (((word >> lane) & 1u) && at < here) {
+                    const int id = (w0 + g * WORDS_PER_THREAD + i) * 32 + lane;
+                    pool.ref[id] = 1;
+                    got(done + at, id);
+                }
+                k += __popc(word);
             }
-            int left = k - (lo > 0 ? sh.upto[lo - 1] : 0);
-            int at = lo * WORDS_PER_THREAD;
-            uint32_t word = sh.words[at];
-            for (int c = __popc(word); left >= c; c = __popc(word)) {
-                left -= c;
-                word = sh.words[++at];
-            }
-            const int id = (w0 + at) * 32 + nth_set_bit(word, left);
-            pool.ref[id] = 1;
-            got(done + k, id);
         }
-        int drop = min(count, here - (upto - count)); // of this thread's blocks, the lowest `drop` are gone
+        int drop = min(count, here - before);         // of this thread's blocks, the lowest `drop` are gone
         if (drop > 0) {
             uint32_t v[WORDS_PER_THREAD] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -148,15 +156,6 @@ __device__ __forceinline__ void take_blocks(const PoolDev &pool, TakeShared<THRE
 }
 
 __device__ __forceinline__ bool id_ok(const PoolDev &pool, int32_t id) { return id >= 0 && id < pool.n_blocks; }
-
-// `by` fewer (or, negative, more) rows name block `id`; a block nobody names is free.  A call only takes
-// away references that rows hold, so a count reaches zero once, with the last of them.
-__device__ __forceinline__ void drop_refs(const PoolDev &pool, int32_t id, int32_t by, int &freed) {
-    if (atomicSub(&pool.ref[id], by) == by) {
-        atomicOr(&pool.free_bits[id >> 5], 1u << (id & 31));
-        ++freed;
-    }
-}
 
 __device__ __forceinline__ void add_freed(const PoolDev &pool, int freed) {   // called by whole warps
     freed = __reduce_add_sync(0xFFFFFFFFu, freed);
@@ -218,17 +217,17 @@ __device__ __forceinline__ void extend_token(const PoolDev &pool, const ExtendAr
         const int32_t len = old_len[s];
         pos = len + (t - cu[s]);
         if (first[s] >= 0) {
-            const int32_t held = blocks_of(len, pool.block_size), col = pos / pool.block_size;
-            const int32_t in = pos - col * pool.block_size;
+            const Blocks at(pool, pos);
+            const int32_t held = Blocks(pool, len).held(), col = at.whole;
             int32_t *entry = a.table + (int64_t)s * a.stride + col;
             int32_t id;
             if (col < held) {
                 id = *entry;
             } else {
                 id = taken[first[s] + col - held];
-                if (in == 0) *entry = id;
+                if (at.rest == 0) *entry = id;
             }
-            if (id_ok(pool, id)) slot = (int64_t)id * pool.block_size + in;
+            if (id_ok(pool, id)) slot = (int64_t)id * (int64_t)pool.block.d + at.rest;
         }
     }
     a.slot[t] = slot;
@@ -262,7 +261,7 @@ extend_plan_kernel(PoolDev pool, ExtendArgs a) {
     const int n_free = *pool.n_free;
     PlanSums before{0, 0};               // of the rounds done
     int granted = 0;                     // blocks granted: the largest prefix that is
-    const int64_t room = (int64_t)a.max_blocks * pool.block_size;
+    const int64_t room = (int64_t)a.max_blocks * pool.block.d;
     for (int s0 = 0; s0 < a.n_seq; s0 += PLAN_THREADS) {
         const int s = s0 + (int)threadIdx.x;
         int32_t len = 0, add = 0, need = 0, st = WG_OK;
@@ -273,7 +272,7 @@ extend_plan_kernel(PoolDev pool, ExtendArgs a) {
                 st = WG_ERR_ARG;
                 add = 0;
             } else {
-                need = blocks_of(len + add, pool.block_size) - blocks_of(len, pool.block_size);
+                need = Blocks(pool, len + add).held() - Blocks(pool, len).held();
             }
         }
         PlanSums total;
@@ -343,14 +342,14 @@ shrink_kernel(PoolDev pool, int32_t *table, int64_t stride, int32_t max_blocks, 
     kv_enter();
     const int s = blockIdx.x;
     const int32_t have = len[s], want = keep[s];
-    const bool ok = have >= 0 && have <= (int64_t)max_blocks * pool.block_size && want >= 0 && want <= have;
+    const bool ok = have >= 0 && have <= (int64_t)max_blocks * pool.block.d && want >= 0 && want <= have;
     if (threadIdx.x == 0 && status) status[s] = ok ? WG_OK : WG_ERR_ARG;
     if (!ok) return;
-    const int32_t end = blocks_of(have, pool.block_size);
+    const int32_t end = Blocks(pool, have).held();
     int32_t *row = table + (int64_t)s * stride;
     int freed = 0;
     constexpr int AT_ONCE = 4;
-    for (int c0 = blocks_of(want, pool.block_size) + (int)threadIdx.x; c0 < end; c0 += AT_ONCE * SHRINK_THREADS) {
+    for (int c0 = Blocks(pool, want).held() + (int)threadIdx.x; c0 < end; c0 += AT_ONCE * SHRINK_THREADS) {
         int32_t id[AT_ONCE], left[AT_ONCE];
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u) {
@@ -395,6 +394,7 @@ struct MoveShared {
     int32_t children[WG_BEAM_MAX_BEAMS];
     int32_t first[WG_BEAM_MAX_BEAMS];     // first child, or n_beam
     int32_t bad[WG_BEAM_MAX_BEAMS];       // the length lay outside
+    int32_t most, alive;                  // columns in use by any row; rows that have a parent
 };
 
 constexpr int MOVE_ROWS = 4;              // rows a thread of the last block takes per round
@@ -402,9 +402,10 @@ constexpr int MOVE_ROWS = 4;              // rows a thread of the last block tak
 // First kernel: grid = (tiles of MOVE_THREADS columns, requests); a thread holds one column of all the
 // request's rows, so the rows move in place with no other thread in the way.  Row b's block of the
 // column was held once and is held by its children afterwards: the count changes by children - 1 (a
-// partly filled last block stays with one child only).  Rows that name the same block are summed
-// first: in the columns of a shared prompt nothing is left to count.  The block that finishes last
-// hands out the blocks for the copies.
+// partly filled last block stays with one child only).  A count never reaches zero before the last row that
+// named the block has been dealt with: what is not yet dealt with still counts 1 for each row.  In a
+// column that all rows share (a prompt's) the changes cancel.  The block that finishes last hands out the
+// blocks for the copies.
 __global__ void __launch_bounds__(MOVE_THREADS)
 move_rows_kernel(PoolDev pool, MoveArgs a) {
     extern __shared__ int32_t column[];   // [n_beam][MOVE_THREADS]
@@ -412,30 +413,39 @@ move_rows_kernel(PoolDev pool, MoveArgs a) {
     __shared__ TakeShared<MOVE_THREADS> take;
     __shared__ int32_t is_last;
     kv_enter();
-    const int K = a.n_beam, row0 = blockIdx.y * K, bs = pool.block_size;
-    const int64_t room = (int64_t)a.max_blocks * bs;
+    const int K = a.n_beam, row0 = blockIdx.y * K;
+    const int64_t room = (int64_t)a.max_blocks * pool.block.d;
     if ((int)threadIdx.x < K) {
         const int32_t p = a.parent[row0 + threadIdx.x], l = a.len[row0 + threadIdx.x];
         const int32_t len = l >= 0 && l <= room ? l : 0;
+        const Blocks n(pool, len);
         sh.parent[threadIdx.x] = p >= 0 && p < K ? p : -1;
         sh.len[threadIdx.x] = len;
         sh.bad[threadIdx.x] = len != l;
-        sh.blocks[threadIdx.x] = blocks_of(len, bs);
-        sh.partly[threadIdx.x] = len % bs != 0 ? len / bs : -1;
+        sh.blocks[threadIdx.x] = n.held();
+        sh.partly[threadIdx.x] = n.rest != 0 ? n.whole : -1;
     }
     __syncthreads();
-    if ((int)threadIdx.x < K) {
-        int n = 0, first = K;
-        for (int j = K - 1; j >= 0; --j)
-            if (sh.parent[j] == (int)threadIdx.x) {
-                ++n;
-                first = j;
-            }
-        sh.children[threadIdx.x] = n;
-        sh.first[threadIdx.x] = first;
+    if (threadIdx.x < 32) {
+        int children = 0, first = K, most = 0;
+        if ((int)threadIdx.x < K) {
+#pragma unroll 1
+            for (int j = K - 1; j >= 0; --j)
+                if (sh.parent[j] == (int)threadIdx.x) {
+                    ++children;
+                    first = j;
+                }
+            sh.children[threadIdx.x] = children;
+            sh.first[threadIdx.x] = first;
+            most = sh.blocks[threadIdx.x];
+        }
+        most = __reduce_max_sync(0xFFFFFFFFu, most);
+        const int alive = __reduce_add_sync(0xFFFFFFFFu, children);
+        if (threadIdx.x == 0) {
+            sh.most = most;
+            sh.alive = alive;
+        }
     }
-    int32_t most = 0;
-    for (int b = 0; b < K; ++b) most = max(most, sh.blocks[b]);
     __syncthreads();
     // what the last block needs of a row: its length, and that there is nothing to copy (where there is,
     // the thread that holds the column says so below)
@@ -447,45 +457,54 @@ move_rows_kernel(PoolDev pool, MoveArgs a) {
     }
     int freed = 0;
     const int c = blockIdx.x * MOVE_THREADS + (int)threadIdx.x;
-    if (c < most) {
+    if (c < sh.most) {
+        constexpr int AT_ONCE = 8;
         int32_t *col = a.table + (int64_t)row0 * a.stride + c;
         int32_t *v = column + threadIdx.x;
+        const int alive = sh.alive;
         bool same = true, plain = true;   // all rows name one block; no row's partly filled one
         int32_t id0 = -1;
-        for (int b0 = 0; b0 < K; b0 += 8) {
-            int32_t id[8];
+#pragma unroll 1
+        for (int b0 = 0; b0 < K; b0 += AT_ONCE) {
+            int32_t id[AT_ONCE];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) id[u] = b0 + u < K && c < sh.blocks[b0 + u] ? col[(b0 + u) * a.stride] : -1;
+            for (int u = 0; u < AT_ONCE; ++u) id[u] = b0 + u < K && c < sh.blocks[b0 + u] ? col[(b0 + u) * a.stride] : -1;
             if (b0 == 0) id0 = id[0];
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
+            for (int u = 0; u < AT_ONCE; ++u)
                 if (b0 + u < K) {
                     v[(b0 + u) * MOVE_THREADS] = id_ok(pool, id[u]) ? id[u] : -1;
                     same = same && id[u] == id0;
                     plain = plain && c != sh.partly[b0 + u];
                 }
         }
-        // counts
-        int alive = 0;
-        for (int j = 0; j < K; ++j) alive += sh.parent[j] >= 0;
-        if (same && plain && id_ok(pool, id0)) {
-            if (alive != K) drop_refs(pool, id0, K - alive, freed);
-        } else {
-            for (int b = 0; b < K; ++b) {
-                const int32_t id = v[b * MOVE_THREADS];
-                if (id < 0) continue;
-                bool seen = false;
-                int32_t change = 0;
-                for (int o = 0; o < K; ++o) {
-                    if (v[o * MOVE_THREADS] != id) continue;
-                    if (o < b) { seen = true; break; }
-                    change += (c == sh.partly[o] ? min(sh.children[o], 1) : sh.children[o]) - 1;
+        same = same && plain && id_ok(pool, id0);
+        if (!(same && alive == K)) {
+            // counts (the atomics of several rows in flight together)
+#pragma unroll 1
+            for (int b0 = 0; b0 < K; b0 += AT_ONCE) {
+                int32_t left[AT_ONCE];
+#pragma unroll
+                for (int u = 0; u < AT_ONCE; ++u) {
+                    const int b = b0 + u;
+                    left[u] = -1;
+                    if (b < K) {
+                        const int32_t id = v[b * MOVE_THREADS];
+                        const int children = sh.children[b];
+                        const int change = (c == sh.partly[b] ? min(children, 1) : children) - 1;
+                        if (id >= 0 && change != 0) left[u] = atomicAdd(&pool.ref[id], change) + change;
+                    }
                 }
-                if (!seen && change != 0) drop_refs(pool, id, -change, freed);
+#pragma unroll
+                for (int u = 0; u < AT_ONCE; ++u)
+                    if (left[u] == 0) {
+                        const int32_t id = v[(b0 + u) * MOVE_THREADS];
+                        atomicOr(&pool.free_bits[id >> 5], 1u << (id & 31));
+                        ++freed;
+                    }
             }
-        }
-        // rows
-        if (!(same && plain && alive == K)) {
+            // rows
+#pragma unroll 1
             for (int j = 0; j < K; ++j) {
                 const int p = sh.parent[j];
                 int32_t id = p >= 0 ? v[p * MOVE_THREADS] : -1;
@@ -499,16 +518,19 @@ move_rows_kernel(PoolDev pool, MoveArgs a) {
     }
     add_freed(pool, freed);
     // ---- the last block to finish
-    __threadfence();
     __syncthreads();
-    if (threadIdx.x == 0) is_last = atomicAdd(pool.arrived, 1) == (int)(gridDim.x * gridDim.y) - 1;
+    if (threadIdx.x == 0) {
+        __threadfence();
+        is_last = atomicAdd(pool.arrived, 1) == (int)(gridDim.x * gridDim.y) - 1;
+        __threadfence();
+    }
     __syncthreads();
     if (!is_last) return;
-    __threadfence();
     const uint4 free0 = free_words(pool, (int)threadIdx.x * WORDS_PER_THREAD);
     const int n_rows = a.n_req * K;
     const int n_free = __ldcg(pool.n_free);
     int done = 0;
+#pragma unroll 1
     for (int r0 = 0; r0 < n_rows; r0 += MOVE_THREADS * MOVE_ROWS) {
         const int i0 = r0 + (int)threadIdx.x * MOVE_ROWS;
         int32_t src[MOVE_ROWS], len[MOVE_ROWS];
@@ -526,12 +548,11 @@ move_rows_kernel(PoolDev pool, MoveArgs a) {
             const int i = i0 + u;
             if (i >= n_rows) break;
             const bool got = src[u] >= 0 && rank < n_free;
+            const Blocks n(pool, len[u]);
             if (got) {
-                pool.dst[rank] = i;               // the row, until its block is known
-                pool.from[rank] = src[u];
-                pool.filled[rank] = len[u] % bs;
+                pool.copy[rank] = make_int4(src[u], i, n.rest, n.whole);   // (the row, until its block is known)
             } else if (src[u] >= 0) {
-                len[u] -= len[u] % bs;
+                len[u] -= n.rest;
                 if (a.status) a.status[i] = WG_ERR_CAPACITY;
             }
             rank += src[u] >= 0;
@@ -544,10 +565,10 @@ move_rows_kernel(PoolDev pool, MoveArgs a) {
     const int granted = min(done, n_free);
     __syncthreads();
     take_blocks(pool, take, granted, free0, [&](int k, int id) {
-        const int row = pool.dst[k];
-        a.table[(int64_t)row * a.stride + a.len[row] / bs] = id;
-        if (a.copy_dst) a.copy_dst[row] = id;
-        pool.dst[k] = id;
+        const int4 copy = pool.copy[k];
+        a.table[(int64_t)copy.y * a.stride + copy.w] = id;
+        if (a.copy_dst) a.copy_dst[copy.y] = id;
+        pool.copy[k].y = id;
     });
     if (threadIdx.x == 0) {
         *pool.n_free = n_free - granted;
@@ -565,10 +586,11 @@ copy_blocks_kernel(PoolDev pool, const wg_kv_plane *planes, int32_t n_planes) {
     for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
         const int k = (int)(i / n_planes);
         const wg_kv_plane pl = planes[i - (int64_t)k * n_planes];
-        const int64_t per_block = (int64_t)pool.block_size * pl.token_bytes;
-        const char *src = static_cast<const char *>(pl.base) + (int64_t)pool.from[k] * per_block;
-        char *dst = static_cast<char *>(pl.base) + (int64_t)pool.dst[k] * per_block;
-        const int64_t bytes = (int64_t)pool.filled[k] * pl.token_bytes;
+        const int4 copy = pool.copy[k];
+        const int64_t per_block = (int64_t)pool.block.d * pl.token_bytes;
+        const char *src = static_cast<const char *>(pl.base) + (int64_t)copy.x * per_block;
+        char *dst = static_cast<char *>(pl.base) + (int64_t)copy.y * per_block;
+        const int64_t bytes = (int64_t)copy.z * pl.token_bytes;
         if ((((uintptr_t)src | (uintptr_t)dst | (uint64_t)bytes) & 15) == 0) {
             const uint4 *s = reinterpret_cast<const uint4 *>(src);
             uint4 *d = reinterpret_cast<uint4 *>(dst);
@@ -618,14 +640,14 @@ int32_t wg_kv_pool_create(int32_t n_blocks, int32_t block_size, int32_t max_seqs
     NvtxRange nvtx_range("wg_kv_pool_create");
     if (!out) return WG_ERR_ARG;
     *out = nullptr;
-    if (n_blocks < 1 || n_blocks > (1 << 30) || block_size < 1 || max_seqs < 1 || max_seqs > WG_MAX_ROWS)
+    if (n_blocks < 1 || n_blocks > (1 << 30) || block_size < 1 || block_size > (1 << 30) || max_seqs < 1 || max_seqs > WG_MAX_ROWS)
         return WG_ERR_ARG;
     wg_kv_pool *p = new (std::nothrow) wg_kv_pool();
     if (!p) return WG_ERR_ARG;
     PoolDev &d = p->dev;
     p->max_seqs = max_seqs;
     d.n_blocks = n_blocks;
-    d.block_size = block_size;
+    d.block = Divisor::of((uint32_t)block_size);
     d.n_words = (n_blocks + 31) / 32;
     const size_t words = ((size_t)d.n_words + WORDS_PER_THREAD - 1) / WORDS_PER_THREAD * WORDS_PER_THREAD;
     int32_t rc = dev_alloc(&d.ref, (size_t)n_blocks);
@@ -634,7 +656,8 @@ int32_t wg_kv_pool_create(int32_t n_blocks, int32_t block_size, int32_t max_seqs
     if (rc == WG_OK) rc = dev_alloc(&d.n_free, 1);
     if (rc == WG_OK) rc = dev_alloc(&d.n_copies, 1);
     if (rc == WG_OK) rc = dev_alloc(&d.arrived, 1);
-    for (int32_t **a : {&d.first, &d.old_len, &d.new_len, &d.src, &d.from, &d.dst, &d.filled})
+    if (rc == WG_OK) rc = dev_alloc(&d.copy, (size_t)max_seqs);
+    for (int32_t **a : {&d.first, &d.old_len, &d.new_len, &d.src})
         if (rc == WG_OK) rc = dev_alloc(a, (size_t)max_seqs);
     if (rc == WG_OK && (cudaMemset(d.free_bits, 0, words * sizeof(uint32_t)) != cudaSuccess ||
                         cudaMemset(d.arrived, 0, sizeof(int32_t)) != cudaSuccess))
@@ -654,7 +677,7 @@ void wg_kv_pool_free(wg_kv_pool *p) {
     const PoolDev &d = p->dev;
     for (void *q : {(void *)d.ref, (void *)d.free_bits, (void *)d.taken, (void *)d.n_free, (void *)d.n_copies,
                     (void *)d.arrived, (void *)d.first, (void *)d.old_len, (void *)d.new_len, (void *)d.src,
-                    (void *)d.from, (void *)d.dst, (void *)d.filled})
+                    (void *)d.copy})
         cudaFree(q);
     delete p;
 }
