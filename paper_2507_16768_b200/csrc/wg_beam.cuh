@@ -858,17 +858,18 @@ beam_pick_kernel(BeamArgs a, CtxDev ctx, VocabDev v, BeamStepArgs st, float *sco
 // tile for each block; the parts' maps are exchanged through the cluster's shared memory.  Within a
 // block a thread walks one column of one of the part's segments.
 // ---------------------------------------------------------------------------------------
-constexpr int BACK_THREADS = 1024;
+constexpr int BACK_THREADS = 512;
 constexpr int BACK_STEPS = 512;         // most steps of a block's part
 constexpr int BACK_CLUSTER = 8;         // most blocks of a cluster
-constexpr int BACK_DEAD = 255;
+constexpr int BACK_DEAD = 32;           // the column of a way that broke off: it leads to itself, its token is -1
+constexpr int BACK_ROW = 33;            // columns of a step (odd: a column's steps lie in different banks)
 
 struct BackShared {
-    int32_t token[BACK_STEPS * 33];     // [step][column], a row padded by one: columns lie in other banks
-    uint8_t parent[BACK_STEPS * 32];    // [step][column]
-    uint8_t path[BACK_STEPS * 32];      // [step][column]: the column of the step that this final one comes by
-    uint8_t maps[2][BACK_THREADS];      // [segment][column]
-    uint8_t part[32];                   // the whole part's map
+    int32_t token[BACK_STEPS * BACK_ROW];     // [step][column]
+    uint8_t parent[BACK_STEPS * BACK_ROW];    // [step][column]: a column of the step before
+    uint8_t path[BACK_STEPS * BACK_ROW];      // [step][column]: the step's column that this final one comes by
+    uint8_t maps[2][BACK_THREADS / 32 * BACK_ROW];   // [segment][column]
+    uint8_t part[BACK_ROW];                   // the whole part's map
     uint8_t at[32], from[32];           // where the final columns stand before the tile; where they enter the part
 };
 
@@ -892,7 +893,7 @@ __device__ __forceinline__ uint32_t cluster_byte(const uint8_t *p, uint32_t rank
     return x;
 }
 
-__global__ void __launch_bounds__(BACK_THREADS, 1)
+__global__ void __launch_bounds__(BACK_THREADS, 2)
 beam_backtrack_kernel(BackArgs a) {
     extern __shared__ uint8_t back_smem[];
     BackShared &sh = *reinterpret_cast<BackShared *>(back_smem);
@@ -907,83 +908,96 @@ beam_backtrack_kernel(BackArgs a) {
     const int base = lane / a.K * a.K;                               // the lane's request's first column
     const int tile = n_parts * a.steps;
     if (threadIdx.x < 32) sh.at[threadIdx.x] = (uint8_t)(mine ? lane : BACK_DEAD);
+    for (int t = threadIdx.x; t < a.steps; t += BACK_THREADS) {      // (nothing else is written there)
+        sh.parent[t * BACK_ROW + BACK_DEAD] = (uint8_t)BACK_DEAD;
+        sh.token[t * BACK_ROW + BACK_DEAD] = -1;
+    }
+    if (threadIdx.x < 2 * SEGMENTS)
+        sh.maps[threadIdx.x / SEGMENTS][threadIdx.x % SEGMENTS * BACK_ROW + BACK_DEAD] = (uint8_t)BACK_DEAD;
     for (int t1 = a.T; t1 > 0; t1 -= tile) {                         // tiles from the last to the first
         const int t0 = t1 - tile + part * a.steps;                   // this block's part: [max(t0, 0), t0 + steps)
         const int first = max(t0, 0), n = max(0, t0 + a.steps - first);
         __syncthreads();                                             // the previous tile is done with
         // ---- in: a warp reads a step's line
         {
-            const int32_t *parent = a.parent + first * step + col0 + lane, *token = a.token + first * step + col0 + lane;
-            constexpr int LOADS = BACK_STEPS / SEGMENTS;
-            int32_t p[LOADS], x[LOADS];
+            constexpr int LOADS = 8;                                 // in flight, of each array
+            const int64_t stride = SEGMENTS * step;
+            const int64_t at0 = (first + warp) * step + col0 + (mine ? lane : 0);
+            const int32_t *parent = a.parent + at0, *token = a.token + at0;
+            const uint32_t most = mine ? (uint32_t)a.K : 0u;
+            int to = warp * BACK_ROW + lane;
+            const auto put = [&](int32_t p, int32_t x) {
+                sh.parent[to] = (uint8_t)((uint32_t)p < most ? base + p : BACK_DEAD);
+                sh.token[to] = x;
+                to += SEGMENTS * BACK_ROW;
+            };
+            int s = warp;
+#pragma unroll 1
+            for (; s + (LOADS - 1) * SEGMENTS < n; s += LOADS * SEGMENTS) {
+                int32_t p[LOADS], x[LOADS];
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int t = warp + i * SEGMENTS;
-                p[i] = x[i] = 0;
-                if (t < n && mine) {
-                    p[i] = __ldcs(parent + t * step);
-                    x[i] = __ldcs(token + t * step);
+                for (int i = 0; i < LOADS; ++i, parent += stride, token += stride) {
+                    p[i] = __ldcs(parent);
+                    x[i] = __ldcs(token);
                 }
-            }
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int t = warp + i * SEGMENTS;
-                if (t < n) {
-                    sh.parent[t * 32 + lane] = mine && p[i] >= 0 && p[i] < a.K ? (uint8_t)(base + p[i]) : (uint8_t)BACK_DEAD;
-                    sh.token[t * 33 + lane] = x[i];
-                }
+                for (int i = 0; i < LOADS; ++i) put(p[i], x[i]);
             }
+#pragma unroll 1
+            for (; s < n; s += SEGMENTS, parent += stride, token += stride) put(__ldcs(parent), __ldcs(token));
         }
         __syncthreads();
         // ---- the segments' maps
         const int per = (n + SEGMENTS - 1) / SEGMENTS;
         const int lo = min(n, warp * per), hi = min(n, lo + per);
         int b = lane;
-        for (int t = hi - 1; t >= lo; --t)
-            if (b != BACK_DEAD) b = sh.parent[t * 32 + b];
-        sh.maps[0][threadIdx.x] = (uint8_t)b;
+#pragma unroll 4
+        for (int t = (hi - 1) * BACK_ROW; t >= lo * BACK_ROW; t -= BACK_ROW) b = sh.parent[t + b];
+        sh.maps[0][warp * BACK_ROW + lane] = (uint8_t)b;
         __syncthreads();
         // maps[s] becomes the composition of the maps of all segments from the last down to s
         int now = 0;
-#pragma unroll
+#pragma unroll 1
         for (int d = 1; d < SEGMENTS; d <<= 1) {
-            if (warp + d < SEGMENTS) {
-                const int far = sh.maps[now][threadIdx.x + d * 32];
-                b = far == BACK_DEAD ? BACK_DEAD : sh.maps[now][warp * 32 + far];
-            }
+            if (warp + d < SEGMENTS) b = sh.maps[now][warp * BACK_ROW + sh.maps[now][(warp + d) * BACK_ROW + lane]];
             now ^= 1;
-            sh.maps[now][threadIdx.x] = (uint8_t)b;
+            sh.maps[now][warp * BACK_ROW + lane] = (uint8_t)b;
             __syncthreads();
         }
         // ---- the parts: from the last one down to this one, and on to the first
-        if (threadIdx.x < 32) sh.part[threadIdx.x] = sh.maps[now][threadIdx.x];
-        cluster_sync();
+        if (threadIdx.x < BACK_ROW) sh.part[threadIdx.x] = sh.maps[now][threadIdx.x];
+        if (n_parts > 1) cluster_sync();
+        else __syncthreads();
         if (threadIdx.x < 32) {
             int c = sh.at[threadIdx.x];
             for (int q = n_parts - 1; q >= 0; --q) {
                 if (q == part) sh.from[threadIdx.x] = (uint8_t)c;
-                if (c != BACK_DEAD) c = (int)cluster_byte(&sh.part[c], (uint32_t)q);
+                c = (int)cluster_byte(&sh.part[c], (uint32_t)q);
             }
             sh.at[threadIdx.x] = (uint8_t)c;
         }
-        cluster_sync();                                              // the maps have been read, and `from` is there
+        if (n_parts > 1) cluster_sync();                             // the maps have been read, and `from` is there
+        else __syncthreads();
         // ---- the way
         b = sh.from[lane];
-        if (warp + 1 < SEGMENTS && b != BACK_DEAD) b = sh.maps[now][(warp + 1) * 32 + b];
-        for (int t = hi - 1; t >= lo; --t) {
-            sh.path[t * 32 + lane] = (uint8_t)b;
-            if (b != BACK_DEAD) b = sh.parent[t * 32 + b];
+        if (warp + 1 < SEGMENTS) b = sh.maps[now][(warp + 1) * BACK_ROW + b];
+#pragma unroll 4
+        for (int t = (hi - 1) * BACK_ROW; t >= lo * BACK_ROW; t -= BACK_ROW) {
+            sh.path[t + lane] = (uint8_t)b;
+            b = sh.parent[t + b];
         }
         __syncthreads();
-        // ---- out: a warp writes 32 steps of a column
-        const int columns = (n + 31) / 32;
-        for (int i = warp; i < columns * width; i += SEGMENTS) {
-            const int c = i / columns, t = (i - c * columns) * 32 + lane;
-            if (t < n) {
-                const int from = sh.path[t * 32 + c];
-                // (a way back that broke off in this tile, or is known to have: no sequence)
-                const bool gone = from == BACK_DEAD || sh.at[c] == BACK_DEAD;
-                a.out[(col0 + c) * a.T + first + t] = gone ? -1 : sh.token[t * 33 + from];
+        // ---- out: a warp writes a column, 32 steps at a time
+        for (int c = warp; c < width; c += SEGMENTS) {
+            int32_t *out = a.out + (col0 + c) * a.T + first;
+            const bool gone = sh.at[c] == BACK_DEAD;                 // it broke off here or further on: no sequence
+            const int32_t *token = sh.token + lane * BACK_ROW;
+            const uint8_t *path = sh.path + lane * BACK_ROW + c;
+            if (gone) {
+                for (int t = lane; t < n; t += 32) out[t] = -1;
+            } else {
+#pragma unroll 4
+                for (int t = lane; t < n; t += 32, token += 32 * BACK_ROW, path += 32 * BACK_ROW) out[t] = token[*path];
             }
         }
     }
