@@ -18,10 +18,7 @@
 #include "wg_kernels.cuh"
 
 constexpr int BEAM_THREADS = 256;           // scan
-#ifndef WGB
-#define WGB 4
-#endif
-constexpr int BEAM_BLOCKS = WGB;              // per SM
+constexpr int BEAM_BLOCKS = 4;              // per SM
 constexpr int BEAM_WARPS = BEAM_THREADS / 32;
 constexpr int BEAM_CHUNK = 512;             // positions per chunk maximum
 constexpr int PICK_THREADS = 512;
@@ -552,50 +549,8 @@ struct PickShared {
     MaskSource mask[WG_BEAM_MAX_BEAMS];
     float bound[2];                        // scores that n_out candidates reach: chunks, elements
     int32_t n[2];
-    int32_t count[PICK_WARPS];
+    int32_t digit[256], found_digit, found_above, found_upto;
 };
-
-// Sum of v over the block, in every thread.
-__device__ __forceinline__ int block_sum(PickShared &sh, int v) {
-    v = __reduce_add_sync(0xFFFFFFFFu, v);
-    if ((threadIdx.x & 31) == 0) sh.count[threadIdx.x >> 5] = v;
-    __syncthreads();
-    int total = 0;
-#pragma unroll
-    for (int i = 0; i < PICK_WARPS; ++i) total += sh.count[i];
-    __syncthreads();
-    return total;
-}
-
-// Puts the candidates that `each` enumerates into the (empty) list: all whose score reaches `bound` (and
-// is above -inf), or, where those are more than it holds (many equal scores), exactly the n_out
-// largest, found by bisection over the packed keys.  `each(f)` calls f(score, index) for the calling
-// thread's share; no two candidates have an index in common.  Returns how many are listed.
-template <typename Each>
-__device__ __forceinline__ int collect(PickShared &sh, int which, float bound, int n_out, const Each &each) {
-    const auto push = [&](unsigned long long k) {
-        const int at = atomicAdd(&sh.n[which], 1);
-        if (at < PICK_LIST) sh.list[which][at] = k;
-    };
-    each([&](float s, uint32_t idx) { if (s >= bound && s > -INFINITY) push(pack_key(score_key(s), idx)); });
-    __syncthreads();
-    const int n = sh.n[which];
-    if (n <= PICK_LIST) return n;
-    unsigned long long cut = 0ull;         // the largest value that n_out packed keys reach
-#pragma unroll 1
-    for (int bit = 63; bit >= 0; --bit) {
-        const unsigned long long trial = cut | (1ull << bit);
-        int mine = 0;
-        each([&](float s, uint32_t idx) { mine += pack_key(score_key(s), idx) >= trial; });
-        if (block_sum(sh, mine) >= n_out) cut = trial;
-    }
-    if (threadIdx.x == 0) sh.n[which] = 0;
-    sh.list[which][threadIdx.x] = 0ull;
-    __syncthreads();
-    each([&](float s, uint32_t idx) { if (pack_key(score_key(s), idx) >= cut) push(pack_key(score_key(s), idx)); });
-    __syncthreads();
-    return sh.n[which];
-}
 
 // Calls f(rank, packed key) for the listed candidates of rank below n_out (0 = the largest).
 template <typename F>
@@ -637,6 +592,81 @@ __device__ __forceinline__ void group_bound(PickShared &sh, float top, int n_out
         if (rank == n_out - 1) sh.bound[0] = mine;
     }
     __syncthreads();
+}
+
+// Puts the candidates that `each` enumerates into the (empty) list: those whose score reaches `bound` (and
+// is above -inf).  Where they are more than it holds, the bound is raised to that of the candidates' own
+// group maxima; where it is overrun still (hosts of equal scores), the packed keys' value that at least
+// n_out of them reach and no more than the list holds is found digit by digit.  `each(f)` calls
+// f(score, index) for the calling thread's share; no two candidates have an index in common.  Returns how
+// many are listed, at least n_out of the best if there are so many.
+template <typename Each>
+__device__ __forceinline__ int collect(PickShared &sh, int which, float bound, int n_out, const Each &each) {
+    const auto push = [&](float s, uint32_t idx) {
+        const int at = atomicAdd(&sh.n[which], 1);
+        if (at < PICK_LIST) sh.list[which][at] = pack_key(score_key(s), idx);
+    };
+    each([&](float s, uint32_t idx) { if (s >= bound && s > -INFINITY) push(s, idx); });
+    __syncthreads();
+    if (__builtin_expect(sh.n[which] <= PICK_LIST, 1)) return sh.n[which];
+    enum { RAISE, PUSH, COUNT, PUSH_FROM_CUT } mode = RAISE;
+    unsigned long long cut = 0ull;         // its digits above `shift` are known
+    int shift = 56, above = 0;             // keys beyond the known digits
+#pragma unroll 1
+    while (true) {
+        __syncthreads();                   // everybody has read what is cleared now
+        if (threadIdx.x < 256) sh.digit[threadIdx.x] = 0;
+        for (int i = threadIdx.x; i < PICK_LIST; i += PICK_THREADS) sh.list[which][i] = 0ull;
+        if (threadIdx.x == 0) sh.n[which] = 0;
+        __syncthreads();
+        float top = -INFINITY;
+        each([&](float s, uint32_t idx) {
+            if (mode == RAISE) {
+                top = fmaxf(top, s);
+                return;
+            }
+            if (!(s >= bound && s > -INFINITY)) return;
+            const unsigned long long k = pack_key(score_key(s), idx);
+            if (mode == COUNT) {
+                if (shift == 56 || (k ^ cut) >> (shift + 8) == 0ull) atomicAdd(&sh.digit[k >> shift & 255u], 1);
+            } else if (k >= cut) {
+                push(s, idx);
+            }
+        });
+        __syncthreads();
+        if (mode == RAISE) {
+            group_bound(sh, top, n_out);
+            bound = fmaxf(bound, sh.bound[0]);
+            mode = PUSH;
+        } else if (mode != COUNT) {
+            if (sh.n[which] <= PICK_LIST) return sh.n[which];
+            mode = COUNT;                  // only after the raised bound: the cut leaves no more than fit
+        } else {
+            // the digit that the n_out-th largest key has, by warp 0 with eight of them to a lane
+            if (threadIdx.x < 32) {
+                int mine = 0;
+                for (int i = 0; i < 8; ++i) mine += sh.digit[255 - (int)threadIdx.x * 8 - i];
+                int upto = mine;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int y = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+                    if ((int)threadIdx.x >= o) upto += y;
+                }
+                if (above + upto >= n_out && above + upto - mine < n_out) {
+                    int before = above + upto - mine, d = 255 - (int)threadIdx.x * 8;
+                    while (before + sh.digit[d] < n_out) before += sh.digit[d--];
+                    sh.found_digit = d;
+                    sh.found_above = before;
+                    sh.found_upto = before + sh.digit[d];
+                }
+            }
+            __syncthreads();
+            cut |= (unsigned long long)sh.found_digit << shift;
+            above = sh.found_above;
+            if (sh.found_upto <= PICK_LIST) mode = PUSH_FROM_CUT;   // (at the last digit it is: keys differ)
+            else shift -= 8;
+        }
+    }
 }
 
 // The request's best candidates, listed in sh.list[1]: the n_out best and possibly more.  Returns how

@@ -149,6 +149,20 @@ def test_ties_go_to_the_lowest_index(wg, dtype, norm, n_out):
     assert got[1].tolist() == [[0] * n_out] and got[2].tolist() == [ones[V // 4:][:n_out].tolist()]
 
 
+@pytest.mark.parametrize("n_req,K,V,n_out", [(2, 4, 1000, 64), (1, 16, 1000, 32), (3, 12, 1537, 24), (1, 32, 520, 64), (1, 1, 4000, 9)])
+def test_fewer_chunks_than_results(wg, n_req, K, V, n_out):
+    """Nothing can be told from the chunk maxima: all elements are candidates, more than are ranked at once."""
+    x, xf, allowed, score, finished, eos = make(V + K, n_req, K, V, "fp32", "most", ref.NORM_ALLOWED, n_out)
+    want = ref.select(xf, allowed, score, finished, eos, ref.NORM_ALLOWED, n_req, n_out)
+    check(run(wg, x, allowed, score, finished, eos, ref.NORM_ALLOWED, n_req, n_out), want)
+    # with hosts of equal scores among them, on several beams, so that no bound cuts the list short
+    rng = np.random.default_rng(V)
+    x = as_dtype(rng.integers(-3, 2, (n_req * K, V)), "fp32")
+    score = np.zeros(n_req * K, np.float32)
+    want = ref.select(x.numpy(), allowed, score, np.zeros(n_req * K, bool), eos, ref.NORM_NONE, n_req, n_out)
+    check(run(wg, x, allowed, score, None, eos, ref.NORM_NONE, n_req, n_out), want, 0)
+
+
 def test_negative_zero_ties_with_zero(wg):
     x = np.full((1, 300), -5.0, np.float32)
     x[0, 40], x[0, 260] = -0.0, 0.0
