@@ -21,6 +21,9 @@ constexpr int BEAM_THREADS = 256;           // scan
 constexpr int BEAM_BLOCKS = 4;              // per SM
 constexpr int BEAM_WARPS = BEAM_THREADS / 32;
 constexpr int BEAM_CHUNK = 512;             // positions per chunk maximum
+constexpr uint32_t SCAN_LONG = 4;           // steps of a long item
+constexpr uint32_t SCAN_GROUPS = 2;
+constexpr int SCAN_COUNTER = 64;            // words from one group's counter to the next
 constexpr int PICK_THREADS = 512;
 constexpr int PICK_WARPS = PICK_THREADS / 32;
 constexpr int PICK_GROUPS = 128;            // at most
@@ -35,13 +38,16 @@ struct BeamArgs {
     const int32_t *finished;  // or NULL
     const int32_t *gid, *sid; // with a context: the rows' states (finished = DONE)
     int32_t n_beam, V, W, n_out, eos, norm;
-    uint32_t n_steps, n_items;  // steps of all rows, and those eight by eight
+    uint32_t n_steps;           // of all rows
+    uint32_t n_long, n_two;     // items of SCAN_LONG steps, then of two; the rest is dealt step by step
+    uint32_t groups, per_group; // of blocks that share a counter
+    bool more;                  // there are more items than warps
     Divisor per_row;            // steps of a row
     int32_t chunk_stride;     // chunk maxima per row, a multiple of 4
     int32_t chunk_log2;       // the pick's threads side by side on a row: 32 .. 512
     float *chunk_max;         // [rows][chunk_stride]
     float2 *parts;            // [n_steps] (max, sum) of every step
-    int32_t *next_item;       // items taken beyond the first two of every block; zero between calls
+    int32_t *next_item;       // a counter per group: its items taken beyond the first of every warp; zero between calls
 };
 
 // What a step under grammars does with the selection.
@@ -287,9 +293,14 @@ __device__ __forceinline__ float log_sum(float m, float s) {
 
 // ---------------------------------------------------------------------------------------
 // Scan.  A warp works in steps of 4 KB of one row (eight 16-byte loads per lane, all in flight
-// together): 2048 bf16 or 1024 fp32 positions, and takes items of a.per_item consecutive steps of a row
-// from a device counter (rows differ a lot: a finished one costs nothing, a literal state a few
-// sectors, a free-text slot every logit).
+// together): 2048 bf16 or 1024 fp32 positions.  Rows differ a lot (a finished one costs nothing, a
+// literal state a few sectors, a free-text slot every logit), and so do SMs: with equal shares the
+// first was done after 27 us and the last after 58.  So warps take their steps from a counter.
+// Additions to one address pass at about 1 per ns, which single steps would be held up by (1024 rows x
+// 128256: 68 us), and long items end unevenly; so the items shrink, from four steps to two to one, and
+// two halves of the grid, each with a block or more on every SM, have a counter of their own.  No warp
+// waits for another (blocks that took eight steps together: 40 us instead of 37 on 512 misaligned rows
+// x 151937 summed whole).
 // ---------------------------------------------------------------------------------------
 template <typename E>
 struct ScanShape {
@@ -464,16 +475,22 @@ __global__ void __launch_bounds__(BEAM_THREADS, BEAM_BLOCKS)
 beam_scan_kernel(BeamArgs a, CtxDev ctx) {
     using S = ScanShape<E>;
     using Row = ScanRow<E, NORM, CTX>;
-    __shared__ uint32_t published[2];
     pdl_enter();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const auto look = [&](uint32_t item) -> ScanNext<E> {
+    const int lane = threadIdx.x & 31;
+    const uint32_t group = blockIdx.x / a.per_group, n_warps = a.per_group * BEAM_WARPS;
+    uint32_t step, end;                     // the step that is looked at next, and where its item ends
+    const auto item_of = [&](uint32_t nth) {
+        const uint32_t item = nth * a.groups + group, two = item - a.n_long, one = two - a.n_two;
+        if (item < a.n_long) step = SCAN_LONG * item, end = step + SCAN_LONG;
+        else if (two < a.n_two) step = SCAN_LONG * a.n_long + 2 * two, end = step + 2;
+        else step = SCAN_LONG * a.n_long + 2 * a.n_two + one, end = step + 1;
+    };
+    const auto look = [&]() -> ScanNext<E> {
         ScanNext<E> n;
-        const uint32_t step = item * BEAM_WARPS + warp;
         n.row = -1;
 #pragma unroll
         for (int i = 0; i < S::WORDS; ++i) n.word[i] = 0u;
-        if (item >= a.n_items || step >= a.n_steps) return n;
+        if (step >= a.n_steps) return n;
         n.row = (int)a.per_row.quotient(step);
         n.s = (int)(step - n.row * a.per_row.d);
         n.score = a.score[n.row];
@@ -481,16 +498,17 @@ beam_scan_kernel(BeamArgs a, CtxDev ctx) {
         Row(a, ctx, n.row).words(n.word, n.s);
         return n;
     };
-    uint32_t item = blockIdx.x, after = gridDim.x + blockIdx.x;
-    ScanNext<E> n = look(item);
+    item_of((blockIdx.x - group * a.per_group) * BEAM_WARPS + (threadIdx.x >> 5));
+    ScanNext<E> n = look();
     uint32_t v[2][S::HALF][4] = {};
 #pragma unroll 1
-    for (int turn = 0; item < a.n_items; turn ^= 1) {
-        uint32_t taken = 0;
-        if (threadIdx.x == 0) taken = (uint32_t)atomicAdd(a.next_item, 1);
+    while (n.row >= 0) {
+        const bool need = ++step == end;
+        uint32_t taken = n_warps;
+        if (need && a.more && lane == 0) taken += (uint32_t)atomicAdd(a.next_item + group * SCAN_COUNTER, 1);
         const int row = n.row, s = n.s;
-        const bool live = row >= 0 && (CTX ? beam_row_kind<CTX>(a, ctx, row, n.score) == BEAM_ROW_LIVE
-                                           : n.score > -INFINITY && !n.finished);
+        const bool live = CTX ? beam_row_kind<CTX>(a, ctx, row, n.score) == BEAM_ROW_LIVE
+                              : n.score > -INFINITY && !n.finished;
         // (most steps of a state inside a literal allow nothing)
         const bool any = NORM == WG_BEAM_NORM_FULL || __any_sync(0xFFFFFFFFu, (n.word[0] | n.word[S::WORDS - 1]) != 0u);
         uint32_t bits[2];
@@ -498,7 +516,8 @@ beam_scan_kernel(BeamArgs a, CtxDev ctx) {
             Row::deal(n.word, bits);
             Row(a, ctx, row).load(v, s, bits);
         }
-        n = look(after);
+        if (need) item_of(__shfl_sync(0xFFFFFFFFu, taken, 0));
+        n = look();
         if (live && !any) {
             if (lane < S::CHUNKS) a.chunk_max[(int64_t)row * a.chunk_stride + s * S::CHUNKS + lane] = -INFINITY;
             if (NORM != WG_BEAM_NORM_NONE && lane == 0)
@@ -515,10 +534,6 @@ beam_scan_kernel(BeamArgs a, CtxDev ctx) {
                 if (lane == 0) a.parts[(uint32_t)row * a.per_row.d + s] = make_float2(m, total);
             }
         }
-        if (threadIdx.x == 0) published[turn] = 2 * gridDim.x + taken;
-        __syncthreads();
-        item = after;
-        after = published[turn];
     }
 }
 
@@ -828,7 +843,7 @@ beam_pick_kernel(BeamArgs a, CtxDev ctx, VocabDev v, BeamStepArgs st, float *sco
     __shared__ PickShared sh;
     pdl_enter();
     const int req = blockIdx.x;
-    if (req == 0 && threadIdx.x == 0) *a.next_item = 0;
+    if (req == 0 && threadIdx.x < a.groups) a.next_item[threadIdx.x * SCAN_COUNTER] = 0;
     const int n = beam_pick<E, CTX>(sh, a, ctx, req);
     // ---- out, best first
     const int64_t out0 = (int64_t)req * a.n_out;

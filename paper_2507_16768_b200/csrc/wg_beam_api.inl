@@ -37,15 +37,23 @@ int32_t launch_beam(const BeamArgs &a, const CtxDev &ctx, const VocabDev &v, con
     return WG_OK;
 }
 
-// The scan's grid: as many blocks as are resident at once, or a step per warp.
+// The scan's grid (as many blocks as are resident at once, or a step per warp) and the items it deals out:
+// the last one and a half steps of every warp one by one, the step before those in twos.
 unsigned beam_grid(BeamArgs &a, int32_t rows, int32_t dtype) {
     const int step = dtype == WG_DTYPE_BF16 ? ScanShape<uint16_t>::STEP : ScanShape<uint32_t>::STEP;
     a.per_row = Divisor::of((uint32_t)(((long long)a.V + 7 + step - 1) / step));
     a.n_steps = (uint32_t)rows * a.per_row.d;
-    a.n_items = (a.n_steps + BEAM_WARPS - 1) / BEAM_WARPS;
+    const uint32_t blocks = std::min((a.n_steps + BEAM_WARPS - 1) / BEAM_WARPS, (uint32_t)sm_count() * BEAM_BLOCKS);
+    const uint32_t warps = blocks * BEAM_WARPS;
+    const uint32_t ones = std::min(a.n_steps, warps * 3 / 2), twos = std::min(a.n_steps - ones, warps);
+    a.n_two = twos / 2;
+    a.n_long = (a.n_steps - ones - twos) / SCAN_LONG;
+    a.more = a.n_steps - (SCAN_LONG - 1) * a.n_long - a.n_two > warps;
+    a.groups = a.more ? SCAN_GROUPS : 1;   // (more items than warps: the whole grid, which the groups divide)
+    a.per_group = blocks / a.groups;
     a.chunk_log2 = 5;
     while (a.chunk_log2 < 9 && (1 << a.chunk_log2) < a.chunk_stride) ++a.chunk_log2;
-    return std::min(a.n_items, (uint32_t)sm_count() * BEAM_BLOCKS);
+    return blocks;
 }
 
 bool beam_sizes_ok(const wg_beam *beam, int32_t n_req, int32_t n_beam, int32_t n_out, int32_t norm) {
@@ -80,8 +88,8 @@ int32_t wg_beam_create(int32_t V, int32_t max_requests, int32_t max_beams, int32
     const size_t rows = (size_t)max_requests * max_beams;
     int32_t rc = dev_alloc(&b->chunk_max, rows * b->chunk_stride);
     if (rc == WG_OK) rc = dev_alloc(&b->parts, rows * beam_spans(V) * 2);   // (an fp32 span is two steps)
-    if (rc == WG_OK) rc = dev_alloc(&b->next_item, 1);
-    if (rc == WG_OK && cudaMemset(b->next_item, 0, sizeof(int32_t)) != cudaSuccess) rc = WG_ERR_CUDA;
+    if (rc == WG_OK) rc = dev_alloc(&b->next_item, SCAN_GROUPS * SCAN_COUNTER);
+    if (rc == WG_OK && cudaMemset(b->next_item, 0, SCAN_GROUPS * SCAN_COUNTER * sizeof(int32_t)) != cudaSuccess) rc = WG_ERR_CUDA;
     if (rc != WG_OK) {
         wg_beam_free(b);
         return rc;
@@ -114,7 +122,7 @@ int32_t wg_beam_select(wg_beam *beam, const void *logits, int32_t dtype, int64_t
     if (finished && (eos_id < 0 || eos_id >= V)) return WG_ERR_ARG;
     if (score_out == score && n_out != n_beam) return WG_ERR_ARG;
     BeamArgs a{logits, row_stride_elems, bitmask, mask_stride_words, score, finished, nullptr, nullptr,
-               n_beam, V, W, n_out, eos_id, norm, 0u, 0u, Divisor{}, beam->chunk_stride, 0, beam->chunk_max, beam->parts,
+               n_beam, V, W, n_out, eos_id, norm, 0u, 0u, 0u, 0u, 0u, false, Divisor{}, beam->chunk_stride, 0, beam->chunk_max, beam->parts,
                beam->next_item};
     const unsigned grid = beam_grid(a, n_req * n_beam, dtype);
     const CtxDev none{};
@@ -157,7 +165,7 @@ int32_t wg_beam_step(wg_beam *beam, wg_ctx *c, int32_t *gid, int32_t *sid, float
     const int32_t rc = launch_build(c, work, rows, st, true);
     if (rc != WG_OK) return rc;
     BeamArgs a{logits, row_stride_elems, bitmask, mask_stride_words, score, nullptr, gid, sid,
-               n_beam, v.V, v.W, n_beam, v.eos_id, norm, 0u, 0u, Divisor{}, beam->chunk_stride, 0, beam->chunk_max, beam->parts,
+               n_beam, v.V, v.W, n_beam, v.eos_id, norm, 0u, 0u, 0u, 0u, 0u, false, Divisor{}, beam->chunk_stride, 0, beam->chunk_max, beam->parts,
                beam->next_item};
     const unsigned grid = beam_grid(a, rows, dtype);
     const BeamStepArgs step{gid, sid, status};
