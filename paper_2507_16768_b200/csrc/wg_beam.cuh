@@ -301,6 +301,14 @@ __device__ __forceinline__ float log_sum(float m, float s) {
 // two halves of the grid, each with a block or more on every SM, have a counter of their own.  No warp
 // waits for another (blocks that took eight steps together: 40 us instead of 37 on 512 misaligned rows
 // x 151937 summed whole).
+//
+// Measured with the pick behind it: 47.5 us for 1024 rows x 128256 bf16 (229 MB; the scan itself about
+// 43, 5.3 TB/s), 37 us for 512 x 151937 (136 MB), 18 us for 128 x 256000 fp32 of which most are in
+// literals, 8.4 us for 32 rows in literals.  What bounds it: 570 instructions a step (250 of them the
+// exponentials, 70 the mask) in 32 warps per SM, beside the memory; without exponentials and masks the
+// same walk streams at the memory's rate.  More loads in flight did not help where it cost registers or
+// instructions: rings in shared memory 53 to 60 us, loads a turn ahead at 80 registers 59, three blocks
+// per SM 54.
 // ---------------------------------------------------------------------------------------
 template <typename E>
 struct ScanShape {
@@ -538,7 +546,15 @@ beam_scan_kernel(BeamArgs a, CtxDev ctx) {
 }
 
 // ---------------------------------------------------------------------------------------
-// Pick.  One block per request.
+// Pick.  One block per request.  A few KB are read, so it is a chain of latencies, about 4.5 us behind the
+// scan whether for one request of 4 beams or for 128 of 8: the rows' facts (with the log-sums of the
+// steps' parts), the chunks' scores, a bound that n_out of them reach, the list of those above it and its
+// ranks; then the elements of the chosen chunks the same way.  The bound is the n_out-th largest of 16 to
+// 128 group maxima, at least twice n_out of them: it lets through little more than n_out, so that every
+// listed candidate can be ranked against all others by one thread (no sort, no histogram).  Scores stay
+// floats until a candidate is listed (4 beams x 32000 fp32: 8.2 -> 6.5 us a call).  A block that
+// finishes last in the scan picking for its request was slower (6.5 -> 7.9 us; 8 requests of 4 beams:
+// 9.0 -> 10.6): it comes after a fence and an atomic, where the second launch is already waiting.
 // ---------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t score_key(float s) {   // 0: not a candidate
     return s > -INFINITY ? order_key(__float_as_uint(s)) : 0u;
@@ -614,7 +630,9 @@ __device__ __forceinline__ void group_bound(PickShared &sh, float top, int n_out
 // group maxima; where it is overrun still (hosts of equal scores), the packed keys' value that at least
 // n_out of them reach and no more than the list holds is found digit by digit.  `each(f)` calls
 // f(score, index) for the calling thread's share; no two candidates have an index in common.  Returns how
-// many are listed, at least n_out of the best if there are so many.
+// many are listed, at least n_out of the best if there are so many.  (Where a request has fewer chunks than
+// n_out, its elements come here without a bound: 4 x 16 beams x 1000, 32 results: 22 us; 64 bits found
+// one by one: 108.)
 template <typename Each>
 __device__ __forceinline__ int collect(PickShared &sh, int which, float bound, int n_out, const Each &each) {
     const auto push = [&](float s, uint32_t idx) {
@@ -902,6 +920,11 @@ beam_pick_kernel(BeamArgs a, CtxDev ctx, VocabDev v, BeamStepArgs st, float *sco
 // as make up to 32 columns: 128 bytes of every step, read in whole lines) and a tile of steps, a part of the
 // tile for each block; the parts' maps are exchanged through the cluster's shared memory.  Within a
 // block a thread walks one column of one of the part's segments.
+//
+// Measured: 4.3 us for 256 steps of 8 x 4, 12.8 us for 4096 steps of 128 x 8 (50 MB, 3.9 TB/s).  Bound by
+// the staging of a part in shared memory and by the two walks' chains of look-ups (32 steps each), which
+// the loads of the next tile do not overlap.  A broken way follows a column of its own instead of being
+// tested for at every step (27 -> 13 us).
 // ---------------------------------------------------------------------------------------
 constexpr int BACK_THREADS = 512;
 constexpr int BACK_STEPS = 512;         // most steps of a block's part

@@ -248,7 +248,11 @@ __device__ __forceinline__ PlanSums up(const PlanSums &x, int o) {
     return {__shfl_up_sync(0xFFFFFFFFu, x.tokens, o), __shfl_up_sync(0xFFFFFFFFu, x.wanted, o)};
 }
 
-// One block: who gets how many blocks, which ones, and where each sequence's tokens begin.
+// One block: who gets how many blocks, which ones, and where each sequence's tokens begin.  A block is
+// enough: a batch has few thousand sequences, and what it takes lies at the front of the free bits.
+// Bound by latency: lengths, scan, free words, scan, table entry.  Measured, with the tokens taken back again
+// (the shrink): 7.6 us for one token of each of 1024 sequences, 9.6 us for 64 prompts of 8192 tokens
+// in all, whose tokens the fill kernel places in parallel.
 template <bool FILL>
 __global__ void __launch_bounds__(PLAN_THREADS, 1)
 extend_plan_kernel(PoolDev pool, ExtendArgs a) {
@@ -334,7 +338,9 @@ extend_fill_kernel(PoolDev pool, ExtendArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------
-// Shrink: a block per sequence.
+// Shrink: a block per sequence.  A count that reaches zero sets the block's free bit; a sequence's blocks are
+// counted down four to a thread, all in flight together, since each waits for what the atomic returns.
+// Measured in the extend's figures above.
 // ---------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(SHRINK_THREADS)
 shrink_kernel(PoolDev pool, int32_t *table, int64_t stride, int32_t max_blocks, int32_t *len,
@@ -405,7 +411,9 @@ constexpr int MOVE_ROWS = 4;              // rows a thread of the last block tak
 // partly filled last block stays with one child only).  A count never reaches zero before the last row that
 // named the block has been dealt with: what is not yet dealt with still counts 1 for each row.  In a
 // column that all rows share (a prompt's) the changes cancel.  The block that finishes last hands out the
-// blocks for the copies.
+// blocks for the copies.  Bound by latency (a chain of lengths, table, counts, the finished blocks' counter,
+// free bits): 22 us for 64 x 8 beams with their copies, which are 13 of them, and 10.3 us for 4 x 4.
+// Divisions by a block's length are multiplications; they and counts in flight together made 22 of 29 us.
 __global__ void __launch_bounds__(MOVE_THREADS)
 move_rows_kernel(PoolDev pool, MoveArgs a) {
     extern __shared__ int32_t column[];   // [n_beam][MOVE_THREADS]
@@ -578,7 +586,8 @@ move_rows_kernel(PoolDev pool, MoveArgs a) {
 }
 
 // Second kernel: the filled tokens of every copied block, in all planes.  The blocks take (copy, plane)
-// pairs in turn.
+// pairs in turn.  Bound by memory: 64 x 8 beams with 16 planes of 2 KB tokens, 87 MB read and written, 13 us
+// (6.6 TB/s, the writes still in L2).
 __global__ void __launch_bounds__(COPY_THREADS)
 copy_blocks_kernel(PoolDev pool, const wg_kv_plane *planes, int32_t n_planes) {
     kv_enter();
