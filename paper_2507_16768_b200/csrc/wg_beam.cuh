@@ -921,9 +921,12 @@ beam_pick_kernel(BeamArgs a, CtxDev ctx, VocabDev v, BeamStepArgs st, float *sco
 // tile for each block; the parts' maps are exchanged through the cluster's shared memory.  Within a
 // block a thread walks one column of one of the part's segments.
 //
-// Measured: 4.3 us for 256 steps of 8 x 4, 12.8 us for 4096 steps of 128 x 8 (50 MB, 3.9 TB/s).  Bound by
-// the staging of a part in shared memory and by the two walks' chains of look-ups (32 steps each), which
-// the loads of the next tile do not overlap.  A broken way follows a column of its own instead of being
+// Measured: 4.2 us for 256 steps of 8 x 4; for 4096 steps of 128 x 8 (50 MB) 17.4 us from memory
+// (2.9 TB/s), 12.5 from L2.  Bound by the staging of a part in shared memory and by the two walks' chains of
+// look-ups (32 steps each), during which nothing is loaded.  What would load meanwhile cost more than it
+// gave: tokens copied past the registers, word by word: 22.7 us; sixteen loads of each array in flight,
+// kept across the walks: 19.7 (everything runs once: longer code is fetched for longer, 4.2 -> 7.1 us
+// for the small search).  A broken way follows a column of its own instead of being
 // tested for at every step (27 -> 13 us).
 // ---------------------------------------------------------------------------------------
 constexpr int BACK_THREADS = 512;

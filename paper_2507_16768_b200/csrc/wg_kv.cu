@@ -412,8 +412,9 @@ constexpr int MOVE_ROWS = 4;              // rows a thread of the last block tak
 // named the block has been dealt with: what is not yet dealt with still counts 1 for each row.  In a
 // column that all rows share (a prompt's) the changes cancel.  The block that finishes last hands out the
 // blocks for the copies.  Bound by latency (a chain of lengths, table, counts, the finished blocks' counter,
-// free bits): 22 us for 64 x 8 beams with their copies, which are 13 of them, and 10.3 us for 4 x 4.
-// Divisions by a block's length are multiplications; they and counts in flight together made 22 of 29 us.
+// free bits): 28 us for 64 x 8 beams with their copies, which are about 18 of them, and 9.8 us for 4 x 4.
+// Divisions by a block's length are multiplications; they and counts in flight together made 22 of 29 us
+// (with the planes in L2).
 __global__ void __launch_bounds__(MOVE_THREADS)
 move_rows_kernel(PoolDev pool, MoveArgs a) {
     extern __shared__ int32_t column[];   // [n_beam][MOVE_THREADS]
@@ -586,8 +587,11 @@ move_rows_kernel(PoolDev pool, MoveArgs a) {
 }
 
 // Second kernel: the filled tokens of every copied block, in all planes.  The blocks take (copy, plane)
-// pairs in turn.  Bound by memory: 64 x 8 beams with 16 planes of 2 KB tokens, 87 MB read and written, 13 us
-// (6.6 TB/s, the writes still in L2).
+// pairs in turn; there are four times as many as are resident, since pairs differ in length (one block of
+// every SM's eight taking two to three pairs: 29.0 -> 27.9 us with the tables; the hardware deals the rest
+// out).  Bound by memory: 64 x 8 beams with 16 planes of 2 KB tokens, 87 MB read and written, about 18 us
+// (4.8 TB/s) from memory, 13 where the planes lie in L2.  Asking L2 for the sources while the
+// first kernel finds places for the copies was slower (29 -> 35 us), 512 threads too (31).
 __global__ void __launch_bounds__(COPY_THREADS)
 copy_blocks_kernel(PoolDev pool, const wg_kv_plane *planes, int32_t n_planes) {
     kv_enter();
@@ -756,8 +760,8 @@ int32_t wg_kv_reorder(wg_kv_pool *p, int32_t *table, int64_t table_stride, int32
     if (n_planes == 0) return WG_OK;
     const int64_t most = (int64_t)n_req * (n_beam - 1) * n_planes;   // copies cannot be more
     if (most == 0) return WG_OK;
-    const int64_t resident = (int64_t)sm_count() * 8;
-    WG_CUDA(launch_pdl(copy_blocks_kernel, dim3((unsigned)(most < resident ? most : resident)), dim3(COPY_THREADS), st,
+    const int64_t waves = (int64_t)sm_count() * 8 * 4;
+    WG_CUDA(launch_pdl(copy_blocks_kernel, dim3((unsigned)(most < waves ? most : waves)), dim3(COPY_THREADS), st,
                        p->dev, planes, n_planes));
     WG_LAUNCHED();
     return WG_OK;
