@@ -468,6 +468,30 @@ __device__ __forceinline__ void scan_step(uint32_t (&v)[2][ScanShape<E>::HALF][4
     }
 }
 
+// A step's results out: of one that allows something (or is summed whole), and of one that does not.
+template <typename E, int NORM>
+__device__ __forceinline__ void end_step(const BeamArgs &a, int row, int s, bool any,
+                                         uint32_t (&v)[2][ScanShape<E>::HALF][4], const uint32_t (&bits)[2]) {
+    using S = ScanShape<E>;
+    const int lane = threadIdx.x & 31;
+    if (!any) {
+        if (lane < S::CHUNKS) a.chunk_max[(int64_t)row * a.chunk_stride + s * S::CHUNKS + lane] = -INFINITY;
+        if (NORM != WG_BEAM_NORM_NONE && lane == 0)
+            a.parts[(uint32_t)row * a.per_row.d + s] = make_float2(-INFINITY, 0.f);
+        return;
+    }
+    float m = -INFINITY;
+    Pair sum[2] = {0ull, 0ull};
+    scan_step<E, NORM>(v, bits, a.chunk_max + (int64_t)row * a.chunk_stride + s * S::CHUNKS, m, sum);
+    if (NORM != WG_BEAM_NORM_NONE) {
+        const float2 two = halves(add2(sum[0], sum[1]));
+        float total = two.x + two.y;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+        if (lane == 0) a.parts[(uint32_t)row * a.per_row.d + s] = make_float2(m, total);
+    }
+}
+
 // What a warp knows of its next step: where it is, and, asked for a turn ahead, its mask words and
 // whether the row counts.
 template <typename E>
@@ -526,22 +550,7 @@ beam_scan_kernel(BeamArgs a, CtxDev ctx) {
         }
         if (need) item_of(__shfl_sync(0xFFFFFFFFu, taken, 0));
         n = look();
-        if (live && !any) {
-            if (lane < S::CHUNKS) a.chunk_max[(int64_t)row * a.chunk_stride + s * S::CHUNKS + lane] = -INFINITY;
-            if (NORM != WG_BEAM_NORM_NONE && lane == 0)
-                a.parts[(uint32_t)row * a.per_row.d + s] = make_float2(-INFINITY, 0.f);
-        } else if (live) {
-            float m = -INFINITY;
-            Pair sum[2] = {0ull, 0ull};
-            scan_step<E, NORM>(v, bits, a.chunk_max + (int64_t)row * a.chunk_stride + s * S::CHUNKS, m, sum);
-            if (NORM != WG_BEAM_NORM_NONE) {
-                const float2 two = halves(add2(sum[0], sum[1]));
-                float total = two.x + two.y;
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
-                if (lane == 0) a.parts[(uint32_t)row * a.per_row.d + s] = make_float2(m, total);
-            }
-        }
+        if (live) end_step<E, NORM>(a, row, s, any, v, bits);
     }
 }
 
@@ -854,14 +863,11 @@ __device__ __forceinline__ int beam_pick(PickShared &sh, const BeamArgs &a, cons
     });
 }
 
+// The request's selection out and, with a context, its states moved on.
 template <typename E, bool CTX>
-__global__ void __launch_bounds__(PICK_THREADS)
-beam_pick_kernel(BeamArgs a, CtxDev ctx, VocabDev v, BeamStepArgs st, float *score_out,
-                 int32_t *parent_out, int32_t *token_out) {
-    __shared__ PickShared sh;
-    pdl_enter();
-    const int req = blockIdx.x;
-    if (req == 0 && threadIdx.x < a.groups) a.next_item[threadIdx.x * SCAN_COUNTER] = 0;
+__device__ __forceinline__ void select_request(PickShared &sh, const BeamArgs &a, const CtxDev &ctx, const VocabDev &v,
+                                               const BeamStepArgs &st, int req, float *score_out, int32_t *parent_out,
+                                               int32_t *token_out) {
     const int n = beam_pick<E, CTX>(sh, a, ctx, req);
     // ---- out, best first
     const int64_t out0 = (int64_t)req * a.n_out;
@@ -912,6 +918,54 @@ beam_pick_kernel(BeamArgs a, CtxDev ctx, VocabDev v, BeamStepArgs st, float *sco
     }
 }
 
+template <typename E, bool CTX>
+__global__ void __launch_bounds__(PICK_THREADS)
+beam_pick_kernel(BeamArgs a, CtxDev ctx, VocabDev v, BeamStepArgs st, float *score_out,
+                 int32_t *parent_out, int32_t *token_out) {
+    __shared__ PickShared sh;
+    pdl_enter();
+    if (blockIdx.x == 0 && threadIdx.x < a.groups) a.next_item[threadIdx.x * SCAN_COUNTER] = 0;
+    select_request<E, CTX>(sh, a, ctx, v, st, blockIdx.x, score_out, parent_out, token_out);
+}
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+
+// Both in one launch, for few requests: a cluster per request, large enough that every step of its rows has
+// a warp; the cluster's first block picks.  On the device it takes what two launches take (1 x 4 beams x
+// 32000 fp32: 6.6 us; the cluster's start and barrier are as long as the overlapped second launch), and the
+// host is done 2.5 us earlier.  With a second step for a warp it lost (8 x 4 beams x 128256: 9.9 us
+// instead of 8.4).
+constexpr int SMALL_CLUSTER = 16;           // blocks, at most
+
+template <typename E, int NORM, bool CTX>
+__global__ void __launch_bounds__(PICK_THREADS)
+beam_small_kernel(BeamArgs a, CtxDev ctx, VocabDev v, BeamStepArgs st, float *score_out,
+                  int32_t *parent_out, int32_t *token_out) {
+    using S = ScanShape<E>;
+    using Row = ScanRow<E, NORM, CTX>;
+    __shared__ PickShared sh;
+    pdl_enter();
+    const int i = blockIdx.x * PICK_WARPS + (threadIdx.x >> 5);
+    const int b = (int)a.per_row.quotient((uint32_t)i), s = i - b * (int)a.per_row.d, row = blockIdx.y * a.n_beam + b;
+    if (b < a.n_beam) {
+        const float score = a.score[row];
+        uint32_t word[S::WORDS], bits[2], x[2][S::HALF][4] = {};
+        Row(a, ctx, row).words(word, s);
+        if (beam_row_kind<CTX>(a, ctx, row, score) == BEAM_ROW_LIVE) {
+            const bool any = NORM == WG_BEAM_NORM_FULL || __any_sync(0xFFFFFFFFu, (word[0] | word[S::WORDS - 1]) != 0u);
+            if (any) {
+                Row::deal(word, bits);
+                Row(a, ctx, row).load(x, s, bits);
+            }
+            end_step<E, NORM>(a, row, s, any, x, bits);
+        }
+    }
+    cluster_sync();
+    if (blockIdx.x == 0) select_request<E, CTX>(sh, a, ctx, v, st, blockIdx.y, score_out, parent_out, token_out);
+}
+
 // ---------------------------------------------------------------------------------------
 // Back-track.  The walk from the last step to the first is a chain of dependent look-ups, so the steps are
 // cut into segments: every segment is first walked from all beams at once (a map from its last beams
@@ -951,10 +1005,6 @@ struct BackArgs {
     int32_t group;                      // requests of a block
     int32_t steps;                      // of a part (at most BACK_STEPS)
 };
-
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
-}
 
 // The byte at `p` of this block's shared memory, in the shared memory of the cluster's block `rank`.
 __device__ __forceinline__ uint32_t cluster_byte(const uint8_t *p, uint32_t rank) {
