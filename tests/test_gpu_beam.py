@@ -128,6 +128,17 @@ def test_large(wg, n_req, K, V, n_out, dtype, kind):
     check(run(wg, x, allowed, score, finished, eos, ref.NORM_ALLOWED, n_req, n_out), want)
 
 
+@pytest.mark.parametrize("norm,kind", [(ref.NORM_ALLOWED, "most"), (ref.NORM_FULL, "few"), (ref.NORM_NONE, "few")])
+@pytest.mark.parametrize("n_req,K,V,dtype", [
+    (1, 16, 2040, "bf16"), (1, 17, 2040, "bf16"), (148, 1, 2040, "bf16"), (149, 1, 2040, "bf16"), (2, 16, 16377, "bf16"),
+    (1, 8, 32761, "fp32"), (4, 16, 32760, "bf16"), (5, 16, 32760, "bf16"), (1, 17, 32760, "bf16"), (18, 4, 32761, "fp32")])
+def test_one_launch_and_two(wg, n_req, K, V, dtype, norm, kind):
+    """Batches on both sides of what one launch takes, at every size of its clusters."""
+    x, xf, allowed, score, finished, eos = make(n_req + K, n_req, K, V, dtype, kind, norm, K)
+    want = ref.select(xf, allowed, score, finished, eos, norm, n_req, K)
+    check(run(wg, x, allowed, score, finished, eos, norm, n_req, K), want)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("norm", [ref.NORM_ALLOWED, ref.NORM_FULL, ref.NORM_NONE])
 @pytest.mark.parametrize("n_out", [1, 7, 64])

@@ -107,6 +107,17 @@ def test_search(wg, vocab, R, K, kind, norm):
     assert s.ctx.stats()["empty_masks"] == s.empty and s.ctx.stats()["bad_states"] == 0
 
 
+@pytest.mark.parametrize("R,K,kind", [(150, 2, "dense"), (150, 2, "compact"), (10, 32, "dense"), (20, 32, "compact")])
+def test_search_of_many_requests(wg, vocab, R, K, kind):
+    """Batches on both sides of what one launch takes."""
+    s = Search(wg, vocab, [op() for op in OPS], R, K, mode=wg.WG_CACHE_COMPACT if kind == "compact" else None)
+    rng = np.random.default_rng(R + K)
+    bonus = 6.0 * has_structural_byte(vocab).astype(np.float32)
+    for _ in range(4):
+        s.step(as_dtype(rng.standard_normal((R * K, vocab.size)) * 2 + bonus, "fp32"))
+    s.check_states()
+
+
 def test_search_to_the_end(wg):
     """A language of a few short words: beams finish, keep their scores, and there are fewer words than beams."""
     vocab = make_vocab(600, seed=9)
