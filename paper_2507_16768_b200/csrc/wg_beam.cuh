@@ -863,6 +863,14 @@ __device__ __forceinline__ int beam_pick(PickShared &sh, const BeamArgs &a, cons
     });
 }
 
+// With a context the selection writes grammar ids, which the kernels of a step that follows read ahead of
+// their wait: dependents start at its end then.
+template <bool CTX>
+__device__ __forceinline__ void select_enter() {
+    if constexpr (CTX) pdl_wait();
+    else pdl_enter();
+}
+
 // The request's selection out and, with a context, its states moved on.
 template <typename E, bool CTX>
 __device__ __forceinline__ void select_request(PickShared &sh, const BeamArgs &a, const CtxDev &ctx, const VocabDev &v,
@@ -923,7 +931,7 @@ __global__ void __launch_bounds__(PICK_THREADS)
 beam_pick_kernel(BeamArgs a, CtxDev ctx, VocabDev v, BeamStepArgs st, float *score_out,
                  int32_t *parent_out, int32_t *token_out) {
     __shared__ PickShared sh;
-    pdl_enter();
+    select_enter<CTX>();
     if (blockIdx.x == 0 && threadIdx.x < a.groups) a.next_item[threadIdx.x * SCAN_COUNTER] = 0;
     select_request<E, CTX>(sh, a, ctx, v, st, blockIdx.x, score_out, parent_out, token_out);
 }
@@ -946,7 +954,7 @@ beam_small_kernel(BeamArgs a, CtxDev ctx, VocabDev v, BeamStepArgs st, float *sc
     using S = ScanShape<E>;
     using Row = ScanRow<E, NORM, CTX>;
     __shared__ PickShared sh;
-    pdl_enter();
+    select_enter<CTX>();
     const int i = blockIdx.x * PICK_WARPS + (threadIdx.x >> 5);
     const int b = (int)a.per_row.quotient((uint32_t)i), s = i - b * (int)a.per_row.d, row = blockIdx.y * a.n_beam + b;
     if (b < a.n_beam) {

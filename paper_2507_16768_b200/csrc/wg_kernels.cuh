@@ -824,9 +824,10 @@ __global__ void cache_lookup_kernel(CtxDev ctx, const int32_t *gid, const int32_
 //
 // The kernel sits between the previous step's advance and this step's apply with nothing to hide
 // its latency, so the usual case -- the state is cached and found at its first probe position --
-// is kept to two round trips after the wait: the state id, then key and pool row together.  What
-// never changes while steps are in flight (the row's grammar id, that grammar's state count) is
-// read before the wait, for the first row of every thread.
+// is kept to two round trips after the wait: the state id, then key and pool row together.  The
+// row's grammar id and that grammar's state count are read before the wait, for the first row of
+// every thread: no kernel that lets its dependents start early writes them (beam search, which
+// moves grammar ids with the hypotheses, starts its dependents at its end).
 __global__ void __launch_bounds__(1024)
 cache_lookup_insert_kernel(CtxDev ctx, const int32_t *gid, const int32_t *sid, int B,
                            uint32_t *bitmask, int64_t mask_stride) {
@@ -1123,6 +1124,10 @@ __device__ __forceinline__ void pdl_enter() {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
+
+// For a kernel that writes what later kernels read ahead of their wait: its dependents start when it
+// has ended, and the kernels behind those no earlier.
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // The two sweeps of the apply kernels over the spans [span_begin, span_end) of one row, for the
 // calling block: this warp's spans are span_begin + warp, + APPLY_WARPS, ...; words[k] holds mask
@@ -1450,9 +1455,10 @@ __global__ void advance_kernel(VocabDev v, CtxDev ctx, const int32_t *gid, int32
                                const int32_t *token_in, int32_t *token_out, int B,
                                int32_t *status, uint32_t flags, int from_keys,
                                const long long *ext_keys) {
-    // What never changes while steps are in flight (the row's grammar id, the grammar's record)
-    // is read BEFORE waiting for the kernel ahead, so that these two dependent loads run under
-    // its tail; states and tokens are only touched after the wait.
+    // The row's grammar id and the grammar's record are read BEFORE waiting for the kernel ahead,
+    // so that these two dependent loads run under its tail: no kernel that lets its dependents
+    // start early writes them (see cache_lookup_insert_kernel).  States and tokens are only
+    // touched after the wait.
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int r = blockIdx.x * blockDim.x + threadIdx.x;
     const int g = r < B ? gid[r] : -1;
