@@ -422,6 +422,22 @@ __device__ __forceinline__ void raise(float high, float &m, Pair (&sum)[2]) {
     }
 }
 
+// Maxima pass over NaN, so a step that counts nothing but -inf and NaN has a maximum of -inf, and no
+// exponentials are formed.  Where there is a NaN among them (what is not -inf, then), it goes into the sum,
+// and from there into the row's: times what moves it to another maximum it is NaN still.
+template <typename E, int N>
+__device__ __forceinline__ void keep_nan(const uint32_t (&v)[2][N][4], Pair (&sum)[2]) {
+    constexpr uint32_t NOTHING = sizeof(E) == 2 ? NEG_INF_BF16X2 : NEG_INF_F32;
+    uint32_t other = 0u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) other |= v[h][i][j] ^ NOTHING;
+    if (__any_sync(0xFFFFFFFFu, other != 0u)) sum[0] = pair(__int_as_float(0x7FC00000), 0.f);
+}
+
 // One step's share of a row: its chunk maxima out, its exponentials added to (m, sum); m is the same in
 // all lanes.
 template <typename E, int NORM>
@@ -439,6 +455,8 @@ __device__ __forceinline__ void scan_step(uint32_t (&v)[2][ScanShape<E>::HALF][4
         if (m > -INFINITY) {
             pieces_exp<E>(v[0], m, sum);
             pieces_exp<E>(v[1], m, sum);
+        } else {
+            keep_nan<E>(v, sum);
         }
     }
     if (__any_sync(0xFFFFFFFFu, (bits[0] | bits[1]) != 0u)) {
@@ -459,6 +477,8 @@ __device__ __forceinline__ void scan_step(uint32_t (&v)[2][ScanShape<E>::HALF][4
             if (m > -INFINITY) {
                 pieces_exp<E>(v[0], m, sum);
                 pieces_exp<E>(v[1], m, sum);
+            } else {
+                keep_nan<E>(v, sum);
             }
         }
     }
