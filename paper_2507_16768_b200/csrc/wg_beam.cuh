@@ -5,7 +5,7 @@
 // and a candidate's score is c + (x[t] - lse).  The n_out best of a request are found without ever
 // writing scores out:
 //   * the scan reads every logit once and keeps, per chunk of 512 tokens, the largest allowed logit,
-//     and per warp (m, s) with the running-maximum rescaling of an online softmax;
+//     and per step of a warp (4 KB of a row) its own (m, s); the pick moves the steps' sums to the row's m;
 //   * a score is a non-decreasing function of the logit within a row (two fp32 roundings, both
 //     monotonic), so a chunk's best score is the score of its largest logit.  Rank the chunks of all
 //     beams by (best score, then the lower chunk number).  An element outside the first n_out
@@ -411,17 +411,6 @@ struct ScanRow {
     }
 };
 
-// m becomes high (if that is more), and the sums are measured from there.
-__device__ __forceinline__ void raise(float high, float &m, Pair (&sum)[2]) {
-    if (high > m) {
-        const float f = moved(m, high);
-        const Pair both = pair(f, f), zero = pair(-0.f, -0.f);
-        sum[0] = fma2(sum[0], both, zero);
-        sum[1] = fma2(sum[1], both, zero);
-        m = high;
-    }
-}
-
 // Maxima pass over NaN, so a step that counts nothing but -inf and NaN has a maximum of -inf, and no
 // exponentials are formed.  Where there is a NaN among them (what is not -inf, then), it goes into the sum,
 // and from there into the row's: times what moves it to another maximum it is NaN still.
@@ -438,8 +427,8 @@ __device__ __forceinline__ void keep_nan(const uint32_t (&v)[2][N][4], Pair (&su
     if (__any_sync(0xFFFFFFFFu, other != 0u)) sum[0] = pair(__int_as_float(0x7FC00000), 0.f);
 }
 
-// One step's share of a row: its chunk maxima out, its exponentials added to (m, sum); m is the same in
-// all lanes.
+// One step's share of a row: its chunk maxima out, and m, the maximum of what is counted (the same in all
+// lanes; -inf coming in), with this lane's sums of exp(x - m) (zero coming in).
 template <typename E, int NORM>
 __device__ __forceinline__ void scan_step(uint32_t (&v)[2][ScanShape<E>::HALF][4], const uint32_t (&bits)[2],
                                           float *chunks, float &m, Pair (&sum)[2]) {
@@ -451,7 +440,7 @@ __device__ __forceinline__ void scan_step(uint32_t (&v)[2][ScanShape<E>::HALF][4
     for (int i = 0; i < S::CHUNKS; ++i) best[i] = -INFINITY;
     if (NORM == WG_BEAM_NORM_FULL) {
         // the whole vocabulary is summed; the maxima are those of what is allowed
-        raise(warp_max(fmaxf(pieces_max<E>(v[0], 0, S::HALF), pieces_max<E>(v[1], 0, S::HALF))), m, sum);
+        m = warp_max(fmaxf(pieces_max<E>(v[0], 0, S::HALF), pieces_max<E>(v[1], 0, S::HALF)));
         if (m > -INFINITY) {
             pieces_exp<E>(v[0], m, sum);
             pieces_exp<E>(v[1], m, sum);
@@ -470,10 +459,9 @@ __device__ __forceinline__ void scan_step(uint32_t (&v)[2][ScanShape<E>::HALF][4
             best[i] = warp_max(pieces_max<E>(v[i / PER_HALF], at, at + S::PER_CHUNK));
         }
         if (NORM == WG_BEAM_NORM_ALLOWED) {
-            float high = best[0];
+            m = best[0];
 #pragma unroll
-            for (int i = 1; i < S::CHUNKS; ++i) high = fmaxf(high, best[i]);
-            raise(high, m, sum);
+            for (int i = 1; i < S::CHUNKS; ++i) m = fmaxf(m, best[i]);
             if (m > -INFINITY) {
                 pieces_exp<E>(v[0], m, sum);
                 pieces_exp<E>(v[1], m, sum);
