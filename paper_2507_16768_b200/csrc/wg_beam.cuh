@@ -224,16 +224,20 @@ __device__ __forceinline__ float exp2_fast(float x) {
 constexpr float LOG2_E = 1.4426950408889634f;
 
 // Where a row's exponentials are measured from: 2^(x * log2 e - reference).  Kept in the logarithm's own
-// base, so that one fused multiply-add makes the exponent and no rounding of m * log2 e is lost.
-// Beyond |m| = 2^100 that product could overflow (masks of the type's lowest value, infinities): the
-// difference x - m is formed first there.
-constexpr float FAR_M = 1.2676506e30f;
+// base, so that one fused multiply-add makes the exponent.  m * log2 e is rounded there, by up to |m| * 2^-24,
+// and every exponent is off by that: harmless while it is small (the logarithm takes it out again), but
+// beyond |m| = 2^31 or so the sum overflows or vanishes.  From 2^20 on the difference x - m is formed first
+// (finite values that stand for a mask, infinities).
+constexpr float FAR_M = 1048576.f;
 
 __device__ __forceinline__ float reference(float m) { return __fmul_rn(m, LOG2_E); }
 
 // What a sum measured from m is multiplied by to be measured from high >= m (-inf: a sum of nothing).
+// Either may be measured from its rounded reference or, far out, from itself.
 __device__ __forceinline__ float moved(float m, float high) {
-    return exp2_fast(fabsf(high) < FAR_M ? reference(m) - reference(high) : (m - high) * LOG2_E);
+    const bool near = fabsf(m) < FAR_M;
+    if (fabsf(high) < FAR_M) return exp2_fast(near ? reference(m) - reference(high) : fmaf(m, LOG2_E, -reference(high)));
+    return exp2_fast(near ? fmaf(-high, LOG2_E, reference(m)) : (m - high) * LOG2_E);
 }
 
 // Two fp32 values in one 64-bit register, for the instructions that work on both.
