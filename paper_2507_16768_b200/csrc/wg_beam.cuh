@@ -223,21 +223,19 @@ __device__ __forceinline__ float exp2_fast(float x) {
 
 constexpr float LOG2_E = 1.4426950408889634f;
 
-// Where a row's exponentials are measured from: 2^(x * log2 e - reference).  Kept in the logarithm's own
+// Where a step's exponentials are measured from: 2^(x * log2 e - reference).  Kept in the logarithm's own
 // base, so that one fused multiply-add makes the exponent.  m * log2 e is rounded there, by up to |m| * 2^-24,
-// and every exponent is off by that: harmless while it is small (the logarithm takes it out again), but
-// beyond |m| = 2^31 or so the sum overflows or vanishes.  From 2^20 on the difference x - m is formed first
-// (finite values that stand for a mask, infinities).
+// and every exponent is off by that, which is put right where the sum is moved.  Beyond |m| = 2^31 or so the sum
+// would overflow or vanish first; from 2^20 on the difference x - m is formed instead (finite values that stand
+// for a mask, infinities).
 constexpr float FAR_M = 1048576.f;
 
 __device__ __forceinline__ float reference(float m) { return __fmul_rn(m, LOG2_E); }
 
-// What a sum measured from m is multiplied by to be measured from high >= m (-inf: a sum of nothing).
-// Either may be measured from its rounded reference or, far out, from itself.
+// What the sum of a step with maximum m is multiplied by to be measured from high >= m itself (m = -inf: a sum of
+// nothing).
 __device__ __forceinline__ float moved(float m, float high) {
-    const bool near = fabsf(m) < FAR_M;
-    if (fabsf(high) < FAR_M) return exp2_fast(near ? reference(m) - reference(high) : fmaf(m, LOG2_E, -reference(high)));
-    return exp2_fast(near ? fmaf(-high, LOG2_E, reference(m)) : (m - high) * LOG2_E);
+    return exp2_fast(fmaf(m - high, LOG2_E, fabsf(m) < FAR_M ? fmaf(-m, LOG2_E, reference(m)) : 0.f));
 }
 
 // Two fp32 values in one 64-bit register, for the instructions that work on both.
@@ -289,11 +287,9 @@ __device__ __forceinline__ void pieces_exp(const uint32_t (&w)[N][4], float m, P
     }
 }
 
-// What (m, s) say of the sum of exp: its logarithm.
-__device__ __forceinline__ float log_sum(float m, float s) {
-    if (fabsf(m) < FAR_M) return (reference(m) + log2f(s)) * 0.6931471805599453f;
-    return m + logf(s);
-}
+// What (m, s) say of the sum of exp: its logarithm.  (Of one token, whose s is 1 to 2^-22, this is m itself
+// from 16 on: a row in a literal keeps its score however long that is.)
+__device__ __forceinline__ float log_sum(float m, float s) { return m + logf(s); }
 
 // ---------------------------------------------------------------------------------------
 // Scan.  A warp works in steps of 4 KB of one row (eight 16-byte loads per lane, all in flight
