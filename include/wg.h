@@ -624,8 +624,8 @@ int32_t wg_kv_pool_n_free(wg_kv_pool *pool, int32_t *n_free, void *stream);
  *   slot, pos, seq  device, n_tokens entries each: the slot, the position within its sequence and the
  *               sequence of every token; -1 from cu[n_seq] on
  *   status      device, n_seq, or NULL: WG_OK; WG_ERR_ARG: n_new < 0, or len outside the table, or
- *               the sequence would outgrow it (taken as n_new = 0); WG_ERR_CAPACITY: not enough
- *               free blocks or not enough room in `slot`
+ *               the sequence would outgrow it or INT32_MAX tokens (taken as n_new = 0);
+ *               WG_ERR_CAPACITY: not enough free blocks or not enough room in `slot`
  * Blocks are granted in order: a sequence that needs some is refused when those wanted up to and
  * including it are more than there are.  A refused sequence keeps its length and table; its tokens
  * keep their places, with slot -1.  cu is cut off at n_tokens. */

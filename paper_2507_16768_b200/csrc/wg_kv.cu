@@ -265,7 +265,7 @@ extend_plan_kernel(PoolDev pool, ExtendArgs a) {
     const int n_free = *pool.n_free;
     PlanSums before{0, 0};               // of the rounds done
     int granted = 0;                     // blocks granted: the largest prefix that is
-    const int64_t room = (int64_t)a.max_blocks * pool.block.d;
+    const int64_t room = min((int64_t)a.max_blocks * pool.block.d, (int64_t)INT32_MAX);   // lengths have 32 bits
     for (int s0 = 0; s0 < a.n_seq; s0 += PLAN_THREADS) {
         const int s = s0 + (int)threadIdx.x;
         int32_t len = 0, add = 0, need = 0, st = WG_OK;
