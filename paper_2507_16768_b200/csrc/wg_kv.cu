@@ -728,7 +728,7 @@ int32_t wg_kv_extend(wg_kv_pool *p, int32_t *table, int64_t table_stride, int32_
     WG_CUDA(launch_pdl(extend_plan_kernel<false>, dim3(1), dim3(PLAN_THREADS), st, p->dev, a));
     WG_LAUNCHED();
     if (n_tokens == 0) return WG_OK;         // nothing to place
-    WG_CUDA(launch_pdl(extend_fill_kernel, dim3((unsigned)((n_tokens + FILL_THREADS - 1) / FILL_THREADS)),
+    WG_CUDA(launch_pdl(extend_fill_kernel, dim3(((unsigned)n_tokens + FILL_THREADS - 1) / FILL_THREADS),
                        dim3(FILL_THREADS), st, p->dev, a));
     WG_LAUNCHED();
     return WG_OK;

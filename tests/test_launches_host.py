@@ -1,0 +1,50 @@
+"""What the host code launches, without a GPU: the library in a process of its own, over stand-ins for the CUDA runtime
+(fake_cudart.c) that write the launches down."""
+import os
+import subprocess
+import sys
+import textwrap
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
+
+
+@pytest.fixture(scope="module")
+def fake(tmp_path_factory):
+    out = str(tmp_path_factory.mktemp("fake") / "libfake_cudart.so")
+    subprocess.check_call(["gcc", "-O1", "-std=c11", "-Wall", "-shared", "-fPIC", "-o", out, os.path.join(HERE, "fake_cudart.c")])
+    return out
+
+
+PRELUDE = """
+import ctypes as C
+fake = C.CDLL({fake!r}, mode=C.RTLD_GLOBAL)      # found before the runtime that the library is linked to
+lib = C.CDLL({lib!r})
+fake.fake_log.restype = C.c_char_p
+lib.wg_beam_select.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p] + [C.c_int] * 5 + [C.c_void_p] * 4
+lib.wg_kv_extend.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_void_p, C.c_int] + [C.c_void_p] * 4 + [C.c_int, C.c_void_p, C.c_void_p]
+at = 1 << 20                                     # an address that nothing looks at
+def log():
+    return fake.fake_log().decode().split('\\n')[:-1]
+"""
+
+
+def lines(fake, body):
+    code = PRELUDE.format(fake=fake, lib=os.path.join(ROOT, "paper_2507_16768_b200", "libwg.so")) + textwrap.dedent(body)
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stderr
+    return r.stdout.splitlines()
+
+
+@pytest.mark.parametrize("n_tokens,blocks", [(2049, 9), (2304, 9), (2305, 10), (2 ** 31 - 256, 2 ** 23 - 1), (2 ** 31 - 255, 2 ** 23), (2 ** 31 - 1, 2 ** 23)])
+def test_extend_places_any_number_of_tokens(fake, n_tokens, blocks):
+    got = lines(fake, f"""
+        pool = C.c_void_p()
+        assert lib.wg_kv_pool_create(100, 16, 4, C.byref(pool)) == 0
+        fake.fake_reset(-1)
+        print(lib.wg_kv_extend(pool, at, 8, 8, at, at, 4, at, at, at, at, {n_tokens}, None, None))
+        print(*log(), sep='\\n')
+    """)
+    assert got == ["0", "launch 1 1 1", f"launch {blocks} 1 1"]
