@@ -11,6 +11,8 @@ struct wg_beam {
 
 namespace {
 
+constexpr size_t SCAN_COUNTERS = SCAN_GROUPS * SCAN_COUNTER * sizeof(int32_t);
+
 // Spans of 2048 positions per row, for the worst alignment of a row (it may begin up to 7 elements into
 // a piece).
 int32_t beam_spans(int32_t V) { return (V + 7 + 2047) / 2048; }
@@ -34,6 +36,23 @@ cudaError_t launch_beam_small(const BeamArgs &a, const CtxDev &ctx, const VocabD
 }
 
 template <typename E, bool CTX>
+int32_t launch_scan_and_pick(const BeamArgs &a, const CtxDev &ctx, const VocabDev &v, const BeamStepArgs &step,
+                             int32_t n_req, unsigned grid, float *score_out, int32_t *parent_out, int32_t *token_out,
+                             cudaStream_t st) {
+    if (a.norm == WG_BEAM_NORM_ALLOWED)
+        WG_CUDA((launch_beam_scan<E, WG_BEAM_NORM_ALLOWED, CTX>(a, ctx, grid, st)));
+    else if (a.norm == WG_BEAM_NORM_FULL)
+        WG_CUDA((launch_beam_scan<E, WG_BEAM_NORM_FULL, CTX>(a, ctx, grid, st)));
+    else
+        WG_CUDA((launch_beam_scan<E, WG_BEAM_NORM_NONE, CTX>(a, ctx, grid, st)));
+    WG_LAUNCHED();
+    WG_CUDA(launch_pdl(beam_pick_kernel<E, CTX>, dim3((unsigned)n_req), dim3(PICK_THREADS), st, a, ctx, v,
+                       step, score_out, parent_out, token_out));
+    WG_LAUNCHED();
+    return WG_OK;
+}
+
+template <typename E, bool CTX>
 int32_t launch_beam(const BeamArgs &a, const CtxDev &ctx, const VocabDev &v, const BeamStepArgs &step,
                     int32_t n_req, unsigned grid, float *score_out, int32_t *parent_out, int32_t *token_out,
                     cudaStream_t st) {
@@ -53,17 +72,10 @@ int32_t launch_beam(const BeamArgs &a, const CtxDev &ctx, const VocabDev &v, con
         WG_LAUNCHED();
         return WG_OK;
     }
-    if (a.norm == WG_BEAM_NORM_ALLOWED)
-        WG_CUDA((launch_beam_scan<E, WG_BEAM_NORM_ALLOWED, CTX>(a, ctx, grid, st)));
-    else if (a.norm == WG_BEAM_NORM_FULL)
-        WG_CUDA((launch_beam_scan<E, WG_BEAM_NORM_FULL, CTX>(a, ctx, grid, st)));
-    else
-        WG_CUDA((launch_beam_scan<E, WG_BEAM_NORM_NONE, CTX>(a, ctx, grid, st)));
-    WG_LAUNCHED();
-    WG_CUDA(launch_pdl(beam_pick_kernel<E, CTX>, dim3((unsigned)n_req), dim3(PICK_THREADS), st, a, ctx, v,
-                       step, score_out, parent_out, token_out));
-    WG_LAUNCHED();
-    return WG_OK;
+    const int32_t rc = launch_scan_and_pick<E, CTX>(a, ctx, v, step, n_req, grid, score_out, parent_out, token_out, st);
+    // the pick sets the counters back that the scan takes its items from: where it was not launched, this does
+    if (rc != WG_OK) cudaMemsetAsync(a.next_item, 0, SCAN_COUNTERS, st);
+    return rc;
 }
 
 // The scan's grid (as many blocks as are resident at once, or a step per warp) and the items it deals out:
@@ -118,7 +130,7 @@ int32_t wg_beam_create(int32_t V, int32_t max_requests, int32_t max_beams, int32
     int32_t rc = dev_alloc(&b->chunk_max, rows * b->chunk_stride);
     if (rc == WG_OK) rc = dev_alloc(&b->parts, rows * beam_spans(V) * 2);   // (an fp32 span is two steps)
     if (rc == WG_OK) rc = dev_alloc(&b->next_item, SCAN_GROUPS * SCAN_COUNTER);
-    if (rc == WG_OK && cudaMemset(b->next_item, 0, SCAN_GROUPS * SCAN_COUNTER * sizeof(int32_t)) != cudaSuccess) rc = WG_ERR_CUDA;
+    if (rc == WG_OK && cudaMemset(b->next_item, 0, SCAN_COUNTERS) != cudaSuccess) rc = WG_ERR_CUDA;
     if (rc != WG_OK) {
         wg_beam_free(b);
         return rc;

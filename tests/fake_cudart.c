@@ -10,14 +10,16 @@ typedef struct { dim3_ grid, block; size_t smem; void *stream; void *attrs; unsi
 
 static char text[1 << 16];
 static size_t used;
-static int launches, failing = -1;
+static int launches, failing = -1, stale = -1;
 
 static void note(const char *line) {
     if (used + strlen(line) + 2 < sizeof text) used += (size_t)sprintf(text + used, "%s\n", line);
 }
 
 const char *fake_log(void) { return text; }
-void fake_reset(int fail_launch) { text[0] = 0; used = 0; launches = 0; failing = fail_launch; }
+void fake_reset(int fail_launch) { text[0] = 0; used = 0; launches = 0; failing = fail_launch; stale = -1; }
+/* after the n-th launch an error of somebody else's is found */
+void fake_stale_error(int after_launch) { stale = after_launch; }
 
 static int launch(dim3_ g) {
     char line[96];
@@ -33,7 +35,7 @@ int cudaLaunchKernel(const void *f, dim3_ g, dim3_ b, void **args, size_t smem, 
     return launch(g);
 }
 int cudaFuncSetAttribute(const void *f, int attr, int value) { (void)f; (void)attr; (void)value; return 0; }
-int cudaGetLastError(void) { return 0; }
+int cudaGetLastError(void) { return launches - 1 == stale ? 9 : 0; }
 int cudaGetDevice(int *d) { *d = 0; return 0; }
 int cudaDeviceGetAttribute(int *v, int attr, int d) { (void)attr; (void)d; *v = 148; return 0; }
 int cudaMalloc(void **p, size_t n) { *p = aligned_alloc(256, (n + 255) / 256 * 256); return *p ? 0 : 2; }

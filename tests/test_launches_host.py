@@ -48,3 +48,29 @@ def test_extend_places_any_number_of_tokens(fake, n_tokens, blocks):
         print(*log(), sep='\\n')
     """)
     assert got == ["0", "launch 1 1 1", f"launch {blocks} 1 1"]
+
+
+SELECT = """
+    beam, n_req = C.c_void_p(), 400
+    assert lib.wg_beam_create(30000, n_req, 8, 8, C.byref(beam)) == 0
+    def select():
+        return lib.wg_beam_select(beam, at, 0, 30000, None, 0, at, None, 0, n_req, 8, 8, 0, at, at, at, 77)
+"""
+
+
+def test_a_selection_that_was_cut_short_leaves_no_counts(fake):
+    """The scan deals its items out from counters that the pick behind it sets back.  Where the pick could not be
+    launched, they are set back all the same, behind the scan and on its stream."""
+    got = lines(fake, SELECT + """
+    fake.fake_reset(-1)
+    print(select(), [l.split()[0] for l in log()])
+    fake.fake_reset(1)
+    print(select(), [l.split()[0] for l in log()], log()[-1])
+    fake.fake_reset(-1)
+    fake.fake_stale_error(0)
+    print(select(), [l.split()[0] for l in log()], log()[-1])
+    fake.fake_reset(-1)
+    print(select(), [l.split()[0] for l in log()])
+""")
+    assert got == ["0 ['launch', 'launch']", "-5 ['launch', 'failed-launch', 'memset'] memset 0 512 on 77",
+                   "-5 ['launch', 'memset'] memset 0 512 on 77", "0 ['launch', 'launch']"]
