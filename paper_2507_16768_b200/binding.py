@@ -708,13 +708,22 @@ def wg_decode_step_host(ctx: Context, gid, sid, logits_host, logits_dev, bitmask
         "wg_decode_step_host")
 
 
+_torch_c = None      # torch._C, looked up once (an import statement is 65 ns at every call)
+
+
 def _on_stream(stream, device: int):
-    """The raw stream of a call: the given one, else the current one of the device that the call's arrays
-    are on (asked for by number: making a stream object costs more than a small launch)."""
+    """The raw stream of a call whose arrays are on ``device``: the given one, else the device's current one (asked
+    for by number: making a stream object costs more than a small launch).  A launch goes to the current
+    device, and a default stream has the same handle on all of them, so that device has to be the current one."""
+    global _torch_c
+    if _torch_c is None:
+        import torch
+        _torch_c = torch._C
+    if _torch_c._cuda_getDevice() != device:
+        raise ValueError(f"the call's arrays are on cuda:{device}, which is not the current device")
     if stream is not None:
         return stream.cuda_stream
-    import torch
-    return torch._C._cuda_getCurrentRawStream(device)
+    return _torch_c._cuda_getCurrentRawStream(device)
 
 
 # ---- constrained beam search ---------------------------------------------------------------------
@@ -817,6 +826,8 @@ def wg_beam_step(beam: Beam, ctx: Context, n_beam: int, gid, sid, score, logits,
         raise ValueError("parent_out and token_out are required")
     n_req, n_beam = _beam_rows(n_beam, rows)
     dev = _device_of(ctx)
+    if beam.device != dev:
+        raise ValueError(f"the beam's scratch is on cuda:{beam.device}, the context on cuda:{dev}")
     _check(_lib.wg_beam_step(beam.handle, ctx.handle, g, s, _vec(score, rows, torch.float32, "score", dev), n_req,
                              n_beam, lp, dtype, stride, mp, mstride, int(norm),
                              _vec(parent_out, rows, torch.int32, "parent_out", dev), tok, st, int(flags),
