@@ -838,14 +838,14 @@ def wg_beam_backtrack(token, parent, out, stream=None) -> None:
     """``token``, ``parent``: [n_steps, n_req, n_beam] as the steps returned them; ``out``:
     [n_req, n_beam, n_steps], the sequence of every final beam."""
     import torch
-    if token.dim() != 3 or parent.shape != token.shape:
+    shape, dev, int32 = token.shape, token.device.index, torch.int32
+    if len(shape) != 3 or parent.shape != shape:
         raise ValueError("token and parent must be [n_steps, n_req, n_beam]")
-    T, R, K = token.shape
-    dev = token.device.index
+    T, R, K = shape
     if out.shape != (R, K, T):
         raise ValueError(f"out must be [{R}, {K}, {T}]")
     for t, what in ((token, "token"), (parent, "parent"), (out, "out")):
-        if not t.is_cuda or t.dtype != torch.int32:
+        if not t.is_cuda or t.dtype is not int32:
             raise TypeError(f"{what} must be an int32 CUDA tensor")
         if t.device.index != dev or not t.is_contiguous():
             raise ValueError(f"{what} must be contiguous, all on one device")
