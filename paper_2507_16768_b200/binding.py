@@ -775,7 +775,7 @@ class BeamPlan:
     def __init__(self, beam: Beam, n_beam: int, score, score_out, parent_out, token_out, bitmask=None,
                  finished=None, eos_id: int = 0, norm: int = WG_BEAM_NORM_ALLOWED, stream=None):
         import torch
-        self._keep = (beam, score, score_out, parent_out, token_out, bitmask, finished)
+        self._keep = (score, score_out, parent_out, token_out, bitmask, finished)
         dev = beam.device
         rows = int(score.numel())
         self.n_req, self.n_beam = _beam_rows(n_beam, rows)
@@ -789,7 +789,7 @@ class BeamPlan:
             _mat(bitmask, rows, (beam.V + 31) // 32, (torch.int32, torch.uint32), "bitmask", dev)
         if finished is not None and not 0 <= int(eos_id) < beam.V:
             raise ValueError(f"eos_id {eos_id} is not in the vocabulary")
-        self._head = beam.handle
+        self._beam = beam                # (its handle is asked for at every call: none once it is closed)
         self._tail = (mask, mstride, _vec(score, rows, torch.float32, "score", dev),
                       _vec(finished, rows, torch.int32, "finished", dev), int(eos_id), self.n_req,
                       self.n_beam, n_out, int(norm), so, po, to)
@@ -803,7 +803,7 @@ class BeamPlan:
             raise ValueError("logits must be a tensor [rows, V] with unit inner stride on the beam's device")
         if logits.dtype not in self._dtypes:
             raise TypeError(f"logits must be bfloat16 or float32, not {logits.dtype}")
-        rc = self._fn(self._head, logits.data_ptr(), self._dtypes[logits.dtype], logits.stride(0), *self._tail,
+        rc = self._fn(self._beam.handle, logits.data_ptr(), self._dtypes[logits.dtype], logits.stride(0), *self._tail,
                       _on_stream(self._stream, self._device))
         if rc != WG_OK:
             raise WgError(rc, "wg_beam_select")
