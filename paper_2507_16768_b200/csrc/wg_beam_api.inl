@@ -130,7 +130,9 @@ int32_t wg_beam_create(int32_t V, int32_t max_requests, int32_t max_beams, int32
     int32_t rc = dev_alloc(&b->chunk_max, rows * b->chunk_stride);
     if (rc == WG_OK) rc = dev_alloc(&b->parts, rows * beam_spans(V) * 2);   // (an fp32 span is two steps)
     if (rc == WG_OK) rc = dev_alloc(&b->next_item, SCAN_GROUPS * SCAN_COUNTER);
-    if (rc == WG_OK && cudaMemset(b->next_item, 0, SCAN_COUNTERS) != cudaSuccess) rc = WG_ERR_CUDA;
+    // (the first call may be on a stream that does not wait for the default one)
+    if (rc == WG_OK && (cudaMemset(b->next_item, 0, SCAN_COUNTERS) != cudaSuccess || cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess))
+        rc = WG_ERR_CUDA;
     if (rc != WG_OK) {
         wg_beam_free(b);
         return rc;

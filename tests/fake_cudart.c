@@ -40,7 +40,11 @@ int cudaGetDevice(int *d) { *d = 0; return 0; }
 int cudaDeviceGetAttribute(int *v, int attr, int d) { (void)attr; (void)d; *v = 148; return 0; }
 int cudaMalloc(void **p, size_t n) { *p = aligned_alloc(256, (n + 255) / 256 * 256); return *p ? 0 : 2; }
 int cudaFree(void *p) { free(p); return 0; }
-int cudaMemset(void *p, int v, size_t n) { memset(p, v, n); return 0; }
+int cudaMemset(void *p, int v, size_t n) {
+    memset(p, v, n);
+    note("memset on the default stream");
+    return 0;
+}
 int cudaMemsetAsync(void *p, int v, size_t n, void *st) {
     char line[96];
     memset(p, v, n);
@@ -48,4 +52,7 @@ int cudaMemsetAsync(void *p, int v, size_t n, void *st) {
     note(line);
     return 0;
 }
-int cudaStreamSynchronize(void *st) { (void)st; return 0; }
+int cudaStreamSynchronize(void *st) {
+    note((uintptr_t)st <= 1 ? "wait for the default stream" : "wait for another stream");   /* (1: cudaStreamLegacy) */
+    return 0;
+}

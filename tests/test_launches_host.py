@@ -74,3 +74,15 @@ def test_a_selection_that_was_cut_short_leaves_no_counts(fake):
 """)
     assert got == ["0 ['launch', 'launch']", "-5 ['launch', 'failed-launch', 'memset'] memset 0 512 on 77",
                    "-5 ['launch', 'memset'] memset 0 512 on 77", "0 ['launch', 'launch']"]
+
+
+def test_new_scratch_is_ready_for_every_stream(fake):
+    """What is set when a handle is made is queued on the default stream, which other streams do not wait for: the call
+    ends when it is done."""
+    got = lines(fake, """
+        h = C.c_void_p()
+        for make in (lambda: lib.wg_beam_create(30000, 4, 8, 8, C.byref(h)), lambda: lib.wg_kv_pool_create(100, 16, 4, C.byref(h))):
+            fake.fake_reset(-1)
+            print(make(), "memset on the default stream" in log(), log()[-1])
+    """)
+    assert got == ["0 True wait for the default stream"] * 2
