@@ -19,11 +19,14 @@ struct NvtxRange {
 inline thread_local int32_t g_last_cuda_error = 0;
 inline std::atomic<int64_t> g_launches{0};
 
+// The runtime keeps an error until it is asked for: taken here, so that the next launch, of this library or of
+// anybody else in the process, does not find it.
 #define WG_CUDA(expr)                                   \
     do {                                                \
         cudaError_t e__ = (expr);                       \
         if (e__ != cudaSuccess) {                       \
             g_last_cuda_error = (int32_t)e__;           \
+            cudaGetLastError();                         \
             return WG_ERR_CUDA;                         \
         }                                               \
     } while (0)

@@ -10,23 +10,26 @@ typedef struct { dim3_ grid, block; size_t smem; void *stream; void *attrs; unsi
 
 static char text[1 << 16];
 static size_t used;
-static int launches, failing = -1, stale = -1;
+static int launches, failing = -1, stale = -1, mallocs, no_room = -1, last;
 
 static void note(const char *line) {
     if (used + strlen(line) + 2 < sizeof text) used += (size_t)sprintf(text + used, "%s\n", line);
 }
 
 const char *fake_log(void) { return text; }
-void fake_reset(int fail_launch) { text[0] = 0; used = 0; launches = 0; failing = fail_launch; stale = -1; }
+void fake_reset(int fail_launch) { text[0] = 0; used = 0; launches = 0; failing = fail_launch; stale = -1; mallocs = last = 0; no_room = -1; }
 /* after the n-th launch an error of somebody else's is found */
 void fake_stale_error(int after_launch) { stale = after_launch; }
+
+/* the n-th allocation from now on finds no memory; errors are kept until they are asked for, as the runtime keeps them */
+void fake_no_room(int allocation) { mallocs = 0; no_room = allocation; }
 
 static int launch(dim3_ g) {
     char line[96];
     const int fails = launches++ == failing;
     snprintf(line, sizeof line, "%s %u %u %u", fails ? "failed-launch" : "launch", g.x, g.y, g.z);
     note(line);
-    return fails ? 701 : 0;
+    return fails ? last = 701 : 0;
 }
 
 int cudaLaunchKernelExC(const config_ *c, const void *f, void **args) { (void)f; (void)args; return launch(c->grid); }
@@ -35,10 +38,17 @@ int cudaLaunchKernel(const void *f, dim3_ g, dim3_ b, void **args, size_t smem, 
     return launch(g);
 }
 int cudaFuncSetAttribute(const void *f, int attr, int value) { (void)f; (void)attr; (void)value; return 0; }
-int cudaGetLastError(void) { return launches - 1 == stale ? 9 : 0; }
+int cudaGetLastError(void) {
+    const int e = launches - 1 == stale ? 9 : last;
+    last = 0;
+    return e;
+}
 int cudaGetDevice(int *d) { *d = 0; return 0; }
 int cudaDeviceGetAttribute(int *v, int attr, int d) { (void)attr; (void)d; *v = 148; return 0; }
-int cudaMalloc(void **p, size_t n) { *p = aligned_alloc(256, (n + 255) / 256 * 256); return *p ? 0 : 2; }
+int cudaMalloc(void **p, size_t n) {
+    *p = mallocs++ == no_room ? NULL : aligned_alloc(256, (n + 255) / 256 * 256);
+    return *p ? 0 : (last = 2);
+}
 int cudaFree(void *p) { free(p); return 0; }
 int cudaMemset(void *p, int v, size_t n) {
     memset(p, v, n);

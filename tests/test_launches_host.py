@@ -86,3 +86,23 @@ def test_new_scratch_is_ready_for_every_stream(fake):
             print(make(), "memset on the default stream" in log(), log()[-1])
     """)
     assert got == ["0 True wait for the default stream"] * 2
+
+
+@pytest.mark.parametrize("allocation", [0, 1, 2])
+def test_a_failed_call_leaves_no_error_to_the_next(fake, allocation):
+    """No memory for a handle: that call fails, and the next one, on another handle, does not."""
+    got = lines(fake, SELECT + f"""
+    other = C.c_void_p()
+    fake.fake_reset(-1)
+    fake.fake_no_room({allocation})
+    print(lib.wg_beam_create(500, 4, 8, 8, C.byref(other)), other.value, lib.wg_last_cuda_error())
+    print(select())
+    fake.fake_no_room({allocation})
+    print(lib.wg_kv_pool_create(100, 16, 4, C.byref(other)), other.value, lib.wg_last_cuda_error())
+    print(lib.wg_kv_pool_create(100, 16, 4, C.byref(other)), select())
+    fake.fake_reset(1)
+    print(select(), lib.wg_last_cuda_error())
+    fake.fake_reset(-1)
+    print(select())
+""")
+    assert got == ["-5 None 2", "0", "-5 None 2", "0 0", "-5 701", "0"]
