@@ -302,9 +302,10 @@ __device__ __forceinline__ float log_sum(float m, float s) { return m + logf(s);
 // waits for another (blocks that took eight steps together: 40 us instead of 37 on 512 misaligned rows
 // x 151937 summed whole).
 //
-// Measured with the pick behind it: 47.5 us for 1024 rows x 128256 bf16 (229 MB; the scan itself about
+// Measured with the pick behind it: 47.2 us for 1024 rows x 128256 bf16 (229 MB; the scan itself about
 // 43, 5.3 TB/s), 37 us for 512 x 151937 (136 MB), 18 us for 128 x 256000 fp32 of which most are in
-// literals, 8.4 us for 32 rows in literals.  What bounds it: 570 instructions a step (250 of them the
+// literals, 8.4 us for 32 rows in literals.  What bounds it: 490 instructions a step (the mean over the first
+// case's rows, a fifth of which count nothing; about 600 in a step that counts, 250 of them the
 // exponentials, 70 the mask) in 32 warps per SM, beside the memory; without exponentials and masks the
 // same walk streams at the memory's rate.  More loads in flight did not help where it cost registers or
 // instructions: rings in shared memory 53 to 60 us, loads a turn ahead at 80 registers 59, three blocks
