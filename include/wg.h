@@ -68,6 +68,7 @@ typedef enum wg_status {
 
 /* Logit element types of wg_apply_mask / wg_decode_step. */
 enum { WG_DTYPE_BF16 = 0, WG_DTYPE_FP32 = 1 };
+#define WG_DTYPE_FP16 2 /* wg_kv_write, wg_kv_read and wg_kv_attend only */
 
 /* Flags of wg_build_masks and wg_decode_step. */
 enum {
@@ -668,6 +669,125 @@ int32_t wg_kv_reorder(wg_kv_pool *pool, int32_t *table, int64_t table_stride, in
                       int32_t *len, const int32_t *parent, int32_t n_req, int32_t n_beam,
                       const wg_kv_plane *planes, int32_t n_planes, int32_t *copy_src,
                       int32_t *copy_dst, int32_t *status, void *stream);
+
+/* ---- what a paged cache holds --------------------------------------------------------- *
+ * Block tables say where a token's keys and values are; these calls put them there, read them back and attend to
+ * them.  A cache is two planes of n_blocks x block_size x n_heads x head_dim elements, in 8 bits with two planes
+ * of scales, n_blocks x block_size x n_heads, beside them: all of the form that wg_kv_reorder copies.  Slot
+ * s = block * block_size + token, as wg_kv_extend returns it, is row s of each plane.
+ *
+ * 8-bit vectors.  The n_heads vectors of a token are quantised one by one.  With `top` the largest magnitude in a
+ * vector x and C the type's largest value (448, 127): scale = top / C and code[i] = x[i] * (C / top) rounded to the
+ * nearest value of the type, ties to even, all in fp32; the value held is code * scale.  A vector whose `top` is below
+ * 2^-100 is held as zeros with scale 1.  A vector with an infinity or a NaN has scale NaN and reads back as
+ * NaN.  Scales that a caller writes himself are >= 0 or NaN. */
+enum {
+    WG_KV_BF16 = 0,
+    WG_KV_FP16 = 1,
+    WG_KV_E4M3 = 2, /* 8-bit floats: 4 exponent bits, 3 fraction bits, largest value 448 */
+    WG_KV_INT8 = 3  /* -127 .. 127 */
+};
+#define WG_KV_MAX_HEAD_DIM 256
+typedef struct wg_kv_cache {
+    void *k, *v;              /* device, 16-byte aligned */
+    float *k_scale, *v_scale; /* device; NULL for the 16-bit types */
+    int32_t storage;          /* WG_KV_* */
+    int32_t n_blocks, block_size;
+    int32_t n_heads;          /* heads of the keys and values */
+    int32_t head_dim;         /* a multiple of 16, at most WG_KV_MAX_HEAD_DIM */
+} wg_kv_cache;
+
+/* Rotary positions.  The first rot_dim dimensions of a vector form pairs, (i, i + rot_dim / 2) or, interleaved,
+ * (2 i, 2 i + 1); at position p pair i = (a, b) becomes (a cos - b sin, b cos + a sin) of the angle p * freq[i].  The
+ * angles are taken from a table. */
+typedef struct wg_rope {
+    const float *table; /* device: n_pos rows of rot_dim floats, rot_dim / 2 cosines, then as many sines; 16-byte aligned */
+    int32_t n_pos;
+    int32_t rot_dim;    /* a multiple of 16, at most head_dim */
+    int32_t interleaved;
+} wg_rope;
+
+/* freq[i] = base^(-2 i / rot_dim), host, rot_dim / 2 entries, scaled for contexts longer than the model was trained on:
+ *   factor 1         as they are
+ *   original 0       freq / factor (all positions are interpolated)
+ *   original > 0     by how often a pair turns within `original` positions, n = original * freq / (2 pi): pairs with
+ *                    n >= high keep their frequency, those with n <= low get freq / factor, and between them
+ *                    freq * (w + (1 - w) / factor) with w = (n - low) / (high - low)
+ * Errors: WG_ERR_ARG (rot_dim no positive even number up to WG_KV_MAX_HEAD_DIM; base or factor not above 0 or not finite;
+ * original < 0; original > 0 without 0 <= low < high). */
+int32_t wg_rope_frequencies(int32_t rot_dim, double base, double factor, double original, double low, double high,
+                            double *freq);
+/* The table of n_pos positions: cosines and sines of p * freq[i] in fp64, times `magnitude`, rounded to fp32.
+ *   freq  host, n_freq entries, read during the call;  table  device, n_pos rows of 2 n_freq floats
+ * Errors: WG_ERR_ARG (n_freq outside 1 .. WG_KV_MAX_HEAD_DIM / 2, n_pos < 1), WG_ERR_CUDA. */
+int32_t wg_rope_table(const double *freq, int32_t n_freq, int32_t n_pos, double magnitude, float *table, void *stream);
+
+/* A step's tokens into the cache: token t's keys, rotated by pos[t], and values go to slot[t]; its queries, rotated,
+ * to q_out.  One rounding from the rotated value (fp32, every product rounded) to what is held.
+ *   k, v     device, n_tokens rows of n_heads x head_dim elements, k_stride / v_stride elements apart
+ *   q        device, n_tokens rows of n_q_heads x head_dim, or NULL (n_q_heads then 0); q_out may be q itself
+ *            (with the same stride) but may not overlap it otherwise
+ *   dtype    WG_DTYPE_BF16 or WG_DTYPE_FP16, of q, k, v and q_out; a 16-bit cache has the same type
+ *   rope     host struct, or NULL: nothing is rotated (pos is not looked at; q and q_out must be NULL)
+ *   slot     device, n_tokens; -1: nothing is written for the token.  The slots of a call differ from each other.
+ *   pos      device, n_tokens
+ *   status   device, n_tokens, or NULL: WG_OK; WG_ERR_ARG for a slot outside the cache (other than -1) or a position
+ *            outside the table, for which nothing is written either
+ * All pointers and strides are multiples of 16 bytes (slot, pos and status: of their elements).  n_tokens = 0 does nothing.
+ * Errors: WG_ERR_ARG, WG_ERR_CUDA. */
+int32_t wg_kv_write(const wg_kv_cache *cache, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                    const void *q, int64_t q_stride, void *q_out, int64_t q_out_stride, int32_t n_q_heads, int32_t dtype,
+                    const wg_rope *rope, const int64_t *slot, const int32_t *pos, int32_t n_tokens, int32_t *status,
+                    void *stream);
+
+/* Sequences read back, dense: position p of sequence s goes to row cu[s] + p of k_out and v_out, for all p < len[s].
+ *   table, len    as in wg_kv_extend
+ *   cu            device, n_seq + 1, non-decreasing, cu[s + 1] - cu[s] = len[s] (rows between cu[s] + len[s] and cu[s + 1]
+ *                 are left as they were; so are those from cu[n_seq] on)
+ *   k_out, v_out  device, n_rows rows of n_heads x head_dim elements without gaps, 16-byte aligned; either may be NULL
+ *   dtype         WG_DTYPE_BF16, WG_DTYPE_FP16 or WG_DTYPE_FP32; one rounding from the value held
+ * A position whose table entry is no block of the cache reads as zeros.
+ * Errors: WG_ERR_ARG, WG_ERR_CUDA. */
+int32_t wg_kv_read(const wg_kv_cache *cache, const int32_t *table, int64_t table_stride, int32_t max_blocks,
+                   const int32_t *len, int32_t n_seq, const int32_t *cu, void *k_out, void *v_out, int32_t dtype,
+                   int32_t n_rows, void *stream);
+
+/* Attention of a step's tokens to their sequences, keys and values from the cache.  Token t of sequence s at position p sees
+ * the positions up to and including p, with window > 0 only the last `window` of them.  For each of its heads h, with
+ * g = h / (n_q_heads / n_heads) and k[i], v[i] the values that the cache holds for head g at position i:
+ *   x[i] = scale * (q . k[i]);  lse = log sum of exp(x[i]);  out = sum of exp(x[i] - lse) v[i]
+ * in fp32, one rounding at the end; the weights exp(x[i] - max) enter the second product in the cache's 16-bit type (8-bit
+ * caches: fp16).  Positions whose table entry is no block of the cache are passed over.  A token that sees nothing (no
+ * row, all passed over, or all scores -inf) has out = 0, lse = -inf; a NaN or +inf among its scores makes them NaN.
+ * Nothing that a token does not see has an effect on it, NaN included.
+ *
+ * The work is dealt out evenly over the GPU by the lengths as they are, each long row to several blocks; the last of them to
+ * finish joins their parts, in the order of positions, so results do not depend on the order in which blocks run.
+ *
+ * A wg_attend is scratch for up to max_tokens tokens a call; calls that share one are issued like calls that share a
+ * wg_ctx: one at a time, on one stream or on streams ordered by events (recorded calls too).
+ *   q, out     device, n_tokens rows of n_q_heads x head_dim elements, q_stride / out_stride elements apart (16-byte
+ *              multiples); out may be q itself
+ *   dtype      WG_DTYPE_BF16 or WG_DTYPE_FP16, of q and out; a 16-bit cache has the same type
+ *   lse        device, n_tokens x n_q_heads, or NULL
+ *   n_q_heads  a multiple of the cache's n_heads
+ *   table, len, n_seq   as in wg_kv_extend, the step's tokens included in len
+ *   seq, pos, slot      device, n_tokens each, as wg_kv_extend returned them (a token with slot -1 has no row); or all
+ *              NULL: one token per sequence, n_tokens <= n_seq, token t is the last one of sequence t.  A sequence or
+ *              position outside the table makes a token without a row, too.
+ *   window     0: everything
+ *   group      tokens t = i * group .. i * group + group - 1 are looked at together (1 .. WG_BEAM_MAX_BEAMS): what their
+ *              tables have in common from the first position on (a request's beams, the drafted tokens of a sequence) is
+ *              read once for all of them.  Results are the same up to rounding.  With a window nothing is shared.
+ * Errors: WG_ERR_ARG, WG_ERR_CUDA. */
+typedef struct wg_attend wg_attend;
+int32_t wg_attend_create(int32_t max_tokens, int32_t n_q_heads, int32_t n_heads, int32_t head_dim, wg_attend **out);
+void wg_attend_free(wg_attend *attend);
+int32_t wg_kv_attend(wg_attend *attend, const wg_kv_cache *cache, const void *q, int64_t q_stride, void *out,
+                     int64_t out_stride, float *lse, int32_t dtype, int32_t n_q_heads, const int32_t *table,
+                     int64_t table_stride, int32_t max_blocks, const int32_t *len, int32_t n_seq, const int32_t *seq,
+                     const int32_t *pos, const int64_t *slot, int32_t n_tokens, float scale, int32_t window, int32_t group,
+                     void *stream);
 
 /* ---- diagnostics ------------------------------------------------------------------- */
 

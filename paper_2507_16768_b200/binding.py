@@ -27,6 +27,12 @@ WG_ERR_STATE = -7
 
 WG_DTYPE_BF16 = 0
 WG_DTYPE_FP32 = 1
+WG_DTYPE_FP16 = 2
+WG_KV_BF16 = 0
+WG_KV_FP16 = 1
+WG_KV_E4M3 = 2
+WG_KV_INT8 = 3
+WG_KV_MAX_HEAD_DIM = 256
 WG_USE_CACHE = 0
 WG_NO_CACHE = 1
 WG_RESTART_ON_DONE = 2
@@ -55,6 +61,15 @@ class WgStats(C.Structure):
 
     def as_dict(self):
         return {n: int(getattr(self, n)) for n, _ in self._fields_}
+
+
+class _WgKvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)] + \
+        [(n, C.c_int32) for n in ("storage", "n_blocks", "block_size", "n_heads", "head_dim")]
+
+
+class _WgRope(C.Structure):
+    _fields_ = [("table", C.c_void_p)] + [(n, C.c_int32) for n in ("n_pos", "rot_dim", "interleaved")]
 
 
 _vp, _i32, _i64, _u32 = C.c_void_p, C.c_int32, C.c_int64, C.c_uint32
@@ -124,6 +139,14 @@ _SIGNATURES = {
     "wg_kv_extend": (_i32, [_vp, _vp, _i64, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _i32, _vp, _vp]),
     "wg_kv_shrink": (_i32, [_vp, _vp, _i64, _i32, _vp, _vp, _i32, _vp, _vp]),
     "wg_kv_reorder": (_i32, [_vp, _vp, _i64, _i32, _vp, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _vp]),
+    "wg_rope_frequencies": (_i32, [_i32] + [C.c_double] * 5 + [_vp]),
+    "wg_rope_table": (_i32, [_vp, _i32, _i32, C.c_double, _vp, _vp]),
+    "wg_kv_write": (_i32, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _i32, _vp, _vp]),
+    "wg_kv_read": (_i32, [_vp, _vp, _i64, _i32, _vp, _i32, _vp, _vp, _vp, _i32, _i32, _vp]),
+    "wg_attend_create": (_i32, [_i32, _i32, _i32, _i32, C.POINTER(_vp)]),
+    "wg_attend_free": (None, [_vp]),
+    "wg_kv_attend": (_i32, [_vp, _vp, _vp, _i64, _vp, _i64, _vp, _i32, _i32, _vp, _i64, _i32, _vp, _i32, _vp, _vp, _vp, _i32,
+                            C.c_float, _i32, _i32, _vp]),
     "wg_ctx_set_timing": (_i32, [_vp, _i32]),
     "wg_ctx_get_timing": (_i32, [_vp, C.POINTER(C.c_double), C.POINTER(C.c_double),
                                  C.POINTER(_i64)]),
@@ -1001,3 +1024,239 @@ class KvTables:
                                 _on_stream(stream, self.device))
         if rc != WG_OK:
             raise WgError(rc, "wg_kv_reorder")
+
+
+# ---- what a paged cache holds --------------------------------------------------------------------
+class Rope:
+    """The cosines and sines of rotary positions 0 .. n_pos - 1 (wg_rope_table), on the current device; ready for every
+    stream when the constructor returns.
+
+    The first ``rot_dim`` dimensions of a head are rotated in pairs (i, i + rot_dim / 2), or (2i, 2i + 1) if
+    ``interleaved``.  For contexts longer than the model was trained on, ``factor`` slows the rotation down: all of it,
+    or, with ``original`` (the positions trained on), ``low`` and ``high``, only that of pairs that turn less than ``high`` times
+    within ``original`` positions (those below ``low`` in full).  ``magnitude`` multiplies what is rotated."""
+
+    def __init__(self, n_pos: int, rot_dim: int, base: float = 10000.0, interleaved: bool = False, factor: float = 1.0,
+                 low: float = 0.0, high: float = 0.0, original: float = 0.0, magnitude: float = 1.0):
+        import torch
+        self.n_pos, self.rot_dim, self.interleaved = int(n_pos), int(rot_dim), bool(interleaved)
+        if self.rot_dim < 16 or self.rot_dim % 16:
+            raise ValueError(f"rot_dim must be a multiple of 16, not {rot_dim}")
+        if self.n_pos < 1:
+            raise ValueError(f"{n_pos} positions")
+        freq = np.zeros(self.rot_dim // 2, np.float64)
+        if self.rot_dim > WG_KV_MAX_HEAD_DIM:
+            raise ValueError(f"rot_dim is at most {WG_KV_MAX_HEAD_DIM}")
+        _check(_lib.wg_rope_frequencies(self.rot_dim, float(base), float(factor), float(original), float(low), float(high),
+                                        _np_ptr(freq)), "wg_rope_frequencies")
+        self.frequencies = freq
+        self.device = torch.cuda.current_device()
+        self.table = torch.empty((self.n_pos, self.rot_dim), dtype=torch.float32, device=f"cuda:{self.device}")
+        _check(_lib.wg_rope_table(_np_ptr(freq), self.rot_dim // 2, self.n_pos, float(magnitude),
+                                  _dev_ptr(self.table), _stream_ptr(None)), "wg_rope_table")
+        torch.cuda.current_stream().synchronize()
+        self._struct = _WgRope(self.table.data_ptr(), self.n_pos, self.rot_dim, int(self.interleaved))
+        self._arg = C.addressof(self._struct)
+
+
+def _model_dtype(t, what: str) -> int:
+    import torch
+    if t.dtype is torch.bfloat16:
+        return WG_DTYPE_BF16
+    if t.dtype is torch.float16:
+        return WG_DTYPE_FP16
+    raise TypeError(f"{what} must be bfloat16 or float16, not {t.dtype}")
+
+
+def _heads(t, n: int, heads: int, dim: int, dtype, device: int, what: str):
+    """(pointer, elements from token to token) of a [n, heads, dim] array whose tokens are whole: 16-byte aligned rows
+    of heads * dim elements without gaps, any distance apart."""
+    if not t.is_cuda or t.dtype is not dtype:
+        raise TypeError(f"{what} must be a CUDA tensor of {dtype}")
+    if tuple(t.shape) != (n, heads, dim):
+        raise ValueError(f"{what} must be [{n}, {heads}, {dim}], not {list(t.shape)}")
+    if t.device.index != device:
+        raise ValueError(f"{what} lives on cuda:{t.device.index}, the cache on cuda:{device}")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+        raise ValueError(f"the heads of a token of {what} must follow each other without gaps")
+    p, stride = t.data_ptr(), t.stride(0) if n > 1 else heads * dim
+    if p & 15 or stride & 7 or stride < heads * dim:
+        raise ValueError(f"the tokens of {what} must begin at multiples of 16 bytes and not overlap")
+    return p, stride
+
+
+class KvCache:
+    """wg_kv_cache: keys and values, ``[n_blocks, block_size, n_heads, head_dim]`` contiguous CUDA tensors of bfloat16,
+    float16, float8_e4m3fn or int8, the last two with float32 scales ``[n_blocks, block_size, n_heads]``.
+
+    The tensors are kept and must stay where they are.  ``planes`` are the same arrays for ``KvTables.reorder``."""
+
+    def __init__(self, keys, values, key_scale=None, value_scale=None):
+        import torch
+        storages = {torch.bfloat16: WG_KV_BF16, torch.float16: WG_KV_FP16, torch.float8_e4m3fn: WG_KV_E4M3, torch.int8: WG_KV_INT8}
+        if keys.dtype not in storages or values.dtype is not keys.dtype:
+            raise TypeError("keys and values must both be bfloat16, float16, float8_e4m3fn or int8")
+        if keys.dim() != 4 or tuple(values.shape) != tuple(keys.shape):
+            raise ValueError("keys and values must both be [n_blocks, block_size, n_heads, head_dim]")
+        self.n_blocks, self.block_size, self.n_heads, self.head_dim = (int(n) for n in keys.shape)
+        if self.head_dim < 16 or self.head_dim % 16 or self.head_dim > WG_KV_MAX_HEAD_DIM:
+            raise ValueError(f"head_dim must be a multiple of 16 up to {WG_KV_MAX_HEAD_DIM}, not {self.head_dim}")
+        if min(self.n_blocks, self.block_size, self.n_heads) < 1:
+            raise ValueError("an empty cache")
+        self.storage, self.dtype = storages[keys.dtype], keys.dtype
+        narrow = self.storage >= WG_KV_E4M3
+        if (key_scale is not None) != narrow or (value_scale is not None) != narrow:
+            raise ValueError("8-bit caches, and no others, have key_scale and value_scale")
+        self.device = keys.device.index
+        for t, what in ((keys, "keys"), (values, "values"), (key_scale, "key_scale"), (value_scale, "value_scale")):
+            if t is None:
+                continue
+            if not t.is_cuda or t.device.index != self.device or not t.is_contiguous() or t.data_ptr() & 15:
+                raise ValueError(f"{what} must be contiguous, 16-byte aligned, and on the keys' CUDA device")
+            if what.endswith("scale") and (t.dtype is not torch.float32 or tuple(t.shape) != tuple(keys.shape[:3])):
+                raise ValueError(f"{what} must be float32 [n_blocks, block_size, n_heads]")
+        self.keys, self.values, self.key_scale, self.value_scale = keys, values, key_scale, value_scale
+        ptr = [None if t is None else t.data_ptr() for t in (keys, values, key_scale, value_scale)]
+        self._struct = _WgKvCache(*ptr, self.storage, self.n_blocks, self.block_size, self.n_heads, self.head_dim)
+        self._arg = C.addressof(self._struct)
+        self._planes = None
+
+    @classmethod
+    def empty(cls, n_blocks: int, block_size: int, n_heads: int, head_dim: int, dtype) -> "KvCache":
+        """A cache of zeros on the current device."""
+        import torch
+        shape = (int(n_blocks), int(block_size), int(n_heads), int(head_dim))
+        planes = [torch.zeros(shape, dtype=dtype, device="cuda") for _ in range(2)]
+        if dtype in (torch.float8_e4m3fn, torch.int8):
+            planes += [torch.ones(shape[:3], dtype=torch.float32, device="cuda") for _ in range(2)]
+        return cls(*planes)
+
+    @property
+    def planes(self) -> "KvPlanes":
+        if self._planes is None:
+            self._planes = KvPlanes([t for t in (self.keys, self.values, self.key_scale, self.value_scale) if t is not None],
+                                    self.block_size)
+        return self._planes
+
+    def write(self, k, v, slots: SlotMap, rope: Optional[Rope] = None, q=None, q_out=None, status=None, stream=None) -> None:
+        """wg_kv_write: the tokens of ``slots`` into the cache.  ``k``, ``v`` are ``[n_tokens, n_heads, head_dim]`` (views into
+        a fused projection will do), ``q`` and ``q_out`` ``[n_tokens, query heads, head_dim]``; without ``q_out`` the queries
+        are rotated in place.  ``status`` [n_tokens] gets WG_ERR_ARG for slots outside the cache and positions outside ``rope``."""
+        import torch
+        n, dev, dtype = slots.n_tokens, self.device, k.dtype
+        kind = _model_dtype(k, "k")
+        if self.storage <= WG_KV_FP16 and dtype is not self.dtype:
+            raise TypeError(f"k is {dtype}, the cache holds {self.dtype}")
+        if slots.device != dev:
+            raise ValueError(f"slots live on cuda:{slots.device}, the cache on cuda:{dev}")
+        kp, ks = _heads(k, n, self.n_heads, self.head_dim, dtype, dev, "k")
+        vp, vs = _heads(v, n, self.n_heads, self.head_dim, dtype, dev, "v")
+        qp = qs = op = os_ = None
+        heads = 0
+        if q is not None:
+            if rope is None:
+                raise ValueError("queries are rotated: rope is required with q")
+            heads = int(q.shape[1]) if q.dim() == 3 else 0
+            if heads < 1:
+                raise ValueError("q must be [n_tokens, query heads, head_dim]")
+            qp, qs = _heads(q, n, heads, self.head_dim, dtype, dev, "q")
+            op, os_ = (qp, qs) if q_out is None else _heads(q_out, n, heads, self.head_dim, dtype, dev, "q_out")
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        if rope is not None:
+            if rope.device != dev:
+                raise ValueError(f"rope lives on cuda:{rope.device}, the cache on cuda:{dev}")
+            if rope.rot_dim > self.head_dim:
+                raise ValueError(f"rope rotates {rope.rot_dim} dimensions, a head has {self.head_dim}")
+        st = None if status is None else _vec(status, n, torch.int32, "status", dev)
+        _, slot, pos, _ = slots._args[:4]
+        rc = _lib.wg_kv_write(self._arg, kp, ks, vp, vs, qp, qs or 0, op, os_ or 0, heads, kind,
+                              None if rope is None else rope._arg, slot, pos, n, st, _on_stream(stream, dev))
+        if rc != WG_OK:
+            raise WgError(rc, "wg_kv_write")
+
+    def _check_tables(self, tables: "KvTables") -> None:
+        pool = tables.pool
+        if pool.block_size != self.block_size or pool.n_blocks > self.n_blocks or tables.device != self.device:
+            raise ValueError("tables were made for another cache")
+
+    def read(self, tables: "KvTables", cu, k_out=None, v_out=None, stream=None) -> None:
+        """wg_kv_read: position p of sequence s goes to row ``cu[s] + p`` of ``k_out`` and ``v_out``, contiguous
+        ``[rows, n_heads, head_dim]`` of bfloat16, float16 or float32.  ``cu``: int32 [n_seq + 1], the sums of the lengths."""
+        import torch
+        self._check_tables(tables)
+        outs = [t for t in (k_out, v_out) if t is not None]
+        if not outs:
+            raise ValueError("neither k_out nor v_out")
+        kinds = {torch.bfloat16: WG_DTYPE_BF16, torch.float16: WG_DTYPE_FP16, torch.float32: WG_DTYPE_FP32}
+        dtype, rows, dev = outs[0].dtype, int(outs[0].shape[0]), self.device
+        if dtype not in kinds:
+            raise TypeError(f"outputs must be bfloat16, float16 or float32, not {dtype}")
+        for t in outs:
+            if not t.is_cuda or t.dtype is not dtype or t.device.index != dev or not t.is_contiguous() \
+                    or tuple(t.shape) != (rows, self.n_heads, self.head_dim) or t.data_ptr() & 15:
+                raise ValueError("outputs must be alike: contiguous [rows, n_heads, head_dim], 16-byte aligned, on the cache's device")
+        _, table, stride, max_blocks, lens = tables._head
+        rc = _lib.wg_kv_read(self._arg, table, stride, max_blocks, lens, tables.n_seq,
+                             _vec(cu, tables.n_seq + 1, torch.int32, "cu", dev), None if k_out is None else k_out.data_ptr(),
+                             None if v_out is None else v_out.data_ptr(), kinds[dtype], rows, _on_stream(stream, dev))
+        if rc != WG_OK:
+            raise WgError(rc, "wg_kv_read")
+
+
+class Attend:
+    """wg_attend: scratch of the attention over a paged cache, for up to ``max_tokens`` tokens a call."""
+
+    def __init__(self, max_tokens: int, n_q_heads: int, n_heads: int, head_dim: int):
+        import torch
+        self.max_tokens, self.n_q_heads, self.n_heads, self.head_dim = int(max_tokens), int(n_q_heads), int(n_heads), int(head_dim)
+        self.device = torch.cuda.current_device()
+        self.scale = max(1, self.head_dim) ** -0.5
+        h = _vp()
+        _check(_lib.wg_attend_create(self.max_tokens, self.n_q_heads, self.n_heads, self.head_dim, C.byref(h)), "wg_attend_create")
+        self.handle = h
+
+    def close(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.wg_attend_free(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        self.close()
+
+    def __call__(self, q, cache: KvCache, tables: KvTables, out, slots: Optional[SlotMap] = None, scale: Optional[float] = None,
+                 window: int = 0, group: int = 1, lse=None, stream=None) -> None:
+        """wg_kv_attend: ``q`` and ``out`` are ``[n_tokens, n_q_heads, head_dim]``, ``lse`` float32 ``[n_tokens, n_q_heads]``.
+
+        With ``slots`` (the map that placed the step's tokens) row t is token t of the map; without, row t is the last
+        token of sequence t.  ``scale`` is 1 / sqrt(head_dim) if it is not given.  ``group``: so many neighbouring tokens, the beams of a
+        request or the drafted tokens of a sequence, read what their tables have in common together."""
+        import torch
+        cache._check_tables(tables)
+        dev = self.device
+        if cache.device != dev or cache.n_heads != self.n_heads or cache.head_dim != self.head_dim:
+            raise ValueError("the scratch was made for another device, number of heads or head size")
+        n = tables.n_seq if slots is None else slots.n_tokens
+        if slots is None and q.shape[0] <= n:
+            n = int(q.shape[0])
+        if n > self.max_tokens:
+            raise ValueError(f"{n} tokens, the scratch takes {self.max_tokens}")
+        if slots is not None and (slots.device != dev or slots.n_seq != tables.n_seq):
+            raise ValueError("slots were made for another batch or device")
+        dtype, kind = q.dtype, _model_dtype(q, "q")
+        if cache.storage <= WG_KV_FP16 and dtype is not cache.dtype:
+            raise TypeError(f"q is {dtype}, the cache holds {cache.dtype}")
+        qp, qs = _heads(q, n, self.n_q_heads, self.head_dim, dtype, dev, "q")
+        op, os_ = _heads(out, n, self.n_q_heads, self.head_dim, dtype, dev, "out")
+        if lse is not None:
+            if not lse.is_cuda or lse.dtype is not torch.float32 or tuple(lse.shape) != (n, self.n_q_heads) \
+                    or not lse.is_contiguous() or lse.device.index != dev:
+                raise ValueError(f"lse must be a contiguous float32 tensor [{n}, {self.n_q_heads}] on cuda:{dev}")
+            lse = lse.data_ptr()
+        _, table, stride, max_blocks, lens = tables._head
+        _, slot, pos, seq = (None,) * 4 if slots is None else slots._args[:4]
+        rc = _lib.wg_kv_attend(self.handle, cache._arg, qp, qs, op, os_, lse, kind, self.n_q_heads, table, stride, max_blocks, lens,
+                               tables.n_seq, seq, pos, slot, n, self.scale if scale is None else float(scale), int(window),
+                               int(group), _on_stream(stream, dev))
+        if rc != WG_OK:
+            raise WgError(rc, "wg_kv_attend")

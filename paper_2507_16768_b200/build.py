@@ -9,14 +9,16 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libwg.so")
-SOURCES = ["wg_api.cu", "wg_kv.cu", "wg_lower.cpp", "wg_regex.cpp", "wg_template.cpp"]
+SOURCES = ["wg_api.cu", "wg_kv.cu", "wg_cache.cu", "wg_attend.cu", "wg_attend_bf16.cu", "wg_attend_fp16.cu",
+           "wg_attend_e4m3.cu", "wg_attend_int8.cu", "wg_lower.cpp", "wg_regex.cpp", "wg_template.cpp"]
 HEADERS = [os.path.join(CSRC, "wg_kernels.cuh"), os.path.join(CSRC, "wg_internal.h"),
            os.path.join(CSRC, "wg_host.h"), os.path.join(CSRC, "wg_beam.cuh"),
            os.path.join(CSRC, "wg_beam_api.inl"),
-           os.path.join(CSRC, "wg_divide.cuh"),
+           os.path.join(CSRC, "wg_divide.cuh"), os.path.join(CSRC, "wg_cache.cuh"),
+           os.path.join(CSRC, "wg_attend.cuh"), os.path.join(CSRC, "wg_attend.h"),
            os.path.join(ROOT, "include", "wg.h")]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-              "-Xcompiler", "-fPIC", "-shared", "-cudart", "shared", "-ldl"]
+              "-Xcompiler", "-fPIC", "-shared", "-cudart", "shared", "-ldl", "--threads", "8"]
 
 
 def _nvcc() -> str:

@@ -1,0 +1,114 @@
+// Attention over a paged cache (wg_attend_*, wg_kv_attend of wg.h): scratch, checks and launches.
+#include <new>
+
+#include "wg_attend.h"
+
+struct wg_attend {
+    int32_t max_tokens = 0, n_q_heads = 0, n_heads = 0, head_dim = 0;
+    int32_t *shared = nullptr, *arrived = nullptr;
+    int64_t *units = nullptr;
+    float *parts = nullptr, *shared_rows = nullptr, *private_rows = nullptr;
+};
+
+namespace {
+
+// A row of partial results: the head size as the kernels round it, a maximum and a sum.
+int64_t part_row(int32_t head_dim) { return (head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256) + 4; }
+
+}  // namespace
+
+extern "C" {
+
+int32_t wg_attend_create(int32_t max_tokens, int32_t n_q_heads, int32_t n_heads, int32_t head_dim, wg_attend **out) {
+    NvtxRange nvtx_range("wg_attend_create");
+    if (!out) return WG_ERR_ARG;
+    *out = nullptr;
+    if (max_tokens < 1 || n_heads < 1 || n_heads > 1024 || n_q_heads < n_heads || n_q_heads > 65535 || n_q_heads % n_heads ||
+        head_dim < 16 || head_dim > WG_KV_MAX_HEAD_DIM || head_dim % 16)
+        return WG_ERR_ARG;
+    wg_attend *p = new (std::nothrow) wg_attend();
+    if (!p) return WG_ERR_ARG;
+    p->max_tokens = max_tokens, p->n_q_heads = n_q_heads, p->n_heads = n_heads, p->head_dim = head_dim;
+    const size_t counters = (size_t)max_tokens * n_heads * ((n_q_heads / n_heads + 15) / 16);
+    const size_t rows = (size_t)max_tokens * n_q_heads * part_row(head_dim);
+    const size_t parts = (size_t)sm_count() * 2 * 2 * (16 * ATTEND_SHARED_WARPS) * part_row(head_dim);
+    int32_t rc = dev_alloc(&p->shared, (size_t)MAX_GROUPS);
+    if (rc == WG_OK) rc = dev_alloc(&p->units, (size_t)MAX_GROUPS);
+    if (rc == WG_OK) rc = dev_alloc(&p->arrived, counters);
+    if (rc == WG_OK) rc = dev_alloc(&p->parts, parts);
+    if (rc == WG_OK) rc = dev_alloc(&p->shared_rows, rows);
+    if (rc == WG_OK) rc = dev_alloc(&p->private_rows, rows);
+    // (the memory is set on the default stream, which other streams do not wait for)
+    if (rc == WG_OK && (cudaMemset(p->arrived, 0, counters * sizeof(int32_t)) != cudaSuccess ||
+                        cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess)) {
+        g_last_cuda_error = (int32_t)cudaGetLastError();
+        rc = WG_ERR_CUDA;
+    }
+    if (rc != WG_OK) {
+        wg_attend_free(p);
+        return rc;
+    }
+    *out = p;
+    return WG_OK;
+}
+
+void wg_attend_free(wg_attend *p) {
+    if (!p) return;
+    for (void *q : {(void *)p->shared, (void *)p->units, (void *)p->arrived, (void *)p->parts, (void *)p->shared_rows, (void *)p->private_rows})
+        cudaFree(q);
+    delete p;
+}
+
+int32_t wg_kv_attend(wg_attend *attend, const wg_kv_cache *cache, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                     float *lse, int32_t dtype, int32_t n_q_heads, const int32_t *table, int64_t table_stride, int32_t max_blocks,
+                     const int32_t *len, int32_t n_seq, const int32_t *seq, const int32_t *pos, const int64_t *slot,
+                     int32_t n_tokens, float scale, int32_t window, int32_t group, void *stream) {
+    NvtxRange nvtx_range("wg_kv_attend");
+    if (!attend || !cache_ok(cache) || n_tokens < 0 || n_tokens > attend->max_tokens) return WG_ERR_ARG;
+    if (dtype != WG_DTYPE_BF16 && dtype != WG_DTYPE_FP16) return WG_ERR_ARG;
+    if (cache->storage <= WG_KV_FP16 && (cache->storage == WG_KV_FP16) != (dtype == WG_DTYPE_FP16)) return WG_ERR_ARG;
+    if (n_q_heads != attend->n_q_heads || cache->n_heads != attend->n_heads || cache->head_dim != attend->head_dim) return WG_ERR_ARG;
+    if (!table || max_blocks < 1 || table_stride < max_blocks || n_seq < 1) return WG_ERR_ARG;
+    const bool mapped = seq != nullptr;
+    if (mapped != (pos != nullptr) || mapped != (slot != nullptr) || (!mapped && (!len || n_tokens > n_seq))) return WG_ERR_ARG;
+    if (window < 0 || group < 1 || group > WG_BEAM_MAX_BEAMS) return WG_ERR_ARG;
+    if (n_tokens == 0) return WG_OK;
+    const int64_t width = (int64_t)n_q_heads * cache->head_dim;
+    if (!rows_ok(q, q_stride, width) || !rows_ok(out, out_stride, width)) return WG_ERR_ARG;
+    const CacheDev c = cache_dev(cache);
+    const int32_t rows = n_q_heads / cache->n_heads, row_blocks = (rows + 15) / 16;
+    const int64_t room = (int64_t)max_blocks * cache->block_size, most_tokens = room < (1ll << 31) ? room : 1ll << 31;
+    const int64_t per_token = (most_tokens + UNIT_TOKENS - 1) / UNIT_TOKENS * row_blocks * cache->n_heads;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    for (int64_t t0 = 0; t0 < n_tokens; t0 += (int64_t)MAX_GROUPS * group) {
+        AttendArgs a{};
+        a.n_tokens = (int32_t)(n_tokens - t0 < (int64_t)MAX_GROUPS * group ? n_tokens - t0 : (int64_t)MAX_GROUPS * group);
+        a.q = static_cast<const uint16_t *>(q) + t0 * q_stride, a.q_stride = q_stride;
+        a.out = static_cast<uint16_t *>(out) + t0 * out_stride, a.out_stride = out_stride;
+        a.lse = lse ? lse + t0 * n_q_heads : nullptr;
+        a.table = table, a.stride = table_stride, a.max_blocks = max_blocks, a.n_seq = n_seq;
+        if (mapped) {
+            a.seq = seq + t0, a.pos = pos + t0, a.slot = slot + t0;
+        } else {
+            a.table += t0 * table_stride, a.len = len + t0, a.n_seq -= (int32_t)t0;
+        }
+        a.window = window, a.n_q_heads = n_q_heads, a.rows = rows, a.row_blocks = row_blocks;
+        a.group = group, a.n_groups = (a.n_tokens + group - 1) / group;
+        a.q_bf16 = dtype == WG_DTYPE_BF16;
+        a.scale = scale * 1.44269504088896f;
+        a.shared = attend->shared, a.units = attend->units, a.arrived = attend->arrived;
+        a.parts = attend->parts, a.shared_rows = attend->shared_rows, a.private_rows = attend->private_rows;
+        const int64_t most = per_token * a.n_tokens;
+        int32_t rc;
+        switch (cache->storage) {
+            case WG_KV_BF16: rc = attend_bf16(c, a, most, st); break;
+            case WG_KV_FP16: rc = attend_fp16(c, a, most, st); break;
+            case WG_KV_E4M3: rc = attend_e4m3(c, a, most, st); break;
+            default: rc = attend_int8(c, a, most, st); break;
+        }
+        if (rc != WG_OK) return rc;
+    }
+    return WG_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,72 @@
+// What the kernels on a cache's contents share: element types, 8-bit codes, the cache as a kernel sees it.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <cstdint>
+
+#include "wg.h"
+#include "wg_divide.cuh"
+
+struct CacheDev {
+    char *k, *v;
+    float *k_scale, *v_scale;
+    int32_t n_blocks, n_heads, head_dim;
+    Divisor block;        // tokens of a block
+};
+
+// A cache whose sizes and pointers the kernels can work with.
+inline bool cache_ok(const wg_kv_cache *c) {
+    if (!c || !c->k || !c->v || c->storage < WG_KV_BF16 || c->storage > WG_KV_INT8) return false;
+    const bool narrow = c->storage >= WG_KV_E4M3;
+    if (narrow != (c->k_scale != nullptr) || narrow != (c->v_scale != nullptr)) return false;
+    if (c->n_blocks < 1 || c->n_blocks > (1 << 30) || c->block_size < 1 || c->block_size > (1 << 30)) return false;
+    if (c->n_heads < 1 || c->n_heads > 1024 || c->head_dim < 16 || c->head_dim > WG_KV_MAX_HEAD_DIM || c->head_dim % 16) return false;
+    return (((uintptr_t)c->k | (uintptr_t)c->v) & 15) == 0 && (((uintptr_t)c->k_scale | (uintptr_t)c->v_scale) & 3) == 0;
+}
+
+inline CacheDev cache_dev(const wg_kv_cache *c) {
+    return {static_cast<char *>(c->k), static_cast<char *>(c->v), c->k_scale, c->v_scale, c->n_blocks, c->n_heads, c->head_dim,
+            Divisor::of((uint32_t)c->block_size)};
+}
+
+// Rows of 16-bit elements that are read and written 16 bytes at a time.
+inline bool rows_ok(const void *p, int64_t stride, int64_t width) {
+    return p && ((uintptr_t)p & 15) == 0 && stride >= width && stride % 8 == 0;
+}
+
+__device__ __forceinline__ float2 unpack(uint32_t w, __nv_bfloat16) {
+    return {__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)};
+}
+__device__ __forceinline__ float2 unpack(uint32_t w, __half) { return __half22float2(*reinterpret_cast<__half2 *>(&w)); }
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack(float a, float b);
+template <>
+__device__ __forceinline__ uint32_t pack<__nv_bfloat16>(float a, float b) {
+    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&x);
+}
+template <>
+__device__ __forceinline__ uint32_t pack<__half>(float a, float b) {
+    const __half2 x = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&x);
+}
+
+struct E4m3 {};
+struct Int8 {};
+
+// Two neighbouring codes of a word as a pair of fp16 (exact for both types).  `pair`: 0 or 1.
+__device__ __forceinline__ uint32_t codes_to_half2(uint32_t w, int pair, E4m3) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(pair ? w >> 16 : w & 0xFFFFu), __NV_E4M3);
+    return (uint32_t)h.x | ((uint32_t)h.y << 16);
+}
+__device__ __forceinline__ uint32_t codes_to_half2(uint32_t w, int pair, Int8) {
+    // 0x6400 + u is 1024 + u in fp16 for a byte u = code + 128
+    const uint32_t u = __byte_perm(w ^ 0x80808080u, 0x64646464u, pair ? 0x4342 : 0x4140);
+    const uint32_t bias = 0x64806480u;    // 1024 + 128
+    const __half2 x = __hsub2(*reinterpret_cast<const __half2 *>(&u), *reinterpret_cast<const __half2 *>(&bias));
+    return *reinterpret_cast<const uint32_t *>(&x);
+}
