@@ -692,7 +692,7 @@ typedef struct wg_kv_cache {
     void *k, *v;              /* device, 16-byte aligned */
     float *k_scale, *v_scale; /* device; NULL for the 16-bit types */
     int32_t storage;          /* WG_KV_* */
-    int32_t n_blocks, block_size;
+    int32_t n_blocks, block_size; /* n_blocks * block_size < 2^32 */
     int32_t n_heads;          /* heads of the keys and values */
     int32_t head_dim;         /* a multiple of 16, at most WG_KV_MAX_HEAD_DIM */
 } wg_kv_cache;

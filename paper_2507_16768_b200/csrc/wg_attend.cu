@@ -6,7 +6,6 @@
 struct wg_attend {
     int32_t max_tokens = 0, n_q_heads = 0, n_heads = 0, head_dim = 0;
     int32_t *shared = nullptr, *arrived = nullptr;
-    int64_t *units = nullptr;
     float *parts = nullptr, *shared_rows = nullptr, *private_rows = nullptr;
 };
 
@@ -31,9 +30,8 @@ int32_t wg_attend_create(int32_t max_tokens, int32_t n_q_heads, int32_t n_heads,
     p->max_tokens = max_tokens, p->n_q_heads = n_q_heads, p->n_heads = n_heads, p->head_dim = head_dim;
     const size_t counters = (size_t)max_tokens * n_heads * ((n_q_heads / n_heads + 15) / 16);
     const size_t rows = (size_t)max_tokens * n_q_heads * part_row(head_dim);
-    const size_t parts = (size_t)sm_count() * 2 * 2 * (16 * ATTEND_SHARED_WARPS) * part_row(head_dim);
-    int32_t rc = dev_alloc(&p->shared, (size_t)MAX_GROUPS);
-    if (rc == WG_OK) rc = dev_alloc(&p->units, (size_t)MAX_GROUPS);
+    const size_t parts = (size_t)sm_count() * 2 * PART_ROWS * part_row(head_dim);
+    int32_t rc = dev_alloc(&p->shared, (size_t)MAX_TOKENS);
     if (rc == WG_OK) rc = dev_alloc(&p->arrived, counters);
     if (rc == WG_OK) rc = dev_alloc(&p->parts, parts);
     if (rc == WG_OK) rc = dev_alloc(&p->shared_rows, rows);
@@ -54,7 +52,7 @@ int32_t wg_attend_create(int32_t max_tokens, int32_t n_q_heads, int32_t n_heads,
 
 void wg_attend_free(wg_attend *p) {
     if (!p) return;
-    for (void *q : {(void *)p->shared, (void *)p->units, (void *)p->arrived, (void *)p->parts, (void *)p->shared_rows, (void *)p->private_rows})
+    for (void *q : {(void *)p->shared, (void *)p->arrived, (void *)p->parts, (void *)p->shared_rows, (void *)p->private_rows})
         cudaFree(q);
     delete p;
 }
@@ -76,13 +74,14 @@ int32_t wg_kv_attend(wg_attend *attend, const wg_kv_cache *cache, const void *q,
     const int64_t width = (int64_t)n_q_heads * cache->head_dim;
     if (!rows_ok(q, q_stride, width) || !rows_ok(out, out_stride, width)) return WG_ERR_ARG;
     const CacheDev c = cache_dev(cache);
-    const int32_t rows = n_q_heads / cache->n_heads, row_blocks = (rows + 15) / 16;
+    const int32_t rows = n_q_heads / cache->n_heads, row_blocks = rows <= 8 ? 1 : (rows + 15) / 16;
     const int64_t room = (int64_t)max_blocks * cache->block_size, most_tokens = room < (1ll << 31) ? room : 1ll << 31;
-    const int64_t per_token = (most_tokens + UNIT_TOKENS - 1) / UNIT_TOKENS * row_blocks * cache->n_heads;
+    const int64_t tiles = (most_tokens + 15) / 16 * row_blocks * cache->n_heads;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    for (int64_t t0 = 0; t0 < n_tokens; t0 += (int64_t)MAX_GROUPS * group) {
+    const int32_t most = MAX_TOKENS / group * group;       // tokens of a launch
+    for (int64_t t0 = 0; t0 < n_tokens; t0 += most) {
         AttendArgs a{};
-        a.n_tokens = (int32_t)(n_tokens - t0 < (int64_t)MAX_GROUPS * group ? n_tokens - t0 : (int64_t)MAX_GROUPS * group);
+        a.n_tokens = (int32_t)(n_tokens - t0 < most ? n_tokens - t0 : most);
         a.q = static_cast<const uint16_t *>(q) + t0 * q_stride, a.q_stride = q_stride;
         a.out = static_cast<uint16_t *>(out) + t0 * out_stride, a.out_stride = out_stride;
         a.lse = lse ? lse + t0 * n_q_heads : nullptr;
@@ -96,15 +95,16 @@ int32_t wg_kv_attend(wg_attend *attend, const wg_kv_cache *cache, const void *q,
         a.group = group, a.n_groups = (a.n_tokens + group - 1) / group;
         a.q_bf16 = dtype == WG_DTYPE_BF16;
         a.scale = scale * 1.44269504088896f;
-        a.shared = attend->shared, a.units = attend->units, a.arrived = attend->arrived;
+        a.together = cache->n_heads % 4 == 0 ? 4 : cache->n_heads % 2 == 0 ? 2 : 1;
+        a.shared = attend->shared, a.arrived = attend->arrived;
         a.parts = attend->parts, a.shared_rows = attend->shared_rows, a.private_rows = attend->private_rows;
-        const int64_t most = per_token * a.n_tokens;
+        const int64_t most_tiles = tiles * a.n_tokens;
         int32_t rc;
         switch (cache->storage) {
-            case WG_KV_BF16: rc = attend_bf16(c, a, most, st); break;
-            case WG_KV_FP16: rc = attend_fp16(c, a, most, st); break;
-            case WG_KV_E4M3: rc = attend_e4m3(c, a, most, st); break;
-            default: rc = attend_int8(c, a, most, st); break;
+            case WG_KV_BF16: rc = attend_bf16(c, a, most_tiles, st); break;
+            case WG_KV_FP16: rc = attend_fp16(c, a, most_tiles, st); break;
+            case WG_KV_E4M3: rc = attend_e4m3(c, a, most_tiles, st); break;
+            default: rc = attend_int8(c, a, most_tiles, st); break;
         }
         if (rc != WG_OK) return rc;
     }

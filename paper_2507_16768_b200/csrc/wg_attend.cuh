@@ -6,13 +6,14 @@
 // is a segment; a token whose units went to several blocks is joined by the block that arrives last, from
 // partial results in scratch, always in the order of positions.
 //
-// Within a block a warp has rings of tiles of its own, filled with cp.async, 16 positions each, and the usual running
-// maximum and sum: for x = scale q.k and the maximum m so far, p = 2^(x - m), l = sum of p, o = sum of p v, all
-// multiplied by 2^(m_old - m) when m grows.  Rows are the M of mma.m16n8k16.  Both products read their second
-// operand with plain 16-byte loads: the order of a dot product's terms is free, so a lane takes eight neighbouring
-// dimensions of a key instead of the instruction's scattered pairs (and the queries are loaded the same way), and of the
-// values it takes the same eight dimensions of four positions and pairs them with byte permutes, which makes
-// the columns of the result neighbouring dimensions too.
+// Within a block a warp has a ring of tiles of its own, filled with cp.async, and the usual running maximum and sum: for x =
+// scale q.k and the maximum m so far, p = 2^(x - m), l = sum of p, o = sum of p v, all multiplied by 2^(m_old - m) when m
+// grows.  Both products are taken transposed, positions by rows and dimensions by rows: the few rows are then the N of
+// mma.m16n8k16, which comes in eights, and the keys and values the M.  Scores become the second product's operand by
+// transposing 8 x 8 pieces in registers.  Keys and values are read with plain 16-byte loads: the order of a dot product's terms
+// is free, so a lane takes eight neighbouring dimensions of a key instead of the instruction's scattered pairs (and the
+// queries are loaded the same way), and of the values it takes the same eight dimensions of four positions and pairs
+// them with byte permutes, which makes the rows of the result neighbouring dimensions too.
 //
 // 8-bit caches.  Codes are exact in fp16.  Queries enter in fp16, divided by a power of two per row (a query of 2^-14 of the
 // row's largest loses its last bits: 2^-25 of the largest).  A key's scale multiplies the score.  A value's scale s cannot
@@ -25,7 +26,7 @@
 
 #include "wg_cache.cuh"
 
-constexpr int MAX_GROUPS = 1024;        // groups of tokens of one launch: their prefix sums are in shared memory
+constexpr int MAX_TOKENS = 384;         // of one launch: their ranges and prefix sums are in shared memory
 
 struct AttendArgs {
     const uint16_t *q;
@@ -38,22 +39,22 @@ struct AttendArgs {
     int32_t max_blocks, n_seq, n_tokens, window;
     int32_t n_q_heads, rows;      // rows: query heads of a key head
     int32_t group, n_groups;
-    int32_t row_blocks;           // of 16 rows each, of one token and key head
+    int32_t row_blocks;           // of 8 or 16 rows each, of one token and key head
+    int32_t together;             // key heads that the warps of a block take side by side: 1, 2 or 4
     int32_t q_bf16;
     float scale;                  // times log2(e)
     // scratch
-    int32_t *shared;              // [n_groups] positions from 0 on that all of a group see in the same blocks
-    int64_t *units;               // [n_groups]
-    float *parts;                 // two per block: a segment that begins with the block's share, and one that does not
-    float *shared_rows;           // [n_tokens][n_q_heads]: results of shared pairs that one block did by itself
-    float *private_rows;          // ... and of the same tokens' private pairs
+    int32_t *shared;              // [n_groups] positions from 0 on that a group has in the same blocks
+    float *parts;                 // PART_ROWS rows per block: what begins with a share of the work, and what begins within
+    float *shared_rows;           // [n_tokens][n_q_heads]: shared results that one block did by itself
+    float *private_rows;          // ... and what is to be joined with them
     int32_t *arrived;             // zero between calls
 };
 
 namespace {
 
 constexpr int ATTEND_WARPS = 4, ATTEND_THREADS = 32 * ATTEND_WARPS;
-constexpr int UNIT_TOKENS = 64;         // positions of a unit: a tile for each warp
+constexpr int PART_ROWS = 128;           // rows of partial results that a block has room for
 constexpr float NEG_INFINITY = -__builtin_huge_valf();
 
 __device__ __forceinline__ void attend_enter() {
@@ -83,20 +84,14 @@ __device__ __forceinline__ Seen seen_by(const AttendArgs &a, const CacheDev &cac
     return r;
 }
 
-__device__ __forceinline__ int32_t units_of(int32_t first, int32_t end) {
-    return first < end ? (int32_t)(((uint32_t)(end - first) + UNIT_TOKENS - 1) / UNIT_TOKENS) : 0;
+// Tiles of `size` positions.
+__device__ __forceinline__ int32_t tiles_of(int32_t first, int32_t end, uint32_t size) {
+    return first < end ? (int32_t)(((uint32_t)(end - first) + size - 1) / size) : 0;
 }
 
-__device__ __forceinline__ void store_nothing(const AttendArgs &a, const CacheDev &cache, int t, int at, int threads) {
-    uint4 *row = reinterpret_cast<uint4 *>(a.out + t * a.out_stride);
-    for (int i = at; i < a.n_q_heads * cache.head_dim / 8; i += threads) row[i] = make_uint4(0, 0, 0, 0);
-    if (a.lse)
-        for (int i = at; i < a.n_q_heads; i += threads) a.lse[(int64_t)t * a.n_q_heads + i] = NEG_INFINITY;
-}
-
-// A block per group of tokens: how far their tables agree, and the units that makes.
+// A block per group of tokens: how far their tables agree.  A token has a say about the columns that it sees.
 __global__ void __launch_bounds__(ATTEND_THREADS)
-attend_plan_kernel(CacheDev cache, AttendArgs a, int32_t shared_row_blocks) {
+attend_plan_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ AttendArgs a) {
     attend_enter();
     __shared__ Seen seen[WG_BEAM_MAX_BEAMS];
     __shared__ int32_t differs;
@@ -104,44 +99,31 @@ attend_plan_kernel(CacheDev cache, AttendArgs a, int32_t shared_row_blocks) {
     if (threadIdx.x == 0) differs = 0x7FFFFFFF;
     if ((int)threadIdx.x < a.group) seen[threadIdx.x] = seen_by(a, cache, t0 + (int)threadIdx.x);
     __syncthreads();
-    int leader = -1, end = 0x7FFFFFFF;
-    for (int m = a.group - 1; m >= 0; --m)
-        if (seen[m].end > 0) leader = m, end = min(end, seen[m].end);
-    for (int m = 0; m < a.group && t0 + m < a.n_tokens; ++m)
-        if (seen[m].end == 0) store_nothing(a, cache, t0 + m, threadIdx.x, ATTEND_THREADS);
-    if (leader < 0 || a.window > 0) end = 0;
-    if (end > 0) {
-        const int cols = (int)cache.block.quotient((uint32_t)(end - 1)) + 1;
-        const int32_t *mine = a.table + seen[leader].s * a.stride;
-        for (int c0 = 0; c0 < cols; c0 += 4 * ATTEND_THREADS) {
-            int at = 0x7FFFFFFF;
+    int leader = -1, end = 0, second = 0;     // the longest token, and how far any other one of another sequence goes
+    for (int m = 0; m < a.group; ++m)
+        if (seen[m].end > end) leader = m, end = seen[m].end;
+    for (int m = 0; m < a.group; ++m)
+        if (leader >= 0 && seen[m].s != seen[leader].s) second = max(second, seen[m].end);
+    const int cols = second > 0 ? (int)cache.block.quotient((uint32_t)(second - 1)) + 1 : 0;
+    const int32_t *mine = a.table + (leader >= 0 ? seen[leader].s * a.stride : 0);
+    for (int c0 = 0; c0 < cols; c0 += 4 * ATTEND_THREADS) {
+        int at = 0x7FFFFFFF;
 #pragma unroll
-            for (int u = 3; u >= 0; --u) {
-                const int c = c0 + u * ATTEND_THREADS + (int)threadIdx.x;
-                if (c >= cols) continue;
-                const int32_t b = mine[c];
-                bool same = true;
-                for (int m = leader + 1; m < a.group; ++m)
-                    if (seen[m].end > 0 && seen[m].s != seen[leader].s) same &= a.table[seen[m].s * a.stride + c] == b;
-                if (!same) at = c;
-            }
-            if (at < 0x7FFFFFFF) atomicMin(&differs, at);
-            if (__syncthreads_or(at < 0x7FFFFFFF)) break;
+        for (int u = 3; u >= 0; --u) {
+            const int c = c0 + u * ATTEND_THREADS + (int)threadIdx.x;
+            if (c >= cols) continue;
+            const int32_t b = mine[c];
+            bool same = true;
+            for (int m = 0; m < a.group; ++m)
+                if (seen[m].s != seen[leader].s && (int64_t)c * cache.block.d < seen[m].end)
+                    same &= a.table[seen[m].s * a.stride + c] == b;
+            if (!same) at = c;
         }
-        if (differs < 0x7FFFFFFF) end = (int)min((int64_t)end, (int64_t)differs * cache.block.d);
+        if (at < 0x7FFFFFFF) atomicMin(&differs, at);
+        if (__syncthreads_or(at < 0x7FFFFFFF)) break;
     }
-    if (threadIdx.x < 32) {
-        int64_t n = 0;
-        if ((int)threadIdx.x < a.group && seen[threadIdx.x].end > 0) {
-            const Seen r = seen[threadIdx.x];
-            n = (int64_t)units_of(max(r.first, end), r.end) * a.row_blocks;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xFFFFFFFFu, n, o);
-        if (threadIdx.x == 0) {
-            a.shared[g] = end;
-            a.units[g] = (n + (int64_t)units_of(0, end) * shared_row_blocks) * cache.n_heads;
-        }
+    if (threadIdx.x == 0) {
+        a.shared[g] = a.window > 0 ? 0 : (int)min((int64_t)end, (int64_t)differs * cache.block.d);
     }
 }
 
@@ -150,6 +132,9 @@ attend_plan_kernel(CacheDev cache, AttendArgs a, int32_t shared_row_blocks) {
 __device__ __forceinline__ uint32_t shared_address(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copy16(uint32_t to, const void *from, bool real) {   // zeros where it is not
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copy4(uint32_t to, const void *from, bool real) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(real ? 4 : 0) : "memory");
@@ -181,6 +166,12 @@ __device__ __forceinline__ void multiply(float (&c)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {     // of 16-bit elements
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
 // KV: what the cache holds; DP: the head size, rounded up (dimensions beyond it are zeros).
 template <typename KV, int DP>
 struct Shape {
@@ -188,13 +179,16 @@ struct Shape {
     using Mma = typename std::conditional<std::is_same<KV, __nv_bfloat16>::value, __nv_bfloat16, __half>::type;
     static constexpr int BYTES = NARROW ? 1 : 2;
     static constexpr int CHUNKS = DP * BYTES / 16;          // 16-byte pieces of a vector
-    static constexpr int PLANE = 16 * DP * BYTES;           // a tile of keys, or of values
+    static constexpr int TILE = DP * BYTES <= 128 ? 32 : 16;      // positions
+    static constexpr int SUBS = TILE / 16;
+    static constexpr uint32_t ALL = TILE == 32 ? 0xFFFFFFFFu : 0xFFFFu;
+    static constexpr int PLANE = TILE * DP * BYTES;         // a tile of keys, or of values
     static constexpr int STAGE = 2 * PLANE;
-    static constexpr int STAGES = 24576 / STAGE > 8 ? 8 : 24576 / STAGE < 3 ? 3 : 24576 / STAGE;
+    static constexpr int STAGES = 3;
     static constexpr int SMEM = ATTEND_WARPS * STAGES * STAGE;
     static constexpr int BLOCKS = SMEM > 110 * 1024 ? 1 : 2;        // on an SM
     static constexpr int STEPS = DP / 16;                   // of the first product
-    static constexpr int HALVES = DP / 64;                  // of the second, 64 columns each
+    static constexpr int HALVES = DP / 64;                  // of the second, 64 dimensions each
     static constexpr int PITCH = DP + 4;                    // of a row of partial results in shared memory, in floats
     static_assert(16 * PITCH * 4 + 128 <= STAGES * STAGE, "a warp's partial result takes the place of its ring");
 
@@ -207,423 +201,375 @@ struct Shape {
     static __device__ __forceinline__ int value_at(int r, int c) { return ((r * CHUNKS + c) ^ (r & 6)) * 16; }
 };
 
-// One row block's running results in a warp: lane holds rows lane / 4 and lane / 4 + 8.
-template <int HALVES>
+// Running results of 8 NT rows in a warp: with n = lane / 4 and j = lane % 4 a lane has rows 8 nt + 2 j + c, c = 0, 1.
+template <int HALVES, int NT>
 struct Running {
-    float m[2], l[2];
-    float o[HALVES][8][4];        // [.][d][.]: dimensions 64 half + 16 (lane % 4) + d and + 8 + d, of both rows
+    float m[NT][2], l[NT][2];     // (l: the lane's share until sum_up)
+    float o[HALVES][4][NT][4];    // [h][i][nt][2 e + c]: dimension 64 h + 8 n + 2 i + e
     __device__ __forceinline__ void reset() {
-        m[0] = m[1] = NEG_INFINITY;
-        l[0] = l[1] = 0.0f;
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h)
+        for (int nt = 0; nt < NT; ++nt) {
+            m[nt][0] = m[nt][1] = NEG_INFINITY;
+            l[nt][0] = l[nt][1] = 0.0f;
 #pragma unroll
-            for (int d = 0; d < 8; ++d)
+            for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[h][d][i] = 0.0f;
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[h][i][nt][e] = 0.0f;
+        }
+    }
+    __device__ __forceinline__ void sum_up() {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[nt][c] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][c], d);
+    }
+    __device__ __forceinline__ void eight(int h, int nt, int c, float (&y)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = o[h][i / 2][nt][2 * (i & 1) + c];
     }
 };
 
-// Queries of a warp's 16 rows as the first operand.
-template <typename KV, int DP>
+// Queries as the second operand of the first product: a lane loads rows 8 nt + n.
+template <typename KV, int DP, int NT>
 struct Queries {
     using S = Shape<KV, DP>;
-    uint32_t a[S::STEPS][4];
-    float factor[2];              // of the rows' scores
+    uint32_t b[S::STEPS][NT][2];
+    float factor[NT][2];          // of the scores of the lane's result rows, above 0; the sign is in the queries
 
-    // row: NULL for none; `inside`: head_dim
-    __device__ __forceinline__ void load(const uint16_t *row0, const uint16_t *row1, int head_dim, bool bf16, float scale, int j) {
-        const uint16_t *row[2] = {row0, row1};
-        factor[0] = factor[1] = scale;
-        if constexpr (!S::NARROW) {
+    // row[nt]: NULL for none
+    __device__ __forceinline__ void load(const uint16_t *const (&row)[NT], int head_dim, bool bf16, float scale, int j) {
+        // (2^-126 for 0: a score that stands for nothing stays -inf)
+        const float up = fmaxf(fabsf(scale), 0x1p-126f);
+        const uint32_t sign = scale < 0.0f ? 0x80008000u : 0u;
 #pragma unroll
-            for (int kk = 0; kk < S::STEPS / 2; ++kk)
+        for (int nt = 0; nt < NT; ++nt) {
+            factor[nt][0] = factor[nt][1] = up;
+            constexpr int PER = S::NARROW ? 2 : 1;      // 16-byte loads that make up a lane's share of a piece of a key
+            uint32_t top = 0;
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int d = (kk * 4 + j) * 8;
-                    const uint4 x = row[u] && d < head_dim ? *reinterpret_cast<const uint4 *>(row[u] + d) : make_uint4(0, 0, 0, 0);
-                    a[2 * kk][u] = x.x, a[2 * kk][2 + u] = x.y, a[2 * kk + 1][u] = x.z, a[2 * kk + 1][2 + u] = x.w;
-                }
-        } else {
+            for (int kk = 0; kk < S::CHUNKS / 4; ++kk)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                uint32_t top = 0;
+                for (int half = 0; half < PER; ++half) {
+                    const int d = ((kk * 4 + j) * PER + half) * 8;
+                    const uint4 x = row[nt] && d < head_dim ? *reinterpret_cast<const uint4 *>(row[nt] + d) : make_uint4(0, 0, 0, 0);
+                    const uint32_t w[4] = {x.x ^ sign, x.y ^ sign, x.z ^ sign, x.w ^ sign};
 #pragma unroll
-                for (int kk = 0; kk < S::STEPS / 4; ++kk)
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const int d = (kk * 4 + j) * 16 + half * 8;
-                        const uint4 x = row[u] && d < head_dim ? *reinterpret_cast<const uint4 *>(row[u] + d) : make_uint4(0, 0, 0, 0);
-                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            // word i belongs to step half * 2 + i / 2 of the four, registers u and 2 + u in turn
-                            a[kk * 4 + half * 2 + i / 2][(i & 1) * 2 + u] = w[i];
+                    for (int i = 0; i < 4; ++i) {
+                        b[(kk * PER + half) * 2 + i / 2][nt][i & 1] = w[i];
+                        if constexpr (S::NARROW) {
                             const float2 f = bf16 ? unpack(w[i], __nv_bfloat16{}) : unpack(w[i], __half{});
                             top = max(top, max(__float_as_uint(f.x) & 0x7FFFFFFFu, __float_as_uint(f.y) & 0x7FFFFFFFu));
                         }
                     }
+                }
+            if constexpr (S::NARROW) {
                 top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
                 top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
                 const uint32_t e = min(max(top >> 23, 1u), 253u);
                 const float down = __uint_as_float((254u - e) << 23);
-                factor[u] = scale * __uint_as_float(e << 23);
 #pragma unroll
                 for (int st = 0; st < S::STEPS; ++st)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        uint32_t &w = a[st][i * 2 + u];
+                        uint32_t &w = b[st][nt][i];
                         const float2 f = bf16 ? unpack(w, __nv_bfloat16{}) : unpack(w, __half{});
                         w = pack<__half>(f.x * down, f.y * down);
                     }
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    factor[nt][c] = fmaxf(up * __uint_as_float(__shfl_sync(0xFFFFFFFFu, e, (2 * j + c) * 4) << 23), 0x1p-126f);
             }
         }
     }
 };
 
-// 16 positions: keys at `keys`, values at `values` in shared memory; bit i of `real`: position i counts.  scales: 16 of
-// keys, then 16 of values.
-template <typename KV, int DP>
-__device__ __forceinline__ void take_tile(Running<DP / 64> &run, const Queries<KV, DP> &q, uint32_t keys, uint32_t values,
-                                          const float *scales, uint32_t real, int lane) {
+// A tile: keys at `keys`, values at `values` in shared memory; bit i of `real`: position i counts.  scales: TILE of keys,
+// then TILE of values.  PART: the positions that do not count may hold anything (otherwise zeros), and only the rows of
+// which `in` says so take them in; whatever the positions hold, the other rows stay as they are.
+template <typename KV, int DP, int NT, bool PART>
+__device__ __forceinline__ void take_tile(Running<DP / 64, NT> &run, const Queries<KV, DP, NT> &q, uint32_t keys, uint32_t values,
+                                          const float *scales, uint32_t real, int n, int j, const bool (&in)[NT][2]) {
     using S = Shape<KV, DP>;
-    const int n = lane >> 2, j = lane & 3;
-    float x[2][4] = {};
+    using Mma = typename S::Mma;
+    float x[S::SUBS][NT][4] = {};            // [2 e + c]: of position 16 s + n + 8 e
 #pragma unroll
     for (int kk = 0; kk < S::CHUNKS / 4; ++kk)
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-            const uint4 k = load16(keys + S::key_at(nt * 8 + n, kk * 4 + j));
+        for (int s = 0; s < S::SUBS; ++s) {
+            const uint4 k0 = load16(keys + S::key_at(s * 16 + n, kk * 4 + j)), k1 = load16(keys + S::key_at(s * 16 + n + 8, kk * 4 + j));
+            const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
             if constexpr (!S::NARROW) {
-                multiply(x[nt], q.a[2 * kk], k.x, k.y, typename S::Mma{});
-                multiply(x[nt], q.a[2 * kk + 1], k.z, k.w, typename S::Mma{});
-            } else {
-                const uint32_t w[4] = {k.x, k.y, k.z, k.w};
 #pragma unroll
-                for (int st = 0; st < 4; ++st)
-                    multiply(x[nt], q.a[4 * kk + st], codes_to_half2(w[st], 0, KV{}), codes_to_half2(w[st], 1, KV{}), __half{});
+                for (int st = 0; st < 2; ++st) {
+                    const uint32_t a[4] = {w0[2 * st], w1[2 * st], w0[2 * st + 1], w1[2 * st + 1]};
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) multiply(x[s][nt], a, q.b[2 * kk + st][nt][0], q.b[2 * kk + st][nt][1], Mma{});
+                }
+            } else {
+#pragma unroll
+                for (int st = 0; st < 4; ++st) {
+                    const uint32_t a[4] = {codes_to_half2(w0[st], 0, KV{}), codes_to_half2(w1[st], 0, KV{}), codes_to_half2(w0[st], 1, KV{}),
+                                           codes_to_half2(w1[st], 1, KV{})};
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) multiply(x[s][nt], a, q.b[4 * kk + st][nt][0], q.b[4 * kk + st][nt][1], Mma{});
+                }
             }
         }
-    float up[2][2];                      // log2 of a value's scale
+    float up[S::SUBS][2];                    // log2 of a value's scale
+    if constexpr (S::NARROW) {
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-        if constexpr (S::NARROW) {
-            const float2 ks = *reinterpret_cast<const float2 *>(scales + nt * 8 + 2 * j);
-            const float2 vs = *reinterpret_cast<const float2 *>(scales + 16 + nt * 8 + 2 * j);
-            up[nt][0] = __log2f(vs.x < 0x1p-100f ? 0x1p-100f : vs.x);      // (a NaN stays one)
-            up[nt][1] = __log2f(vs.y < 0x1p-100f ? 0x1p-100f : vs.y);
-            x[nt][0] *= q.factor[0] * ks.x, x[nt][1] *= q.factor[0] * ks.y;
-            x[nt][2] *= q.factor[1] * ks.x, x[nt][3] *= q.factor[1] * ks.y;
-        } else {
+        for (int s = 0; s < S::SUBS; ++s)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[nt][i] *= q.factor[i >> 1];
-            up[nt][0] = up[nt][1] = 0.0f;
-        }
-        if (real != 0xFFFFu) {
+            for (int e = 0; e < 2; ++e) {
+                const float ks = scales[s * 16 + n + 8 * e], vs = scales[S::TILE + s * 16 + n + 8 * e];
+                up[s][e] = __log2f(vs < 0x1p-100f ? 0x1p-100f : vs);      // (a NaN stays one)
+                if (PART && !((real >> (s * 16 + n + 8 * e)) & 1u)) up[s][e] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (!((real >> (nt * 8 + 2 * j + (i & 1))) & 1u)) x[nt][i] = NEG_INFINITY;
-        }
+                for (int nt = 0; nt < NT; ++nt) x[s][nt][2 * e] *= ks, x[s][nt][2 * e + 1] *= ks;
+            }
     }
-    float base[2];
+    if (PART || real != S::ALL) {
+#pragma unroll
+        for (int s = 0; s < S::SUBS; ++s)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (!((real >> (s * 16 + n + 8 * e)) & 1u)) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) x[s][nt][2 * e] = x[s][nt][2 * e + 1] = NEG_INFINITY;
+                }
+    }
+    if constexpr (PART) {
+#pragma unroll
+        for (int s = 0; s < S::SUBS; ++s)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!in[nt][i & 1]) x[s][nt][i] = NEG_INFINITY;
+    }
+    // maxima: of x itself, which the factor (above 0) multiplies later; with scales of x' = factor x + up
+    float base[NT][2], shrink[NT][2];
     bool grew = false;
-    float shrink[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        float m = fmaxf(fmaxf(x[0][2 * u] + up[0][0], x[0][2 * u + 1] + up[0][1]), fmaxf(x[1][2 * u] + up[1][0], x[1][2 * u + 1] + up[1][1]));
-        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-        m = fmaxf(m, run.m[u]);
-        base[u] = m == NEG_INFINITY ? 0.0f : m;
-        shrink[u] = m > run.m[u] ? power2(run.m[u] - base[u]) : 1.0f;
-        grew |= m > run.m[u];
-        run.m[u] = m;
-    }
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const float f = q.factor[nt][c];
+            float m = run.m[nt][c];
+#pragma unroll
+            for (int s = 0; s < S::SUBS; ++s)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) m = fmaxf(m, S::NARROW ? fmaf(x[s][nt][2 * e + c], f, up[s][e]) : x[s][nt][2 * e + c]);
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+            const float g = S::NARROW ? 1.0f : f;
+            base[nt][c] = m == NEG_INFINITY ? 0.0f : m * g;
+            shrink[nt][c] = m > run.m[nt][c] ? power2(fmaf(run.m[nt][c], g, -base[nt][c])) : 1.0f;
+            grew |= m > run.m[nt][c];
+            run.m[nt][c] = m;
+        }
     if (__any_sync(0xFFFFFFFFu, grew)) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) run.l[u] *= shrink[u];
+        for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-        for (int h = 0; h < S::HALVES; ++h)
+            for (int c = 0; c < 2; ++c) run.l[nt][c] *= shrink[nt][c];
 #pragma unroll
-            for (int d = 0; d < 8; ++d)
+            for (int h = 0; h < S::HALVES; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) run.o[h][d][i] *= shrink[i >> 1];
-    }
-    uint32_t p[4];
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const float x0 = x[nt][2 * u] - base[u], x1 = x[nt][2 * u + 1] - base[u];
-            float p0 = power2(x0), p1 = power2(x1);
-            run.l[u] += p0 + p1;
-            if constexpr (S::NARROW) p0 = power2(x0 + up[nt][0]), p1 = power2(x1 + up[nt][1]);
-            p[nt * 2 + u] = pack<typename S::Mma>(p0, p1);
-        }
-#pragma unroll
-    for (int h = 0; h < S::HALVES; ++h) {
-        const int r[4] = {2 * j, 2 * j + 1, 2 * j + 8, 2 * j + 9};
-        if constexpr (!S::NARROW) {
-            uint4 v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = load16(values + S::value_at(r[i], h * 8 + n));
-            const uint32_t w[4][4] = {{v[0].x, v[0].y, v[0].z, v[0].w}, {v[1].x, v[1].y, v[1].z, v[1].w},
-                                      {v[2].x, v[2].y, v[2].z, v[2].w}, {v[3].x, v[3].y, v[3].z, v[3].w}};
-#pragma unroll
-            for (int d = 0; d < 8; ++d) {
-                const uint32_t sel = d & 1 ? 0x7632 : 0x5410;
-                multiply(run.o[h][d], p, __byte_perm(w[0][d / 2], w[1][d / 2], sel), __byte_perm(w[2][d / 2], w[3][d / 2], sel),
-                         typename S::Mma{});
-            }
-        } else {
-            uint2 v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = load8(values + S::value_at(r[i], h * 4 + n / 2) + (n & 1) * 8);
-            const uint32_t w[4][2] = {{v[0].x, v[0].y}, {v[1].x, v[1].y}, {v[2].x, v[2].y}, {v[3].x, v[3].y}};
-#pragma unroll
-            for (int d = 0; d < 8; d += 2) {
-                const uint32_t sel = d & 2 ? 0x7362 : 0x5140;
-                const uint32_t b0 = __byte_perm(w[0][d / 4], w[1][d / 4], sel), b1 = __byte_perm(w[2][d / 4], w[3][d / 4], sel);
-                multiply(run.o[h][d], p, codes_to_half2(b0, 0, KV{}), codes_to_half2(b1, 0, KV{}), __half{});
-                multiply(run.o[h][d + 1], p, codes_to_half2(b0, 1, KV{}), codes_to_half2(b1, 1, KV{}), __half{});
-            }
+                    for (int e = 0; e < 4; ++e) run.o[h][i][nt][e] *= shrink[nt][e & 1];
         }
     }
+    uint32_t p[S::SUBS][NT][2];
+#pragma unroll
+    for (int s = 0; s < S::SUBS; ++s)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float y[2];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const float z = fmaf(x[s][nt][2 * e + c], q.factor[nt][c], -base[nt][c]);
+                    y[c] = power2(z);
+                    run.l[nt][c] += y[c];
+                    if constexpr (S::NARROW) y[c] = power2(z + up[s][e]);
+                }
+                p[s][nt][e] = transpose8x8(pack<Mma>(y[0], y[1]));
+            }
+    const auto add = [&](float (&o)[NT][4], int s, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+        const uint32_t v[4] = {a0, a1, a2, a3};
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if constexpr (PART) {
+                float y[4] = {};
+                multiply(y, v, p[s][nt][0], p[s][nt][1], Mma{});
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (in[nt][i & 1]) o[nt][i] += y[i];
+            } else {
+                multiply(o[nt], v, p[s][nt][0], p[s][nt][1], Mma{});
+            }
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < S::SUBS; ++s)
+#pragma unroll
+        for (int h = 0; h < S::HALVES; ++h) {
+            const int r[4] = {s * 16 + 2 * j, s * 16 + 2 * j + 1, s * 16 + 2 * j + 8, s * 16 + 2 * j + 9};
+            if constexpr (!S::NARROW) {
+                uint4 v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[i] = load16(values + S::value_at(r[i], h * 8 + n));
+                    if (PART && !((real >> r[i]) & 1u)) v[i] = make_uint4(0, 0, 0, 0);
+                }
+                const uint32_t w[4][4] = {{v[0].x, v[0].y, v[0].z, v[0].w}, {v[1].x, v[1].y, v[1].z, v[1].w},
+                                          {v[2].x, v[2].y, v[2].z, v[2].w}, {v[3].x, v[3].y, v[3].z, v[3].w}};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    add(run.o[h][i], s, __byte_perm(w[0][i], w[1][i], 0x5410), __byte_perm(w[0][i], w[1][i], 0x7632),
+                        __byte_perm(w[2][i], w[3][i], 0x5410), __byte_perm(w[2][i], w[3][i], 0x7632));
+            } else {
+                uint2 v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[i] = load8(values + S::value_at(r[i], h * 4 + n / 2) + (n & 1) * 8);
+                    if (PART && !((real >> r[i]) & 1u)) v[i] = make_uint2(0, 0);
+                }
+                const uint32_t w[4][2] = {{v[0].x, v[0].y}, {v[1].x, v[1].y}, {v[2].x, v[2].y}, {v[3].x, v[3].y}};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t sel = i & 1 ? 0x7362 : 0x5140;
+                    const uint32_t lo = __byte_perm(w[0][i / 2], w[1][i / 2], sel), hi = __byte_perm(w[2][i / 2], w[3][i / 2], sel);
+                    add(run.o[h][i], s, codes_to_half2(lo, 0, KV{}), codes_to_half2(lo, 1, KV{}), codes_to_half2(hi, 0, KV{}), codes_to_half2(hi, 1, KV{}));
+                }
+            }
+        }
 }
 
 // ---- where things are ------------------------------------------------------------------------------------------
 
-// Units of a call, dealt out: share w is [total * w / workers, total * (w + 1) / workers).
+// Units of work, dealt out: share w is [total * w / workers, total * (w + 1) / workers).
 struct Deal {
     int64_t total;
     int32_t workers;
     __device__ __forceinline__ int64_t begin(int w) const { return total * w / workers; }
     __device__ __forceinline__ int owner(int64_t unit) const { return (int)(((unit + 1) * workers + total - 1) / total) - 1; }
-    // the slot of scratch for worker w's segment of the units from `first` on
-    __device__ __forceinline__ int64_t slot(int w, int64_t first) const { return 2 * (int64_t)w + (begin(w) >= first ? 0 : 1); }
 };
 
-// A run of units with the same rows and head.
+// What a launch is about, in shared memory.
+struct Book {
+    int64_t upto[MAX_TOKENS + 1];         // private units before a token
+    int64_t shared_upto[MAX_TOKENS + 1];  // shared units before a group
+    int32_t seq[MAX_TOKENS], from[MAX_TOKENS], end[MAX_TOKENS];   // a token's private positions: from .. end - 1; end 0: it has no row
+    int32_t to[MAX_TOKENS];               // shared positions of a group: 0 .. to - 1 (without groups: from[t] .. to[t] - 1)
+    int32_t last[WG_BEAM_MAX_BEAMS];      // of a group's tokens: all that belongs to them is there
+};
+
+// A run of units with the same rows and head that a block works on as one.
 struct Pair {
     int64_t first;            // unit
     int32_t units;
-    int32_t token;            // of a private pair; the group's first of a shared one
-    int32_t head, row_block;
+    int32_t group, head, row_block;
     int32_t from, to, seq;    // positions, and a sequence whose table has them
-    bool shared;
 };
 
-// The units of a group, in registers of a warp: lane m has member m's private pairs.
-struct Group {
-    Seen seen;
-    int32_t units;            // per pair
-    int64_t offset;           // of the member's first pair, from the group's first unit
-    int32_t shared_to, shared_units;
-
-    __device__ __forceinline__ void load(const AttendArgs &a, const CacheDev &cache, int g, int shared_row_blocks, int lane) {
-        seen = Seen{0, 0, 0};
-        if (lane < a.group) seen = seen_by(a, cache, g * a.group + lane);
-        shared_to = a.shared[g];
-        shared_units = units_of(0, shared_to);
-        units = units_of(max(seen.first, shared_to), seen.end);
-        const int64_t mine = (int64_t)units * a.row_blocks * cache.n_heads;
-        int64_t upto = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t y = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-            if (lane >= o) upto += y;
-        }
-        offset = upto - mine + (int64_t)shared_units * shared_row_blocks * cache.n_heads;
-    }
-};
-
-template <typename KV, int DP, int WMS, bool GROUPED>
+// SHARED_WARPS: a block's warps work on the same tiles, each for 8 NT rows of its own (4), or on tiles of their own for
+// the same rows (1), or there are no pairs for whole blocks (0).
+template <typename KV, int DP, int SHARED_WARPS, bool GROUPED, int NT>
 struct Attend {
     using S = Shape<KV, DP>;
-    static constexpr int ROWS = 16 * WMS;                       // of a shared pair
+    static constexpr int WM = SHARED_WARPS == 0 ? 1 : SHARED_WARPS;
+    static constexpr int WARP_ROWS = 8 * NT;
+    static constexpr int ROWS = WARP_ROWS * WM;                 // of a shared pair
+    static constexpr int UNIT = ATTEND_WARPS * S::TILE;         // positions of a shared unit
     static constexpr int PART_ROW = DP + 4;                     // floats of a row's partial result: o, m, l
-    static constexpr int64_t PART = (int64_t)ROWS * PART_ROW;
 
     const CacheDev &cache;
     const AttendArgs &a;
+    Book &book;
     char *ring;
-    float *scales;          // [warp][stage][32]
-    uint32_t *real;         // [warp][stage]
-    Deal deal;
+    float *scales;            // [warp][stage][2 TILE]
+    uint32_t *real;           // [warp][stage]
+    Deal shared, own;         // the blocks' units, and the warps'
+    int32_t shared_blocks;    // blocks that work on shared pairs: the first ones
     int32_t shared_row_blocks;
 
-    // The token and query head of row i of a pair (token -1: none).
-    __device__ __forceinline__ int row_of(const Pair &p, int i, int &head) const {
-        if (!p.shared) {
-            const int r = p.row_block * 16 + i;
-            head = p.head * a.rows + r;
-            return i < 16 && r < a.rows ? p.token : -1;
-        }
-        const int r = p.row_block * ROWS + i, m = r / a.rows;
-        head = p.head * a.rows + (r - m * a.rows);
-        return m < a.group && seen_by(a, cache, p.token + m).end > 0 ? p.token + m : -1;
+    // ---- partial results ----
+    // Scratch for the rows of what a block or warp began with its share (which = 0) or within it (1): nothing else is left
+    // unfinished at its ends.
+    __device__ __forceinline__ float *block_part(int block, int which, int row) const {
+        return a.parts + ((int64_t)block * PART_ROWS + which * (PART_ROWS / 2) + row) * PART_ROW;
     }
-
-    // The warps that work on the same tiles: one, or all of the block.
-    template <int WM>
-    static __device__ __forceinline__ void stream_sync() {
-        static_assert(WM == 1 || WM == ATTEND_WARPS, "");
-        if constexpr (WM == 1)
-            __syncwarp();
-        else
-            __syncthreads();
+    __device__ __forceinline__ float *warp_part(int warp, int which, int row) const {
+        return a.parts + ((int64_t)shared_blocks * PART_ROWS + (int64_t)warp * (PART_ROWS / ATTEND_WARPS) + which * (PART_ROWS / ATTEND_WARPS / 2) + row) * PART_ROW;
     }
+    static_assert(PART_ROWS == 2 * 16 * ATTEND_WARPS, "two of 64 rows for a block, or two of 16 for each of its warps");
 
-    // Units [u0, u1) of a pair, written where they belong.  `whole`: they are all of the pair's.  `final`: and nothing
-    // else belongs to its rows.
-    template <int WM>
-    __device__ __forceinline__ void segment(const Pair &pair, int64_t u0, int64_t u1, bool whole, bool final) {
-        constexpr int STREAMS = ATTEND_WARPS / WM, STREAM_TOKENS = 16 * WM;
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
-        const int stream = warp / WM, wm = warp % WM;
-        const int from = pair.from + (int)(u0 - pair.first) * UNIT_TOKENS;
-        const int to = (int)min((int64_t)pair.to, (int64_t)pair.from + (u1 - pair.first) * UNIT_TOKENS);
-        const int tiles = (int)(((uint32_t)(to - from) + STREAM_TOKENS - 1) / STREAM_TOKENS);   // of all streams
-        const int mine = tiles > stream ? (tiles - stream + STREAMS - 1) / STREAMS : 0;
-        const int32_t *row = a.table + pair.seq * a.stride;
-        const int es = S::BYTES, width = cache.head_dim * es;
-        const int pieces = width / 16;
-        char *const my_ring = ring + warp * S::STAGES * S::STAGE;                    // this warp's tiles
-        char *const stream_ring = ring + stream * WM * S::STAGES * S::STAGE;
+    // The pieces of a pair: by `n` workers from w on.
+    struct Pieces {
+        int32_t n, w;
+        int64_t first;
+    };
+    static __device__ __forceinline__ Pieces pieces_of(const Deal &deal, int64_t first, int32_t units) {
+        if (units == 0) return {0, 0, 0};
+        const int w = deal.owner(first);
+        return {deal.owner(first + units - 1) - w + 1, w, first};
+    }
+    __device__ __forceinline__ int32_t shared_units(int g) const {
+        return SHARED_WARPS == 0 ? 0 : tiles_of(GROUPED ? 0 : book.from[g], book.to[g], UNIT);
+    }
+    __device__ __forceinline__ int32_t own_units(int t) const { return GROUPED || SHARED_WARPS == 0 ? tiles_of(book.from[t], book.end[t], S::TILE) : 0; }
+    __device__ __forceinline__ Pieces shared_pieces(int g, int head, int row_block) const {
+        const int32_t n = shared_units(g);
+        return pieces_of(shared, book.shared_upto[g] + ((int64_t)head * shared_row_blocks + row_block) * n, n);
+    }
+    __device__ __forceinline__ Pieces own_pieces(int t, int head, int row_block) const {
+        const int32_t n = own_units(t);
+        return pieces_of(own, book.upto[t] + ((int64_t)(head / a.together) * a.row_blocks + row_block) * n, n);
+    }
+    __device__ __forceinline__ int group_of(int t) const { return GROUPED ? t / a.group : t; }
 
-        const auto position = [&](int i) { return from + (i * STREAMS + stream) * STREAM_TOKENS + wm * 16 + (lane & 15); };
-        const auto entry = [&](int i) {            // of the table; anything but a block where there is none
-            const int p = position(i);
-            return i < mine && p < to ? row[cache.block.quotient((uint32_t)p)] : -1;
-        };
-        const auto issue = [&](int i, int32_t block) {
-            const int stage = i % S::STAGES;
-            int64_t vec = -1;
-            if ((uint32_t)block < (uint32_t)cache.n_blocks) {
-                const uint32_t p = (uint32_t)position(i);
-                vec = ((int64_t)block * cache.block.d + (p - cache.block.quotient(p) * cache.block.d)) * cache.n_heads + pair.head;
+    // Partial results of a token and head that have to arrive before they can be joined: those of row block `only`, or, where
+    // something is shared, all.  (A shared pair that one block did is final for tokens without anything of their own.)
+    __device__ __forceinline__ int expected(int t, int head, int only) const {
+        const int g = group_of(t);
+        int n = 0;
+        if (SHARED_WARPS > 0 && shared_units(g) > 0) {
+            const bool alone = own_units(t) == 0;
+            const int r0 = (t - g * a.group) * a.rows;
+            for (int b = r0 / ROWS; b <= (r0 + a.rows - 1) / ROWS; ++b) {
+                const int k = shared_pieces(g, head, b).n;
+                n += alone && k == 1 ? 0 : k;
             }
-            const uint32_t ok = __ballot_sync(0xFFFFFFFFu, vec >= 0) & 0xFFFFu;
-            if (i < mine) {
-                const uint32_t keys = shared_address(my_ring + stage * S::STAGE), values = keys + S::PLANE;
-#pragma unroll
-                for (int it = 0; it < S::CHUNKS / 2; ++it) {
-                    const int r = (it * 32 + lane) / S::CHUNKS, c = lane % S::CHUNKS;
-                    const int64_t v = __shfl_sync(0xFFFFFFFFu, vec, r);
-                    const bool is = v >= 0 && c < pieces;
-                    const int64_t off = is ? v * width + c * 16 : 0;
-                    copy16(keys + S::key_at(r, c), cache.k + off, is);
-                    copy16(values + S::value_at(r, c), cache.v + off, is);
-                }
-                if constexpr (S::NARROW)
-                    copy4(shared_address(scales + (warp * S::STAGES + stage) * 32 + lane),
-                          (lane < 16 ? cache.k_scale : cache.v_scale) + (vec < 0 ? 0 : vec), vec >= 0);
-                if (lane == 0) real[warp * S::STAGES + stage] = ok;
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
-        int32_t first_blocks[S::STAGES - 1];
-#pragma unroll
-        for (int i = 0; i < S::STAGES - 1; ++i) first_blocks[i] = entry(i);
-        int32_t next = entry(S::STAGES - 1);
-        Queries<KV, DP> q;
-        {
-            const uint16_t *rows[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                int head;
-                const int t = row_of(pair, wm * 16 + n + 8 * u, head);
-                rows[u] = t < 0 ? nullptr : a.q + t * a.q_stride + (int64_t)head * cache.head_dim;
-            }
-#pragma unroll
-            for (int i = 0; i < S::STAGES - 1; ++i) issue(i, first_blocks[i]);
-            q.load(rows[0], rows[1], cache.head_dim, a.q_bf16, a.scale, j);
+            if (!alone)
+                for (int b = 0; b < a.row_blocks; ++b) n += own_pieces(t, head, b).n;
+            return n;
         }
-        Running<S::HALVES> run;
-        run.reset();
-#pragma unroll 1
-        for (int i = 0; i < mine; ++i) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 2) : "memory");
-            stream_sync<WM>();
-            // (the tile that was used last is free: all warps of the stream are past it)
-            issue(i + S::STAGES - 1, next);
-            next = entry(i + S::STAGES);
-            const int stage = i % S::STAGES;
-#pragma unroll 1
-            for (int w = 0; w < WM; ++w) {
-                const int of = stream * WM + w;
-                const uint32_t ok = real[of * S::STAGES + stage];
-                const uint32_t keys = shared_address(stream_ring + (w * S::STAGES + stage) * S::STAGE);
-                if (ok)
-                    take_tile<KV, DP>(run, q, keys, keys + S::PLANE, scales + (of * S::STAGES + stage) * 32, ok, lane);
-            }
-        }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            run.l[u] += __shfl_xor_sync(0xFFFFFFFFu, run.l[u], 1);
-            run.l[u] += __shfl_xor_sync(0xFFFFFFFFu, run.l[u], 2);
-        }
-        stream_sync<WM>();
-        // every warp's results into its ring
-        float *const part = reinterpret_cast<float *>(my_ring);
-        float2 *const stats = reinterpret_cast<float2 *>(part + 16 * S::PITCH);
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int r = n + 8 * u;
-            if (j == 0) stats[r] = make_float2(run.m[u], run.l[u]);
-#pragma unroll
-            for (int h = 0; h < S::HALVES; ++h)
-#pragma unroll
-                for (int half = 0; half < 2; ++half)
-#pragma unroll
-                    for (int d = 0; d < 8; d += 4)
-                        *reinterpret_cast<float4 *>(part + r * S::PITCH + h * 64 + j * 16 + half * 8 + d) =
-                            make_float4(run.o[h][d][2 * u + half], run.o[h][d + 1][2 * u + half], run.o[h][d + 2][2 * u + half],
-                                        run.o[h][d + 3][2 * u + half]);
-        }
-        __syncthreads();
-        // joined over the streams: a thread takes eight dimensions of a row
-        const int n_rows = pair.shared ? STREAM_TOKENS : min(16, a.rows - pair.row_block * 16);
-        float *const to_part = a.parts + deal.slot(blockIdx.x, pair.first) * PART;
-        for (int i = threadIdx.x; i < n_rows * (DP / 8); i += ATTEND_THREADS) {
-            const int r = i / (DP / 8), d = (i % (DP / 8)) * 8;
-            const char *base = ring + (r / 16) * S::STAGES * S::STAGE;
-            float m = NEG_INFINITY, l = 0.0f, y[8] = {};
-            float2 st[STREAMS];
-#pragma unroll
-            for (int s = 0; s < STREAMS; ++s) {
-                const float *of = reinterpret_cast<const float *>(base + s * WM * S::STAGES * S::STAGE);
-                st[s] = reinterpret_cast<const float2 *>(of + 16 * S::PITCH)[r & 15];
-                m = fmaxf(m, st[s].x);
-            }
-#pragma unroll
-            for (int s = 0; s < STREAMS; ++s) {
-                const float *of = reinterpret_cast<const float *>(base + s * WM * S::STAGES * S::STAGE) + (r & 15) * S::PITCH + d;
-                const float w = st[s].x == NEG_INFINITY ? (st[s].y == 0.0f ? 0.0f : 1.0f) : power2(st[s].x - m);   // (a sum without maximum: NaN)
-                l += st[s].y * w;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] += of[e] * w;
-            }
-            int head, t = 0;
-            if (whole) {
-                t = row_of(pair, r, head);
-                if (t < 0) continue;
-            }
-            if (final) {
-                if (d < cache.head_dim) store_row<8>(t, head, d, m, l, y);
-                continue;
-            }
-            float *to_row = whole ? (pair.shared ? a.shared_rows : a.private_rows) + ((int64_t)t * a.n_q_heads + head) * PART_ROW
-                                  : to_part + r * PART_ROW;
-            *reinterpret_cast<float4 *>(to_row + d) = make_float4(y[0], y[1], y[2], y[3]);
-            *reinterpret_cast<float4 *>(to_row + d + 4) = make_float4(y[4], y[5], y[6], y[7]);
-            if (d == 0) *reinterpret_cast<float2 *>(to_row + DP) = make_float2(m, l);
-        }
+        return own_pieces(t, head, only).n;
+    }
+    __device__ __forceinline__ int64_t counter(int t, int head, int row_block) const {
+        return ((int64_t)t * cache.n_heads + head) * a.row_blocks + row_block;
+    }
+    // Says that a partial result is there, written by the threads that this one has synchronised with; whether it was the
+    // last.  (Release and acquire are the atomic's own: a fence of all lanes, with copies in flight, took microseconds.)
+    __device__ __forceinline__ bool arrive(int t, int head, int row_block) const {
+        int32_t *c = a.arrived + counter(t, head, row_block);
+        int32_t before;
+        asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(c) : "memory");
+        const bool last = before == expected(t, head, row_block) - 1;
+        if (last) *c = 0;
+        return last;
     }
 
     template <int N>
-    __device__ __forceinline__ void store_row(int t, int head, int d, float m, float l, const float (&y)[N]) {
+    __device__ __forceinline__ void store_row(int t, int head, int d, float m, float l, const float (&y)[N]) const {
         const float by = l == 0.0f ? 0.0f : 1.0f / l;
         uint32_t w[N / 2];
 #pragma unroll
@@ -641,235 +587,585 @@ struct Attend {
         if (a.lse && d == 0)
             a.lse[(int64_t)t * a.n_q_heads + head] = l == 0.0f ? NEG_INFINITY : (m + log2f(l)) * 0.693147180559945f;
     }
-
-    // The partial results of a row that belong to one pair: those of `n` workers from w on, or of the only one.
-    struct Pieces {
-        int32_t n, w;
-        int64_t first;        // the pair's
-        const float *only;
-    };
-
-    __device__ __forceinline__ Pieces pieces_of(int64_t first, int32_t units, const float *only) const {
-        if (units == 0) return {0, 0, 0, nullptr};
-        const int w = deal.owner(first);
-        return {deal.owner(first + units - 1) - w + 1, w, first, only};
+    static __device__ __forceinline__ void keep_row(float *row, int d, float m, float l, const float (&y)[8]) {
+        *reinterpret_cast<float4 *>(row + d) = make_float4(y[0], y[1], y[2], y[3]);
+        *reinterpret_cast<float4 *>(row + d + 4) = make_float4(y[4], y[5], y[6], y[7]);
+        if (d == 0) *reinterpret_cast<float2 *>(row + DP) = make_float2(m, l);
     }
-    __device__ __forceinline__ const float *piece(const Pieces &p, int i, int row) const {
-        return p.n == 1 ? p.only : a.parts + deal.slot(p.w + i, p.first) * PART + row * PART_ROW;
+    // A running maximum as an exponent of 2: with scales it is one already.
+    static __device__ __forceinline__ float scaled(float m, float factor) { return S::NARROW || m == NEG_INFINITY ? m : m * factor; }
+    // What a partial result counts beside maximum m.  (A sum without a maximum is NaN.)
+    static __device__ __forceinline__ float weight(float mi, float li, float m) {
+        return mi == NEG_INFINITY ? (li == 0.0f ? 0.0f : 1.0f) : power2(mi - m);
     }
 
-    // A row's partial results joined by a warp, x's (row rx of their slots) before z's.
-    __device__ __forceinline__ void join_row(int t, int head, const Pieces &x, int rx, const Pieces &z, int rz, int lane) {
+    // Rows r0 + step k < r1 of a token's and head's rows are joined by a warp, so many at a time, in the order of positions.
+    template <int AT_ONCE>
+    __device__ __forceinline__ void join_rows(int t, int head, int r0, int r1, int step, int lane) const {
         constexpr int PER = DP / 32;
-        const auto part = [&](int i) { return i < x.n ? piece(x, i, rx) : piece(z, i - x.n, rz); };
-        const int n = x.n + z.n;
-        float m = NEG_INFINITY, l = 0.0f, y[PER] = {};
-        for (int i0 = 0; i0 < n; i0 += 32) {
-            const int i = i0 + lane;
-            float mi = NEG_INFINITY, li = 0.0f;
-            if (i < n) {
-                const float2 st = __ldcg(reinterpret_cast<const float2 *>(part(i) + DP));
-                mi = st.x, li = st.y;
+        const int g = group_of(t), first_row = (t - g * a.group) * a.rows;
+        const bool alone = own_units(t) == 0, with_shared = SHARED_WARPS > 0 && shared_units(g) > 0;
+        while (r0 < r1) {
+            // rows of one block of rows, whose pieces are the same
+            int stop = r1;
+            Pieces x{0, 0, 0}, z{0, 0, 0};
+            if (with_shared) {
+                const int b = (first_row + r0) / ROWS;
+                x = shared_pieces(g, head, b);
+                stop = min(stop, (b + 1) * ROWS - first_row);
             }
-            float top = mi;
+            if (!alone) {
+                z = own_pieces(t, head, r0 / WARP_ROWS);
+                stop = min(stop, (r0 / WARP_ROWS + 1) * WARP_ROWS);
+            }
+            const int n_rows = min(AT_ONCE, (stop - r0 + step - 1) / step), n = x.n + z.n;
+            if (!(alone && x.n == 1)) {                         // (stored already)
+                const int64_t kept = ((int64_t)t * a.n_q_heads + head * a.rows + r0) * PART_ROW;
+                const float *const x0 = x.n == 1 ? a.shared_rows + kept : block_part(x.w, shared.begin(x.w) >= x.first ? 0 : 1, (first_row + r0) % ROWS);
+                const float *const z0 = z.n == 1 ? a.private_rows + kept
+                                                 : warp_part(z.w * a.together + head % a.together, own.begin(z.w) >= z.first ? 0 : 1, r0 % WARP_ROWS);
+                // (what is not a pair's first piece begins with its worker's share)
+                const auto part = [&](int i) -> const float * {
+                    if (i < x.n) return i == 0 ? x0 : block_part(x.w + i, 0, (first_row + r0) % ROWS);
+                    i -= x.n;
+                    return i == 0 ? z0 : warp_part((z.w + i) * a.together + head % a.together, 0, r0 % WARP_ROWS);
+                };
+                float m[AT_ONCE], l[AT_ONCE], y[AT_ONCE][PER] = {};
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-            top = fmaxf(top, m);
-            const float w = mi == NEG_INFINITY ? (li == 0.0f ? 0.0f : 1.0f) : power2(mi - top);   // (a sum without maximum: NaN)
-            const float old = m == NEG_INFINITY ? (l == 0.0f ? 0.0f : 1.0f) : power2(m - top);
-            float sum = li * w;
+                for (int k = 0; k < AT_ONCE; ++k) m[k] = NEG_INFINITY, l[k] = 0.0f;
+                for (int i0 = 0; i0 < n; i0 += 32) {
+                    const float *mine = i0 + lane < n ? part(i0 + lane) : nullptr;
+                    float w[AT_ONCE];
+                    float2 st[AT_ONCE];
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-            l = l * old + sum;
-            m = top;
+                    for (int k = 0; k < AT_ONCE; ++k)
+                        st[k] = mine && k < n_rows ? __ldcg(reinterpret_cast<const float2 *>(mine + k * step * PART_ROW + DP)) : make_float2(NEG_INFINITY, 0.0f);
 #pragma unroll
-            for (int e = 0; e < PER; ++e) y[e] *= old;
-            const int here = min(32, n - i0);
-#pragma unroll 4
-            for (int k = 0; k < here; ++k) {
-                const float by = __shfl_sync(0xFFFFFFFFu, w, k);
-                const float *p = part(i0 + k) + lane * PER;
+                    for (int k = 0; k < AT_ONCE; ++k) {
+                        float top = st[k].x;
 #pragma unroll
-                for (int e = 0; e < PER; e += 2) {
-                    const float2 f = __ldcg(reinterpret_cast<const float2 *>(p + e));
-                    y[e] += f.x * by, y[e + 1] += f.y * by;
+                        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                        top = fmaxf(top, m[k]);
+                        w[k] = weight(st[k].x, st[k].y, top);
+                        const float old = weight(m[k], l[k], top);
+                        float sum = st[k].y * w[k];
+#pragma unroll
+                        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+                        l[k] = l[k] * old + sum;
+                        m[k] = top;
+#pragma unroll
+                        for (int e = 0; e < PER; ++e) y[k][e] *= old;
+                    }
+                    const int here = min(32, n - i0);
+#pragma unroll(8 / AT_ONCE)
+                    for (int i = 0; i < here; ++i) {
+                        const float *p = reinterpret_cast<const float *>(__shfl_sync(0xFFFFFFFFu, (unsigned long long)(uintptr_t)mine, i)) + lane * PER;
+                        float2 f[AT_ONCE][PER / 2];
+#pragma unroll
+                        for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+                            for (int e = 0; e < PER / 2; ++e)
+                                f[k][e] = k < n_rows ? __ldcg(reinterpret_cast<const float2 *>(p + k * step * PART_ROW) + e) : make_float2(0.0f, 0.0f);
+#pragma unroll
+                        for (int k = 0; k < AT_ONCE; ++k) {
+                            const float by = __shfl_sync(0xFFFFFFFFu, w[k], i);
+#pragma unroll
+                            for (int e = 0; e < PER / 2; ++e) y[k][2 * e] += f[k][e].x * by, y[k][2 * e + 1] += f[k][e].y * by;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k)
+                    if (k < n_rows && lane * PER < cache.head_dim) store_row<PER>(t, head * a.rows + r0 + k * step, lane * PER, m[k], l[k], y[k]);
+            }
+            r0 += n_rows * step;
+        }
+    }
+
+    // ---- tiles ----
+    // A warp's tile: lane i knows the block of position `pos` of the tile (i % TILE).  Commits a group of copies.
+    __device__ __forceinline__ void copy_tile(int warp, int stage, bool live, int32_t block, uint32_t pos, int head, int lane) const {
+        uint32_t slot = 0xFFFFFFFFu;
+        if ((uint32_t)block < (uint32_t)cache.n_blocks)
+            slot = (uint32_t)block * cache.block.d + (pos - cache.block.quotient(pos) * cache.block.d);
+        const uint32_t ok = __ballot_sync(0xFFFFFFFFu, slot != 0xFFFFFFFFu) & S::ALL;
+        if (live) {
+            constexpr int AT_ONCE = 32 / S::CHUNKS;      // vectors that 32 lanes copy
+            const uint32_t width = (uint32_t)cache.head_dim * S::BYTES, step = width * (uint32_t)cache.n_heads;
+            const uint32_t keys = shared_address(ring + (warp * S::STAGES + stage) * S::STAGE), values = keys + S::PLANE;
+            const int c = lane % S::CHUNKS, r0 = lane / S::CHUNKS;
+            const uint64_t offset = (uint64_t)head * width + (uint32_t)c * 16;
+            const char *k = cache.k + offset, *v = cache.v + offset;
+            if (ok == S::ALL && width == S::CHUNKS * 16) {
+#pragma unroll
+                for (int it = 0; it < S::TILE / AT_ONCE; ++it) {
+                    const int r = it * AT_ONCE + r0;
+                    const uint64_t off = (uint64_t)__shfl_sync(0xFFFFFFFFu, slot, r) * step;
+                    copy16(keys + S::key_at(r, c), k + off);
+                    copy16(values + S::value_at(r, c), v + off);
+                }
+            } else {
+#pragma unroll 1
+                for (int it = 0; it < S::TILE / AT_ONCE; ++it) {
+                    const int r = it * AT_ONCE + r0;
+                    const uint32_t of = __shfl_sync(0xFFFFFFFFu, slot, r);
+                    const bool is = ((ok >> r) & 1u) && (uint32_t)c * 16 < width;
+                    const uint64_t off = (uint64_t)of * step;
+                    copy16(keys + S::key_at(r, c), is ? k + off : cache.k, is);
+                    copy16(values + S::value_at(r, c), is ? v + off : cache.v, is);
+                }
+            }
+            if constexpr (S::NARROW) {
+                const bool is = slot != 0xFFFFFFFFu;
+                const uint64_t at = is ? (uint64_t)slot * (uint32_t)cache.n_heads + head : 0;
+                const uint32_t to = shared_address(scales + (warp * S::STAGES + stage) * (2 * S::TILE) + lane % S::TILE);
+                if (S::TILE == 32 || lane < 16) copy4(to, cache.k_scale + at, is);
+                if (S::TILE == 32 || lane >= 16) copy4(to + S::TILE * 4, cache.v_scale + at, is);
+            }
+            if (lane == 0) real[warp * S::STAGES + stage] = ok;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    __device__ __forceinline__ int32_t entry(const int32_t *row, int pos, int to) const {   // anything but a block where there is none
+        return pos < to ? row[cache.block.quotient((uint32_t)pos)] : -1;
+    }
+    static __device__ __forceinline__ void wait_tile() { asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 2) : "memory"); }
+
+    // ---- pairs of whole blocks ----
+    // The token and query head of row i of a pair (token -1: none).
+    __device__ __forceinline__ int row_of(const Pair &p, int i, int &head) const {
+        const int r = p.row_block * ROWS + i, m = r / a.rows, t = p.group * a.group + m;
+        head = p.head * a.rows + (r - m * a.rows);
+        return m < a.group && t < a.n_tokens && book.end[t] > 0 ? t : -1;
+    }
+    static __device__ __forceinline__ void stream_sync() {     // the warps that work on the same tiles
+        static_assert(WM == 1 || WM == ATTEND_WARPS, "");
+        if constexpr (WM == 1)
+            __syncwarp();
+        else
+            __syncthreads();
+    }
+
+    // Units [u0, u1) of a pair.  Rows that nothing else belongs to are stored, others kept as partial results.
+    __device__ __forceinline__ void segment(const Pair &pair, int64_t u0, int64_t u1) const {
+        constexpr int STREAMS = ATTEND_WARPS / WM, STREAM = S::TILE * WM;
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
+        const int stream = warp / WM, wm = warp % WM;
+        const int from = pair.from + (int)(u0 - pair.first) * UNIT;
+        const int to = (int)min((int64_t)pair.to, (int64_t)pair.from + (u1 - pair.first) * UNIT);
+        const int tiles = tiles_of(from, to, STREAM);                                // of all streams
+        const int mine = tiles > stream ? (tiles - stream + STREAMS - 1) / STREAMS : 0;
+        const int32_t *row = a.table + pair.seq * a.stride;
+        const auto position = [&](int i) { return from + (i * STREAMS + stream) * STREAM + wm * S::TILE + lane % S::TILE; };
+        const auto block_at = [&](int i) { return i < mine ? entry(row, position(i), to) : -1; };
+        int32_t first_blocks[S::STAGES - 1];
+#pragma unroll
+        for (int i = 0; i < S::STAGES - 1; ++i) first_blocks[i] = block_at(i);
+        int32_t next = block_at(S::STAGES - 1);
+        Queries<KV, DP, NT> q;
+        int ends[NT][2], least = 0x7FFFFFFF;    // where the lane's rows end; the first of the warp's rows to end
+        {
+            const uint16_t *rows[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                int head;
+                const int t = row_of(pair, wm * WARP_ROWS + nt * 8 + n, head);
+                rows[nt] = t < 0 ? nullptr : a.q + t * a.q_stride + (int64_t)head * cache.head_dim;
+                if (GROUPED && t >= 0) least = min(least, book.end[t]);
+                if constexpr (GROUPED) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const int of = row_of(pair, wm * WARP_ROWS + nt * 8 + 2 * j + c, head);
+                        ends[nt][c] = of < 0 ? 0 : book.end[of];
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < S::STAGES - 1; ++i) copy_tile(warp, i, i < mine, first_blocks[i], (uint32_t)position(i), pair.head, lane);
+            q.load(rows, cache.head_dim, a.q_bf16, a.scale, j);
+            if constexpr (GROUPED) {
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) least = min(least, __shfl_xor_sync(0xFFFFFFFFu, least, o));
+            }
+        }
+        bool in[NT][2] = {};
+        Running<S::HALVES, NT> run;
+        run.reset();
+#pragma unroll 1
+        for (int i = 0; i < mine; ++i) {
+            wait_tile();
+            stream_sync();
+            // (the tile that was used last is free: all warps of the stream are past it)
+            copy_tile(warp, (i + S::STAGES - 1) % S::STAGES, i + S::STAGES - 1 < mine, next, (uint32_t)position(i + S::STAGES - 1), pair.head, lane);
+            next = block_at(i + S::STAGES);
+            const int stage = i % S::STAGES;
+#pragma unroll 1
+            for (int w = 0; w < WM; ++w) {
+                const int of = (stream * WM + w) * S::STAGES + stage;
+                const uint32_t ok = real[of];
+                if (!ok) continue;
+                const uint32_t keys = shared_address(ring + of * S::STAGE);
+                const int at = from + (i * STREAMS + stream) * STREAM + w * S::TILE;
+                if (!GROUPED || at + S::TILE <= least) {
+                    take_tile<KV, DP, NT, false>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in);
+                    continue;
+                }
+                // rows that end within the tile, or before it, go by themselves
+                int past = at;
+#pragma unroll 1
+                while (true) {
+                    int e = 0x7FFFFFFF;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+                            if (min(ends[nt][c], at + S::TILE) > past) e = min(e, min(ends[nt][c], at + S::TILE));
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) e = min(e, __shfl_xor_sync(0xFFFFFFFFu, e, o));
+                    if (e == 0x7FFFFFFF) break;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) in[nt][c] = min(ends[nt][c], at + S::TILE) == e;
+                    take_tile<KV, DP, NT, true>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok & ((2u << (e - at - 1)) - 1u), n, j, in);
+                    past = e;
                 }
             }
         }
-        if (lane * PER < cache.head_dim) store_row<PER>(t, head, lane * PER, m, l, y);
-    }
-
-    // This block's part of a pair, or of all pairs of a group and head, is written.  Whoever is the last to say so of
-    // `expected` joins them.
-    __device__ __forceinline__ bool arrive(int64_t counter, int expected, int *flag) {
-        __threadfence();
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        run.sum_up();
+        stream_sync();
+        // every warp's results into its ring
+        float *const part = reinterpret_cast<float *>(ring + warp * S::STAGES * S::STAGE);
+        float2 *const stats = reinterpret_cast<float2 *>(part + WARP_ROWS * S::PITCH);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int r = nt * 8 + 2 * j + c;
+                if (n == 0) stats[r] = make_float2(scaled(run.m[nt][c], q.factor[nt][c]), run.l[nt][c]);
+#pragma unroll
+                for (int h = 0; h < S::HALVES; ++h) {
+                    float y[8];
+                    run.eight(h, nt, c, y);
+                    float4 *to = reinterpret_cast<float4 *>(part + r * S::PITCH + h * 64 + n * 8);
+                    to[0] = make_float4(y[0], y[1], y[2], y[3]), to[1] = make_float4(y[4], y[5], y[6], y[7]);
+                }
+            }
         __syncthreads();
-        if (threadIdx.x == 0) {
-            const int before = atomicAdd(a.arrived + counter, 1);
-            const bool last = before == expected - 1;
-            if (last) a.arrived[counter] = 0;
-            *flag = last;
+        // joined over the streams: a thread takes eight dimensions of a row
+        const bool whole = u0 == pair.first && u1 == pair.first + pair.units;
+        const int which = shared.begin(blockIdx.x) >= pair.first ? 0 : 1;
+        const int n_rows = min(ROWS, a.group * a.rows - pair.row_block * ROWS);
+        for (int i = threadIdx.x; i < n_rows * (DP / 8); i += ATTEND_THREADS) {
+            const int r = i / (DP / 8), d = (i % (DP / 8)) * 8, in_warp = r % WARP_ROWS;
+            const char *base = ring + (r / WARP_ROWS) * S::STAGES * S::STAGE;
+            float m = NEG_INFINITY, l = 0.0f, y[8] = {};
+            float2 st[STREAMS];
+#pragma unroll
+            for (int s = 0; s < STREAMS; ++s) {
+                const float *of = reinterpret_cast<const float *>(base + s * WM * S::STAGES * S::STAGE);
+                st[s] = reinterpret_cast<const float2 *>(of + WARP_ROWS * S::PITCH)[in_warp];
+                m = fmaxf(m, st[s].x);
+            }
+#pragma unroll
+            for (int s = 0; s < STREAMS; ++s) {
+                const float *of = reinterpret_cast<const float *>(base + s * WM * S::STAGES * S::STAGE) + in_warp * S::PITCH + d;
+                const float w = weight(st[s].x, st[s].y, m);
+                l += st[s].y * w;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] += of[e] * w;
+            }
+            int head;
+            const int t = row_of(pair, r, head);
+            if (t < 0) continue;
+            if (!whole)
+                keep_row(block_part(blockIdx.x, which, r), d, m, l, y);
+            else if (own_units(t) > 0)
+                keep_row(a.shared_rows + ((int64_t)t * a.n_q_heads + head) * PART_ROW, d, m, l, y);
+            else if (d < cache.head_dim)
+                store_row<8>(t, head, d, m, l, y);
+        }
+        // tokens that have more than this
+        __syncthreads();
+        const int r0 = pair.row_block * ROWS, m0 = r0 / a.rows, m1 = (r0 + n_rows - 1) / a.rows;
+        if ((int)threadIdx.x <= m1 - m0) {
+            const int t = pair.group * a.group + m0 + (int)threadIdx.x;
+            const bool more = t < a.n_tokens && book.end[t] > 0 && (!whole || own_units(t) > 0);
+            book.last[threadIdx.x] = more && arrive(t, pair.head, 0);
         }
         __syncthreads();
-        const bool last = *flag != 0;
-        if (last) __threadfence();
-        return last;
-    }
-};
-
-// Registers: 64 (o) + 32 (queries) + loads at 128 dimensions; two blocks of four warps on an SM.
-template <typename KV, int DP, int WMS, bool GROUPED>
-__global__ void __launch_bounds__(ATTEND_THREADS, Shape<KV, DP>::BLOCKS)
-attend_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ AttendArgs a) {
-    using S = Shape<KV, DP>;
-    extern __shared__ __align__(128) char ring[];
-    __shared__ int64_t upto[MAX_GROUPS + 1];      // units before a group
-    __shared__ int64_t scan[ATTEND_WARPS];
-    __shared__ float scales[S::NARROW ? ATTEND_WARPS * S::STAGES * 32 : 1];
-    __shared__ uint32_t real[ATTEND_WARPS * S::STAGES];
-    __shared__ int flag;
-    attend_enter();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t total = 0;
-    for (int g0 = 0; g0 < a.n_groups; g0 += ATTEND_THREADS) {
-        const int g = g0 + (int)threadIdx.x;
-        int64_t n = 0;
-        if constexpr (GROUPED) {
-            if (g < a.n_groups) n = a.units[g];
+        // (a warp per token; the rows of a single one are dealt out)
+        if (m0 == m1) {
+            if (book.last[0]) join_rows<1>(pair.group * a.group + m0, pair.head, warp, a.rows, ATTEND_WARPS, lane);
         } else {
-            bool nothing = false;
-            if (g < a.n_groups) {
-                const Seen r = seen_by(a, cache, g);
-                n = (int64_t)units_of(r.first, r.end) * a.row_blocks * cache.n_heads;
-                nothing = r.end == 0 && g % gridDim.x == blockIdx.x;
-            }
-            uint32_t which = __ballot_sync(0xFFFFFFFFu, nothing);
-            while (which) {
-                const int i = __ffs(which) - 1;
-                which &= which - 1;
-                store_nothing(a, cache, g0 + warp * 32 + i, lane, 32);
-            }
+            for (int m = warp; m <= m1 - m0; m += ATTEND_WARPS)
+                if (book.last[m]) join_rows<4>(pair.group * a.group + m0 + m, pair.head, 0, a.rows, 1, lane);
         }
-        int64_t x = n;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t y = __shfl_up_sync(0xFFFFFFFFu, x, o);
-            if (lane >= o) x += y;
-        }
-        if (lane == 31) scan[warp] = x;
-        __syncthreads();
-        int64_t before = total;
-#pragma unroll
-        for (int w = 0; w < ATTEND_WARPS; ++w) {
-            if (w < warp) before += scan[w];
-            total += scan[w];
-        }
-        if (g < a.n_groups) upto[g] = before + x - n;
-        __syncthreads();
+        __syncthreads();      // the rings are free again
     }
-    if (threadIdx.x == 0) upto[a.n_groups] = total;
-    __syncthreads();
-    if (total == 0) return;
-    const int32_t workers = (int32_t)min((int64_t)gridDim.x, total);
-    if ((int)blockIdx.x >= workers) return;
-    const int32_t shared_row_blocks = GROUPED ? (a.group * a.rows + 16 * WMS - 1) / (16 * WMS) : 0;
-    Attend<KV, DP, WMS, GROUPED> at{cache, a, ring, scales, real, Deal{total, workers}, shared_row_blocks};
-    int64_t u = at.deal.begin(blockIdx.x);
-    const int64_t end = at.deal.begin(blockIdx.x + 1);
-    int g = 0;
-    {
-        int lo = 0, hi = a.n_groups;              // the last g with upto[g] <= u
+
+    __device__ __forceinline__ void work_on_pairs() const {
+        if ((int)blockIdx.x >= shared.workers) return;
+        int64_t u = shared.begin(blockIdx.x);
+        const int64_t end = shared.begin(blockIdx.x + 1);
+        int g = find(book.shared_upto, a.n_groups, u);
+#pragma unroll 1
+        while (u < end) {
+            while (book.shared_upto[g + 1] <= u) ++g;
+            Pair p;
+            p.units = shared_units(g);
+            const int i = (int)((u - book.shared_upto[g]) / p.units);
+            p.first = book.shared_upto[g] + (int64_t)i * p.units;
+            p.group = g;
+            p.head = i / shared_row_blocks, p.row_block = i % shared_row_blocks;
+            p.from = GROUPED ? 0 : book.from[g], p.to = book.to[g];
+            // (the token that goes furthest has all of the shared positions in its table)
+            int t = g * a.group;
+            if constexpr (GROUPED)
+                for (int m = 1; m < a.group && g * a.group + m < a.n_tokens; ++m)
+                    if (book.end[g * a.group + m] > book.end[t]) t = g * a.group + m;
+            p.seq = book.seq[t];
+            const int64_t stop = min(end, p.first + p.units);
+            segment(p, u, stop);
+            u = stop;
+        }
+    }
+
+    // The last i < n with upto[i] <= u.
+    static __device__ __forceinline__ int find(const int64_t *upto, int n, int64_t u) {
+        int lo = 0, hi = n;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (upto[mid] <= u) lo = mid; else hi = mid;
         }
-        g = lo;
+        return lo;
     }
-#pragma unroll 1
-    while (u < end) {
-        while (upto[g + 1] <= u) ++g;
-        const int64_t o = u - upto[g];
-        Pair p{};
-        Group group;
-        if constexpr (GROUPED) {
-            group.load(a, cache, g, shared_row_blocks, lane);
-            const int64_t n_shared = (int64_t)group.shared_units * shared_row_blocks * cache.n_heads;
-            if (o < n_shared) {
-                const int i = (int)(o / group.shared_units);
-                const uint32_t live = __ballot_sync(0xFFFFFFFFu, group.seen.end > 0);
-                p.shared = true;
-                p.first = upto[g] + (int64_t)i * group.shared_units;
-                p.units = group.shared_units;
-                p.token = g * a.group;
-                p.head = i / shared_row_blocks, p.row_block = i % shared_row_blocks;
-                p.from = 0, p.to = group.shared_to;
-                p.seq = __shfl_sync(0xFFFFFFFFu, group.seen.s, __ffs(live) - 1);
-            } else {
-                const int64_t size = (int64_t)group.units * a.row_blocks * cache.n_heads;
-                const int m = __ffs(__ballot_sync(0xFFFFFFFFu, o >= group.offset && o < group.offset + size)) - 1;
-                const int32_t units = __shfl_sync(0xFFFFFFFFu, group.units, m);
-                const int64_t off = __shfl_sync(0xFFFFFFFFu, group.offset, m);
-                const int i = (int)((o - off) / units);
-                p.first = upto[g] + off + (int64_t)i * units;
-                p.units = units;
-                p.token = g * a.group + m;
-                p.head = i / a.row_blocks, p.row_block = i % a.row_blocks;
-                p.from = max(__shfl_sync(0xFFFFFFFFu, group.seen.first, m), group.shared_to);
-                p.to = __shfl_sync(0xFFFFFFFFu, group.seen.end, m);
-                p.seq = __shfl_sync(0xFFFFFFFFu, group.seen.s, m);
+
+    // ---- pairs of single warps ----
+    // A warp's place in its share: tile i of n of a token and one of its runs (key heads by row blocks).
+    struct Place {
+        int t, run, i, n, from, end;
+        const int32_t *row;
+    };
+    __device__ __forceinline__ void enter(Place &p) const {      // token p.t
+        p.from = book.from[p.t], p.end = book.end[p.t];
+        p.n = own_units(p.t);
+        p.row = a.table + book.seq[p.t] * a.stride;
+    }
+    __device__ __forceinline__ Place place(int64_t u) const {
+        Place p;
+        p.t = find(book.upto, a.n_tokens, u);
+        while (book.upto[p.t + 1] <= u) ++p.t;
+        enter(p);
+        const int64_t o = u - book.upto[p.t];
+        p.run = (int)(o / p.n);
+        p.i = (int)(o - (int64_t)p.run * p.n);
+        return p;
+    }
+    // `runs`: of a token
+    __device__ __forceinline__ void step(Place &p, int runs) const {
+        if (++p.i < p.n) return;
+        p.i = 0;
+        if (++p.run < runs) return;
+        p.run = 0;
+        do ++p.t;
+        while (p.t < a.n_tokens && book.upto[p.t + 1] == book.upto[p.t]);
+        if (p.t < a.n_tokens) enter(p);
+    }
+
+    // Every warp by itself: the tiles of its share one after the other, whatever they belong to, with copies always
+    // STAGES - 1 tiles ahead.  Warps of a block have neighbouring key heads of the same positions where there are enough heads, so
+    // that what they read lies together.
+    __device__ __forceinline__ void work_alone() const {
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
+        const int id = ((int)blockIdx.x - shared_blocks) * ATTEND_WARPS + warp;
+        const int worker = id / a.together, sub = id - worker * a.together;
+        if (worker >= own.workers) return;
+        const int64_t begin = own.begin(worker), end = own.begin(worker + 1);
+        const int runs = cache.n_heads / a.together * a.row_blocks;
+        const auto head_of = [&](int run) { return (a.row_blocks == 1 ? run : run / a.row_blocks) * a.together + sub; };
+        Place front = place(begin), at = front;
+        int64_t ahead = begin;                 // the unit of `front`
+        int32_t blocks[S::STAGES];
+        int pos[S::STAGES], heads[S::STAGES];
+        const auto fetch = [&](int32_t &block, int &p, int &head) {    // the table's entry of the tile in front
+            block = -1;
+            if (ahead < end) {
+                p = front.from + front.i * S::TILE + lane % S::TILE;
+                head = head_of(front.run);
+                block = entry(front.row, p, front.end);
+                step(front, runs);
             }
-        } else {
-            const Seen r = seen_by(a, cache, g);
-            p.units = units_of(r.first, r.end);
-            const int i = (int)(o / p.units);
-            p.first = upto[g] + (int64_t)i * p.units;
-            p.token = g;
-            p.head = i / a.row_blocks, p.row_block = i % a.row_blocks;
-            p.from = r.first, p.to = r.end, p.seq = r.s;
-        }
-        const int64_t stop = min(end, p.first + p.units);
-        bool with_shared = false;
-        if constexpr (GROUPED) with_shared = group.shared_to > 0;     // (then all of the group's pairs of a head are joined)
-        const bool whole = u == p.first && stop == p.first + p.units, final = whole && !with_shared;
-        if (GROUPED && p.shared)
-            at.template segment<WMS>(p, u, stop, whole, final);
-        else
-            at.template segment<1>(p, u, stop, whole, final);
-        if (!final && !with_shared) {
-            const auto all = at.pieces_of(p.first, p.units, nullptr);
-            if (at.arrive(((int64_t)p.token * cache.n_heads + p.head) * a.row_blocks + p.row_block, all.n, &flag)) {
-                const int rows = min(16, a.rows - p.row_block * 16);
-                for (int r = warp; r < rows; r += ATTEND_WARPS)
-                    at.join_row(p.token, p.head * a.rows + p.row_block * 16 + r, all, r, {0, 0, 0, nullptr}, 0, lane);
-            }
-        }
-        if constexpr (GROUPED) {
-            if (with_shared) {
-                const int64_t shared_first = upto[g] + (int64_t)p.head * shared_row_blocks * group.shared_units;
-                const int64_t own_first = upto[g] + group.offset + (int64_t)p.head * a.row_blocks * group.units;   // (of the lane's member)
-                int expected = 0, own = 0;
-                for (int b = 0; b < shared_row_blocks; ++b)
-                    expected += at.pieces_of(shared_first + (int64_t)b * group.shared_units, group.shared_units, nullptr).n;
-                for (int b = 0; b < a.row_blocks; ++b) own += at.pieces_of(own_first + (int64_t)b * group.units, group.units, nullptr).n;
+            ++ahead;
+        };
 #pragma unroll
-                for (int d = 16; d > 0; d >>= 1) own += __shfl_xor_sync(0xFFFFFFFFu, own, d);
-                if (at.arrive(((int64_t)g * a.group * cache.n_heads + p.head) * a.row_blocks, expected + own, &flag)) {
-                    for (int r = warp; r < a.group * a.rows; r += ATTEND_WARPS) {
-                        const int m = r / a.rows, of = r - m * a.rows, t = g * a.group + m, head = p.head * a.rows + of;
-                        const int64_t first = __shfl_sync(0xFFFFFFFFu, own_first, m);
-                        const int32_t units = __shfl_sync(0xFFFFFFFFu, group.units, m);
-                        if (__shfl_sync(0xFFFFFFFFu, group.seen.end, m) == 0) continue;
-                        const int64_t row = ((int64_t)t * a.n_q_heads + head) * at.PART_ROW;
-                        const int rb = r / at.ROWS;
-                        at.join_row(t, head, at.pieces_of(shared_first + (int64_t)rb * group.shared_units, group.shared_units, a.shared_rows + row),
-                                    r - rb * at.ROWS, at.pieces_of(first + (int64_t)(of / 16) * units, units, a.private_rows + row), of % 16, lane);
-                    }
+        for (int i = 0; i < S::STAGES; ++i) fetch(blocks[i], pos[i], heads[i]);
+#pragma unroll
+        for (int i = 0; i < S::STAGES - 1; ++i) copy_tile(warp, i, begin + i < end, blocks[i], (uint32_t)pos[i], heads[i], lane);
+        int32_t block = blocks[S::STAGES - 1];
+        int p = pos[S::STAGES - 1], p_head = heads[S::STAGES - 1];
+        Queries<KV, DP, NT> q;
+        Running<S::HALVES, NT> run;
+        const bool in[NT][2] = {};
+        int stage = 0, head = 0, row0 = 0;
+        bool fresh = true;
+#pragma unroll 1
+        for (int64_t u = begin; u < end; ++u) {
+            if (fresh) {
+                head = head_of(at.run), row0 = at.run % a.row_blocks * WARP_ROWS;
+                const uint16_t *rows[NT];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int r = row0 + nt * 8 + n;
+                    rows[nt] = r < a.rows ? a.q + at.t * a.q_stride + (int64_t)(head * a.rows + r) * cache.head_dim : nullptr;
+                }
+                q.load(rows, cache.head_dim, a.q_bf16, a.scale, j);
+                run.reset();
+            }
+            wait_tile();
+            __syncwarp();
+            copy_tile(warp, stage == 0 ? S::STAGES - 1 : stage - 1, ahead <= end, block, (uint32_t)p, p_head, lane);
+            fetch(block, p, p_head);
+            const int of = warp * S::STAGES + stage;
+            const uint32_t ok = real[of], keys = shared_address(ring + of * S::STAGE);
+            if (ok) take_tile<KV, DP, NT, false>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in);
+            if (++stage == S::STAGES) stage = 0;
+            fresh = at.i == at.n - 1;
+            if (fresh || u + 1 == end) finish(run, q, at, u, begin, end, id, head, row0, n, j, lane);
+            step(at, runs);
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+
+    __device__ __forceinline__ void finish(Running<S::HALVES, NT> &run, const Queries<KV, DP, NT> &q, const Place &at, int64_t u, int64_t begin,
+                                           int64_t end, int id, int head, int row0, int n, int j, int lane) const {
+        const int64_t first = u - at.i;
+        const bool whole = first >= begin && first + at.n <= end;
+        const bool more = GROUPED && shared_units(group_of(at.t)) > 0;
+        const int which = begin >= first ? 0 : 1;
+        run.sum_up();
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int r = row0 + nt * 8 + 2 * j + c, q_head = head * a.rows + r;
+                if (r >= a.rows) continue;
+                float *kept = whole ? a.private_rows + ((int64_t)at.t * a.n_q_heads + q_head) * PART_ROW : warp_part(id, which, r - row0);
+                const float m = scaled(run.m[nt][c], q.factor[nt][c]);
+#pragma unroll
+                for (int h = 0; h < S::HALVES; ++h) {
+                    const int d = h * 64 + n * 8;
+                    float y[8];
+                    run.eight(h, nt, c, y);
+                    if (!whole || more)
+                        keep_row(kept, d, m, run.l[nt][c], y);
+                    else if (d < cache.head_dim)
+                        store_row<8>(at.t, q_head, d, m, run.l[nt][c], y);
                 }
             }
-        }
-        u = stop;
-        __syncthreads();      // the rings are free again
+        if (whole && !more) return;
+        __syncwarp();
+        int last = 0;
+        if (lane == 0) last = arrive(at.t, head, more ? 0 : row0 / WARP_ROWS);
+        last = __shfl_sync(0xFFFFFFFFu, last, 0);
+        if (last) join_rows<4>(at.t, head, more ? 0 : row0, more ? a.rows : min(a.rows, row0 + WARP_ROWS), 1, lane);
     }
+};
+
+// Prefix sums of one number a thread over the block, for as many rounds as it takes: `before` everything so far.
+__device__ __forceinline__ int64_t sums_before(int64_t n, int64_t &total, int64_t *scan) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int64_t x = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        if (lane >= o) x += y;
+    }
+    if (lane == 31) scan[warp] = x;
+    __syncthreads();
+    int64_t before = total;
+#pragma unroll
+    for (int w = 0; w < ATTEND_WARPS; ++w) {
+        if (w < warp) before += scan[w];
+        total += scan[w];
+    }
+    __syncthreads();
+    return before + x - n;
+}
+
+template <typename KV, int DP, int SHARED_WARPS, bool GROUPED, int NT>
+__global__ void __launch_bounds__(ATTEND_THREADS, Shape<KV, DP>::BLOCKS)
+attend_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ AttendArgs a) {
+    using S = Shape<KV, DP>;
+    using A = Attend<KV, DP, SHARED_WARPS, GROUPED, NT>;
+    extern __shared__ __align__(128) char ring[];
+    __shared__ Book book;
+    __shared__ int64_t scan[ATTEND_WARPS];
+    __shared__ float scales[S::NARROW ? ATTEND_WARPS * S::STAGES * 2 * S::TILE : 1];
+    __shared__ uint32_t real[ATTEND_WARPS * S::STAGES];
+    attend_enter();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    A at{cache, a, book, ring, scales, real, Deal{0, 0}, Deal{0, 0}, 0, GROUPED ? (a.group * a.rows + A::ROWS - 1) / A::ROWS : a.row_blocks};
+    int64_t shared = 0, own = 0;
+    for (int t0 = 0; t0 < a.n_tokens; t0 += ATTEND_THREADS) {
+        const int t = t0 + (int)threadIdx.x;
+        int64_t n = 0;
+        bool nothing = false;
+        if (t < a.n_tokens) {
+            const Seen r = seen_by(a, cache, t);
+            nothing = r.end == 0 && t % gridDim.x == blockIdx.x;
+            book.seq[t] = r.s, book.end[t] = r.end;
+            book.from[t] = GROUPED ? max(r.first, a.shared[t / a.group]) : r.first;
+            if (!GROUPED) book.to[t] = r.end;
+            n = (int64_t)(GROUPED || SHARED_WARPS == 0 ? at.own_units(t) * (cache.n_heads / a.together) : at.shared_units(t) * cache.n_heads) * a.row_blocks;
+        }
+        uint32_t which = __ballot_sync(0xFFFFFFFFu, nothing);
+        while (which) {          // tokens without a row, by whole warps
+            const int i = t0 + warp * 32 + __ffs(which) - 1;
+            which &= which - 1;
+            uint4 *row = reinterpret_cast<uint4 *>(a.out + i * a.out_stride);
+            for (int c = lane; c < a.n_q_heads * cache.head_dim / 8; c += 32) row[c] = make_uint4(0, 0, 0, 0);
+            if (a.lse)
+                for (int c = lane; c < a.n_q_heads; c += 32) a.lse[(int64_t)i * a.n_q_heads + c] = NEG_INFINITY;
+        }
+        if (GROUPED || SHARED_WARPS == 0) {
+            const int64_t before = sums_before(n, own, scan);
+            if (t < a.n_tokens) book.upto[t] = before;
+        } else {
+            const int64_t before = sums_before(n, shared, scan);
+            if (t < a.n_tokens) book.shared_upto[t] = before;
+        }
+    }
+    if constexpr (GROUPED) {
+        for (int g0 = 0; g0 < a.n_groups; g0 += ATTEND_THREADS) {
+            const int g = g0 + (int)threadIdx.x;
+            int64_t n = 0;
+            if (g < a.n_groups) {
+                book.to[g] = a.shared[g];
+                n = (int64_t)at.shared_units(g) * at.shared_row_blocks * cache.n_heads;
+            }
+            const int64_t before = sums_before(n, shared, scan);
+            if (g < a.n_groups) book.shared_upto[g] = before;
+        }
+    }
+    if (threadIdx.x == 0) book.upto[a.n_tokens] = own, book.shared_upto[a.n_groups] = shared;
+    __syncthreads();
+    // Blocks for the shared and for the tokens' own positions, by how many of them there are (in tiles of a head).
+    int64_t blocks = GROUPED ? 0 : SHARED_WARPS > 0 ? (int64_t)gridDim.x : 0;
+    if (GROUPED && shared > 0) {
+        const int64_t x = shared * ATTEND_WARPS, y = own * a.together;
+        blocks = own == 0 ? (int64_t)gridDim.x : min(max((int64_t)gridDim.x * x / (x + y), (int64_t)1), (int64_t)gridDim.x - 1);
+    }
+    at.shared_blocks = (int32_t)blocks;
+    at.shared = Deal{shared, (int32_t)min(blocks, shared)};
+    at.own = Deal{own, (int32_t)min(((int64_t)gridDim.x - blocks) * ATTEND_WARPS / a.together, own)};
+    if constexpr (SHARED_WARPS > 0)
+        if ((int)blockIdx.x < at.shared_blocks) {
+            at.work_on_pairs();
+            return;
+        }
+    if constexpr (GROUPED || SHARED_WARPS == 0) at.work_alone();
 }
 
 }  // namespace

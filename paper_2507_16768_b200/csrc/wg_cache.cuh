@@ -23,6 +23,7 @@ inline bool cache_ok(const wg_kv_cache *c) {
     const bool narrow = c->storage >= WG_KV_E4M3;
     if (narrow != (c->k_scale != nullptr) || narrow != (c->v_scale != nullptr)) return false;
     if (c->n_blocks < 1 || c->n_blocks > (1 << 30) || c->block_size < 1 || c->block_size > (1 << 30)) return false;
+    if ((int64_t)c->n_blocks * c->block_size >= (1ll << 32)) return false;      // (slots are counted in 32 bits)
     if (c->n_heads < 1 || c->n_heads > 1024 || c->head_dim < 16 || c->head_dim > WG_KV_MAX_HEAD_DIM || c->head_dim % 16) return false;
     return (((uintptr_t)c->k | (uintptr_t)c->v) & 15) == 0 && (((uintptr_t)c->k_scale | (uintptr_t)c->v_scale) & 3) == 0;
 }
@@ -60,8 +61,12 @@ struct Int8 {};
 
 // Two neighbouring codes of a word as a pair of fp16 (exact for both types).  `pair`: 0 or 1.
 __device__ __forceinline__ uint32_t codes_to_half2(uint32_t w, int pair, E4m3) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(pair ? w >> 16 : w & 0xFFFFu), __NV_E4M3);
-    return (uint32_t)h.x | ((uint32_t)h.y << 16);
+    uint32_t y;
+    if (pair)
+        asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, hi; }" : "=r"(y) : "r"(w));
+    else
+        asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, lo; }" : "=r"(y) : "r"(w));
+    return y;
 }
 __device__ __forceinline__ uint32_t codes_to_half2(uint32_t w, int pair, Int8) {
     // 0x6400 + u is 1024 + u in fp16 for a byte u = code + 128
