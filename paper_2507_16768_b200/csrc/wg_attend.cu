@@ -5,8 +5,9 @@
 
 struct wg_attend {
     int32_t max_tokens = 0, n_q_heads = 0, n_heads = 0, head_dim = 0;
-    int32_t *shared = nullptr, *arrived = nullptr;
-    float *parts = nullptr, *shared_rows = nullptr, *private_rows = nullptr;
+    int32_t *shared = nullptr;
+    int2 *shared_cuts = nullptr, *own_cuts = nullptr;
+    float *block_parts = nullptr, *warp_parts = nullptr, *shared_rows = nullptr, *own_rows = nullptr;
 };
 
 namespace {
@@ -14,7 +15,19 @@ namespace {
 // A row of partial results: the head size as the kernels round it, a maximum and a sum.
 int64_t part_row(int32_t head_dim) { return (head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256) + 4; }
 
+template <int DP>
+int32_t launch_join(const CacheDev &c, const AttendArgs &a, cudaStream_t st) {
+    const dim3 grid((unsigned)((a.n_q_heads + ATTEND_WARPS - 1) / ATTEND_WARPS), (unsigned)a.n_tokens);
+    WG_CUDA(launch_pdl(attend_join_kernel<DP>, grid, dim3(ATTEND_THREADS), st, c, a));
+    WG_LAUNCHED();
+    return WG_OK;
+}
+
 }  // namespace
+
+int32_t attend_join(const CacheDev &c, const AttendArgs &a, int head_dim, cudaStream_t st) {
+    return head_dim == 64 ? launch_join<64>(c, a, st) : head_dim == 128 ? launch_join<128>(c, a, st) : launch_join<256>(c, a, st);
+}
 
 extern "C" {
 
@@ -28,20 +41,18 @@ int32_t wg_attend_create(int32_t max_tokens, int32_t n_q_heads, int32_t n_heads,
     wg_attend *p = new (std::nothrow) wg_attend();
     if (!p) return WG_ERR_ARG;
     p->max_tokens = max_tokens, p->n_q_heads = n_q_heads, p->n_heads = n_heads, p->head_dim = head_dim;
-    const size_t counters = (size_t)max_tokens * n_heads * ((n_q_heads / n_heads + 15) / 16);
-    const size_t rows = (size_t)max_tokens * n_q_heads * part_row(head_dim);
-    const size_t parts = (size_t)sm_count() * 2 * PART_ROWS * part_row(head_dim);
+    const int32_t group_rows = n_q_heads / n_heads, part_rows = group_rows < 16 ? group_rows : 16;
+    const size_t row = part_row(head_dim), blocks = (size_t)sm_count() * 2, warps = blocks * ATTEND_WARPS;
+    const size_t rows = (size_t)max_tokens * n_q_heads * row;
+    // (pairs of a launch: a token's blocks of rows have 8 rows at least, a group's shared ones 16)
+    const size_t pairs = (size_t)MAX_TOKENS * n_heads * ((group_rows + 7) / 8);
     int32_t rc = dev_alloc(&p->shared, (size_t)MAX_TOKENS);
-    if (rc == WG_OK) rc = dev_alloc(&p->arrived, counters);
-    if (rc == WG_OK) rc = dev_alloc(&p->parts, parts);
+    if (rc == WG_OK) rc = dev_alloc(&p->shared_cuts, pairs);
+    if (rc == WG_OK) rc = dev_alloc(&p->own_cuts, pairs);
+    if (rc == WG_OK) rc = dev_alloc(&p->block_parts, blocks * 2 * PART_ROWS * row);
+    if (rc == WG_OK) rc = dev_alloc(&p->warp_parts, warps * 2 * part_rows * row);
     if (rc == WG_OK) rc = dev_alloc(&p->shared_rows, rows);
-    if (rc == WG_OK) rc = dev_alloc(&p->private_rows, rows);
-    // (the memory is set on the default stream, which other streams do not wait for)
-    if (rc == WG_OK && (cudaMemset(p->arrived, 0, counters * sizeof(int32_t)) != cudaSuccess ||
-                        cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess)) {
-        g_last_cuda_error = (int32_t)cudaGetLastError();
-        rc = WG_ERR_CUDA;
-    }
+    if (rc == WG_OK) rc = dev_alloc(&p->own_rows, rows);
     if (rc != WG_OK) {
         wg_attend_free(p);
         return rc;
@@ -52,7 +63,7 @@ int32_t wg_attend_create(int32_t max_tokens, int32_t n_q_heads, int32_t n_heads,
 
 void wg_attend_free(wg_attend *p) {
     if (!p) return;
-    for (void *q : {(void *)p->shared, (void *)p->arrived, (void *)p->parts, (void *)p->shared_rows, (void *)p->private_rows})
+    for (void *q : {(void *)p->shared, (void *)p->shared_cuts, (void *)p->own_cuts, (void *)p->block_parts, (void *)p->warp_parts, (void *)p->shared_rows, (void *)p->own_rows})
         cudaFree(q);
     delete p;
 }
@@ -96,8 +107,9 @@ int32_t wg_kv_attend(wg_attend *attend, const wg_kv_cache *cache, const void *q,
         a.q_bf16 = dtype == WG_DTYPE_BF16;
         a.scale = scale * 1.44269504088896f;
         a.together = cache->n_heads % 4 == 0 ? 4 : cache->n_heads % 2 == 0 ? 2 : 1;
-        a.shared = attend->shared, a.arrived = attend->arrived;
-        a.parts = attend->parts, a.shared_rows = attend->shared_rows, a.private_rows = attend->private_rows;
+        a.part_rows = rows < 16 ? rows : 16;
+        a.shared = attend->shared, a.shared_cuts = attend->shared_cuts, a.own_cuts = attend->own_cuts;
+        a.block_parts = attend->block_parts, a.warp_parts = attend->warp_parts, a.shared_rows = attend->shared_rows, a.own_rows = attend->own_rows;
         const int64_t most_tiles = tiles * a.n_tokens;
         int32_t rc;
         switch (cache->storage) {

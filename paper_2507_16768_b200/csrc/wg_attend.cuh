@@ -3,8 +3,8 @@
 // The work is memory: every key and value is read once, by one warp, for the handful of rows (a head's queries) that
 // need it.  A unit is UNIT_TOKENS positions of one (token, key head); all units of a call, in order of tokens and heads, are
 // dealt out to the blocks in equal contiguous shares, whatever the lengths.  What a block holds of one (token, head)
-// is a segment; a token whose units went to several blocks is joined by the block that arrives last, from
-// partial results in scratch, always in the order of positions.
+// is a segment; rows whose units went to several are joined by a kernel that follows, from partial results in scratch,
+// always in the order of positions.
 //
 // Within a block a warp has a ring of tiles of its own, filled with cp.async, and the usual running maximum and sum: for x =
 // scale q.k and the maximum m so far, p = 2^(x - m), l = sum of p, o = sum of p v, all multiplied by 2^(m_old - m) when m
@@ -28,6 +28,38 @@
 
 constexpr int MAX_TOKENS = 384;         // of one launch: their ranges and prefix sums are in shared memory
 
+constexpr int ATTEND_WARPS = 4, ATTEND_THREADS = 32 * ATTEND_WARPS;
+constexpr int PART_ROWS = 16 * ATTEND_WARPS;      // rows that a block can work on together
+
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {      // of numbers >= 0; mostly small ones
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// Units of work, dealt out to workers in equal contiguous shares: the first `extra` have base + 1 units, the others base.
+struct Deal {
+    int64_t base, extra;
+    int32_t workers;
+    __device__ void make(int64_t units, int32_t n) {
+        workers = (int32_t)min((int64_t)n, units);
+        base = workers > 0 ? quotient(units, workers) : 0;
+        extra = units - base * workers;
+    }
+    __device__ __forceinline__ int64_t begin(int w) const { return w * base + min((int64_t)w, extra); }
+    __device__ __forceinline__ int owner(int64_t unit) const {
+        const int64_t larger = extra * (base + 1);
+        return unit < larger ? (int)quotient(unit, base + 1) : (int)(extra + quotient(unit - larger, base));
+    }
+};
+
+// What a launch is about, in shared memory.
+struct Book {
+    int64_t upto[MAX_TOKENS + 1];         // private units before a token
+    int64_t shared_upto[MAX_TOKENS + 1];  // shared units before a group
+    int32_t seq[MAX_TOKENS], from[MAX_TOKENS], end[MAX_TOKENS];   // a token's private positions: from .. end - 1; end 0: it has no row
+    int32_t to[MAX_TOKENS];               // shared positions of a group: 0 .. to - 1 (without groups: from[t] .. to[t] - 1)
+    Deal shared, own;                     // the blocks' units, and the warps'
+};
+
 struct AttendArgs {
     const uint16_t *q;
     uint16_t *out;
@@ -44,17 +76,21 @@ struct AttendArgs {
     int32_t q_bf16;
     float scale;                  // times log2(e)
     // scratch
+    int32_t part_rows;            // rows of a warp's partial result
     int32_t *shared;              // [n_groups] positions from 0 on that a group has in the same blocks
-    float *parts;                 // PART_ROWS rows per block: what begins with a share of the work, and what begins within
+    float *block_parts;           // [block][2][PART_ROWS]: partial results of a pair that begins before a block's share, or within
+    float *warp_parts;            // [worker][together][2][part_rows]: ... before a share of the warps' work, or within
     float *shared_rows;           // [n_tokens][n_q_heads]: shared results that one block did by itself
-    float *private_rows;          // ... and what is to be joined with them
-    int32_t *arrived;             // zero between calls
+    float *own_rows;              // ... and what is to be joined with them
+    int2 *shared_cuts, *own_cuts; // of every pair, for the kernel that joins
+    // how the kernel is cut out
+    int32_t warp_rows, shared_rows_each;  // rows that a warp works for by itself, and those of a shared pair
+    int32_t shared_row_blocks;    // 0: there are no pairs for whole blocks
+    int32_t grouped;
 };
 
 namespace {
 
-constexpr int ATTEND_WARPS = 4, ATTEND_THREADS = 32 * ATTEND_WARPS;
-constexpr int PART_ROWS = 128;           // rows of partial results that a block has room for
 constexpr float NEG_INFINITY = -__builtin_huge_valf();
 
 __device__ __forceinline__ void attend_enter() {
@@ -455,23 +491,6 @@ __device__ __forceinline__ void take_tile(Running<DP / 64, NT> &run, const Queri
 
 // ---- where things are ------------------------------------------------------------------------------------------
 
-// Units of work, dealt out: share w is [total * w / workers, total * (w + 1) / workers).
-struct Deal {
-    int64_t total;
-    int32_t workers;
-    __device__ __forceinline__ int64_t begin(int w) const { return total * w / workers; }
-    __device__ __forceinline__ int owner(int64_t unit) const { return (int)(((unit + 1) * workers + total - 1) / total) - 1; }
-};
-
-// What a launch is about, in shared memory.
-struct Book {
-    int64_t upto[MAX_TOKENS + 1];         // private units before a token
-    int64_t shared_upto[MAX_TOKENS + 1];  // shared units before a group
-    int32_t seq[MAX_TOKENS], from[MAX_TOKENS], end[MAX_TOKENS];   // a token's private positions: from .. end - 1; end 0: it has no row
-    int32_t to[MAX_TOKENS];               // shared positions of a group: 0 .. to - 1 (without groups: from[t] .. to[t] - 1)
-    int32_t last[WG_BEAM_MAX_BEAMS];      // of a group's tokens: all that belongs to them is there
-};
-
 // A run of units with the same rows and head that a block works on as one.
 struct Pair {
     int64_t first;            // unit
@@ -480,96 +499,26 @@ struct Pair {
     int32_t from, to, seq;    // positions, and a sequence whose table has them
 };
 
-// SHARED_WARPS: a block's warps work on the same tiles, each for 8 NT rows of its own (4), or on tiles of their own for
-// the same rows (1), or there are no pairs for whole blocks (0).
-template <typename KV, int DP, int SHARED_WARPS, bool GROUPED, int NT>
-struct Attend {
-    using S = Shape<KV, DP>;
-    static constexpr int WM = SHARED_WARPS == 0 ? 1 : SHARED_WARPS;
-    static constexpr int WARP_ROWS = 8 * NT;
-    static constexpr int ROWS = WARP_ROWS * WM;                 // of a shared pair
-    static constexpr int UNIT = ATTEND_WARPS * S::TILE;         // positions of a shared unit
-    static constexpr int PART_ROW = DP + 4;                     // floats of a row's partial result: o, m, l
+// Where results go.
+template <int DP>
+struct Results {
+    static constexpr int PART_ROW = DP + 4;       // floats of a row's partial result: o, m, l
 
     const CacheDev &cache;
     const AttendArgs &a;
-    Book &book;
-    char *ring;
-    float *scales;            // [warp][stage][2 TILE]
-    uint32_t *real;           // [warp][stage]
-    Deal shared, own;         // the blocks' units, and the warps'
-    int32_t shared_blocks;    // blocks that work on shared pairs: the first ones
-    int32_t shared_row_blocks;
 
-    // ---- partial results ----
-    // Scratch for the rows of what a block or warp began with its share (which = 0) or within it (1): nothing else is left
+    // Scratch for the rows of what began before a block's or worker's share (which = 0) or within it (1): nothing else is left
     // unfinished at its ends.
     __device__ __forceinline__ float *block_part(int block, int which, int row) const {
-        return a.parts + ((int64_t)block * PART_ROWS + which * (PART_ROWS / 2) + row) * PART_ROW;
+        return a.block_parts + (((int64_t)block * 2 + which) * PART_ROWS + row) * PART_ROW;
     }
-    __device__ __forceinline__ float *warp_part(int warp, int which, int row) const {
-        return a.parts + ((int64_t)shared_blocks * PART_ROWS + (int64_t)warp * (PART_ROWS / ATTEND_WARPS) + which * (PART_ROWS / ATTEND_WARPS / 2) + row) * PART_ROW;
+    __device__ __forceinline__ float *warp_part(int worker, int sub, int which, int row) const {
+        return a.warp_parts + ((((int64_t)worker * a.together + sub) * 2 + which) * a.part_rows + row) * PART_ROW;
     }
-    static_assert(PART_ROWS == 2 * 16 * ATTEND_WARPS, "two of 64 rows for a block, or two of 16 for each of its warps");
-
-    // The pieces of a pair: by `n` workers from w on.
-    struct Pieces {
-        int32_t n, w;
-        int64_t first;
-    };
-    static __device__ __forceinline__ Pieces pieces_of(const Deal &deal, int64_t first, int32_t units) {
-        if (units == 0) return {0, 0, 0};
-        const int w = deal.owner(first);
-        return {deal.owner(first + units - 1) - w + 1, w, first};
-    }
-    __device__ __forceinline__ int32_t shared_units(int g) const {
-        return SHARED_WARPS == 0 ? 0 : tiles_of(GROUPED ? 0 : book.from[g], book.to[g], UNIT);
-    }
-    __device__ __forceinline__ int32_t own_units(int t) const { return GROUPED || SHARED_WARPS == 0 ? tiles_of(book.from[t], book.end[t], S::TILE) : 0; }
-    __device__ __forceinline__ Pieces shared_pieces(int g, int head, int row_block) const {
-        const int32_t n = shared_units(g);
-        return pieces_of(shared, book.shared_upto[g] + ((int64_t)head * shared_row_blocks + row_block) * n, n);
-    }
-    __device__ __forceinline__ Pieces own_pieces(int t, int head, int row_block) const {
-        const int32_t n = own_units(t);
-        return pieces_of(own, book.upto[t] + ((int64_t)(head / a.together) * a.row_blocks + row_block) * n, n);
-    }
-    __device__ __forceinline__ int group_of(int t) const { return GROUPED ? t / a.group : t; }
-
-    // Partial results of a token and head that have to arrive before they can be joined: those of row block `only`, or, where
-    // something is shared, all.  (A shared pair that one block did is final for tokens without anything of their own.)
-    __device__ __forceinline__ int expected(int t, int head, int only) const {
-        const int g = group_of(t);
-        int n = 0;
-        if (SHARED_WARPS > 0 && shared_units(g) > 0) {
-            const bool alone = own_units(t) == 0;
-            const int r0 = (t - g * a.group) * a.rows;
-            for (int b = r0 / ROWS; b <= (r0 + a.rows - 1) / ROWS; ++b) {
-                const int k = shared_pieces(g, head, b).n;
-                n += alone && k == 1 ? 0 : k;
-            }
-            if (!alone)
-                for (int b = 0; b < a.row_blocks; ++b) n += own_pieces(t, head, b).n;
-            return n;
-        }
-        return own_pieces(t, head, only).n;
-    }
-    __device__ __forceinline__ int64_t counter(int t, int head, int row_block) const {
-        return ((int64_t)t * cache.n_heads + head) * a.row_blocks + row_block;
-    }
-    // Says that a partial result is there, written by the threads that this one has synchronised with; whether it was the
-    // last.  (Release and acquire are the atomic's own: a fence of all lanes, with copies in flight, took microseconds.)
-    __device__ __forceinline__ bool arrive(int t, int head, int row_block) const {
-        int32_t *c = a.arrived + counter(t, head, row_block);
-        int32_t before;
-        asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(c) : "memory");
-        const bool last = before == expected(t, head, row_block) - 1;
-        if (last) *c = 0;
-        return last;
-    }
+    __device__ __forceinline__ float *kept(float *rows, int t, int q_head) const { return rows + ((int64_t)t * a.n_q_heads + q_head) * PART_ROW; }
 
     template <int N>
-    __device__ __forceinline__ void store_row(int t, int head, int d, float m, float l, const float (&y)[N]) const {
+    __device__ __forceinline__ void store_row(int t, int q_head, int d, float m, float l, const float (&y)[N]) const {
         const float by = l == 0.0f ? 0.0f : 1.0f / l;
         uint32_t w[N / 2];
 #pragma unroll
@@ -577,7 +526,7 @@ struct Attend {
             const float y0 = l == 0.0f ? 0.0f : y[e] * by, y1 = l == 0.0f ? 0.0f : y[e + 1] * by;
             w[e / 2] = a.q_bf16 ? pack<__nv_bfloat16>(y0, y1) : pack<__half>(y0, y1);
         }
-        uint16_t *to = a.out + t * a.out_stride + (int64_t)head * cache.head_dim + d;
+        uint16_t *to = a.out + t * a.out_stride + (int64_t)q_head * cache.head_dim + d;
         if constexpr (N == 8)
             *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
         else if constexpr (N == 4)
@@ -585,102 +534,134 @@ struct Attend {
         else
             *reinterpret_cast<uint32_t *>(to) = w[0];
         if (a.lse && d == 0)
-            a.lse[(int64_t)t * a.n_q_heads + head] = l == 0.0f ? NEG_INFINITY : (m + log2f(l)) * 0.693147180559945f;
+            a.lse[(int64_t)t * a.n_q_heads + q_head] = l == 0.0f ? NEG_INFINITY : (m + log2f(l)) * 0.693147180559945f;
     }
-    static __device__ __forceinline__ void keep_row(float *row, int d, float m, float l, const float (&y)[8]) {
+    // (m and l lie behind the dimensions)
+    __device__ __forceinline__ void keep_row(float *row, int d, float m, float l, const float (&y)[8]) const {
         *reinterpret_cast<float4 *>(row + d) = make_float4(y[0], y[1], y[2], y[3]);
         *reinterpret_cast<float4 *>(row + d + 4) = make_float4(y[4], y[5], y[6], y[7]);
         if (d == 0) *reinterpret_cast<float2 *>(row + DP) = make_float2(m, l);
     }
-    // A running maximum as an exponent of 2: with scales it is one already.
-    static __device__ __forceinline__ float scaled(float m, float factor) { return S::NARROW || m == NEG_INFINITY ? m : m * factor; }
     // What a partial result counts beside maximum m.  (A sum without a maximum is NaN.)
     static __device__ __forceinline__ float weight(float mi, float li, float m) {
         return mi == NEG_INFINITY ? (li == 0.0f ? 0.0f : 1.0f) : power2(mi - m);
     }
 
-    // Rows r0 + step k < r1 of a token's and head's rows are joined by a warp, so many at a time, in the order of positions.
-    template <int AT_ONCE>
-    __device__ __forceinline__ void join_rows(int t, int head, int r0, int r1, int step, int lane) const {
-        constexpr int PER = DP / 32;
-        const int g = group_of(t), first_row = (t - g * a.group) * a.rows;
-        const bool alone = own_units(t) == 0, with_shared = SHARED_WARPS > 0 && shared_units(g) > 0;
-        while (r0 < r1) {
-            // rows of one block of rows, whose pieces are the same
-            int stop = r1;
-            Pieces x{0, 0, 0}, z{0, 0, 0};
-            if (with_shared) {
-                const int b = (first_row + r0) / ROWS;
-                x = shared_pieces(g, head, b);
-                stop = min(stop, (b + 1) * ROWS - first_row);
+    __device__ __forceinline__ int group_of(int t) const { return a.grouped ? t / a.group : t; }
+
+    // What the joining kernel has to know of a pair: its pieces, whether the first begins within its worker's (or block's) share, and
+    // that worker (or block).  Written by whoever has the first piece; {0, 0} where there is no such pair, {-1, 0} where the token
+    // has no row.
+    static __device__ __forceinline__ int2 cut(int pieces, int which, int worker) { return make_int2(pieces * 2 + which, worker); }
+    __device__ __forceinline__ int2 &shared_cut(int g, int head, int row_block) const {
+        return a.shared_cuts[((int64_t)g * cache.n_heads + head) * a.shared_row_blocks + row_block];
+    }
+    __device__ __forceinline__ int2 &own_cut(int t, int head, int row_block) const {
+        return a.own_cuts[((int64_t)t * cache.n_heads + head) * a.row_blocks + row_block];
+    }
+};
+
+// A warp per row; those that were not cut are stored already.  A row's partial results are joined in the order of positions,
+// and asked for all at once where they are not more than AHEAD.  Latencies: 2 to 5 us, of which a launch is one.  (In
+// the first kernel, by whichever warp is the last to be done with a token, the same took 6.5 us at the end of all others,
+// most of it on an atomic's way and back, and its registers cost the loops theirs.)
+template <int DP>
+__global__ void __launch_bounds__(ATTEND_THREADS)
+attend_join_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ AttendArgs a) {
+    attend_enter();
+    using R = Results<DP>;
+    constexpr int PER = DP / 32, AHEAD = 8;      // dimensions of a lane
+    const R to{cache, a};
+    const int t = blockIdx.y, q_head = (int)blockIdx.x * ATTEND_WARPS + (int)(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (q_head >= a.n_q_heads) return;
+    const int g = to.group_of(t), head = q_head / a.rows, r = q_head - head * a.rows, sub = head % a.together;
+    int2 x = make_int2(0, 0), z = make_int2(0, 0);
+    int x_row = 0, z_row = 0;
+    if (a.shared_row_blocks > 0) {
+        const int i = (t - g * a.group) * a.rows + r, b = i / a.shared_rows_each;
+        x_row = i - b * a.shared_rows_each;
+        x = to.shared_cut(g, head, b);
+    }
+    if (a.grouped || a.shared_row_blocks == 0) {
+        const int b = r / a.warp_rows;
+        z_row = r - b * a.warp_rows;
+        z = to.own_cut(t, head, b);
+    }
+    if (z.x < 0) return;
+    const int n_x = x.x >> 1, n_z = z.x >> 1, n = n_x + n_z;
+    if (n <= 1) return;                       // stored already, or there is nothing
+    // (what is not a pair's first piece begins with its share)
+    const auto piece = [&](int i) -> const float * {
+        if (i < n_x) return n_x == 1 ? to.kept(a.shared_rows, t, q_head) : to.block_part(x.y + i, i == 0 ? x.x & 1 : 0, x_row);
+        i -= n_x;
+        return n_z == 1 ? to.kept(a.own_rows, t, q_head) : to.warp_part(z.y + i, sub, i == 0 ? z.x & 1 : 0, z_row);
+    };
+    float m = NEG_INFINITY, l = 0.0f, y[PER] = {};
+    for (int i0 = 0; i0 < n; i0 += AHEAD) {
+        const int here = min(AHEAD, n - i0);
+        const float *mine = piece(i0 + min(lane % AHEAD, here - 1));
+        float2 st = __ldcg(reinterpret_cast<const float2 *>(mine + DP));
+        float2 f[AHEAD][PER / 2];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const float *p = reinterpret_cast<const float *>(__shfl_sync(0xFFFFFFFFu, (unsigned long long)(uintptr_t)mine, k)) + lane * PER;
+#pragma unroll
+            for (int e = 0; e < PER / 2; ++e) f[k][e] = __ldcg(reinterpret_cast<const float2 *>(p) + e);
+        }
+        if (lane % AHEAD >= here) st = make_float2(NEG_INFINITY, 0.0f);
+        float top = st.x;
+#pragma unroll
+        for (int o = AHEAD / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        top = fmaxf(top, m);
+        const float w = R::weight(st.x, st.y, top), old = R::weight(m, l, top);
+        float sum = st.y * w;
+#pragma unroll
+        for (int o = AHEAD / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        l = l * old + sum;
+        m = top;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) y[e] *= old;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const float by = __shfl_sync(0xFFFFFFFFu, w, k);
+            if (k < here) {
+#pragma unroll
+                for (int e = 0; e < PER / 2; ++e) y[2 * e] += f[k][e].x * by, y[2 * e + 1] += f[k][e].y * by;
             }
-            if (!alone) {
-                z = own_pieces(t, head, r0 / WARP_ROWS);
-                stop = min(stop, (r0 / WARP_ROWS + 1) * WARP_ROWS);
-            }
-            const int n_rows = min(AT_ONCE, (stop - r0 + step - 1) / step), n = x.n + z.n;
-            if (!(alone && x.n == 1)) {                         // (stored already)
-                const int64_t kept = ((int64_t)t * a.n_q_heads + head * a.rows + r0) * PART_ROW;
-                const float *const x0 = x.n == 1 ? a.shared_rows + kept : block_part(x.w, shared.begin(x.w) >= x.first ? 0 : 1, (first_row + r0) % ROWS);
-                const float *const z0 = z.n == 1 ? a.private_rows + kept
-                                                 : warp_part(z.w * a.together + head % a.together, own.begin(z.w) >= z.first ? 0 : 1, r0 % WARP_ROWS);
-                // (what is not a pair's first piece begins with its worker's share)
-                const auto part = [&](int i) -> const float * {
-                    if (i < x.n) return i == 0 ? x0 : block_part(x.w + i, 0, (first_row + r0) % ROWS);
-                    i -= x.n;
-                    return i == 0 ? z0 : warp_part((z.w + i) * a.together + head % a.together, 0, r0 % WARP_ROWS);
-                };
-                float m[AT_ONCE], l[AT_ONCE], y[AT_ONCE][PER] = {};
-#pragma unroll
-                for (int k = 0; k < AT_ONCE; ++k) m[k] = NEG_INFINITY, l[k] = 0.0f;
-                for (int i0 = 0; i0 < n; i0 += 32) {
-                    const float *mine = i0 + lane < n ? part(i0 + lane) : nullptr;
-                    float w[AT_ONCE];
-                    float2 st[AT_ONCE];
-#pragma unroll
-                    for (int k = 0; k < AT_ONCE; ++k)
-                        st[k] = mine && k < n_rows ? __ldcg(reinterpret_cast<const float2 *>(mine + k * step * PART_ROW + DP)) : make_float2(NEG_INFINITY, 0.0f);
-#pragma unroll
-                    for (int k = 0; k < AT_ONCE; ++k) {
-                        float top = st[k].x;
-#pragma unroll
-                        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-                        top = fmaxf(top, m[k]);
-                        w[k] = weight(st[k].x, st[k].y, top);
-                        const float old = weight(m[k], l[k], top);
-                        float sum = st[k].y * w[k];
-#pragma unroll
-                        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-                        l[k] = l[k] * old + sum;
-                        m[k] = top;
-#pragma unroll
-                        for (int e = 0; e < PER; ++e) y[k][e] *= old;
-                    }
-                    const int here = min(32, n - i0);
-#pragma unroll(8 / AT_ONCE)
-                    for (int i = 0; i < here; ++i) {
-                        const float *p = reinterpret_cast<const float *>(__shfl_sync(0xFFFFFFFFu, (unsigned long long)(uintptr_t)mine, i)) + lane * PER;
-                        float2 f[AT_ONCE][PER / 2];
-#pragma unroll
-                        for (int k = 0; k < AT_ONCE; ++k)
-#pragma unroll
-                            for (int e = 0; e < PER / 2; ++e)
-                                f[k][e] = k < n_rows ? __ldcg(reinterpret_cast<const float2 *>(p + k * step * PART_ROW) + e) : make_float2(0.0f, 0.0f);
-#pragma unroll
-                        for (int k = 0; k < AT_ONCE; ++k) {
-                            const float by = __shfl_sync(0xFFFFFFFFu, w[k], i);
-#pragma unroll
-                            for (int e = 0; e < PER / 2; ++e) y[k][2 * e] += f[k][e].x * by, y[k][2 * e + 1] += f[k][e].y * by;
-                        }
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k < AT_ONCE; ++k)
-                    if (k < n_rows && lane * PER < cache.head_dim) store_row<PER>(t, head * a.rows + r0 + k * step, lane * PER, m[k], l[k], y[k]);
-            }
-            r0 += n_rows * step;
         }
     }
+    if (lane * PER < cache.head_dim) to.template store_row<PER>(t, q_head, lane * PER, m, l, y);
+}
+
+// SHARED_WARPS: so many of a block's warps work on the same tiles, each for 8 NTS rows of its own; 0: there are no pairs for
+// whole blocks.  A warp by itself works for 8 NT rows.
+template <typename KV, int DP, int SHARED_WARPS, bool GROUPED, int NTS, int NT>
+struct Attend : Results<DP> {
+    using R = Results<DP>;
+    using R::cache, R::a, R::PART_ROW, R::block_part, R::warp_part, R::kept, R::keep_row, R::weight, R::group_of;
+    using S = Shape<KV, DP>;
+    static constexpr int WM = SHARED_WARPS == 0 ? 1 : SHARED_WARPS;
+    static constexpr int WARP_ROWS = 8 * NT;
+    static constexpr int SHARED_ROWS = 8 * NTS;                 // of a warp
+    static constexpr int ROWS = SHARED_ROWS * WM;               // of a shared pair
+    static constexpr int UNIT = ATTEND_WARPS * S::TILE;         // positions of a shared unit
+
+    Book &book;
+    char *ring;
+    float *scales;            // [warp][stage][2 TILE]
+    uint32_t *real;           // [warp][stage]
+    int32_t shared_blocks = 0;      // blocks that work on shared pairs: the first ones
+
+    __device__ Attend(const CacheDev &cache, const AttendArgs &a, Book &book, char *ring, float *scales, uint32_t *real)
+        : R{cache, a}, book(book), ring(ring), scales(scales), real(real) {}
+
+    __device__ __forceinline__ int32_t shared_units(int g) const {
+        return SHARED_WARPS == 0 ? 0 : tiles_of(GROUPED ? 0 : book.from[g], book.to[g], UNIT);
+    }
+    __device__ __forceinline__ int32_t own_units(int t) const { return GROUPED || SHARED_WARPS == 0 ? tiles_of(book.from[t], book.end[t], S::TILE) : 0; }
+
+    // A running maximum as an exponent of 2: with scales it is one already.
+    static __device__ __forceinline__ float scaled(float m, float factor) { return S::NARROW || m == NEG_INFINITY ? m : m * factor; }
 
     // ---- tiles ----
     // A warp's tile: lane i knows the block of position `pos` of the tile (i % TILE).  Commits a group of copies.
@@ -738,12 +719,13 @@ struct Attend {
         head = p.head * a.rows + (r - m * a.rows);
         return m < a.group && t < a.n_tokens && book.end[t] > 0 ? t : -1;
     }
-    static __device__ __forceinline__ void stream_sync() {     // the warps that work on the same tiles
-        static_assert(WM == 1 || WM == ATTEND_WARPS, "");
+    static __device__ __forceinline__ void stream_sync(int stream) {     // the warps that work on the same tiles
         if constexpr (WM == 1)
             __syncwarp();
-        else
+        else if constexpr (WM == ATTEND_WARPS)
             __syncthreads();
+        else
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + stream), "n"(32 * WM) : "memory");
     }
 
     // Units [u0, u1) of a pair.  Rows that nothing else belongs to are stored, others kept as partial results.
@@ -762,20 +744,20 @@ struct Attend {
 #pragma unroll
         for (int i = 0; i < S::STAGES - 1; ++i) first_blocks[i] = block_at(i);
         int32_t next = block_at(S::STAGES - 1);
-        Queries<KV, DP, NT> q;
-        int ends[NT][2], least = 0x7FFFFFFF;    // where the lane's rows end; the first of the warp's rows to end
+        Queries<KV, DP, NTS> q;
+        int ends[NTS][2], least = 0x7FFFFFFF;    // where the lane's rows end; the first of the warp's rows to end
         {
-            const uint16_t *rows[NT];
+            const uint16_t *rows[NTS];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
+            for (int nt = 0; nt < NTS; ++nt) {
                 int head;
-                const int t = row_of(pair, wm * WARP_ROWS + nt * 8 + n, head);
+                const int t = row_of(pair, wm * SHARED_ROWS + nt * 8 + n, head);
                 rows[nt] = t < 0 ? nullptr : a.q + t * a.q_stride + (int64_t)head * cache.head_dim;
                 if (GROUPED && t >= 0) least = min(least, book.end[t]);
                 if constexpr (GROUPED) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const int of = row_of(pair, wm * WARP_ROWS + nt * 8 + 2 * j + c, head);
+                        const int of = row_of(pair, wm * SHARED_ROWS + nt * 8 + 2 * j + c, head);
                         ends[nt][c] = of < 0 ? 0 : book.end[of];
                     }
                 }
@@ -788,13 +770,13 @@ struct Attend {
                 for (int o = 16; o > 0; o >>= 1) least = min(least, __shfl_xor_sync(0xFFFFFFFFu, least, o));
             }
         }
-        bool in[NT][2] = {};
-        Running<S::HALVES, NT> run;
+        bool in[NTS][2] = {};
+        Running<S::HALVES, NTS> run;
         run.reset();
 #pragma unroll 1
         for (int i = 0; i < mine; ++i) {
             wait_tile();
-            stream_sync();
+            stream_sync(stream);
             // (the tile that was used last is free: all warps of the stream are past it)
             copy_tile(warp, (i + S::STAGES - 1) % S::STAGES, i + S::STAGES - 1 < mine, next, (uint32_t)position(i + S::STAGES - 1), pair.head, lane);
             next = block_at(i + S::STAGES);
@@ -807,7 +789,7 @@ struct Attend {
                 const uint32_t keys = shared_address(ring + of * S::STAGE);
                 const int at = from + (i * STREAMS + stream) * STREAM + w * S::TILE;
                 if (!GROUPED || at + S::TILE <= least) {
-                    take_tile<KV, DP, NT, false>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in);
+                    take_tile<KV, DP, NTS, false>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in);
                     continue;
                 }
                 // rows that end within the tile, or before it, go by themselves
@@ -816,7 +798,7 @@ struct Attend {
                 while (true) {
                     int e = 0x7FFFFFFF;
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int nt = 0; nt < NTS; ++nt)
 #pragma unroll
                         for (int c = 0; c < 2; ++c)
                             if (min(ends[nt][c], at + S::TILE) > past) e = min(e, min(ends[nt][c], at + S::TILE));
@@ -824,22 +806,22 @@ struct Attend {
                     for (int o = 16; o > 0; o >>= 1) e = min(e, __shfl_xor_sync(0xFFFFFFFFu, e, o));
                     if (e == 0x7FFFFFFF) break;
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int nt = 0; nt < NTS; ++nt)
 #pragma unroll
                         for (int c = 0; c < 2; ++c) in[nt][c] = min(ends[nt][c], at + S::TILE) == e;
-                    take_tile<KV, DP, NT, true>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok & ((2u << (e - at - 1)) - 1u), n, j, in);
+                    take_tile<KV, DP, NTS, true>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok & ((2u << (e - at - 1)) - 1u), n, j, in);
                     past = e;
                 }
             }
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         run.sum_up();
-        stream_sync();
+        stream_sync(stream);
         // every warp's results into its ring
         float *const part = reinterpret_cast<float *>(ring + warp * S::STAGES * S::STAGE);
-        float2 *const stats = reinterpret_cast<float2 *>(part + WARP_ROWS * S::PITCH);
+        float2 *const stats = reinterpret_cast<float2 *>(part + SHARED_ROWS * S::PITCH);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NTS; ++nt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const int r = nt * 8 + 2 * j + c;
@@ -855,17 +837,20 @@ struct Attend {
         __syncthreads();
         // joined over the streams: a thread takes eight dimensions of a row
         const bool whole = u0 == pair.first && u1 == pair.first + pair.units;
-        const int which = shared.begin(blockIdx.x) >= pair.first ? 0 : 1;
+        const int which = book.shared.begin(blockIdx.x) >= pair.first ? 0 : 1;
+        if (threadIdx.x == 0 && u0 == pair.first)
+            this->shared_cut(pair.group, pair.head, pair.row_block) =
+                R::cut(whole ? 1 : book.shared.owner(pair.first + pair.units - 1) - (int)blockIdx.x + 1, which, blockIdx.x);
         const int n_rows = min(ROWS, a.group * a.rows - pair.row_block * ROWS);
         for (int i = threadIdx.x; i < n_rows * (DP / 8); i += ATTEND_THREADS) {
-            const int r = i / (DP / 8), d = (i % (DP / 8)) * 8, in_warp = r % WARP_ROWS;
-            const char *base = ring + (r / WARP_ROWS) * S::STAGES * S::STAGE;
+            const int r = i / (DP / 8), d = (i % (DP / 8)) * 8, in_warp = r % SHARED_ROWS;
+            const char *base = ring + (r / SHARED_ROWS) * S::STAGES * S::STAGE;
             float m = NEG_INFINITY, l = 0.0f, y[8] = {};
             float2 st[STREAMS];
 #pragma unroll
             for (int s = 0; s < STREAMS; ++s) {
                 const float *of = reinterpret_cast<const float *>(base + s * WM * S::STAGES * S::STAGE);
-                st[s] = reinterpret_cast<const float2 *>(of + WARP_ROWS * S::PITCH)[in_warp];
+                st[s] = reinterpret_cast<const float2 *>(of + SHARED_ROWS * S::PITCH)[in_warp];
                 m = fmaxf(m, st[s].x);
             }
 #pragma unroll
@@ -882,43 +867,27 @@ struct Attend {
             if (!whole)
                 keep_row(block_part(blockIdx.x, which, r), d, m, l, y);
             else if (own_units(t) > 0)
-                keep_row(a.shared_rows + ((int64_t)t * a.n_q_heads + head) * PART_ROW, d, m, l, y);
+                keep_row(kept(a.shared_rows, t, head), d, m, l, y);
             else if (d < cache.head_dim)
-                store_row<8>(t, head, d, m, l, y);
-        }
-        // tokens that have more than this
-        __syncthreads();
-        const int r0 = pair.row_block * ROWS, m0 = r0 / a.rows, m1 = (r0 + n_rows - 1) / a.rows;
-        if ((int)threadIdx.x <= m1 - m0) {
-            const int t = pair.group * a.group + m0 + (int)threadIdx.x;
-            const bool more = t < a.n_tokens && book.end[t] > 0 && (!whole || own_units(t) > 0);
-            book.last[threadIdx.x] = more && arrive(t, pair.head, 0);
-        }
-        __syncthreads();
-        // (a warp per token; the rows of a single one are dealt out)
-        if (m0 == m1) {
-            if (book.last[0]) join_rows<1>(pair.group * a.group + m0, pair.head, warp, a.rows, ATTEND_WARPS, lane);
-        } else {
-            for (int m = warp; m <= m1 - m0; m += ATTEND_WARPS)
-                if (book.last[m]) join_rows<4>(pair.group * a.group + m0 + m, pair.head, 0, a.rows, 1, lane);
+                this->template store_row<8>(t, head, d, m, l, y);
         }
         __syncthreads();      // the rings are free again
     }
 
     __device__ __forceinline__ void work_on_pairs() const {
-        if ((int)blockIdx.x >= shared.workers) return;
-        int64_t u = shared.begin(blockIdx.x);
-        const int64_t end = shared.begin(blockIdx.x + 1);
+        if ((int)blockIdx.x >= book.shared.workers) return;
+        int64_t u = book.shared.begin(blockIdx.x);
+        const int64_t end = book.shared.begin(blockIdx.x + 1);
         int g = find(book.shared_upto, a.n_groups, u);
 #pragma unroll 1
         while (u < end) {
             while (book.shared_upto[g + 1] <= u) ++g;
             Pair p;
             p.units = shared_units(g);
-            const int i = (int)((u - book.shared_upto[g]) / p.units);
+            const int i = (int)quotient(u - book.shared_upto[g], p.units);
             p.first = book.shared_upto[g] + (int64_t)i * p.units;
             p.group = g;
-            p.head = i / shared_row_blocks, p.row_block = i % shared_row_blocks;
+            p.head = i / a.shared_row_blocks, p.row_block = i % a.shared_row_blocks;
             p.from = GROUPED ? 0 : book.from[g], p.to = book.to[g];
             // (the token that goes furthest has all of the shared positions in its table)
             int t = g * a.group;
@@ -959,7 +928,7 @@ struct Attend {
         while (book.upto[p.t + 1] <= u) ++p.t;
         enter(p);
         const int64_t o = u - book.upto[p.t];
-        p.run = (int)(o / p.n);
+        p.run = (int)quotient(o, p.n);
         p.i = (int)(o - (int64_t)p.run * p.n);
         return p;
     }
@@ -981,14 +950,12 @@ struct Attend {
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
         const int id = ((int)blockIdx.x - shared_blocks) * ATTEND_WARPS + warp;
         const int worker = id / a.together, sub = id - worker * a.together;
-        if (worker >= own.workers) return;
-        const int64_t begin = own.begin(worker), end = own.begin(worker + 1);
+        if (worker >= book.own.workers) return;
+        const int64_t begin = book.own.begin(worker), end = book.own.begin(worker + 1);
         const int runs = cache.n_heads / a.together * a.row_blocks;
         const auto head_of = [&](int run) { return (a.row_blocks == 1 ? run : run / a.row_blocks) * a.together + sub; };
         Place front = place(begin), at = front;
         int64_t ahead = begin;                 // the unit of `front`
-        int32_t blocks[S::STAGES];
-        int pos[S::STAGES], heads[S::STAGES];
         const auto fetch = [&](int32_t &block, int &p, int &head) {    // the table's entry of the tile in front
             block = -1;
             if (ahead < end) {
@@ -999,6 +966,8 @@ struct Attend {
             }
             ++ahead;
         };
+        int32_t blocks[S::STAGES];
+        int pos[S::STAGES], heads[S::STAGES];
 #pragma unroll
         for (int i = 0; i < S::STAGES; ++i) fetch(blocks[i], pos[i], heads[i]);
 #pragma unroll
@@ -1032,18 +1001,20 @@ struct Attend {
             if (ok) take_tile<KV, DP, NT, false>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in);
             if (++stage == S::STAGES) stage = 0;
             fresh = at.i == at.n - 1;
-            if (fresh || u + 1 == end) finish(run, q, at, u, begin, end, id, head, row0, n, j, lane);
+            if (fresh || u + 1 == end) finish(run, q, at, u, begin, end, worker, sub, head, row0, n, j, lane);
             step(at, runs);
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
 
     __device__ __forceinline__ void finish(Running<S::HALVES, NT> &run, const Queries<KV, DP, NT> &q, const Place &at, int64_t u, int64_t begin,
-                                           int64_t end, int id, int head, int row0, int n, int j, int lane) const {
+                                           int64_t end, int worker, int sub, int head, int row0, int n, int j, int lane) const {
         const int64_t first = u - at.i;
         const bool whole = first >= begin && first + at.n <= end;
         const bool more = GROUPED && shared_units(group_of(at.t)) > 0;
         const int which = begin >= first ? 0 : 1;
+        if (lane == 0 && first >= begin)
+            this->own_cut(at.t, head, row0 / WARP_ROWS) = R::cut(whole ? 1 : book.own.owner(first + at.n - 1) - worker + 1, which, worker);
         run.sum_up();
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -1051,7 +1022,7 @@ struct Attend {
             for (int c = 0; c < 2; ++c) {
                 const int r = row0 + nt * 8 + 2 * j + c, q_head = head * a.rows + r;
                 if (r >= a.rows) continue;
-                float *kept = whole ? a.private_rows + ((int64_t)at.t * a.n_q_heads + q_head) * PART_ROW : warp_part(id, which, r - row0);
+                float *to_keep = whole ? kept(a.own_rows, at.t, q_head) : warp_part(worker, sub, which, r - row0);
                 const float m = scaled(run.m[nt][c], q.factor[nt][c]);
 #pragma unroll
                 for (int h = 0; h < S::HALVES; ++h) {
@@ -1059,17 +1030,11 @@ struct Attend {
                     float y[8];
                     run.eight(h, nt, c, y);
                     if (!whole || more)
-                        keep_row(kept, d, m, run.l[nt][c], y);
+                        keep_row(to_keep, d, m, run.l[nt][c], y);
                     else if (d < cache.head_dim)
-                        store_row<8>(at.t, q_head, d, m, run.l[nt][c], y);
+                        this->template store_row<8>(at.t, q_head, d, m, run.l[nt][c], y);
                 }
             }
-        if (whole && !more) return;
-        __syncwarp();
-        int last = 0;
-        if (lane == 0) last = arrive(at.t, head, more ? 0 : row0 / WARP_ROWS);
-        last = __shfl_sync(0xFFFFFFFFu, last, 0);
-        if (last) join_rows<4>(at.t, head, more ? 0 : row0, more ? a.rows : min(a.rows, row0 + WARP_ROWS), 1, lane);
     }
 };
 
@@ -1094,11 +1059,11 @@ __device__ __forceinline__ int64_t sums_before(int64_t n, int64_t &total, int64_
     return before + x - n;
 }
 
-template <typename KV, int DP, int SHARED_WARPS, bool GROUPED, int NT>
+template <typename KV, int DP, int SHARED_WARPS, bool GROUPED, int NTS, int NT>
 __global__ void __launch_bounds__(ATTEND_THREADS, Shape<KV, DP>::BLOCKS)
 attend_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ AttendArgs a) {
     using S = Shape<KV, DP>;
-    using A = Attend<KV, DP, SHARED_WARPS, GROUPED, NT>;
+    using A = Attend<KV, DP, SHARED_WARPS, GROUPED, NTS, NT>;
     extern __shared__ __align__(128) char ring[];
     __shared__ Book book;
     __shared__ int64_t scan[ATTEND_WARPS];
@@ -1106,19 +1071,29 @@ attend_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ At
     __shared__ uint32_t real[ATTEND_WARPS * S::STAGES];
     attend_enter();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    A at{cache, a, book, ring, scales, real, Deal{0, 0}, Deal{0, 0}, 0, GROUPED ? (a.group * a.rows + A::ROWS - 1) / A::ROWS : a.row_blocks};
+    A at(cache, a, book, ring, scales, real);
     int64_t shared = 0, own = 0;
     for (int t0 = 0; t0 < a.n_tokens; t0 += ATTEND_THREADS) {
         const int t = t0 + (int)threadIdx.x;
         int64_t n = 0;
-        bool nothing = false;
+        bool nothing = false, without = false;        // no row; no pairs
         if (t < a.n_tokens) {
             const Seen r = seen_by(a, cache, t);
-            nothing = r.end == 0 && t % gridDim.x == blockIdx.x;
+            const bool mine = t % gridDim.x == blockIdx.x;
+            nothing = r.end == 0 && mine;
             book.seq[t] = r.s, book.end[t] = r.end;
             book.from[t] = GROUPED ? max(r.first, a.shared[t / a.group]) : r.first;
             if (!GROUPED) book.to[t] = r.end;
+            without = mine && (SHARED_WARPS == 0 || GROUPED ? at.own_units(t) : at.shared_units(t)) == 0;
             n = (int64_t)(GROUPED || SHARED_WARPS == 0 ? at.own_units(t) * (cache.n_heads / a.together) : at.shared_units(t) * cache.n_heads) * a.row_blocks;
+        }
+        uint32_t empty = __ballot_sync(0xFFFFFFFFu, without);
+        while (empty) {
+            const int i = t0 + warp * 32 + __ffs(empty) - 1;
+            empty &= empty - 1;
+            for (int c = lane; c < cache.n_heads * a.row_blocks; c += 32)
+                (SHARED_WARPS == 0 || GROUPED ? a.own_cuts : a.shared_cuts)[(int64_t)i * cache.n_heads * a.row_blocks + c] =
+                    make_int2(book.end[i] > 0 ? 0 : -1, 0);
         }
         uint32_t which = __ballot_sync(0xFFFFFFFFu, nothing);
         while (which) {          // tokens without a row, by whole warps
@@ -1143,23 +1118,27 @@ attend_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ At
             int64_t n = 0;
             if (g < a.n_groups) {
                 book.to[g] = a.shared[g];
-                n = (int64_t)at.shared_units(g) * at.shared_row_blocks * cache.n_heads;
+                n = (int64_t)at.shared_units(g) * a.shared_row_blocks * cache.n_heads;
+                if (n == 0 && g % gridDim.x == blockIdx.x)
+                    for (int c = 0; c < cache.n_heads * a.shared_row_blocks; ++c) a.shared_cuts[(int64_t)g * cache.n_heads * a.shared_row_blocks + c] = make_int2(0, 0);
             }
             const int64_t before = sums_before(n, shared, scan);
             if (g < a.n_groups) book.shared_upto[g] = before;
         }
     }
-    if (threadIdx.x == 0) book.upto[a.n_tokens] = own, book.shared_upto[a.n_groups] = shared;
-    __syncthreads();
     // Blocks for the shared and for the tokens' own positions, by how many of them there are (in tiles of a head).
     int64_t blocks = GROUPED ? 0 : SHARED_WARPS > 0 ? (int64_t)gridDim.x : 0;
     if (GROUPED && shared > 0) {
         const int64_t x = shared * ATTEND_WARPS, y = own * a.together;
-        blocks = own == 0 ? (int64_t)gridDim.x : min(max((int64_t)gridDim.x * x / (x + y), (int64_t)1), (int64_t)gridDim.x - 1);
+        blocks = own == 0 ? (int64_t)gridDim.x : min(max(quotient((int64_t)gridDim.x * x, x + y), (int64_t)1), (int64_t)gridDim.x - 1);
     }
     at.shared_blocks = (int32_t)blocks;
-    at.shared = Deal{shared, (int32_t)min(blocks, shared)};
-    at.own = Deal{own, (int32_t)min(((int64_t)gridDim.x - blocks) * ATTEND_WARPS / a.together, own)};
+    if (threadIdx.x == 0) {
+        book.upto[a.n_tokens] = own, book.shared_upto[a.n_groups] = shared;
+        book.shared.make(shared, at.shared_blocks);
+    }
+    if (threadIdx.x == 32) book.own.make(own, ((int32_t)gridDim.x - at.shared_blocks) * ATTEND_WARPS / a.together);
+    __syncthreads();
     if constexpr (SHARED_WARPS > 0)
         if ((int)blockIdx.x < at.shared_blocks) {
             at.work_on_pairs();

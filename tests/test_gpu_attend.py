@@ -175,6 +175,17 @@ def test_long_prompts_in_common(wg, held, beams, prompt):
     s.check(s.run())
 
 
+@pytest.mark.parametrize("dead", [(0,), (3,), (1, 2, 6), (0, 7)])
+def test_ended_beams_beside_long_ones(wg, dead):
+    """Beams that have ended, or have only just begun, beside others whose prompt many blocks work on."""
+    lens = [0 if b in dead else 6000 + b for b in range(8)]
+    lens[4] = 20
+    first = next(b for b in range(8) if lens[b])
+    s = Setup(wg, lens, 8, 2, 64, seed=21, share={b: (first, lens[b] // 16 if b == 4 else 370) for b in range(8) if lens[b] and b != first}).on_gpu()
+    s.check(s.run(group=8))
+    s.check(s.run(group=4))
+
+
 @pytest.mark.parametrize("held", [BF16, FP16, INT8])
 @pytest.mark.parametrize("new", [2, 5])
 @pytest.mark.parametrize("group", [1, 0])
