@@ -723,7 +723,8 @@ int32_t wg_rope_frequencies(int32_t rot_dim, double base, double factor, double 
 int32_t wg_rope_table(const double *freq, int32_t n_freq, int32_t n_pos, double magnitude, float *table, void *stream);
 
 /* A step's tokens into the cache: token t's keys, rotated by pos[t], and values go to slot[t]; its queries, rotated,
- * to q_out.  One rounding from the rotated value (fp32, every product rounded) to what is held.
+ * to q_out.  One rounding from the rotated value to what is held; that is fp32, a cos + (-b sin) and b cos + (a sin) with the
+ * product in brackets rounded by itself and the rest once.
  *   k, v     device, n_tokens rows of n_heads x head_dim elements, k_stride / v_stride elements apart
  *   q        device, n_tokens rows of n_q_heads x head_dim, or NULL (n_q_heads then 0); q_out may be q itself
  *            (with the same stride) but may not overlap it otherwise

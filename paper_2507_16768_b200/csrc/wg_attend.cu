@@ -15,12 +15,19 @@ namespace {
 // A row of partial results: the head size as the kernels round it, a maximum and a sum.
 int64_t part_row(int32_t head_dim) { return (head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256) + 4; }
 
-template <int DP>
-int32_t launch_join(const CacheDev &c, const AttendArgs &a, cudaStream_t st) {
-    const dim3 grid((unsigned)((a.n_q_heads + ATTEND_WARPS - 1) / ATTEND_WARPS), (unsigned)a.n_tokens);
-    WG_CUDA(launch_pdl(attend_join_kernel<DP>, grid, dim3(ATTEND_THREADS), st, c, a));
+template <int DP, int WARPS>
+int32_t launch_join_by(const CacheDev &c, const AttendArgs &a, cudaStream_t st) {
+    const dim3 grid((unsigned)((a.n_q_heads * WARPS + ATTEND_WARPS - 1) / ATTEND_WARPS), (unsigned)a.n_tokens);
+    WG_CUDA(launch_pdl(attend_join_kernel<DP, WARPS>, grid, dim3(ATTEND_THREADS), st, c, a));
     WG_LAUNCHED();
     return WG_OK;
+}
+
+// A block per row where all of them find room at once (few rows have many parts each), else a warp.
+template <int DP>
+int32_t launch_join(const CacheDev &c, const AttendArgs &a, cudaStream_t st) {
+    if ((int64_t)a.n_tokens * a.n_q_heads <= (int64_t)sm_count() * 8) return launch_join_by<DP, ATTEND_WARPS>(c, a, st);
+    return launch_join_by<DP, 1>(c, a, st);
 }
 
 }  // namespace

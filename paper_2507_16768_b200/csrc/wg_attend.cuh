@@ -561,18 +561,20 @@ struct Results {
     }
 };
 
-// A warp per row; those that were not cut are stored already.  A row's partial results are joined in the order of positions,
+// WARPS warps per row; those that were not cut are stored already.  A row's partial results are joined in the order of positions,
 // and asked for all at once where they are not more than AHEAD.  Latencies: 2 to 5 us, of which a launch is one.  (In
 // the first kernel, by whichever warp is the last to be done with a token, the same took 6.5 us at the end of all others,
 // most of it on an atomic's way and back, and its registers cost the loops theirs.)
-template <int DP>
+template <int DP, int WARPS>
 __global__ void __launch_bounds__(ATTEND_THREADS)
 attend_join_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ AttendArgs a) {
     attend_enter();
     using R = Results<DP>;
     constexpr int PER = DP / 32, AHEAD = 8;      // dimensions of a lane
     const R to{cache, a};
-    const int t = blockIdx.y, q_head = (int)blockIdx.x * ATTEND_WARPS + (int)(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    __shared__ float rows[WARPS > 1 ? ATTEND_WARPS : 1][R::PART_ROW];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, which = warp % WARPS;
+    const int t = blockIdx.y, q_head = ((int)blockIdx.x * ATTEND_WARPS + warp) / WARPS;
     if (q_head >= a.n_q_heads) return;
     const int g = to.group_of(t), head = q_head / a.rows, r = q_head - head * a.rows, sub = head % a.together;
     int2 x = make_int2(0, 0), z = make_int2(0, 0);
@@ -597,7 +599,7 @@ attend_join_kernel(const __grid_constant__ CacheDev cache, const __grid_constant
         return n_z == 1 ? to.kept(a.own_rows, t, q_head) : to.warp_part(z.y + i, sub, i == 0 ? z.x & 1 : 0, z_row);
     };
     float m = NEG_INFINITY, l = 0.0f, y[PER] = {};
-    for (int i0 = 0; i0 < n; i0 += AHEAD) {
+    for (int i0 = which * AHEAD; i0 < n; i0 += WARPS * AHEAD) {
         const int here = min(AHEAD, n - i0);
         const float *mine = piece(i0 + min(lane % AHEAD, here - 1));
         float2 st = __ldcg(reinterpret_cast<const float2 *>(mine + DP));
@@ -628,6 +630,21 @@ attend_join_kernel(const __grid_constant__ CacheDev cache, const __grid_constant
 #pragma unroll
                 for (int e = 0; e < PER / 2; ++e) y[2 * e] += f[k][e].x * by, y[2 * e + 1] += f[k][e].y * by;
             }
+        }
+    }
+    if constexpr (WARPS > 1) {                // (a block has one row then, and all of its warps come here)
+        static_assert(WARPS == ATTEND_WARPS, "");
+#pragma unroll
+        for (int e = 0; e < PER; ++e) rows[warp][lane * PER + e] = y[e];
+        if (lane == 0) rows[warp][DP] = m, rows[warp][DP + 1] = l;
+        __syncthreads();
+        if (warp > 0) return;
+        for (int w = 1; w < min(WARPS, (n + AHEAD - 1) / AHEAD); ++w) {
+            const float mw = rows[w][DP], lw = rows[w][DP + 1], top = fmaxf(m, mw);
+            const float old = R::weight(m, l, top), by = R::weight(mw, lw, top);
+            m = top, l = l * old + lw * by;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) y[e] = y[e] * old + rows[w][lane * PER + e] * by;
         }
     }
     if (lane * PER < cache.head_dim) to.template store_row<PER>(t, q_head, lane * PER, m, l, y);

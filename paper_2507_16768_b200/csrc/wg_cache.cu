@@ -46,164 +46,158 @@ struct WriteArgs {
     const int32_t *pos;
     int32_t *status;
     int32_t n_tokens;
-    int32_t parts, per_part;  // a token's vectors are dealt out to `parts` lane groups
+    int32_t per, q_parts, k_parts;     // vectors of a lane group, and the groups of a token's queries and keys
 };
 
-// Eight elements of a vector, rotated: those of chunk c, held by lane c of a group.
+// A lane has two chunks of eight dimensions of a vector, A and B, such that rotation stays within a lane: with pairs (i, i + rot / 2)
+// they are rot / 2 apart, else neighbours.
 struct Rotation {
-    float cosine[8], sine[8];   // (sine: with the sign that the element's partner enters with)
-    int hc;                     // chunks of half the rotated part; 0: interleaved
+    Two cosine[8], sine[8];   // of the words of A and B; sine with the sign that the partner enters with
     bool on;
 
     __device__ __forceinline__ void load(const WriteArgs &a, int32_t pos, int c) {
-        on = a.table && c * 8 < a.rot;
-        hc = a.interleaved ? 0 : a.rot / 16;
+        on = c * 16 < a.rot;
         if (!on) return;
-        const float *row = a.table + (int64_t)pos * a.rot;
-        if (hc == 0) {
-            const float4 x = *reinterpret_cast<const float4 *>(row + c * 4), y = *reinterpret_cast<const float4 *>(row + a.rot / 2 + c * 4);
-            const float cs[4] = {x.x, x.y, x.z, x.w}, sn[4] = {y.x, y.y, y.z, y.w};
+        const float *row = a.table + (int64_t)pos * a.rot + c * 8;
+        float cs[8], sn[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                cosine[i] = cs[i / 2];
-                sine[i] = i & 1 ? sn[i / 2] : -sn[i / 2];
-            }
-        } else {
-            const float *at = row + (c < hc ? c : c - hc) * 8;
+        for (int i = 0; i < 8; i += 4) {
+            const float4 x = *reinterpret_cast<const float4 *>(row + i), y = *reinterpret_cast<const float4 *>(row + a.rot / 2 + i);
+            cs[i] = x.x, cs[i + 1] = x.y, cs[i + 2] = x.z, cs[i + 3] = x.w;
+            sn[i] = y.x, sn[i + 1] = y.y, sn[i + 2] = y.z, sn[i + 3] = y.w;
+        }
 #pragma unroll
-            for (int i = 0; i < 8; i += 4) {
-                const float4 x = *reinterpret_cast<const float4 *>(at + i), y = *reinterpret_cast<const float4 *>(at + a.rot / 2 + i);
-                const float cs[4] = {x.x, x.y, x.z, x.w}, sn[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    cosine[i + u] = cs[u];
-                    sine[i + u] = c < hc ? -sn[u] : sn[u];
-                }
-            }
+        for (int i = 0; i < 8; ++i) {
+            const int u = 2 * (i & 3);
+            cosine[i] = a.interleaved ? Two(cs[i], cs[i]) : Two(cs[u], cs[u + 1]);
+            sine[i] = a.interleaved ? Two(-sn[i], sn[i]) : i < 4 ? Two(-sn[u], -sn[u + 1]) : Two(sn[u], sn[u + 1]);
         }
     }
-
-    // Every product is rounded by itself, as the header says: a fused multiply-add would round one of the two.
-    template <typename T, int LG>
-    __device__ __forceinline__ void turn(uint4 w, float (&y)[8], int c, uint32_t group) const {
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-        uint32_t other[4] = {x[0], x[1], x[2], x[3]};
-        if (hc != 0) {
-            const int from = c < hc ? c + hc : c < 2 * hc ? c - hc : c;
+    // (which of the products is rounded by itself is said in the header: results are the same whatever the layout)
+    __device__ __forceinline__ void turn(Two (&y)[8], bool interleaved) const {
+        Two partner[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) other[i] = __shfl_sync(group, x[i], from, LG);
+        for (int i = 0; i < 8; ++i) {
+            const float2 f = y[i].floats();
+            partner[i] = interleaved ? Two(f.y, f.x) : y[i ^ 4];
         }
+        if (on) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 own = unpack(x[i], T{}), partner = unpack(other[i], T{});
-            if (!on) {
-                y[2 * i] = own.x, y[2 * i + 1] = own.y;
-                continue;
-            }
-            const float p0 = hc == 0 ? own.y : partner.x, p1 = hc == 0 ? own.x : partner.y;
-            y[2 * i] = __fadd_rn(__fmul_rn(own.x, cosine[2 * i]), __fmul_rn(p0, sine[2 * i]));
-            y[2 * i + 1] = __fadd_rn(__fmul_rn(own.y, cosine[2 * i + 1]), __fmul_rn(p1, sine[2 * i + 1]));
+            for (int i = 0; i < 8; ++i) y[i] = fused(y[i], cosine[i], partner[i] * sine[i]);
         }
     }
 };
 
-template <typename T>
-__device__ __forceinline__ uint4 pack8(const float (&y)[8]) {
-    return make_uint4(pack<T>(y[0], y[1]), pack<T>(y[2], y[3]), pack<T>(y[4], y[5]), pack<T>(y[6], y[7]));
+__device__ __forceinline__ uint32_t codes2(float2 f, E4m3) { return __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3); }
+__device__ __forceinline__ uint32_t codes2(float2 f, Int8) { return (uint32_t)(__float2int_rn(f.x) & 0xFF) | ((uint32_t)(__float2int_rn(f.y) & 0xFF) << 8); }
+
+__device__ __forceinline__ float largest(float a, float b) {      // NaN if one of them is
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(fabsf(b)));
+    return y;
 }
 
-__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, E4m3) {
-    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
-    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
-    return lo | (hi << 16);
-}
-__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, Int8) {
-    return (uint32_t)(__float2int_rn(a) & 0xFF) | ((uint32_t)(__float2int_rn(b) & 0xFF) << 8) |
-           ((uint32_t)(__float2int_rn(c) & 0xFF) << 16) | ((uint32_t)__float2int_rn(d) << 24);
-}
-
-// The vector of a lane group, quantised into `codes` (row of head_dim bytes) and `scale`.
-template <typename CODE, int LG>
-__device__ __forceinline__ void quantise(const float (&y)[8], char *codes, float *scale, int c, bool inside, uint32_t group) {
-    // as whole numbers magnitudes have the order of their values, with infinity and NaN above them
-    uint32_t top = 0;
+// The vector of a lane group, quantised: codes in the order of `y`, and its scale.
+template <typename CODE, int LV>
+__device__ __forceinline__ float quantise(const Two (&y)[8], uint32_t (&codes)[4], bool inside, uint32_t group) {
+    float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(y[i]) & 0x7FFFFFFFu);
-    if (!inside) top = 0;
+    for (int i = 0; i < 8; ++i) {
+        const float2 f = y[i].floats();
+        top = largest(largest(top, f.x), f.y);
+    }
+    if (!inside) top = 0.0f;
 #pragma unroll
-    for (int o = LG / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(group, top, o));
-    constexpr float LARGEST = sizeof(CODE) && std::is_same<CODE, E4m3>::value ? 448.0f : 127.0f;
-    const float x = __uint_as_float(top);
-    const bool finite = top < 0x7F800000u, small = x < 0x1p-100f;
-    const float mul = finite && !small ? __fdiv_rn(LARGEST, x) : 0.0f;
-    if (c == 0) *scale = !finite ? __uint_as_float(0x7FC00000u) : small ? 1.0f : __fdiv_rn(x, LARGEST);
-    if (!inside) return;
-    uint2 w = make_uint2(0, 0);
-    if (finite)
-        w = make_uint2(codes4(y[0] * mul, y[1] * mul, y[2] * mul, y[3] * mul, CODE{}),
-                       codes4(y[4] * mul, y[5] * mul, y[6] * mul, y[7] * mul, CODE{}));
-    *reinterpret_cast<uint2 *>(codes + c * 8) = w;
+    for (int o = LV / 2; o > 0; o >>= 1) top = largest(top, __shfl_xor_sync(group, top, o));
+    constexpr float LARGEST = std::is_same<CODE, E4m3>::value ? 448.0f : 127.0f;
+    const bool finite = top < __uint_as_float(0x7F800000u), small = top < 0x1p-100f;
+    const float mul = finite && !small ? __fdiv_rn(LARGEST, top) : 0.0f;
+    const Two by(mul, mul);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        codes[i] = finite ? codes2((y[2 * i] * by).floats(), CODE{}) | (codes2((y[2 * i + 1] * by).floats(), CODE{}) << 16) : 0u;
+    return !finite ? __uint_as_float(0x7FC00000u) : small ? 1.0f : __fdiv_rn(top, LARGEST);
 }
 
-// A group of LG lanes holds a vector, eight elements a lane, and goes over its share of a token's vectors (queries, keys,
-// values) with the token's angles in registers.
-template <typename T, typename CODE, int LG>
+// A group of LV lanes holds a vector, 16 elements a lane, and goes over some of a token's queries, keys or values with the token's
+// angles in registers.  The groups of a warp have different tokens, all for the same.
+//
+// Memory, and instructions close behind: with a chunk a lane, partners by shuffle and single-number arithmetic 12001 tokens with
+// 32 + 16 heads took 102 us.
+template <typename T, typename CODE, int LV>
 __global__ void __launch_bounds__(CACHE_THREADS)
-write_kernel(CacheDev cache, WriteArgs a) {
+write_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ WriteArgs a) {
     cache_enter();
     constexpr int AHEAD = 4;             // vectors in flight
     constexpr bool NARROW = !std::is_same<CODE, T>::value;
-    const int lane = threadIdx.x & 31, c = lane & (LG - 1);
-    const uint32_t group = (LG == 32 ? 0xFFFFFFFFu : ((1u << LG) - 1u) << (lane & ~(LG - 1)));
-    const int64_t id = ((int64_t)blockIdx.x * CACHE_THREADS + threadIdx.x) / LG;
-    const int64_t t = id / a.parts;
+    const int lane = threadIdx.x & 31, c = lane & (LV - 1);
+    const uint32_t group = LV == 32 ? 0xFFFFFFFFu : ((1u << LV) - 1u) << (lane & ~(LV - 1));
+    const int64_t t = ((int64_t)blockIdx.x * CACHE_THREADS + threadIdx.x) / LV;
     if (t >= a.n_tokens) return;
-    const int part = (int)(id - t * a.parts);
     const int64_t slot = a.slot[t];
     const int32_t pos = a.table ? a.pos[t] : 0;
     const bool bad = slot < -1 || slot >= (int64_t)cache.n_blocks * cache.block.d || (slot >= 0 && a.table && (pos < 0 || pos >= a.n_pos));
-    if (a.status && part == 0 && c == 0) a.status[t] = bad ? WG_ERR_ARG : WG_OK;
+    if (a.status && blockIdx.y == 0 && c == 0) a.status[t] = bad ? WG_ERR_ARG : WG_OK;
     if (bad || slot < 0) return;
-    const bool inside = c * 8 < cache.head_dim;
+    const int D = cache.head_dim;
+    const bool inside = c * 16 < D;
+    // what this group is for
+    const int part = blockIdx.y;
+    const bool queries = part < a.q_parts, values = part >= a.q_parts + a.k_parts;
+    const int first = (part - (queries ? 0 : values ? a.q_parts + a.k_parts : a.q_parts)) * a.per;
+    const int last = min(first + a.per, queries ? a.n_q_heads : cache.n_heads);
+    const int half = a.interleaved ? 0 : a.rot / 16;
+    const int at = (c < half ? c : 2 * c) * 8, far = (c < half ? half : 1) * 8;      // A (behind the pairs, 2 half + 2 (c - half)), and B from it
+    const uint16_t *from = (queries ? a.q + t * a.q_stride : values ? a.v + t * a.v_stride : a.k + t * a.k_stride) + at;
     Rotation r;
-    r.load(a, pos, c);
-    const int n_heads = cache.n_heads, D = cache.head_dim, n = a.n_q_heads + 2 * n_heads;
-    const int last = min(n, (part + 1) * a.per_part);
-    for (int h0 = part * a.per_part; h0 < last; h0 += AHEAD) {
-        uint4 w[AHEAD];
+    r.on = false;
+    if (!values && a.table) r.load(a, pos, c);
+    for (int h0 = first; h0 < last; h0 += AHEAD) {
+        uint4 w[AHEAD][2];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            const int h = h0 + u, hk = h - a.n_q_heads, hv = hk - n_heads;
-            const uint16_t *from = hk < 0 ? a.q + t * a.q_stride + (int64_t)h * D : hv < 0 ? a.k + t * a.k_stride + (int64_t)hk * D
-                                                                                          : a.v + t * a.v_stride + (int64_t)hv * D;
-            w[u] = make_uint4(0, 0, 0, 0);
-            if (h < last && inside) w[u] = *reinterpret_cast<const uint4 *>(from + c * 8);
+            w[u][0] = w[u][1] = make_uint4(0, 0, 0, 0);
+            if (h0 + u < last && inside) {
+                const uint16_t *x = from + (h0 + u) * D;
+                w[u][0] = __ldcs(reinterpret_cast<const uint4 *>(x)), w[u][1] = __ldcs(reinterpret_cast<const uint4 *>(x + far));
+            }
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            const int h = h0 + u, hk = h - a.n_q_heads, hv = hk - n_heads;
+            const int h = h0 + u;
             if (h >= last) break;
-            float y[8];
-            if (hv < 0) {
-                r.turn<T, LG>(w[u], y, c, group);
-            } else if constexpr (NARROW) {
-                const uint32_t x[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+            const uint32_t x[8] = {w[u][0].x, w[u][0].y, w[u][0].z, w[u][0].w, w[u][1].x, w[u][1].y, w[u][1].z, w[u][1].w};
+            Two y[8];
+            if (NARROW || !values) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 f = unpack(x[i], T{});
-                    y[2 * i] = f.x, y[2 * i + 1] = f.y;
+                for (int i = 0; i < 8; ++i) y[i] = Two(unpack(x[i], T{}));
+                if (!values) r.turn(y, a.interleaved);
+            }
+            const int64_t row = slot * cache.n_heads + h;
+            if constexpr (NARROW) {
+                if (!queries) {
+                    uint32_t codes[4];
+                    const float scale = quantise<CODE, LV>(y, codes, inside, group);
+                    if (c == 0) (values ? cache.v_scale : cache.k_scale)[row] = scale;
+                    if (inside) {
+                        char *to = (values ? cache.v : cache.k) + row * D + at;
+                        *reinterpret_cast<uint2 *>(to) = make_uint2(codes[0], codes[1]);
+                        *reinterpret_cast<uint2 *>(to + far) = make_uint2(codes[2], codes[3]);
+                    }
+                    continue;
                 }
             }
-            if (hk < 0) {
-                if (inside) *reinterpret_cast<uint4 *>(a.q_out + t * a.q_out_stride + (int64_t)h * D + c * 8) = pack8<T>(y);
-                continue;
-            }
-            const int64_t row = slot * n_heads + (hv < 0 ? hk : hv);
-            char *plane = hv < 0 ? cache.k : cache.v;
-            if constexpr (NARROW) {
-                quantise<CODE, LG>(y, plane + row * D, (hv < 0 ? cache.k_scale : cache.v_scale) + row, c, inside, group);
-            } else if (inside) {
-                *reinterpret_cast<uint4 *>(plane + (row * D + c * 8) * 2) = hv < 0 ? pack8<T>(y) : w[u];
+            if (inside) {
+                uint4 z[2] = {w[u][0], w[u][1]};
+                if (!values) {
+                    uint32_t p[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) p[i] = pack<T>(y[i].floats().x, y[i].floats().y);
+                    z[0] = make_uint4(p[0], p[1], p[2], p[3]), z[1] = make_uint4(p[4], p[5], p[6], p[7]);
+                }
+                uint16_t *to = queries ? a.q_out + t * a.q_out_stride + h * D + at : reinterpret_cast<uint16_t *>(values ? cache.v : cache.k) + row * D + at;
+                *reinterpret_cast<uint4 *>(to) = z[0];
+                *reinterpret_cast<uint4 *>(to + far) = z[1];
             }
         }
     }
@@ -213,18 +207,31 @@ struct ReadArgs {
     const int32_t *table, *len, *cu;
     int64_t stride;
     int32_t max_blocks, n_seq, n_rows, rows_per_block;
+    Divisor per_head;         // pieces of eight elements
     char *k_out, *v_out;
 };
+
+// Two codes of a word as fp32.
+__device__ __forceinline__ Two codes_to_floats(uint32_t w, int pair, E4m3) {
+    const uint32_t h = codes_to_half2(w, pair, E4m3{});
+    return Two(unpack(h, __half{}));
+}
+__device__ __forceinline__ Two codes_to_floats(uint32_t w, int pair, Int8) {      // 0x4B000000 + u is 2^23 + u for a byte u = code + 128
+    const uint32_t u = w ^ 0x80808080u;
+    return Two(__uint_as_float(__byte_perm(u, 0x4B000000u, pair ? 0x7442 : 0x7440)), __uint_as_float(__byte_perm(u, 0x4B000000u, pair ? 0x7443 : 0x7441))) +
+           Two(-8388736.0f, -8388736.0f);
+}
 
 template <typename CODE>
 struct Eight {                       // eight elements as they are held
     using Word = uint2;
     static __device__ __forceinline__ void floats(uint2 w, float scale, float (&y)[8]) {
         const uint32_t x[2] = {w.x, w.y};
+        const Two by(scale, scale);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float2 f = unpack(codes_to_half2(x[i / 2], i & 1, CODE{}), __half{});
-            y[2 * i] = f.x * scale, y[2 * i + 1] = f.y * scale;
+            const float2 f = (codes_to_floats(x[i / 2], i & 1, CODE{}) * by).floats();
+            y[2 * i] = f.x, y[2 * i + 1] = f.y;
         }
     }
 };
@@ -251,7 +258,7 @@ __device__ __forceinline__ void store8(char *to, const float (&y)[8], float) {
 }
 template <typename T>
 __device__ __forceinline__ void store8(char *to, const float (&y)[8], T) {
-    *reinterpret_cast<uint4 *>(to) = pack8<T>(y);
+    *reinterpret_cast<uint4 *>(to) = make_uint4(pack<T>(y[0], y[1]), pack<T>(y[2], y[3]), pack<T>(y[4], y[5]), pack<T>(y[6], y[7]));
 }
 
 // A block takes up to READ_ROWS rows of one plane: a lane per row finds its sequence and slot, then all warps copy.
@@ -286,50 +293,59 @@ read_kernel(CacheDev cache, ReadArgs a) {
     __syncthreads();
     const char *plane = values ? cache.v : cache.k;
     const float *scales = values ? cache.v_scale : cache.k_scale;
-    const int per_head = cache.head_dim / 8, per_row = cache.n_heads * per_head, n = rows * per_row;
-    for (int i0 = threadIdx.x; i0 < n; i0 += AHEAD * CACHE_THREADS) {
-        Word w[AHEAD];
-        float scale[AHEAD];
-        int64_t slot[AHEAD];
+    const int per_head = cache.head_dim / 8, per_row = cache.n_heads * per_head;
+    // a thread goes from piece to piece, CACHE_THREADS apart, without dividing
+    const int down = CACHE_THREADS / per_row, right = CACHE_THREADS - down * per_row;
+    int row = (int)threadIdx.x / per_row, at = (int)threadIdx.x - row * per_row;
+    char *to = out + ((int64_t)row0 * per_row + threadIdx.x) * (8 * (int64_t)sizeof(OUT));
+    const auto take = [&](auto many) {
+        constexpr int N = decltype(many)::value;
+        Word w[N];
+        float scale[N];
+        int64_t slot[N];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const int i = i0 + u * CACHE_THREADS, row = i / per_row, at = i - row * per_row;
-            slot[u] = i < n ? slot_of[row] : -2;
-            w[u] = Word{};
+        for (int u = 0; u < N; ++u) {
+            slot[u] = slot_of[row];
+            const int64_t from = max(slot[u], (int64_t)0);       // (something in any case: branches would keep the loads apart)
+            w[u] = __ldcs(reinterpret_cast<const Word *>(plane + (from * per_row + at) * (int64_t)sizeof(Word)));
             scale[u] = 0.0f;
-            if (slot[u] < 0) continue;
-            w[u] = __ldcs(reinterpret_cast<const Word *>(plane + (slot[u] * per_row + at) * (int64_t)sizeof(Word)));
-            if constexpr (NARROW) scale[u] = scales[slot[u] * cache.n_heads + at / per_head];
+            if constexpr (NARROW) scale[u] = scales[from * cache.n_heads + a.per_head.quotient((uint32_t)at)];
+            row += down, at += right;
+            if (at >= per_row) at -= per_row, ++row;
         }
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            if (slot[u] == -2) continue;
+        for (int u = 0; u < N; ++u) {
             float y[8];
             Eight<CODE>::floats(w[u], scale[u], y);
-            store8(out + ((int64_t)row0 * per_row + i0 + u * CACHE_THREADS) * (8 * (int64_t)sizeof(OUT)), y, OUT{});
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = slot[u] < 0 ? 0.0f : y[i];
+            if (slot[u] != -2) store8(to, y, OUT{});
+            to += CACHE_THREADS * (8 * (int64_t)sizeof(OUT));
         }
-    }
+    };
+    while (row + (AHEAD - 1) * (down + (right != 0)) < rows) take(std::integral_constant<int, AHEAD>{});
+    while (row < rows) take(std::integral_constant<int, 1>{});
 }
 
 template <typename T, typename CODE>
 int32_t launch_write(const CacheDev &c, WriteArgs &a, cudaStream_t st) {
     const int heads = a.n_q_heads + 2 * c.n_heads;
-    const int lanes = c.head_dim <= 64 ? 8 : c.head_dim <= 128 ? 16 : 32;
-    // as few vectors a group as the GPU has room for groups at once, and no more than 16: one for a step of few tokens
-    const int64_t room = (int64_t)sm_count() * 2048 / lanes;
+    const int lanes = c.head_dim <= 64 ? 4 : c.head_dim <= 128 ? 8 : 16;
+    // as few vectors a group as the GPU has room for groups at once (768 threads an SM), and no more than 8: one for a step of few tokens
+    const int64_t room = (int64_t)sm_count() * 768 / lanes;
     int64_t per = ((int64_t)a.n_tokens * heads + room - 1) / room;
-    per = per < 1 ? 1 : per > 16 ? 16 : per;
-    a.parts = (int)((heads + per - 1) / per);
-    a.per_part = (heads + a.parts - 1) / a.parts;
-    const int64_t blocks = ((int64_t)a.n_tokens * a.parts * lanes + CACHE_THREADS - 1) / CACHE_THREADS;
-    if (blocks > 0x7FFFFFFF) return WG_ERR_ARG;
-    const dim3 grid((unsigned)blocks);
-    if (lanes == 8)
+    per = per < 1 ? 1 : per > 8 ? 8 : per;
+    if ((heads + per - 1) / per + 3 > 65535) per = 8;
+    a.per = (int)per;
+    a.q_parts = (int)((a.n_q_heads + per - 1) / per), a.k_parts = (int)((c.n_heads + per - 1) / per);
+    const int64_t blocks = ((int64_t)a.n_tokens * lanes + CACHE_THREADS - 1) / CACHE_THREADS;
+    const dim3 grid((unsigned)blocks, (unsigned)(a.q_parts + 2 * a.k_parts));
+    if (lanes == 4)
+        WG_CUDA(launch_pdl(write_kernel<T, CODE, 4>, grid, dim3(CACHE_THREADS), st, c, a));
+    else if (lanes == 8)
         WG_CUDA(launch_pdl(write_kernel<T, CODE, 8>, grid, dim3(CACHE_THREADS), st, c, a));
-    else if (lanes == 16)
-        WG_CUDA(launch_pdl(write_kernel<T, CODE, 16>, grid, dim3(CACHE_THREADS), st, c, a));
     else
-        WG_CUDA(launch_pdl(write_kernel<T, CODE, 32>, grid, dim3(CACHE_THREADS), st, c, a));
+        WG_CUDA(launch_pdl(write_kernel<T, CODE, 16>, grid, dim3(CACHE_THREADS), st, c, a));
     WG_LAUNCHED();
     return WG_OK;
 }
@@ -423,7 +439,8 @@ int32_t wg_kv_read(const wg_kv_cache *cache, const int32_t *table, int64_t table
     if (dtype != WG_DTYPE_BF16 && dtype != WG_DTYPE_FP16 && dtype != WG_DTYPE_FP32) return WG_ERR_ARG;
     if ((((uintptr_t)k_out | (uintptr_t)v_out) & 15) != 0) return WG_ERR_ARG;
     if (n_rows == 0 || (!k_out && !v_out)) return WG_OK;
-    ReadArgs a{table, len, cu, table_stride, max_blocks, n_seq, n_rows, 0, static_cast<char *>(k_out), static_cast<char *>(v_out)};
+    ReadArgs a{table, len, cu, table_stride, max_blocks, n_seq, n_rows, 0, Divisor::of((uint32_t)cache->head_dim / 8), static_cast<char *>(k_out),
+               static_cast<char *>(v_out)};
     // rows of a block: enough blocks for the GPU, and then enough rows that their look-up is shared
     const int64_t spread = (int64_t)n_rows * 2 / (sm_count() * 8);
     a.rows_per_block = spread < 2 ? 2 : spread > READ_ROWS ? READ_ROWS : (int32_t)spread;

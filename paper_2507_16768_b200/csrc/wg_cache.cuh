@@ -56,6 +56,34 @@ __device__ __forceinline__ uint32_t pack<__half>(float a, float b) {
     return *reinterpret_cast<const uint32_t *>(&x);
 }
 
+// Two fp32 numbers that one instruction works on, each rounded by itself.
+struct Two {
+    uint64_t x;
+    Two() = default;
+    __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ Two(float2 f) : Two(f.x, f.y) {}
+    __device__ __forceinline__ float2 floats() const {
+        float2 f;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(x));
+        return f;
+    }
+};
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+    Two y;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y.x) : "l"(a.x), "l"(b.x));
+    return y;
+}
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+    Two y;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y.x) : "l"(a.x), "l"(b.x));
+    return y;
+}
+__device__ __forceinline__ Two fused(Two a, Two b, Two c) {      // a b + c, rounded once
+    Two y;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y.x) : "l"(a.x), "l"(b.x), "l"(c.x));
+    return y;
+}
+
 struct E4m3 {};
 struct Int8 {};
 

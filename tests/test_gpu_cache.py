@@ -100,7 +100,8 @@ class Write:
         y = x.float().clone()
         a, b = (x[..., 0:self.rot:2], x[..., 1:self.rot:2]) if self.interleaved else (x[..., :n], x[..., n:2 * n])
         a, b = a.float(), b.float()
-        lo, hi = a * c - b * s, b * c + a * s
+        # (a product of two fp32 numbers is exact in 64 bits)
+        lo, hi = (a.double() * c - (b * s).double()).float(), (b.double() * c + (a * s).double()).float()
         if self.interleaved:
             y[..., 0:self.rot:2], y[..., 1:self.rot:2] = lo, hi
         else:
