@@ -1059,30 +1059,40 @@ class Rope:
         self._arg = C.addressof(self._struct)
 
 
+_model_dtypes = {}      # filled when torch is there (see _on_stream)
+_float32 = None
+
+
 def _model_dtype(t, what: str) -> int:
-    import torch
-    if t.dtype is torch.bfloat16:
-        return WG_DTYPE_BF16
-    if t.dtype is torch.float16:
-        return WG_DTYPE_FP16
-    raise TypeError(f"{what} must be bfloat16 or float16, not {t.dtype}")
+    global _float32
+    if not _model_dtypes:
+        import torch
+        _float32 = torch.float32
+        _model_dtypes.update({torch.bfloat16: WG_DTYPE_BF16, torch.float16: WG_DTYPE_FP16})
+    kind = _model_dtypes.get(t.dtype)
+    if kind is None:
+        raise TypeError(f"{what} must be bfloat16 or float16, not {t.dtype}")
+    return kind
 
 
 def _heads(t, n: int, heads: int, dim: int, dtype, device: int, what: str):
     """(pointer, elements from token to token) of a [n, heads, dim] array whose tokens are whole: 16-byte aligned rows
     of heads * dim elements without gaps, any distance apart."""
-    if not t.is_cuda or t.dtype is not dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{what} must be a CUDA tensor of {dtype}")
-    if tuple(t.shape) != (n, heads, dim):
+    if t.get_device() != device:
+        raise ValueError(f"{what} must be on cuda:{device}, as the cache is")
+    if t.shape != (n, heads, dim):
         raise ValueError(f"{what} must be [{n}, {heads}, {dim}], not {list(t.shape)}")
-    if t.device.index != device:
-        raise ValueError(f"{what} lives on cuda:{t.device.index}, the cache on cuda:{device}")
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or (s1 != dim and heads > 1):
         raise ValueError(f"the heads of a token of {what} must follow each other without gaps")
-    p, stride = t.data_ptr(), t.stride(0) if n > 1 else heads * dim
-    if p & 15 or stride & 7 or stride < heads * dim:
+    if n < 2:
+        s0 = heads * dim
+    p = t.data_ptr()
+    if p & 15 or s0 & 7 or s0 < heads * dim:
         raise ValueError(f"the tokens of {what} must begin at multiples of 16 bytes and not overlap")
-    return p, stride
+    return p, s0
 
 
 class KvCache:
@@ -1142,7 +1152,6 @@ class KvCache:
         """wg_kv_write: the tokens of ``slots`` into the cache.  ``k``, ``v`` are ``[n_tokens, n_heads, head_dim]`` (views into
         a fused projection will do), ``q`` and ``q_out`` ``[n_tokens, query heads, head_dim]``; without ``q_out`` the queries
         are rotated in place.  ``status`` [n_tokens] gets WG_ERR_ARG for slots outside the cache and positions outside ``rope``."""
-        import torch
         n, dev, dtype = slots.n_tokens, self.device, k.dtype
         kind = _model_dtype(k, "k")
         if self.storage <= WG_KV_FP16 and dtype is not self.dtype:
@@ -1168,10 +1177,12 @@ class KvCache:
                 raise ValueError(f"rope lives on cuda:{rope.device}, the cache on cuda:{dev}")
             if rope.rot_dim > self.head_dim:
                 raise ValueError(f"rope rotates {rope.rot_dim} dimensions, a head has {self.head_dim}")
-        st = None if status is None else _vec(status, n, torch.int32, "status", dev)
+        if status is not None:
+            import torch
+            status = _vec(status, n, torch.int32, "status", dev)
         _, slot, pos, _ = slots._args[:4]
         rc = _lib.wg_kv_write(self._arg, kp, ks, vp, vs, qp, qs or 0, op, os_ or 0, heads, kind,
-                              None if rope is None else rope._arg, slot, pos, n, st, _on_stream(stream, dev))
+                              None if rope is None else rope._arg, slot, pos, n, status, _on_stream(stream, dev))
         if rc != WG_OK:
             raise WgError(rc, "wg_kv_write")
 
@@ -1231,7 +1242,6 @@ class Attend:
         With ``slots`` (the map that placed the step's tokens) row t is token t of the map; without, row t is the last
         token of sequence t.  ``scale`` is 1 / sqrt(head_dim) if it is not given.  ``group``: so many neighbouring tokens, the beams of a
         request or the drafted tokens of a sequence, read what their tables have in common together."""
-        import torch
         cache._check_tables(tables)
         dev = self.device
         if cache.device != dev or cache.n_heads != self.n_heads or cache.head_dim != self.head_dim:
@@ -1249,8 +1259,7 @@ class Attend:
         qp, qs = _heads(q, n, self.n_q_heads, self.head_dim, dtype, dev, "q")
         op, os_ = _heads(out, n, self.n_q_heads, self.head_dim, dtype, dev, "out")
         if lse is not None:
-            if not lse.is_cuda or lse.dtype is not torch.float32 or tuple(lse.shape) != (n, self.n_q_heads) \
-                    or not lse.is_contiguous() or lse.device.index != dev:
+            if lse.dtype is not _float32 or lse.get_device() != dev or lse.shape != (n, self.n_q_heads) or not lse.is_contiguous():
                 raise ValueError(f"lse must be a contiguous float32 tensor [{n}, {self.n_q_heads}] on cuda:{dev}")
             lse = lse.data_ptr()
         _, table, stride, max_blocks, lens = tables._head

@@ -23,10 +23,12 @@ int32_t launch_join_by(const CacheDev &c, const AttendArgs &a, cudaStream_t st) 
     return WG_OK;
 }
 
-// A block per row where all of them find room at once (few rows have many parts each), else a warp.
+// A block per row where there are few rows, or few pairs, which then have many parts each; else a warp.  (32 x 4096 positions, 1024
+// rows: 76.9 us with blocks, 77.9 with warps; 128 x 128, 4096 rows: 28.1 and 22.3; 24 x 4 drafted tokens, 96 pairs: 32 and 39.)
 template <int DP>
 int32_t launch_join(const CacheDev &c, const AttendArgs &a, cudaStream_t st) {
-    if ((int64_t)a.n_tokens * a.n_q_heads <= (int64_t)sm_count() * 8) return launch_join_by<DP, ATTEND_WARPS>(c, a, st);
+    if ((int64_t)a.n_tokens * a.n_q_heads <= (int64_t)sm_count() * 8 || (int64_t)a.n_groups * c.n_heads <= sm_count())
+        return launch_join_by<DP, ATTEND_WARPS>(c, a, st);
     return launch_join_by<DP, 1>(c, a, st);
 }
 
@@ -50,7 +52,7 @@ int32_t wg_attend_create(int32_t max_tokens, int32_t n_q_heads, int32_t n_heads,
     p->max_tokens = max_tokens, p->n_q_heads = n_q_heads, p->n_heads = n_heads, p->head_dim = head_dim;
     const int32_t group_rows = n_q_heads / n_heads, part_rows = group_rows < 16 ? group_rows : 16;
     const size_t row = part_row(head_dim), blocks = (size_t)sm_count() * 2, warps = blocks * ATTEND_WARPS;
-    const size_t rows = (size_t)max_tokens * n_q_heads * row;
+    const size_t rows = (size_t)(max_tokens < MAX_TOKENS ? max_tokens : MAX_TOKENS) * n_q_heads * row;
     // (pairs of a launch: a token's blocks of rows have 8 rows at least, a group's shared ones 16)
     const size_t pairs = (size_t)MAX_TOKENS * n_heads * ((group_rows + 7) / 8);
     int32_t rc = dev_alloc(&p->shared, (size_t)MAX_TOKENS);

@@ -324,12 +324,15 @@ struct Queries {
 };
 
 // A tile: keys at `keys`, values at `values` in shared memory; bit i of `real`: position i counts.  scales: TILE of keys,
-// then TILE of values.  PART: the positions that do not count may hold anything (otherwise zeros), and only the rows of
-// which `in` says so take them in; whatever the positions hold, the other rows stay as they are.
-template <typename KV, int DP, int NT, bool PART>
+// then TILE of values.  ENDS: a row takes in the positions before its end only (in the tile); values have to be finite, for
+// those behind it get the weight 0.  PART: the positions that do not count may hold anything (otherwise zeros), and only rows whose
+// end is not 0 take them in; whatever the positions hold, the other rows stay as they are.
+enum Rows { ALL_ROWS, ENDS, PART_OF_ROWS };
+template <typename KV, int DP, int NT, Rows ROWS>
 __device__ __forceinline__ void take_tile(Running<DP / 64, NT> &run, const Queries<KV, DP, NT> &q, uint32_t keys, uint32_t values,
-                                          const float *scales, uint32_t real, int n, int j, const bool (&in)[NT][2]) {
+                                          const float *scales, uint32_t real, int n, int j, const int (&ends)[NT][2]) {
     using S = Shape<KV, DP>;
+    constexpr bool PART = ROWS == PART_OF_ROWS;
     using Mma = typename S::Mma;
     float x[S::SUBS][NT][4] = {};            // [2 e + c]: of position 16 s + n + 8 e
 #pragma unroll
@@ -385,7 +388,16 @@ __device__ __forceinline__ void take_tile(Running<DP / 64, NT> &run, const Queri
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (!in[nt][i & 1]) x[s][nt][i] = NEG_INFINITY;
+                    if (ends[nt][i & 1] == 0) x[s][nt][i] = NEG_INFINITY;
+    }
+    if constexpr (ROWS == ENDS) {
+#pragma unroll
+        for (int s = 0; s < S::SUBS; ++s)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (s * 16 + n + 8 * (i >> 1) >= ends[nt][i & 1]) x[s][nt][i] = NEG_INFINITY;
     }
     // maxima: of x itself, which the factor (above 0) multiplies later; with scales of x' = factor x + up
     float base[NT][2], shrink[NT][2];
@@ -447,7 +459,7 @@ __device__ __forceinline__ void take_tile(Running<DP / 64, NT> &run, const Queri
                 multiply(y, v, p[s][nt][0], p[s][nt][1], Mma{});
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (in[nt][i & 1]) o[nt][i] += y[i];
+                    if (ends[nt][i & 1] != 0) o[nt][i] += y[i];
             } else {
                 multiply(o[nt], v, p[s][nt][0], p[s][nt][1], Mma{});
             }
@@ -745,6 +757,29 @@ struct Attend : Results<DP> {
             asm volatile("bar.sync %0, %1;" ::"r"(1 + stream), "n"(32 * WM) : "memory");
     }
 
+    // Whether a tile's values are all finite.
+    static __device__ __forceinline__ bool values_finite(uint32_t values, const float *value_scales, int lane) {
+        bool odd = false;
+        if constexpr (S::NARROW) odd = lane < S::TILE && !(value_scales[lane] < __uint_as_float(0x7F800000u));
+        if constexpr (!std::is_same<KV, Int8>::value) {
+#pragma unroll 4
+            for (int i = lane; i < S::PLANE / 16; i += 32) {
+                const uint4 x = load16(values + i * 16);
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if constexpr (S::NARROW)           // (the only one: all bits but the sign set)
+                        odd |= (((w[k] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
+                    else {
+                        constexpr uint32_t top = std::is_same<KV, __half>::value ? 0x7C00u : 0x7F80u;
+                        odd |= (w[k] & top) == top || ((w[k] >> 16) & top) == top;
+                    }
+                }
+            }
+        }
+        return !__any_sync(0xFFFFFFFFu, odd);
+    }
+
     // Units [u0, u1) of a pair.  Rows that nothing else belongs to are stored, others kept as partial results.
     __device__ __forceinline__ void segment(const Pair &pair, int64_t u0, int64_t u1) const {
         constexpr int STREAMS = ATTEND_WARPS / WM, STREAM = S::TILE * WM;
@@ -787,7 +822,7 @@ struct Attend : Results<DP> {
                 for (int o = 16; o > 0; o >>= 1) least = min(least, __shfl_xor_sync(0xFFFFFFFFu, least, o));
             }
         }
-        bool in[NTS][2] = {};
+        int in[NTS][2] = {};                    // where the rows end in the tile
         Running<S::HALVES, NTS> run;
         run.reset();
 #pragma unroll 1
@@ -806,10 +841,19 @@ struct Attend : Results<DP> {
                 const uint32_t keys = shared_address(ring + of * S::STAGE);
                 const int at = from + (i * STREAMS + stream) * STREAM + w * S::TILE;
                 if (!GROUPED || at + S::TILE <= least) {
-                    take_tile<KV, DP, NTS, false>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in);
+                    take_tile<KV, DP, NTS, ALL_ROWS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in);
                     continue;
                 }
-                // rows that end within the tile, or before it, go by themselves
+                // rows that end within the tile, or before it
+                if (values_finite(keys + S::PLANE, scales + of * (2 * S::TILE) + S::TILE, lane)) {
+#pragma unroll
+                    for (int nt = 0; nt < NTS; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) in[nt][c] = ends[nt][c] - at;
+                    take_tile<KV, DP, NTS, ENDS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in);
+                    continue;
+                }
+                // (an infinity or a NaN would reach them with the weight 0: the rows go by themselves)
                 int past = at;
 #pragma unroll 1
                 while (true) {
@@ -826,7 +870,7 @@ struct Attend : Results<DP> {
                     for (int nt = 0; nt < NTS; ++nt)
 #pragma unroll
                         for (int c = 0; c < 2; ++c) in[nt][c] = min(ends[nt][c], at + S::TILE) == e;
-                    take_tile<KV, DP, NTS, true>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok & ((2u << (e - at - 1)) - 1u), n, j, in);
+                    take_tile<KV, DP, NTS, PART_OF_ROWS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok & ((2u << (e - at - 1)) - 1u), n, j, in);
                     past = e;
                 }
             }
@@ -993,7 +1037,7 @@ struct Attend : Results<DP> {
         int p = pos[S::STAGES - 1], p_head = heads[S::STAGES - 1];
         Queries<KV, DP, NT> q;
         Running<S::HALVES, NT> run;
-        const bool in[NT][2] = {};
+        const int in[NT][2] = {};
         int stage = 0, head = 0, row0 = 0;
         bool fresh = true;
 #pragma unroll 1
@@ -1015,7 +1059,7 @@ struct Attend : Results<DP> {
             fetch(block, p, p_head);
             const int of = warp * S::STAGES + stage;
             const uint32_t ok = real[of], keys = shared_address(ring + of * S::STAGE);
-            if (ok) take_tile<KV, DP, NT, false>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in);
+            if (ok) take_tile<KV, DP, NT, ALL_ROWS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in);
             if (++stage == S::STAGES) stage = 0;
             fresh = at.i == at.n - 1;
             if (fresh || u + 1 == end) finish(run, q, at, u, begin, end, worker, sub, head, row0, n, j, lane);
@@ -1146,7 +1190,8 @@ attend_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ At
     // Blocks for the shared and for the tokens' own positions, by how many of them there are (in tiles of a head).
     int64_t blocks = GROUPED ? 0 : SHARED_WARPS > 0 ? (int64_t)gridDim.x : 0;
     if (GROUPED && shared > 0) {
-        const int64_t x = shared * ATTEND_WARPS, y = own * a.together;
+        // (a shared unit takes 4/3 of the time that a warp's tiles of the same size take: 732 warps were done after 67 us, 452 after 53)
+        const int64_t x = shared * ATTEND_WARPS * 4, y = own * a.together * 3;
         blocks = own == 0 ? (int64_t)gridDim.x : min(max(quotient((int64_t)gridDim.x * x, x + y), (int64_t)1), (int64_t)gridDim.x - 1);
     }
     at.shared_blocks = (int32_t)blocks;

@@ -31,6 +31,12 @@ class At(FakeTensor):
     def data_ptr(self):
         return self.at
 
+    def stride(self, *i):
+        return super().stride(*i) if i else self._strides
+
+    def get_device(self):
+        return self.device.index if self.is_cuda else -1
+
 
 def cache(dtype=BF16, n_blocks=8, block=4, H=2, D=64, **k):
     planes = dict(keys=At((n_blocks, block, H, D), dtype), values=At((n_blocks, block, H, D), dtype))
