@@ -140,20 +140,26 @@ attend_plan_kernel(const __grid_constant__ CacheDev cache, const __grid_constant
         if (seen[m].end > end) leader = m, end = seen[m].end;
     for (int m = 0; m < a.group; ++m)
         if (leader >= 0 && seen[m].s != seen[leader].s) second = max(second, seen[m].end);
+    // (a warp takes every fourth token, its lanes four columns each at a time)
     const int cols = second > 0 ? (int)cache.block.quotient((uint32_t)(second - 1)) + 1 : 0;
     const int32_t *mine = a.table + (leader >= 0 ? seen[leader].s * a.stride : 0);
-    for (int c0 = 0; c0 < cols; c0 += 4 * ATTEND_THREADS) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int c0 = 0; c0 < cols; c0 += 128) {
         int at = 0x7FFFFFFF;
+        for (int m = warp; m < a.group; m += ATTEND_WARPS) {
+            const Seen r = seen[m];
+            if (r.end == 0 || r.s == seen[leader].s) continue;
+            const int mine_cols = (int)cache.block.quotient((uint32_t)(r.end - 1)) + 1;
+            const int32_t *theirs = a.table + r.s * a.stride;
+            int32_t x[4], y[4];
 #pragma unroll
-        for (int u = 3; u >= 0; --u) {
-            const int c = c0 + u * ATTEND_THREADS + (int)threadIdx.x;
-            if (c >= cols) continue;
-            const int32_t b = mine[c];
-            bool same = true;
-            for (int m = 0; m < a.group; ++m)
-                if (seen[m].s != seen[leader].s && (int64_t)c * cache.block.d < seen[m].end)
-                    same &= a.table[seen[m].s * a.stride + c] == b;
-            if (!same) at = c;
+            for (int u = 0; u < 4; ++u) {
+                const int c = c0 + u * 32 + lane;
+                x[u] = c < mine_cols ? theirs[c] : 0, y[u] = c < mine_cols ? mine[c] : 0;
+            }
+#pragma unroll
+            for (int u = 3; u >= 0; --u)
+                if (x[u] != y[u]) at = min(at, c0 + u * 32 + lane);
         }
         if (at < 0x7FFFFFFF) atomicMin(&differs, at);
         if (__syncthreads_or(at < 0x7FFFFFFF)) break;
@@ -276,22 +282,35 @@ struct Queries {
     uint32_t b[S::STEPS][NT][2];
     float factor[NT][2];          // of the scores of the lane's result rows, above 0; the sign is in the queries
 
+    static constexpr int PER = S::NARROW ? 2 : 1;      // 16-byte loads that make up a lane's share of a piece of a key
+    struct Raw {
+        uint4 x[NT][S::CHUNKS / 4][PER];
+    };
     // row[nt]: NULL for none
-    __device__ __forceinline__ void load(const uint16_t *const (&row)[NT], int head_dim, bool bf16, float scale, int j) {
+    static __device__ __forceinline__ void ask(Raw &raw, const uint16_t *const (&row)[NT], int head_dim, int j) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int kk = 0; kk < S::CHUNKS / 4; ++kk)
+#pragma unroll
+                for (int half = 0; half < PER; ++half) {
+                    const int d = ((kk * 4 + j) * PER + half) * 8;
+                    raw.x[nt][kk][half] = row[nt] && d < head_dim ? *reinterpret_cast<const uint4 *>(row[nt] + d) : make_uint4(0, 0, 0, 0);
+                }
+    }
+    __device__ __forceinline__ void take(const Raw &raw, bool bf16, float scale, int j) {
         // (2^-126 for 0: a score that stands for nothing stays -inf)
         const float up = fmaxf(fabsf(scale), 0x1p-126f);
         const uint32_t sign = scale < 0.0f ? 0x80008000u : 0u;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             factor[nt][0] = factor[nt][1] = up;
-            constexpr int PER = S::NARROW ? 2 : 1;      // 16-byte loads that make up a lane's share of a piece of a key
             uint32_t top = 0;
 #pragma unroll
             for (int kk = 0; kk < S::CHUNKS / 4; ++kk)
 #pragma unroll
                 for (int half = 0; half < PER; ++half) {
-                    const int d = ((kk * 4 + j) * PER + half) * 8;
-                    const uint4 x = row[nt] && d < head_dim ? *reinterpret_cast<const uint4 *>(row[nt] + d) : make_uint4(0, 0, 0, 0);
+                    const uint4 x = raw.x[nt][kk][half];
                     const uint32_t w[4] = {x.x ^ sign, x.y ^ sign, x.z ^ sign, x.w ^ sign};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -674,6 +693,9 @@ struct Attend : Results<DP> {
     static constexpr int SHARED_ROWS = 8 * NTS;                 // of a warp
     static constexpr int ROWS = SHARED_ROWS * WM;               // of a shared pair
     static constexpr int UNIT = ATTEND_WARPS * S::TILE;         // positions of a shared unit
+    // What a pair costs besides its tiles, in units: so many are dealt out in front of its own, and passed over.  (48 ragged sequences
+    // of 16 heads, some of a few positions: warps were done after 11 to 22 us without, 14 in the middle.)
+    static constexpr int PAIR_COST = 1, SHARED_PAIR_COST = 2;
 
     Book &book;
     char *ring;
@@ -814,9 +836,11 @@ struct Attend : Results<DP> {
                     }
                 }
             }
+            typename Queries<KV, DP, NTS>::Raw raw;
+            q.ask(raw, rows, cache.head_dim, j);
 #pragma unroll
             for (int i = 0; i < S::STAGES - 1; ++i) copy_tile(warp, i, i < mine, first_blocks[i], (uint32_t)position(i), pair.head, lane);
-            q.load(rows, cache.head_dim, a.q_bf16, a.scale, j);
+            q.take(raw, a.q_bf16, a.scale, j);
             if constexpr (GROUPED) {
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) least = min(least, __shfl_xor_sync(0xFFFFFFFFu, least, o));
@@ -945,8 +969,11 @@ struct Attend : Results<DP> {
             while (book.shared_upto[g + 1] <= u) ++g;
             Pair p;
             p.units = shared_units(g);
-            const int i = (int)quotient(u - book.shared_upto[g], p.units);
-            p.first = book.shared_upto[g] + (int64_t)i * p.units;
+            const int32_t dealt = p.units + SHARED_PAIR_COST;
+            const int i = (int)quotient(u - book.shared_upto[g], dealt);
+            p.first = book.shared_upto[g] + (int64_t)i * dealt + SHARED_PAIR_COST;
+            u = max(u, p.first);
+            if (u >= end) break;
             p.group = g;
             p.head = i / a.shared_row_blocks, p.row_block = i % a.shared_row_blocks;
             p.from = GROUPED ? 0 : book.from[g], p.to = book.to[g];
@@ -983,20 +1010,23 @@ struct Attend : Results<DP> {
         p.n = own_units(p.t);
         p.row = a.table + book.seq[p.t] * a.stride;
     }
-    __device__ __forceinline__ Place place(int64_t u) const {
+    __device__ __forceinline__ Place place(int64_t &u) const {   // (u moves on to a unit with a tile)
         Place p;
         p.t = find(book.upto, a.n_tokens, u);
         while (book.upto[p.t + 1] <= u) ++p.t;
         enter(p);
         const int64_t o = u - book.upto[p.t];
-        p.run = (int)quotient(o, p.n);
-        p.i = (int)(o - (int64_t)p.run * p.n);
+        p.run = (int)quotient(o, p.n + PAIR_COST);
+        p.i = (int)(o - (int64_t)p.run * (p.n + PAIR_COST)) - PAIR_COST;
+        if (p.i < 0) u -= p.i, p.i = 0;
         return p;
     }
     // `runs`: of a token
-    __device__ __forceinline__ void step(Place &p, int runs) const {
+    __device__ __forceinline__ void step(Place &p, int64_t &u, int runs) const {
+        ++u;
         if (++p.i < p.n) return;
         p.i = 0;
+        u += PAIR_COST;
         if (++p.run < runs) return;
         p.run = 0;
         do ++p.t;
@@ -1015,55 +1045,69 @@ struct Attend : Results<DP> {
         const int64_t begin = book.own.begin(worker), end = book.own.begin(worker + 1);
         const int runs = cache.n_heads / a.together * a.row_blocks;
         const auto head_of = [&](int run) { return (a.row_blocks == 1 ? run : run / a.row_blocks) * a.together + sub; };
-        Place front = place(begin), at = front;
-        int64_t ahead = begin;                 // the unit of `front`
-        const auto fetch = [&](int32_t &block, int &p, int &head) {    // the table's entry of the tile in front
-            block = -1;
-            if (ahead < end) {
-                p = front.from + front.i * S::TILE + lane % S::TILE;
-                head = head_of(front.run);
-                block = entry(front.row, p, front.end);
-                step(front, runs);
+        int64_t u = begin;
+        Place front = place(u), at = front;
+        if (u >= end) return;
+        int64_t ahead = u;                     // the unit of `front`
+        using Q = Queries<KV, DP, NT>;
+        typename Q::Raw raw;                   // of the next pair
+        const auto ask = [&](const Place &of) {
+            const int head = head_of(of.run), row0 = of.run % a.row_blocks * WARP_ROWS;
+            const uint16_t *rows[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const int r = row0 + nt * 8 + n;
+                rows[nt] = r < a.rows ? a.q + of.t * a.q_stride + (int64_t)(head * a.rows + r) * cache.head_dim : nullptr;
             }
-            ++ahead;
+            Q::ask(raw, rows, cache.head_dim, j);
+        };
+        ask(at);
+        const auto fetch = [&](int32_t &block, int &p, int &head) -> bool {    // the table's entry of the tile in front
+            block = -1;
+            if (ahead >= end) return false;
+            p = front.from + front.i * S::TILE + lane % S::TILE;
+            head = head_of(front.run);
+            block = entry(front.row, p, front.end);
+            step(front, ahead, runs);
+            return true;
         };
         int32_t blocks[S::STAGES];
         int pos[S::STAGES], heads[S::STAGES];
+        bool lives[S::STAGES];
 #pragma unroll
-        for (int i = 0; i < S::STAGES; ++i) fetch(blocks[i], pos[i], heads[i]);
+        for (int i = 0; i < S::STAGES; ++i) lives[i] = fetch(blocks[i], pos[i], heads[i]);
 #pragma unroll
-        for (int i = 0; i < S::STAGES - 1; ++i) copy_tile(warp, i, begin + i < end, blocks[i], (uint32_t)pos[i], heads[i], lane);
+        for (int i = 0; i < S::STAGES - 1; ++i) copy_tile(warp, i, lives[i], blocks[i], (uint32_t)pos[i], heads[i], lane);
         int32_t block = blocks[S::STAGES - 1];
         int p = pos[S::STAGES - 1], p_head = heads[S::STAGES - 1];
-        Queries<KV, DP, NT> q;
+        bool live = lives[S::STAGES - 1];
+        Q q;
         Running<S::HALVES, NT> run;
         const int in[NT][2] = {};
-        int stage = 0, head = 0, row0 = 0;
+        int stage = 0;
         bool fresh = true;
 #pragma unroll 1
-        for (int64_t u = begin; u < end; ++u) {
+        while (u < end) {
             if (fresh) {
-                head = head_of(at.run), row0 = at.run % a.row_blocks * WARP_ROWS;
-                const uint16_t *rows[NT];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const int r = row0 + nt * 8 + n;
-                    rows[nt] = r < a.rows ? a.q + at.t * a.q_stride + (int64_t)(head * a.rows + r) * cache.head_dim : nullptr;
-                }
-                q.load(rows, cache.head_dim, a.q_bf16, a.scale, j);
+                q.take(raw, a.q_bf16, a.scale, j);
                 run.reset();
+                Place next = at;
+                next.i = next.n - 1;
+                int64_t v = u + next.i - at.i;
+                step(next, v, runs);
+                if (v < end) ask(next);
             }
             wait_tile();
             __syncwarp();
-            copy_tile(warp, stage == 0 ? S::STAGES - 1 : stage - 1, ahead <= end, block, (uint32_t)p, p_head, lane);
-            fetch(block, p, p_head);
+            copy_tile(warp, stage == 0 ? S::STAGES - 1 : stage - 1, live, block, (uint32_t)p, p_head, lane);
+            live = fetch(block, p, p_head);
             const int of = warp * S::STAGES + stage;
             const uint32_t ok = real[of], keys = shared_address(ring + of * S::STAGE);
             if (ok) take_tile<KV, DP, NT, ALL_ROWS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in);
             if (++stage == S::STAGES) stage = 0;
             fresh = at.i == at.n - 1;
-            if (fresh || u + 1 == end) finish(run, q, at, u, begin, end, worker, sub, head, row0, n, j, lane);
-            step(at, runs);
+            if (fresh || u + 1 >= end) finish(run, q, at, u, begin, end, worker, sub, head_of(at.run), at.run % a.row_blocks * WARP_ROWS, n, j, lane);
+            step(at, u, runs);
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
@@ -1145,8 +1189,11 @@ attend_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ At
             book.seq[t] = r.s, book.end[t] = r.end;
             book.from[t] = GROUPED ? max(r.first, a.shared[t / a.group]) : r.first;
             if (!GROUPED) book.to[t] = r.end;
-            without = mine && (SHARED_WARPS == 0 || GROUPED ? at.own_units(t) : at.shared_units(t)) == 0;
-            n = (int64_t)(GROUPED || SHARED_WARPS == 0 ? at.own_units(t) * (cache.n_heads / a.together) : at.shared_units(t) * cache.n_heads) * a.row_blocks;
+            const int32_t units = GROUPED || SHARED_WARPS == 0 ? at.own_units(t) : at.shared_units(t);
+            if (units > 0)
+                n = (int64_t)(GROUPED || SHARED_WARPS == 0 ? units + A::PAIR_COST : units + A::SHARED_PAIR_COST) *
+                    (GROUPED || SHARED_WARPS == 0 ? cache.n_heads / a.together : cache.n_heads) * a.row_blocks;
+            without = mine && units == 0;
         }
         uint32_t empty = __ballot_sync(0xFFFFFFFFu, without);
         while (empty) {
@@ -1179,7 +1226,8 @@ attend_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ At
             int64_t n = 0;
             if (g < a.n_groups) {
                 book.to[g] = a.shared[g];
-                n = (int64_t)at.shared_units(g) * a.shared_row_blocks * cache.n_heads;
+                const int32_t units = at.shared_units(g);
+                if (units > 0) n = (int64_t)(units + A::SHARED_PAIR_COST) * a.shared_row_blocks * cache.n_heads;
                 if (n == 0 && g % gridDim.x == blockIdx.x)
                     for (int c = 0; c < cache.n_heads * a.shared_row_blocks; ++c) a.shared_cuts[(int64_t)g * cache.n_heads * a.shared_row_blocks + c] = make_int2(0, 0);
             }
