@@ -47,6 +47,8 @@ struct WriteArgs {
     int32_t *status;
     int32_t n_tokens;
     int32_t per, q_parts, k_parts;     // vectors of a lane group, and the groups of a token's queries and keys
+    int32_t tokens;           // of a block
+    Divisor lanes;            // of a vector, where they need not meet
 };
 
 // A lane has two chunks of eight dimensions of a vector, A and B, such that rotation stays within a lane: with pairs (i, i + rot / 2)
@@ -119,8 +121,8 @@ __device__ __forceinline__ float quantise(const Two (&y)[8], uint32_t (&codes)[4
     return !finite ? __uint_as_float(0x7FC00000u) : small ? 1.0f : __fdiv_rn(top, LARGEST);
 }
 
-// A group of LV lanes holds a vector, 16 elements a lane, and goes over some of a token's queries, keys or values with the token's
-// angles in registers.  The groups of a warp have different tokens, all for the same.
+// A group of LV lanes (0: just as many as it takes, which do not meet) holds a vector, 16 elements a lane, and goes over some of a
+// token's queries, keys or values with the token's angles in registers.  The groups of a warp have different tokens, all for the same.
 //
 // Memory, and instructions close behind: with a chunk a lane, partners by shuffle and single-number arithmetic 12001 tokens with
 // 32 + 16 heads took 102 us.
@@ -130,10 +132,11 @@ write_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ Wri
     cache_enter();
     constexpr int AHEAD = 4;             // vectors in flight
     constexpr bool NARROW = !std::is_same<CODE, T>::value;
-    const int lane = threadIdx.x & 31, c = lane & (LV - 1);
-    const uint32_t group = LV == 32 ? 0xFFFFFFFFu : ((1u << LV) - 1u) << (lane & ~(LV - 1));
-    const int64_t t = ((int64_t)blockIdx.x * CACHE_THREADS + threadIdx.x) / LV;
-    if (t >= a.n_tokens) return;
+    const int lane = threadIdx.x & 31, of = LV > 0 ? (int)threadIdx.x / (LV > 0 ? LV : 1) : (int)a.lanes.quotient(threadIdx.x);
+    const int c = (int)threadIdx.x - of * (LV > 0 ? LV : (int)a.lanes.d);
+    const uint32_t group = ((1u << LV) - 1u) << (lane & ~(LV - 1));
+    const int64_t t = (int64_t)blockIdx.x * a.tokens + of;
+    if (of >= a.tokens || t >= a.n_tokens) return;
     const int64_t slot = a.slot[t];
     const int32_t pos = a.table ? a.pos[t] : 0;
     const bool bad = slot < -1 || slot >= (int64_t)cache.n_blocks * cache.block.d || (slot >= 0 && a.table && (pos < 0 || pos >= a.n_pos));
@@ -330,7 +333,8 @@ read_kernel(CacheDev cache, ReadArgs a) {
 template <typename T, typename CODE>
 int32_t launch_write(const CacheDev &c, WriteArgs &a, cudaStream_t st) {
     const int heads = a.n_q_heads + 2 * c.n_heads;
-    const int lanes = c.head_dim <= 64 ? 4 : c.head_dim <= 128 ? 8 : 16;
+    constexpr bool NARROW = !std::is_same<CODE, T>::value;
+    const int lanes = !NARROW ? c.head_dim / 16 : c.head_dim <= 64 ? 4 : c.head_dim <= 128 ? 8 : 16;
     // as few vectors a group as the GPU has room for groups at once (768 threads an SM), and no more than 8: one for a step of few tokens
     const int64_t room = (int64_t)sm_count() * 768 / lanes;
     int64_t per = ((int64_t)a.n_tokens * heads + room - 1) / room;
@@ -338,14 +342,18 @@ int32_t launch_write(const CacheDev &c, WriteArgs &a, cudaStream_t st) {
     if ((heads + per - 1) / per + 3 > 65535) per = 8;
     a.per = (int)per;
     a.q_parts = (int)((a.n_q_heads + per - 1) / per), a.k_parts = (int)((c.n_heads + per - 1) / per);
-    const int64_t blocks = ((int64_t)a.n_tokens * lanes + CACHE_THREADS - 1) / CACHE_THREADS;
-    const dim3 grid((unsigned)blocks, (unsigned)(a.q_parts + 2 * a.k_parts));
-    if (lanes == 4)
-        WG_CUDA(launch_pdl(write_kernel<T, CODE, 4>, grid, dim3(CACHE_THREADS), st, c, a));
-    else if (lanes == 8)
-        WG_CUDA(launch_pdl(write_kernel<T, CODE, 8>, grid, dim3(CACHE_THREADS), st, c, a));
-    else
-        WG_CUDA(launch_pdl(write_kernel<T, CODE, 16>, grid, dim3(CACHE_THREADS), st, c, a));
+    a.tokens = CACHE_THREADS / lanes, a.lanes = Divisor::of((uint32_t)lanes);
+    const dim3 grid((unsigned)(((int64_t)a.n_tokens + a.tokens - 1) / a.tokens), (unsigned)(a.q_parts + 2 * a.k_parts));
+    if constexpr (!NARROW) {
+        WG_CUDA(launch_pdl(write_kernel<T, CODE, 0>, grid, dim3(CACHE_THREADS), st, c, a));
+    } else {
+        if (lanes == 4)
+            WG_CUDA(launch_pdl(write_kernel<T, CODE, 4>, grid, dim3(CACHE_THREADS), st, c, a));
+        else if (lanes == 8)
+            WG_CUDA(launch_pdl(write_kernel<T, CODE, 8>, grid, dim3(CACHE_THREADS), st, c, a));
+        else
+            WG_CUDA(launch_pdl(write_kernel<T, CODE, 16>, grid, dim3(CACHE_THREADS), st, c, a));
+    }
     WG_LAUNCHED();
     return WG_OK;
 }
