@@ -1,14 +1,17 @@
 """Beam search under a grammar, with a paged key / value cache.
 
 A toy language model (one attention layer, random weights, synthetic vocabulary) fills in a JSON
-reference lookup.  The model's part is plain PyTorch; what the library does is everything around it:
+reference lookup.  The model's part is plain PyTorch, its attention too unless ``--storage`` says what the library's
+is to hold; what the library does is everything around it:
 
   KvTables.extend      cache slots for the step's tokens (block tables from lengths, on the GPU)
   wg_beam_step         masks of the beams' automaton states, selection, states of the chosen beams
   KvTables.reorder     the block tables follow the selection; shared blocks stay shared
   wg_beam_backtrack    the hypotheses read back
+  KvCache.write        with --storage: keys and queries rotated, keys and values quantised into their slots
+  Attend               and the attention over them, a request's prompt read once for all of its beams
 
-    python examples/beam_search.py [--requests 2] [--beams 4] [--steps 48]
+    python examples/beam_search.py [--requests 2] [--beams 4] [--steps 48] [--storage bf16|e4m3|int8]
 """
 import argparse
 import os
@@ -47,7 +50,10 @@ class ToyModel:
         w = (keys @ e[:, :, None])[:, :, 0]
         w = torch.where(torch.arange(w.shape[1], device=w.device)[None, :] < lens[:, None], w, -1e30)
         w = torch.softmax(w, 1)
-        return (e + (w[:, :, None] * values).sum(1)) @ self.head + self.bias
+        return self.output(tokens, (w[:, :, None] * values).sum(1))
+
+    def output(self, tokens, context):
+        return (self.embed[tokens] + context) @ self.head + self.bias
 
 
 class PagedCache:
@@ -81,6 +87,32 @@ class PagedCache:
         self.tables.reorder(parent, self.planes)
 
 
+class LibraryCache(PagedCache):
+    """The same with the library's cache and attention: one head, 16-bit queries, what is held in 16 or 8 bits."""
+
+    def __init__(self, rows: int, most: int, n_blocks: int, n_beam: int, storage: str = "bf16"):
+        super().__init__(rows, most, n_blocks)
+        held = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "int8": torch.int8}[storage]
+        self.cache = wg.KvCache.empty(n_blocks, BLOCK, 1, DIM, held)
+        self.planes = self.cache.planes
+        self.rope, self.attention, self.n_beam = wg.Rope(most, DIM), wg.Attend(rows, 1, 1, DIM), n_beam
+        self.queries = torch.zeros((rows, 1, DIM), dtype=torch.bfloat16, device="cuda")
+
+    def append(self, n_new, tokens, model):
+        slots = wg.SlotMap(n_new.numel(), tokens.numel())
+        self.tables.extend(n_new, slots)
+        k, v = (x.to(torch.bfloat16)[:, None] for x in model.keys_values(tokens))
+        q = model.embed[tokens].to(torch.bfloat16)[:, None].contiguous()
+        self.cache.write(k, v, slots, rope=self.rope, q=q)
+        last = (slots.cu[1:] - 1).long().clamp(min=0)        # of every row's new tokens
+        self.queries = torch.where((n_new > 0)[:, None, None], q[last], self.queries) if tokens.numel() else self.queries
+
+    def attend(self):
+        out = torch.empty_like(self.queries)
+        self.attention(self.queries, self.cache, self.tables, out, scale=1.0, group=self.n_beam)
+        return out[:, 0].float()
+
+
 def search(model, vocab, grammar, prompts, n_beam: int, steps: int, cache=None):
     """Returns (tokens [requests, beams, steps], scores [requests, beams], finished [requests, beams])."""
     R, rows = len(prompts), len(prompts) * n_beam
@@ -107,8 +139,11 @@ def search(model, vocab, grammar, prompts, n_beam: int, steps: int, cache=None):
         n_new[r * n_beam] = len(p)
     cache.append(n_new, torch.tensor([t for p in prompts for t in p], device="cuda"), model)
     for step in range(steps):
-        keys, values = cache.read()
-        logits = model.logits(last, keys, values, cache.lens)
+        if isinstance(cache, LibraryCache):
+            logits = model.output(last, cache.attend())
+        else:
+            keys, values = cache.read()
+            logits = model.logits(last, keys, values, cache.lens)
         parent, token = parent_steps[step].view(-1), token_steps[step].view(-1)
         wg.wg_beam_step(beam, ctx, n_beam, gid, sid, score, logits, bitmask, parent, token)
         cache.follow(parent.view(R, n_beam))
@@ -126,12 +161,17 @@ def main() -> None:
     ap.add_argument("--requests", type=int, default=2)
     ap.add_argument("--beams", type=int, default=4)
     ap.add_argument("--steps", type=int, default=48)
+    ap.add_argument("--storage", choices=("bf16", "e4m3", "int8"), help="attention by the library, over a cache of this")
     a = ap.parse_args()
     vocab = make_vocab(32000, seed=1)
     grammar = wg.Grammar(flatten(grammars.json_reference_lookup(doc_nodes=60)))
     model = ToyModel(vocab)
     prompts = [[10 + 7 * r + i for i in range(5 + 9 * r)] for r in range(a.requests)]
-    out, score, finished = search(model, vocab, grammar, prompts, a.beams, a.steps)
+    cache = None
+    if a.storage:
+        rows, most = a.requests * a.beams, max(len(p) for p in prompts) + a.steps + 1
+        cache = LibraryCache(rows, most, rows * (-(-most // BLOCK) + 1), a.beams, a.storage)
+    out, score, finished = search(model, vocab, grammar, prompts, a.beams, a.steps, cache)
     for r in range(a.requests):
         for j in range(a.beams):
             text = b"".join(vocab.token(t) for t in out[r, j].tolist() if t >= 0 and t != vocab.eos_id)

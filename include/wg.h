@@ -762,13 +762,15 @@ int32_t wg_kv_read(const wg_kv_cache *cache, const int32_t *table, int64_t table
  * row, all passed over, or all scores -inf) has out = 0, lse = -inf; a NaN or +inf among its scores makes them NaN.
  * Nothing that a token does not see has an effect on it, NaN included.
  *
- * The work is dealt out evenly over the GPU by the lengths as they are, each long row to several blocks; the last of them to
- * finish joins their parts, in the order of positions, so results do not depend on the order in which blocks run.
+ * The work is dealt out evenly over the GPU by the lengths as they are, each long row to several blocks; their parts are
+ * joined in the order of positions, so results do not depend on the order in which blocks run.  The lengths may change
+ * between replays of a recorded call.  Made for one or a few tokens a sequence: every token of a long prompt would read all of
+ * it again (wg_kv_read gives other attention kernels dense keys and values).
  *
  * A wg_attend is scratch for up to max_tokens tokens a call; calls that share one are issued like calls that share a
  * wg_ctx: one at a time, on one stream or on streams ordered by events (recorded calls too).
  *   q, out     device, n_tokens rows of n_q_heads x head_dim elements, q_stride / out_stride elements apart (16-byte
- *              multiples); out may be q itself
+ *              multiples); out may be q itself, but may not overlap it otherwise
  *   dtype      WG_DTYPE_BF16 or WG_DTYPE_FP16, of q and out; a 16-bit cache has the same type
  *   lse        device, n_tokens x n_q_heads, or NULL
  *   n_q_heads  a multiple of the cache's n_heads
@@ -776,6 +778,7 @@ int32_t wg_kv_read(const wg_kv_cache *cache, const int32_t *table, int64_t table
  *   seq, pos, slot      device, n_tokens each, as wg_kv_extend returned them (a token with slot -1 has no row); or all
  *              NULL: one token per sequence, n_tokens <= n_seq, token t is the last one of sequence t.  A sequence or
  *              position outside the table makes a token without a row, too.
+ *   scale      finite
  *   window     0: everything
  *   group      tokens t = i * group .. i * group + group - 1 are looked at together (1 .. WG_BEAM_MAX_BEAMS): what their
  *              tables have in common from the first position on (a request's beams, the drafted tokens of a sequence) is

@@ -1,4 +1,5 @@
 // Attention over a paged cache (wg_attend_*, wg_kv_attend of wg.h): scratch, checks and launches.
+#include <cmath>
 #include <new>
 
 #include "wg_attend.h"
@@ -11,6 +12,8 @@ struct wg_attend {
 };
 
 namespace {
+
+constexpr float LOG2_E = 1.44269504088896f;
 
 // A row of partial results: the head size as the kernels round it, a maximum and a sum.
 int64_t part_row(int32_t head_dim) { return (head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256) + 4; }
@@ -89,7 +92,7 @@ int32_t wg_kv_attend(wg_attend *attend, const wg_kv_cache *cache, const void *q,
     if (!table || max_blocks < 1 || table_stride < max_blocks || n_seq < 1) return WG_ERR_ARG;
     const bool mapped = seq != nullptr;
     if (mapped != (pos != nullptr) || mapped != (slot != nullptr) || (!mapped && (!len || n_tokens > n_seq))) return WG_ERR_ARG;
-    if (window < 0 || group < 1 || group > WG_BEAM_MAX_BEAMS) return WG_ERR_ARG;
+    if (window < 0 || group < 1 || group > WG_BEAM_MAX_BEAMS || !std::isfinite(scale * LOG2_E)) return WG_ERR_ARG;
     if (n_tokens == 0) return WG_OK;
     const int64_t width = (int64_t)n_q_heads * cache->head_dim;
     if (!rows_ok(q, q_stride, width) || !rows_ok(out, out_stride, width)) return WG_ERR_ARG;
@@ -114,7 +117,7 @@ int32_t wg_kv_attend(wg_attend *attend, const wg_kv_cache *cache, const void *q,
         a.window = window, a.n_q_heads = n_q_heads, a.rows = rows, a.row_blocks = row_blocks;
         a.group = group, a.n_groups = (a.n_tokens + group - 1) / group;
         a.q_bf16 = dtype == WG_DTYPE_BF16;
-        a.scale = scale * 1.44269504088896f;
+        a.scale = scale * LOG2_E;
         a.together = cache->n_heads % 4 == 0 ? 4 : cache->n_heads % 2 == 0 ? 2 : 1;
         a.part_rows = rows < 16 ? rows : 16;
         a.shared = attend->shared, a.shared_cuts = attend->shared_cuts, a.own_cuts = attend->own_cuts;

@@ -18,9 +18,9 @@ HEAD = """
         return Cache(at, at, s, s, storage, n_blocks, block, H, D)
     scratch = C.c_void_p()
     def attend(c, n=4, Hq=32, dtype=0, q=at, qs=None, out=at, os=None, lse=None, table=at, stride=64, cols=64, len=at, n_seq=64, seq=None, pos=None, slot=None,
-               window=0, group=1, handle=None):
+               window=0, group=1, handle=None, scale=1.0):
         w = Hq * c.head_dim
-        return lib.wg_kv_attend(handle or scratch, C.byref(c), q, qs or w, out, os or w, lse, dtype, Hq, table, stride, cols, len, n_seq, seq, pos, slot, n, 1.0,
+        return lib.wg_kv_attend(handle or scratch, C.byref(c), q, qs or w, out, os or w, lse, dtype, Hq, table, stride, cols, len, n_seq, seq, pos, slot, n, scale,
                                 window, group, None)
     def launches():
         return sum(x.startswith("launch") for x in log())
@@ -53,7 +53,8 @@ def test_attention_refuses(fake):  # noqa: F811
     odd = at + 8
     bad = [dict(n=-1), dict(n=51), dict(dtype=1), dict(dtype=2), dict(dtype=3), dict(Hq=16), dict(Hq=64), dict(q=None), dict(out=None), dict(q=odd), dict(out=odd),
            dict(qs=4095), dict(qs=4092), dict(os=4100), dict(table=None), dict(cols=0), dict(stride=63), dict(n_seq=0), dict(len=None), dict(n=5, n_seq=4),
-           dict(seq=at), dict(pos=at), dict(slot=at), dict(seq=at, pos=at), dict(seq=at, slot=at), dict(window=-1), dict(group=0), dict(group=33)]
+           dict(seq=at), dict(pos=at), dict(slot=at), dict(seq=at, pos=at), dict(seq=at, slot=at), dict(window=-1), dict(group=0), dict(group=33),
+           dict(scale=float('nan')), dict(scale=float('inf')), dict(scale=3e38)]
     for how in bad:
         assert attend(cache(), **how) == -1, how
     for c in (cache(H=4), cache(D=64), cache(1), cache(n_blocks=1 << 28, block=16), cache(n_blocks=0), cache(4)):

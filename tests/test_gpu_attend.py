@@ -433,3 +433,41 @@ def test_calls_one_after_the_other_share_the_scratch(wg):
         a.attend(q, s.cache, s.tables, out, group=group)
     for i, out in enumerate(outs):
         assert torch.equal(out.cpu(), want[i % 2][0])
+
+
+def test_codes_that_are_nan_and_the_smallest(wg):
+    """e4m3's NaN in a key or a value of one position; int8's -128, which this library does not write."""
+    s = Setup(wg, [40, 40], 4, 2, 64, E4M3, seed=30)
+    b = int(s.table[0, 1])
+    s.k.view(torch.uint8)[b, 3, 0, 5] = 0x7F
+    s.v.view(torch.uint8)[b, 4, 1, 7] = 0xFF
+    s.on_gpu()
+    out, lse = s.run()
+    assert torch.isnan(out[0, :2]).all() and torch.isnan(lse[0, :2]).all()               # the key's head
+    assert torch.isnan(out[0, 2:, 7]).all() and int(torch.isnan(out[0, 2:]).sum()) == 2 and torch.isfinite(lse[0, 2:]).all()
+    assert torch.isfinite(out[1]).all()
+    s = Setup(wg, [40, 40], 4, 2, 64, INT8, seed=31)
+    s.k[int(s.table[0, 0]), 2], s.v[int(s.table[1, 2]), 1] = -128, -128
+    s.on_gpu()
+    s.check(s.run())
+
+
+@pytest.mark.parametrize("held", [BF16, FP16, E4M3, INT8])
+def test_the_end_of_a_shared_tile_holds_nan_for_some(wg, held):
+    """Beams that share a block and end at different places in it; what lies behind the shorter ones' ends is NaN or infinite for
+    the longer ones, and nothing to the shorter."""
+    model = held if held in (BF16, FP16) else BF16
+    lens = [70, 75, 79, 72]
+    s = Setup(wg, lens, 8, 2, 64, held, model, seed=32, share={b: (2, 5) for b in (0, 1, 3)})
+    clean = Setup(wg, lens, 8, 2, 64, held, model, seed=32, share={b: (2, 5) for b in (0, 1, 3)}).on_gpu()
+    b = int(s.table[2, 4])
+    if held in (E4M3, INT8):
+        s.vs[b, 73 - 64], s.vs[b, 76 - 64] = math.nan, math.inf
+    else:
+        s.v[b, 73 - 64], s.v[b, 76 - 64] = math.nan, math.inf
+    s.on_gpu()
+    for group in (2, 4):
+        out, want = s.run(group=group)[0], clean.run(group=group)[0]
+        assert torch.equal(out[[0, 3]], want[[0, 3]])                  # 70 and 72 positions
+        assert not torch.isfinite(out[1]).any() and not torch.isfinite(out[2]).any()
+    clean.check(clean.run(group=4))
