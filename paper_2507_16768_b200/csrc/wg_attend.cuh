@@ -19,7 +19,7 @@
 // row's largest loses its last bits: 2^-25 of the largest).  A key's scale multiplies the score.  A value's scale s cannot
 // simply multiply p, which then might fall below fp16's range while it matters: with x' = x + log2 s and the maximum m taken
 // over x', p' = 2^(x' - m) is at most 1 and largest where the result comes from, and l is the sum of 2^(x - m).  Scales
-// below 2^-100 count as that, which keeps l below 2^100 times the number of positions.
+// below 2^-80 count as that, which keeps l below 2^95 times the number of positions.
 #pragma once
 
 #include <type_traits>
@@ -229,6 +229,9 @@ struct Shape {
     static constexpr int STAGES = 3;
     static constexpr int SMEM = ATTEND_WARPS * STAGES * STAGE;
     static constexpr int BLOCKS = SMEM > 110 * 1024 ? 1 : 2;        // on an SM
+    // fp16 weights are 2^15 times as large as they need be (and so are sums and results): what is below 2^-29 of the largest loses
+    // bits, instead of what is below 2^-14.
+    static constexpr float UP = std::is_same<Mma, __half>::value ? 15.0f : 0.0f;
     static constexpr int STEPS = DP / 16;                   // of the first product
     static constexpr int HALVES = DP / 64;                  // of the second, 64 dimensions each
     static constexpr int PITCH = DP + 4;                    // of a row of partial results in shared memory, in floats
@@ -384,7 +387,7 @@ __device__ __forceinline__ void take_tile(Running<DP / 64, NT> &run, const Queri
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const float ks = scales[s * 16 + n + 8 * e], vs = scales[S::TILE + s * 16 + n + 8 * e];
-                up[s][e] = __log2f(vs < 0x1p-100f ? 0x1p-100f : vs);      // (a NaN stays one)
+                up[s][e] = __log2f(vs < 0x1p-80f ? 0x1p-80f : vs);      // (a NaN stays one)
                 if (PART && !((real >> (s * 16 + n + 8 * e)) & 1u)) up[s][e] = 0.0f;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) x[s][nt][2 * e] *= ks, x[s][nt][2 * e + 1] *= ks;
@@ -434,8 +437,8 @@ __device__ __forceinline__ void take_tile(Running<DP / 64, NT> &run, const Queri
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
             const float g = S::NARROW ? 1.0f : f;
-            base[nt][c] = m == NEG_INFINITY ? 0.0f : m * g;
-            shrink[nt][c] = m > run.m[nt][c] ? power2(fmaf(run.m[nt][c], g, -base[nt][c])) : 1.0f;
+            base[nt][c] = m == NEG_INFINITY ? 0.0f : fmaf(m, g, -S::UP);
+            shrink[nt][c] = m > run.m[nt][c] ? power2(fmaf(run.m[nt][c], g, -S::UP) - base[nt][c]) : 1.0f;
             grew |= m > run.m[nt][c];
             run.m[nt][c] = m;
         }
@@ -711,8 +714,10 @@ struct Attend : Results<DP> {
     }
     __device__ __forceinline__ int32_t own_units(int t) const { return GROUPED || SHARED_WARPS == 0 ? tiles_of(book.from[t], book.end[t], S::TILE) : 0; }
 
-    // A running maximum as an exponent of 2: with scales it is one already.
-    static __device__ __forceinline__ float scaled(float m, float factor) { return S::NARROW || m == NEG_INFINITY ? m : m * factor; }
+    // The exponent of 2 that a running maximum stands for beside its sum.  (With scales it is one already.)
+    static __device__ __forceinline__ float scaled(float m, float factor) {
+        return m == NEG_INFINITY ? m : fmaf(m, S::NARROW ? 1.0f : factor, -S::UP);
+    }
 
     // ---- tiles ----
     // A warp's tile: lane i knows the block of position `pos` of the tile (i % TILE).  Commits a group of copies.
