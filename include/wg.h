@@ -729,7 +729,7 @@ int32_t wg_rope_table(const double *freq, int32_t n_freq, int32_t n_pos, double 
  *   q        device, n_tokens rows of n_q_heads x head_dim, or NULL (n_q_heads then 0); q_out may be q itself
  *            (with the same stride) but may not overlap it otherwise
  *   dtype    WG_DTYPE_BF16 or WG_DTYPE_FP16, of q, k, v and q_out; a 16-bit cache has the same type
- *   rope     host struct, or NULL: nothing is rotated (pos is not looked at; q and q_out must be NULL)
+ *   rope     host struct, or NULL: nothing is rotated (pos is not looked at; q is copied to q_out)
  *   slot     device, n_tokens; -1: nothing is written for the token.  The slots of a call differ from each other.
  *   pos      device, n_tokens
  *   status   device, n_tokens, or NULL: WG_OK; WG_ERR_ARG for a slot outside the cache (other than -1) or a position

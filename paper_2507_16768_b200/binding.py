@@ -1151,7 +1151,7 @@ class KvCache:
     def write(self, k, v, slots: SlotMap, rope: Optional[Rope] = None, q=None, q_out=None, status=None, stream=None) -> None:
         """wg_kv_write: the tokens of ``slots`` into the cache.  ``k``, ``v`` are ``[n_tokens, n_heads, head_dim]`` (views into
         a fused projection will do), ``q`` and ``q_out`` ``[n_tokens, query heads, head_dim]``; without ``q_out`` the queries
-        are rotated in place.  ``status`` [n_tokens] gets WG_ERR_ARG for slots outside the cache and positions outside ``rope``."""
+        are rotated in place; without ``rope`` nothing is rotated.  ``status`` [n_tokens] gets WG_ERR_ARG for slots outside the cache and positions outside ``rope``."""
         n, dev, dtype = slots.n_tokens, self.device, k.dtype
         kind = _model_dtype(k, "k")
         if self.storage <= WG_KV_FP16 and dtype is not self.dtype:
@@ -1163,8 +1163,6 @@ class KvCache:
         qp = qs = op = os_ = None
         heads = 0
         if q is not None:
-            if rope is None:
-                raise ValueError("queries are rotated: rope is required with q")
             heads = int(q.shape[1]) if q.dim() == 3 else 0
             if heads < 1:
                 raise ValueError("q must be [n_tokens, query heads, head_dim]")

@@ -419,7 +419,7 @@ int32_t wg_kv_write(const wg_kv_cache *cache, const void *k, int64_t k_stride, c
     if (!cache_ok(cache) || n_tokens < 0 || n_q_heads < 0 || n_q_heads > 65535) return WG_ERR_ARG;
     if (dtype != WG_DTYPE_BF16 && dtype != WG_DTYPE_FP16) return WG_ERR_ARG;
     if (cache->storage <= WG_KV_FP16 && (cache->storage == WG_KV_FP16) != (dtype == WG_DTYPE_FP16)) return WG_ERR_ARG;
-    if ((q != nullptr) != (q_out != nullptr) || (q != nullptr) != (n_q_heads > 0) || (q && !rope)) return WG_ERR_ARG;
+    if ((q != nullptr) != (q_out != nullptr) || (q != nullptr) != (n_q_heads > 0)) return WG_ERR_ARG;
     if (rope && (!rope->table || ((uintptr_t)rope->table & 15) || rope->n_pos < 1 || rope->rot_dim < 16 || rope->rot_dim % 16 ||
                  rope->rot_dim > cache->head_dim))
         return WG_ERR_ARG;

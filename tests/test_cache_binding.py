@@ -93,7 +93,7 @@ def write(c=None, **k):
 
 def test_a_good_write_reaches_the_library(no_library):  # noqa: F811
     strided = dict(k=At((6, 2, 64), strides=(1024, 64, 1)), q_out=None)
-    for how in ({}, strided, dict(q=None, q_out=None), dict(rope=None, q=None, q_out=None), dict(status=FakeTensor((6,)))):
+    for how in ({}, strided, dict(q=None, q_out=None), dict(rope=None, q=None, q_out=None), dict(rope=None), dict(status=FakeTensor((6,)))):
         with pytest.raises(AssertionError, match="wg_kv_write was called"):
             write(**how)
     with pytest.raises(AssertionError, match="wg_kv_write was called"):
@@ -105,7 +105,7 @@ def test_a_good_write_reaches_the_library(no_library):  # noqa: F811
     dict(v=At((6, 2, 64), FP16)), dict(v=At((6, 2, 64), device=1)), dict(v=At((6, 2, 64), cuda=False)), dict(v=At((6, 2, 64), at=0x1002)),
     dict(v=At((6, 2, 64), strides=(132, 64, 1))), dict(v=At((6, 2, 64), strides=(64, 64, 1))), dict(v=At((6, 2, 64), strides=(0, 64, 1))),
     dict(v=At((6, 2, 64), strides=(128, 1, 2))), dict(v=At((6, 2, 64), strides=(256, 128, 1))), dict(q=At((7, 8, 64))), dict(q=At((6, 0, 64))),
-    dict(q=At((6, 512))), dict(q_out=At((6, 4, 64))), dict(q_out=At((6, 8, 64), FP16)), dict(q=None), dict(rope=None),
+    dict(q=At((6, 512))), dict(q_out=At((6, 4, 64))), dict(q_out=At((6, 8, 64), FP16)), dict(q=None),
     dict(slots=other(FakeSlots, device=1)), dict(slots=other(FakeSlots, n_tokens=7)), dict(rope=other(FakeRope, device=1)),
     dict(rope=other(FakeRope, rot_dim=80)), dict(status=FakeTensor((5,))), dict(status=FakeTensor((6,), torch.int64))])
 def test_a_write_refuses(no_library, bad):  # noqa: F811
@@ -206,7 +206,7 @@ def lib_write(cache_=None, k=0x1000, ks=128, v=0x1000, vs=128, q=0x1000, qs=512,
 
 
 @pytest.mark.parametrize("bad", [dict(cache_=c) for c in BAD_CACHES] + [
-    dict(n=-1), dict(heads=-1), dict(heads=0), dict(heads=70000), dict(dtype=1), dict(dtype=2), dict(dtype=3), dict(q=None), dict(o=None), dict(rope_=None),
+    dict(n=-1), dict(heads=-1), dict(heads=0), dict(heads=70000), dict(dtype=1), dict(dtype=2), dict(dtype=3), dict(q=None), dict(o=None),
     dict(rope_=dict(table=None)), dict(rope_=dict(table=0x1004)), dict(rope_=dict(n_pos=0)), dict(rope_=dict(rot_dim=8)), dict(rope_=dict(rot_dim=24)),
     dict(rope_=dict(rot_dim=80)), dict(k=None), dict(v=None), dict(k=0x1002), dict(ks=120), dict(ks=132), dict(vs=64), dict(qs=504), dict(os=508),
     dict(q=0x1008), dict(slot=None), dict(pos=None)])

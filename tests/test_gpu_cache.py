@@ -149,6 +149,8 @@ def test_without_queries_and_without_rotation(wg, held):
     w.run(with_q=False)
     w.slots.pos.fill_(-7)            # (not looked at)
     w.run(with_q=False)
+    w.run()                          # (queries pass through)
+    w.run(in_place=True)
 
 
 @pytest.mark.parametrize("interleaved", [False, True])
