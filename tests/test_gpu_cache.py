@@ -419,15 +419,14 @@ def test_prompts_steps_beams_and_reads_together(wg, model, held):
         given[:] = [list(given[p]) for p in flat]
         step([1] * N, K)
         parents = torch.randint(0, K, (R, K), generator=g).to(torch.int32).cuda()
-    keep = [len(x) - 1 - i % 2 for i, x in enumerate(given)]
-    # (cut into a block of one's own: what is shared must not be written to)
+    # (the last token lies in a block of the sequence's own: what is shared must not be written to)
     step([1] * N, 1)
     tables.shrink(torch.tensor([len(x) - 1 for x in given], dtype=torch.int32, device="cuda"))
     given[:] = [x[:-1] for x in given]
     step([2] * N, 2)
     cu = torch.zeros(N + 1, dtype=torch.int32, device="cuda")
     cu[1:] = torch.cumsum(lens, 0)
-    assert lens.tolist() == [len(x) for x in given] and keep
+    assert lens.tolist() == [len(x) for x in given]
     v_out = torch.empty((int(cu[-1]), H, D), dtype=FP32, device="cuda")
     cache.read(tables, cu, None, v_out)
     want = torch.cat([torch.stack([v for _, v in x]) for x in given])
