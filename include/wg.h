@@ -759,7 +759,8 @@ int32_t wg_kv_read(const wg_kv_cache *cache, const int32_t *table, int64_t table
  *   x[i] = scale * (q . k[i]);  lse = log sum of exp(x[i]);  out = sum of exp(x[i] - lse) v[i]
  * in fp32, one rounding at the end; the weights exp(x[i] - max) enter the second product in the cache's 16-bit type (8-bit
  * caches: fp16).  Positions whose table entry is no block of the cache are passed over.  A token that sees nothing (no
- * row, all passed over, or all scores -inf) has out = 0, lse = -inf; a NaN or +inf among its scores makes them NaN.
+ * row, all passed over, or all scores -inf) has out = 0, lse = -inf; a NaN or +inf among its scores makes them NaN.  Infinite and NaN
+ * values (and scales of values) are in out, not in lse.
  * Nothing that a token does not see has an effect on it, NaN included.
  *
  * The work is dealt out evenly over the GPU by the lengths as they are, each long row to several blocks; their parts are

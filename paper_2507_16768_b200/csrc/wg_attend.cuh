@@ -20,7 +20,8 @@
 // row's largest loses its last bits: 2^-25 of the largest).  A key's scale multiplies the score.  A value's scale s cannot
 // simply multiply p, which then might fall below fp16's range while it matters: with x' = x + log2 s and the maximum m taken
 // over x', p' = 2^(x' - m) is at most 1 and largest where the result comes from, and l is the sum of 2^(x - m).  Scales
-// below 2^-80 count as that, which keeps l below 2^95 times the number of positions.
+// below 2^-80 count as that, which keeps l below 2^95 times the number of positions, and so do infinities and NaN: those are put into
+// the second product where a tile has some, and the sum, which has no values in it, goes without.
 #pragma once
 
 #include <type_traits>
@@ -383,17 +384,19 @@ __device__ __forceinline__ void take_tile(Running<DP / 64, NT> &run, const Queri
             }
         }
     float up[S::SUBS][2];                    // log2 of a value's scale
+    bool odd = false;                        // some scales are infinite or NaN
     if constexpr (S::NARROW) {
 #pragma unroll
         for (int s = 0; s < S::SUBS; ++s)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const float ks = scales[s * 16 + n + 8 * e], vs = scales[S::TILE + s * 16 + n + 8 * e];
-                up[s][e] = __log2f(vs < 0x1p-80f ? 0x1p-80f : vs);      // (a NaN stays one)
-                if (PART && !((real >> (s * 16 + n + 8 * e)) & 1u)) up[s][e] = 0.0f;
+                up[s][e] = __log2f(vs >= 0x1p-80f && vs < -NEG_INFINITY ? vs : 0x1p-80f);
+                odd |= !(vs < -NEG_INFINITY);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) x[s][nt][2 * e] *= ks, x[s][nt][2 * e + 1] *= ks;
             }
+        odd = __any_sync(0xFFFFFFFFu, odd);
     }
     if (PART || real != S::ALL) {
 #pragma unroll
@@ -470,7 +473,15 @@ __device__ __forceinline__ void take_tile(Running<DP / 64, NT> &run, const Queri
                     const float z = fmaf(x[s][nt][2 * e + c], q.factor[nt][c], -base[nt][c]);
                     y[c] = power2(z);
                     run.l[nt][c] += y[c];
-                    if constexpr (S::NARROW) y[c] = power2(z + up[s][e]);
+                    if constexpr (S::NARROW) {
+                        const float weight = y[c];
+                        y[c] = power2(z + up[s][e]);
+                        if (odd) {
+                            const int at = s * 16 + n + 8 * e;
+                            const float vs = scales[S::TILE + at];
+                            if (!(vs < -NEG_INFINITY) && (!PART || ((real >> at) & 1u))) y[c] = weight == 0.0f ? __uint_as_float(0x7FC00000u) : vs;
+                        }
+                    }
                 }
                 p[s][nt][e] = transpose8x8(pack<Mma>(y[0], y[1]));
             }
