@@ -20,8 +20,13 @@
 // row's largest loses its last bits: 2^-25 of the largest).  A key's scale multiplies the score.  A value's scale s cannot
 // simply multiply p, which then might fall below fp16's range while it matters: with x' = x + log2 s and the maximum m taken
 // over x', p' = 2^(x' - m) is at most 1 and largest where the result comes from, and l is the sum of 2^(x - m).  Scales
-// below 2^-80 count as that, which keeps l below 2^95 times the number of positions, and so do infinities and NaN: those are put into
+// below 2^-80 count as that, which keeps l below 2^80 times the number of positions, and so do infinities and NaN: those are put into
 // the second product where a tile has some, and the sum, which has no values in it, goes without.
+//
+// Scores of any size.  A score of 10^7 is rounded to whole numbers in fp32, and so would be x less a rounded maximum, or log2 s
+// beside it.  So the maximum is subtracted before anything else is done: with 16 bits m is one of the dot products as they are, and
+// p = 2^((x - m) scale) is 1 at m.  With 8 bits x' is made from dot products less an origin, 0 until x' passes 256 and then
+// moved to where the scores are, and what is kept of a row comes with its origin (Frame).
 #pragma once
 
 #include <type_traits>
@@ -232,13 +237,13 @@ struct Shape {
     static constexpr int STAGES = 3;
     static constexpr int SMEM = ATTEND_WARPS * STAGES * STAGE;
     static constexpr int BLOCKS = SMEM > 110 * 1024 ? 1 : 2;        // on an SM
-    // fp16 weights are 2^15 times as large as they need be (and so are sums and results): what is below 2^-29 of the largest loses
+    // fp16 weights are 2^15 times as large as they need be (and so are results): what is below 2^-29 of the largest loses
     // bits, instead of what is below 2^-14.
-    static constexpr float UP = std::is_same<Mma, __half>::value ? 15.0f : 0.0f;
+    static constexpr float UP = std::is_same<Mma, __half>::value ? 15.0f : 0.0f, DOWN = std::is_same<Mma, __half>::value ? 0x1p-15f : 1.0f;
     static constexpr int STEPS = DP / 16;                   // of the first product
     static constexpr int HALVES = DP / 64;                  // of the second, 64 dimensions each
     static constexpr int PITCH = DP + 4;                    // of a row of partial results in shared memory, in floats
-    static_assert(16 * PITCH * 4 + 128 <= STAGES * STAGE, "a warp's partial result takes the place of its ring");
+    static_assert(16 * PITCH * 4 + 256 <= STAGES * STAGE, "a warp's partial result takes the place of its ring");
 
     // Where piece c of vector r lies in a tile.  Eight lanes read 128 bytes at a time: four pieces of two neighbouring keys, one
     // or two of four values two rows apart; the pieces are swapped about so that those lie in different banks.
@@ -249,16 +254,26 @@ struct Shape {
     static __device__ __forceinline__ int value_at(int r, int c) { return ((r * CHUNKS + c) ^ (r & 6)) * 16; }
 };
 
+// What results are relative to: 2^(origin factor + near), the largest exponent; near is -infinity where there is none.
+struct Frame {
+    float origin, factor, near;
+    static __device__ __forceinline__ Frame none() { return {0.0f, 0.0f, NEG_INFINITY}; }
+    __device__ __forceinline__ float less(const Frame &f) const { return fmaf(origin - f.origin, factor, near - f.near); }
+    __device__ __forceinline__ float exponent() const { return fmaf(origin, factor, near); }
+};
+
 // Running results of 8 NT rows in a warp: with n = lane / 4 and j = lane % 4 a lane has rows 8 nt + 2 j + c, c = 0, 1.
-template <int HALVES, int NT>
+template <typename S, int NT>
 struct Running {
+    static constexpr int HALVES = S::HALVES;
     float m[NT][2], l[NT][2];     // (l: the lane's share until sum_up)
+    float origin[NT][2];          // 8 bits: of the scores that m has been taken from
     float o[HALVES][4][NT][4];    // [h][i][nt][2 e + c]: dimension 64 h + 8 n + 2 i + e
     __device__ __forceinline__ void reset() {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             m[nt][0] = m[nt][1] = NEG_INFINITY;
-            l[nt][0] = l[nt][1] = 0.0f;
+            l[nt][0] = l[nt][1] = origin[nt][0] = origin[nt][1] = 0.0f;
 #pragma unroll
             for (int h = 0; h < HALVES; ++h)
 #pragma unroll
@@ -275,9 +290,14 @@ struct Running {
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) l[nt][c] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][c], d);
     }
+    // A row's frame, its sum, and eight dimensions, without the factor 2^UP.  (8-bit caches' sums do not have it.)
+    __device__ __forceinline__ Frame frame(int nt, int c, float factor) const {
+        return S::NARROW ? Frame{origin[nt][c], factor, m[nt][c] - S::UP} : Frame{0.0f, 0.0f, m[nt][c] * factor};
+    }
+    __device__ __forceinline__ float sum(int nt, int c) const { return S::NARROW ? l[nt][c] : l[nt][c] * S::DOWN; }
     __device__ __forceinline__ void eight(int h, int nt, int c, float (&y)[8]) const {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = o[h][i / 2][nt][2 * (i & 1) + c];
+        for (int i = 0; i < 8; ++i) y[i] = o[h][i / 2][nt][2 * (i & 1) + c] * S::DOWN;
     }
 };
 
@@ -352,13 +372,28 @@ struct Queries {
 // then TILE of values.  ENDS: a row takes in the positions before its end only (in the tile); values have to be finite, for
 // those behind it get the weight 0.  PART: the positions that do not count may hold anything (otherwise zeros), and only rows whose
 // end is not 0 take them in; whatever the positions hold, the other rows stay as they are.
+// False: nothing was taken in, for an origin has moved (`moves`: how often, for this tile), and the tile has to be given once more.  (A
+// loop in here around the scores kept them apart from what follows: 64 x 16384 e4m3 315 us instead of 291.)
 enum Rows { ALL_ROWS, ENDS, PART_OF_ROWS };
 template <typename KV, int DP, int NT, Rows ROWS>
-__device__ __forceinline__ void take_tile(Running<DP / 64, NT> &run, const Queries<KV, DP, NT> &q, uint32_t keys, uint32_t values,
-                                          const float *scales, uint32_t real, int n, int j, const int (&ends)[NT][2]) {
+__device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const Queries<KV, DP, NT> &q, uint32_t keys, uint32_t values,
+                                          const float *scales, uint32_t real, int n, int j, const int (&ends)[NT][2], int moves) {
     using S = Shape<KV, DP>;
     constexpr bool PART = ROWS == PART_OF_ROWS;
     using Mma = typename S::Mma;
+    float up[S::SUBS][2];                    // log2 of a value's scale, and UP
+    bool odd = false;                        // some scales are infinite or NaN
+    if constexpr (S::NARROW) {
+#pragma unroll
+        for (int s = 0; s < S::SUBS; ++s)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float vs = scales[S::TILE + s * 16 + n + 8 * e];
+                up[s][e] = __log2f(vs >= 0x1p-80f && vs < -NEG_INFINITY ? vs : 0x1p-80f) + S::UP;
+                odd |= !(vs < -NEG_INFINITY);
+            }
+        odd = __any_sync(0xFFFFFFFFu, odd);
+    }
     float x[S::SUBS][NT][4] = {};            // [2 e + c]: of position 16 s + n + 8 e
 #pragma unroll
     for (int kk = 0; kk < S::CHUNKS / 4; ++kk)
@@ -383,20 +418,17 @@ __device__ __forceinline__ void take_tile(Running<DP / 64, NT> &run, const Queri
                 }
             }
         }
-    float up[S::SUBS][2];                    // log2 of a value's scale
-    bool odd = false;                        // some scales are infinite or NaN
     if constexpr (S::NARROW) {
 #pragma unroll
         for (int s = 0; s < S::SUBS; ++s)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const float ks = scales[s * 16 + n + 8 * e], vs = scales[S::TILE + s * 16 + n + 8 * e];
-                up[s][e] = __log2f(vs >= 0x1p-80f && vs < -NEG_INFINITY ? vs : 0x1p-80f);
-                odd |= !(vs < -NEG_INFINITY);
+                const float ks = scales[s * 16 + n + 8 * e];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) x[s][nt][2 * e] *= ks, x[s][nt][2 * e + 1] *= ks;
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) x[s][nt][2 * e + c] = fmaf(x[s][nt][2 * e + c], ks, -run.origin[nt][c]);
             }
-        odd = __any_sync(0xFFFFFFFFu, odd);
     }
     if (PART || real != S::ALL) {
 #pragma unroll
@@ -428,30 +460,53 @@ __device__ __forceinline__ void take_tile(Running<DP / 64, NT> &run, const Queri
     }
     // maxima: of x itself, which the factor (above 0) multiplies later; with scales of x' = factor x + up
     float base[NT][2], shrink[NT][2];
-    bool grew = false;
+    bool grew = false, far = false;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            const float f = q.factor[nt][c];
             float m = run.m[nt][c];
 #pragma unroll
             for (int s = 0; s < S::SUBS; ++s)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) m = fmaxf(m, S::NARROW ? fmaf(x[s][nt][2 * e + c], f, up[s][e]) : x[s][nt][2 * e + c]);
+                for (int e = 0; e < 2; ++e) {
+                    float &y = x[s][nt][2 * e + c];
+                    if constexpr (S::NARROW) y = fmaf(y, q.factor[nt][c], up[s][e]);
+                    m = fmaxf(m, y);
+                }
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-            const float g = S::NARROW ? 1.0f : f;
-            base[nt][c] = m == NEG_INFINITY ? 0.0f : fmaf(m, g, -S::UP);
-            shrink[nt][c] = m > run.m[nt][c] ? power2(fmaf(run.m[nt][c], g, -S::UP) - base[nt][c]) : 1.0f;
+            base[nt][c] = m;
             grew |= m > run.m[nt][c];
-            run.m[nt][c] = m;
+            far |= S::NARROW && m > run.m[nt][c] && fabsf(m) > 256.0f;
         }
     if (__any_sync(0xFFFFFFFFu, grew)) {
+        // x' of a few hundred has more bits behind the point than a weight: where there is more the origin follows.  (The second time
+        // takes what the first one's rounding left.)
+        if (S::NARROW && moves < 2 && __any_sync(0xFFFFFFFFu, far)) {
+            bool moved = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const float was = run.origin[nt][c], to = was + base[nt][c] / q.factor[nt][c], by = to - was;
+                    if (base[nt][c] > run.m[nt][c] && fabsf(base[nt][c]) > 256.0f && fabsf(to) < -NEG_INFINITY && fabsf(by) < -NEG_INFINITY && by != 0.0f) {
+                        run.origin[nt][c] = to;
+                        run.m[nt][c] -= by * q.factor[nt][c];
+                        moved = true;
+                    }
+                }
+            if (__any_sync(0xFFFFFFFFu, moved)) return false;
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c) run.l[nt][c] *= shrink[nt][c];
+            for (int c = 0; c < 2; ++c) {
+                const float less = run.m[nt][c] - base[nt][c];
+                shrink[nt][c] = base[nt][c] > run.m[nt][c] ? power2(S::NARROW ? less : less * q.factor[nt][c]) : 1.0f;
+                run.m[nt][c] = base[nt][c];
+                run.l[nt][c] *= shrink[nt][c];
+            }
 #pragma unroll
             for (int h = 0; h < S::HALVES; ++h)
 #pragma unroll
@@ -460,31 +515,41 @@ __device__ __forceinline__ void take_tile(Running<DP / 64, NT> &run, const Queri
                     for (int e = 0; e < 4; ++e) run.o[h][i][nt][e] *= shrink[nt][e & 1];
         }
     }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const float m = run.m[nt][c];
+            base[nt][c] = m == NEG_INFINITY ? 0.0f : S::NARROW ? m - S::UP : m;
+        }
     uint32_t p[S::SUBS][NT][2];
+    const auto weigh = [&](auto some_odd) {
+        constexpr bool ODD = decltype(some_odd)::value;
 #pragma unroll
-    for (int s = 0; s < S::SUBS; ++s)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int s = 0; s < S::SUBS; ++s)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float y[2];
+                const int at = s * 16 + n + 8 * e;
+                const float vs = ODD ? scales[S::TILE + at] : 0.0f;
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const float z = fmaf(x[s][nt][2 * e + c], q.factor[nt][c], -base[nt][c]);
-                    y[c] = power2(z);
-                    run.l[nt][c] += y[c];
-                    if constexpr (S::NARROW) {
-                        const float weight = y[c];
-                        y[c] = power2(z + up[s][e]);
-                        if (odd) {
-                            const int at = s * 16 + n + 8 * e;
-                            const float vs = scales[S::TILE + at];
-                            if (!(vs < -NEG_INFINITY) && (!PART || ((real >> at) & 1u))) y[c] = weight == 0.0f ? __uint_as_float(0x7FC00000u) : vs;
-                        }
+                for (int nt = 0; nt < NT; ++nt) {
+                    float y[2];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const float z = x[s][nt][2 * e + c] - base[nt][c];
+                        y[c] = power2(S::NARROW ? z : fmaf(z, q.factor[nt][c], S::UP));
+                        const float weight = S::NARROW ? power2(z - up[s][e]) : y[c];
+                        run.l[nt][c] += weight;
+                        if (ODD && !(vs < -NEG_INFINITY) && (!PART || ((real >> at) & 1u))) y[c] = weight == 0.0f ? __uint_as_float(0x7FC00000u) : vs;
                     }
+                    p[s][nt][e] = transpose8x8(pack<Mma>(y[0], y[1]));
                 }
-                p[s][nt][e] = transpose8x8(pack<Mma>(y[0], y[1]));
             }
+    };
+    if (S::NARROW && odd)
+        weigh(std::true_type{});
+    else
+        weigh(std::false_type{});
     const auto add = [&](float (&o)[NT][4], int s, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
         const uint32_t v[4] = {a0, a1, a2, a3};
 #pragma unroll
@@ -534,6 +599,7 @@ __device__ __forceinline__ void take_tile(Running<DP / 64, NT> &run, const Queri
                 }
             }
         }
+    return true;
 }
 
 // ---- where things are ------------------------------------------------------------------------------------------
@@ -549,7 +615,7 @@ struct Pair {
 // Where results go.
 template <int DP>
 struct Results {
-    static constexpr int PART_ROW = DP + 4;       // floats of a row's partial result: o, m, l
+    static constexpr int PART_ROW = DP + 4;       // floats of a row's partial result: o, its frame, l
 
     const CacheDev &cache;
     const AttendArgs &a;
@@ -565,12 +631,15 @@ struct Results {
     __device__ __forceinline__ float *kept(float *rows, int t, int q_head) const { return rows + ((int64_t)t * a.n_q_heads + q_head) * PART_ROW; }
 
     template <int N>
-    __device__ __forceinline__ void store_row(int t, int q_head, int d, float m, float l, const float (&y)[N]) const {
-        const float by = l == 0.0f ? 0.0f : 1.0f / l;
+    __device__ __forceinline__ void store_row(int t, int q_head, int d, const Frame &f, float l, const float (&y)[N]) const {
+        // (no score, or one beyond fp32's range)
+        const bool nothing = f.near == NEG_INFINITY && l == l;
+        if (f.exponent() == -NEG_INFINITY) l = __uint_as_float(0x7FC00000u);
+        const float by = 1.0f / l;
         uint32_t w[N / 2];
 #pragma unroll
         for (int e = 0; e < N; e += 2) {
-            const float y0 = l == 0.0f ? 0.0f : y[e] * by, y1 = l == 0.0f ? 0.0f : y[e + 1] * by;
+            const float y0 = nothing ? 0.0f : y[e] * by, y1 = nothing ? 0.0f : y[e + 1] * by;
             w[e / 2] = a.q_bf16 ? pack<__nv_bfloat16>(y0, y1) : pack<__half>(y0, y1);
         }
         uint16_t *to = a.out + t * a.out_stride + (int64_t)q_head * cache.head_dim + d;
@@ -581,17 +650,17 @@ struct Results {
         else
             *reinterpret_cast<uint32_t *>(to) = w[0];
         if (a.lse && d == 0)
-            a.lse[(int64_t)t * a.n_q_heads + q_head] = l == 0.0f ? NEG_INFINITY : (m + log2f(l)) * 0.693147180559945f;
+            a.lse[(int64_t)t * a.n_q_heads + q_head] = nothing ? NEG_INFINITY : (f.exponent() + log2f(l)) * 0.693147180559945f;
     }
-    // (m and l lie behind the dimensions)
-    __device__ __forceinline__ void keep_row(float *row, int d, float m, float l, const float (&y)[8]) const {
+    // (the frame and l lie behind the dimensions)
+    __device__ __forceinline__ void keep_row(float *row, int d, const Frame &f, float l, const float (&y)[8]) const {
         *reinterpret_cast<float4 *>(row + d) = make_float4(y[0], y[1], y[2], y[3]);
         *reinterpret_cast<float4 *>(row + d + 4) = make_float4(y[4], y[5], y[6], y[7]);
-        if (d == 0) *reinterpret_cast<float2 *>(row + DP) = make_float2(m, l);
+        if (d == 0) *reinterpret_cast<float4 *>(row + DP) = make_float4(f.origin, f.factor, f.near, l);
     }
-    // What a partial result counts beside maximum m.  (A sum without a maximum is NaN.)
-    static __device__ __forceinline__ float weight(float mi, float li, float m) {
-        return mi == NEG_INFINITY ? (li == 0.0f ? 0.0f : 1.0f) : power2(mi - m);
+    // What a partial result counts beside frame `top`.  (Without a maximum its sum is 0, or NaN, which stays.)
+    static __device__ __forceinline__ float weight(const Frame &f, float l, const Frame &top) {
+        return f.near == NEG_INFINITY ? (l == l ? 0.0f : 1.0f) : power2(f.less(top));
     }
 
     __device__ __forceinline__ int group_of(int t) const { return a.grouped ? t / a.group : t; }
@@ -645,11 +714,12 @@ attend_join_kernel(const __grid_constant__ CacheDev cache, const __grid_constant
         i -= n_x;
         return n_z == 1 ? to.kept(a.own_rows, t, q_head) : to.warp_part(z.y + i, sub, i == 0 ? z.x & 1 : 0, z_row);
     };
-    float m = NEG_INFINITY, l = 0.0f, y[PER] = {};
+    Frame m = Frame::none();
+    float l = 0.0f, y[PER] = {};
     for (int i0 = which * AHEAD; i0 < n; i0 += WARPS * AHEAD) {
         const int here = min(AHEAD, n - i0);
         const float *mine = piece(i0 + min(lane % AHEAD, here - 1));
-        float2 st = __ldcg(reinterpret_cast<const float2 *>(mine + DP));
+        float4 st = __ldcg(reinterpret_cast<const float4 *>(mine + DP));
         float2 f[AHEAD][PER / 2];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
@@ -657,13 +727,19 @@ attend_join_kernel(const __grid_constant__ CacheDev cache, const __grid_constant
 #pragma unroll
             for (int e = 0; e < PER / 2; ++e) f[k][e] = __ldcg(reinterpret_cast<const float2 *>(p) + e);
         }
-        if (lane % AHEAD >= here) st = make_float2(NEG_INFINITY, 0.0f);
-        float top = st.x;
+        if (lane % AHEAD >= here) st = make_float4(0.0f, 0.0f, NEG_INFINITY, 0.0f);
+        const Frame at{st.x, st.y, st.z};
+        Frame top = at;
 #pragma unroll
-        for (int o = AHEAD / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        top = fmaxf(top, m);
-        const float w = R::weight(st.x, st.y, top), old = R::weight(m, l, top);
-        float sum = st.y * w;
+        for (int o = AHEAD / 2; o > 0; o >>= 1) {
+            const Frame x{__shfl_xor_sync(0xFFFFFFFFu, top.origin, o), __shfl_xor_sync(0xFFFFFFFFu, top.factor, o), __shfl_xor_sync(0xFFFFFFFFu, top.near, o)};
+            if (x.less(top) > 0.0f) top = x;
+        }
+        // (frames that are equal up to rounding may have left lanes with different ones)
+        top = {__shfl_sync(0xFFFFFFFFu, top.origin, 0), __shfl_sync(0xFFFFFFFFu, top.factor, 0), __shfl_sync(0xFFFFFFFFu, top.near, 0)};
+        if (m.less(top) > 0.0f) top = m;
+        const float w = R::weight(at, st.w, top), old = R::weight(m, l, top);
+        float sum = st.w * w;
 #pragma unroll
         for (int o = AHEAD / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
         l = l * old + sum;
@@ -683,12 +759,12 @@ attend_join_kernel(const __grid_constant__ CacheDev cache, const __grid_constant
         static_assert(WARPS == ATTEND_WARPS, "");
 #pragma unroll
         for (int e = 0; e < PER; ++e) rows[warp][lane * PER + e] = y[e];
-        if (lane == 0) rows[warp][DP] = m, rows[warp][DP + 1] = l;
+        if (lane == 0) rows[warp][DP] = m.origin, rows[warp][DP + 1] = m.factor, rows[warp][DP + 2] = m.near, rows[warp][DP + 3] = l;
         __syncthreads();
         if (warp > 0) return;
         for (int w = 1; w < min(WARPS, (n + AHEAD - 1) / AHEAD); ++w) {
-            const float mw = rows[w][DP], lw = rows[w][DP + 1], top = fmaxf(m, mw);
-            const float old = R::weight(m, l, top), by = R::weight(mw, lw, top);
+            const Frame mw{rows[w][DP], rows[w][DP + 1], rows[w][DP + 2]}, top = mw.less(m) > 0.0f ? mw : m;
+            const float lw = rows[w][DP + 3], old = R::weight(m, l, top), by = R::weight(mw, lw, top);
             m = top, l = l * old + lw * by;
 #pragma unroll
             for (int e = 0; e < PER; ++e) y[e] = y[e] * old + rows[w][lane * PER + e] * by;
@@ -726,11 +802,6 @@ struct Attend : Results<DP> {
         return SHARED_WARPS == 0 ? 0 : tiles_of(GROUPED ? 0 : book.from[g], book.to[g], UNIT);
     }
     __device__ __forceinline__ int32_t own_units(int t) const { return GROUPED || SHARED_WARPS == 0 ? tiles_of(book.from[t], book.end[t], S::TILE) : 0; }
-
-    // The exponent of 2 that a running maximum stands for beside its sum.  (With scales it is one already.)
-    static __device__ __forceinline__ float scaled(float m, float factor) {
-        return m == NEG_INFINITY ? m : fmaf(m, S::NARROW ? 1.0f : factor, -S::UP);
-    }
 
     // ---- tiles ----
     // A warp's tile: lane i knows the block of position `pos` of the tile (i % TILE).  Commits a group of copies.
@@ -865,7 +936,7 @@ struct Attend : Results<DP> {
             }
         }
         int in[NTS][2] = {};                    // where the rows end in the tile
-        Running<S::HALVES, NTS> run;
+        Running<S, NTS> run;
         run.reset();
 #pragma unroll 1
         for (int i = 0; i < mine; ++i) {
@@ -875,6 +946,11 @@ struct Attend : Results<DP> {
             copy_tile(warp, (i + S::STAGES - 1) % S::STAGES, i + S::STAGES - 1 < mine, next, (uint32_t)position(i + S::STAGES - 1), pair.head, lane);
             next = block_at(i + S::STAGES);
             const int stage = i % S::STAGES;
+            int moves = 0;
+            const auto again = [&](bool taken, int &w) {      // the same tile once more where it was not taken in
+                moves = taken ? 0 : moves + 1;
+                w -= !taken;
+            };
 #pragma unroll 1
             for (int w = 0; w < WM; ++w) {
                 const int of = (stream * WM + w) * S::STAGES + stage;
@@ -883,7 +959,7 @@ struct Attend : Results<DP> {
                 const uint32_t keys = shared_address(ring + of * S::STAGE);
                 const int at = from + (i * STREAMS + stream) * STREAM + w * S::TILE;
                 if (!GROUPED || at + S::TILE <= least) {
-                    take_tile<KV, DP, NTS, ALL_ROWS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in);
+                    again(take_tile<KV, DP, NTS, ALL_ROWS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in, moves), w);
                     continue;
                 }
                 // rows that end within the tile, or before it
@@ -892,7 +968,7 @@ struct Attend : Results<DP> {
                     for (int nt = 0; nt < NTS; ++nt)
 #pragma unroll
                         for (int c = 0; c < 2; ++c) in[nt][c] = ends[nt][c] - at;
-                    take_tile<KV, DP, NTS, ENDS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in);
+                    again(take_tile<KV, DP, NTS, ENDS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in, moves), w);
                     continue;
                 }
                 // (an infinity or a NaN would reach them with the weight 0: the rows go by themselves)
@@ -912,8 +988,10 @@ struct Attend : Results<DP> {
                     for (int nt = 0; nt < NTS; ++nt)
 #pragma unroll
                         for (int c = 0; c < 2; ++c) in[nt][c] = min(ends[nt][c], at + S::TILE) == e;
-                    take_tile<KV, DP, NTS, PART_OF_ROWS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok & ((2u << (e - at - 1)) - 1u), n, j, in);
-                    past = e;
+                    if (take_tile<KV, DP, NTS, PART_OF_ROWS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok & ((2u << (e - at - 1)) - 1u), n, j, in, moves))
+                        past = e, moves = 0;
+                    else
+                        ++moves;
                 }
             }
         }
@@ -922,13 +1000,14 @@ struct Attend : Results<DP> {
         stream_sync(stream);
         // every warp's results into its ring
         float *const part = reinterpret_cast<float *>(ring + warp * S::STAGES * S::STAGE);
-        float2 *const stats = reinterpret_cast<float2 *>(part + SHARED_ROWS * S::PITCH);
+        float4 *const stats = reinterpret_cast<float4 *>(part + SHARED_ROWS * S::PITCH);
 #pragma unroll
         for (int nt = 0; nt < NTS; ++nt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const int r = nt * 8 + 2 * j + c;
-                if (n == 0) stats[r] = make_float2(scaled(run.m[nt][c], q.factor[nt][c]), run.l[nt][c]);
+                const Frame f = run.frame(nt, c, q.factor[nt][c]);
+                if (n == 0) stats[r] = make_float4(f.origin, f.factor, f.near, run.sum(nt, c));
 #pragma unroll
                 for (int h = 0; h < S::HALVES; ++h) {
                     float y[8];
@@ -948,19 +1027,21 @@ struct Attend : Results<DP> {
         for (int i = threadIdx.x; i < n_rows * (DP / 8); i += ATTEND_THREADS) {
             const int r = i / (DP / 8), d = (i % (DP / 8)) * 8, in_warp = r % SHARED_ROWS;
             const char *base = ring + (r / SHARED_ROWS) * S::STAGES * S::STAGE;
-            float m = NEG_INFINITY, l = 0.0f, y[8] = {};
-            float2 st[STREAMS];
+            Frame m = Frame::none();
+            float l = 0.0f, y[8] = {};
+            float4 st[STREAMS];
 #pragma unroll
             for (int s = 0; s < STREAMS; ++s) {
                 const float *of = reinterpret_cast<const float *>(base + s * WM * S::STAGES * S::STAGE);
-                st[s] = reinterpret_cast<const float2 *>(of + SHARED_ROWS * S::PITCH)[in_warp];
-                m = fmaxf(m, st[s].x);
+                st[s] = reinterpret_cast<const float4 *>(of + SHARED_ROWS * S::PITCH)[in_warp];
+                const Frame f{st[s].x, st[s].y, st[s].z};
+                if (f.less(m) > 0.0f) m = f;
             }
 #pragma unroll
             for (int s = 0; s < STREAMS; ++s) {
                 const float *of = reinterpret_cast<const float *>(base + s * WM * S::STAGES * S::STAGE) + in_warp * S::PITCH + d;
-                const float w = weight(st[s].x, st[s].y, m);
-                l += st[s].y * w;
+                const float w = weight(Frame{st[s].x, st[s].y, st[s].z}, st[s].w, m);
+                l += st[s].w * w;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] += of[e] * w;
             }
@@ -1100,7 +1181,7 @@ struct Attend : Results<DP> {
         int p = pos[S::STAGES - 1], p_head = heads[S::STAGES - 1];
         bool live = lives[S::STAGES - 1];
         Q q;
-        Running<S::HALVES, NT> run;
+        Running<S, NT> run;
         const int in[NT][2] = {};
         int stage = 0;
         bool fresh = true;
@@ -1121,7 +1202,11 @@ struct Attend : Results<DP> {
             live = fetch(block, p, p_head);
             const int of = warp * S::STAGES + stage;
             const uint32_t ok = real[of], keys = shared_address(ring + of * S::STAGE);
-            if (ok) take_tile<KV, DP, NT, ALL_ROWS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in);
+            if (ok) {
+                int moves = 0;
+#pragma unroll 1
+                while (!take_tile<KV, DP, NT, ALL_ROWS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in, moves)) ++moves;
+            }
             if (++stage == S::STAGES) stage = 0;
             fresh = at.i == at.n - 1;
             if (fresh || u + 1 >= end) finish(run, q, at, u, begin, end, worker, sub, head_of(at.run), at.run % a.row_blocks * WARP_ROWS, n, j, lane);
@@ -1130,7 +1215,7 @@ struct Attend : Results<DP> {
         asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
 
-    __device__ __forceinline__ void finish(Running<S::HALVES, NT> &run, const Queries<KV, DP, NT> &q, const Place &at, int64_t u, int64_t begin,
+    __device__ __forceinline__ void finish(Running<S, NT> &run, const Queries<KV, DP, NT> &q, const Place &at, int64_t u, int64_t begin,
                                            int64_t end, int worker, int sub, int head, int row0, int n, int j, int lane) const {
         const int64_t first = u - at.i;
         const bool whole = first >= begin && first + at.n <= end;
@@ -1146,16 +1231,17 @@ struct Attend : Results<DP> {
                 const int r = row0 + nt * 8 + 2 * j + c, q_head = head * a.rows + r;
                 if (r >= a.rows) continue;
                 float *to_keep = whole ? kept(a.own_rows, at.t, q_head) : warp_part(worker, sub, which, r - row0);
-                const float m = scaled(run.m[nt][c], q.factor[nt][c]);
+                const Frame m = run.frame(nt, c, q.factor[nt][c]);
+                const float l = run.sum(nt, c);
 #pragma unroll
                 for (int h = 0; h < S::HALVES; ++h) {
                     const int d = h * 64 + n * 8;
                     float y[8];
                     run.eight(h, nt, c, y);
                     if (!whole || more)
-                        keep_row(to_keep, d, m, run.l[nt][c], y);
+                        keep_row(to_keep, d, m, l, y);
                     else if (d < cache.head_dim)
-                        this->template store_row<8>(at.t, q_head, d, m, run.l[nt][c], y);
+                        this->template store_row<8>(at.t, q_head, d, m, l, y);
                 }
             }
     }
