@@ -19,9 +19,11 @@
 // 8-bit caches.  Codes are exact in fp16.  Queries enter in fp16, divided by a power of two per row (a query of 2^-14 of the
 // row's largest loses its last bits: 2^-25 of the largest).  A key's scale multiplies the score.  A value's scale s cannot
 // simply multiply p, which then might fall below fp16's range while it matters: with x' = x + log2 s and the maximum m taken
-// over x', p' = 2^(x' - m) is at most 1 and largest where the result comes from, and l is the sum of 2^(x - m).  Scales
-// below 2^-80 count as that, which keeps l below 2^80 times the number of positions, and so do infinities and NaN: those are put into
-// the second product where a tile has some, and the sum, which has no values in it, goes without.
+// over x', p' = 2^(x' - m) is at most 1 and largest where the result comes from, and l is the sum of 2^(x - m), held 2^12 times as
+// large: beside a scale of 2^121, the largest that is written, it has weights down to 2^-17 of the largest, beside 2^100 down to 2^-38.
+// For m, scales below 2^-96 count as that, which keeps l below 2^108 times the number of positions (all of them below that, and 2^20 of
+// them, are too much), and so do infinities and NaN: the rest of such a scale, or what it is, is put into p' where a tile has some, and
+// the sum, which has no values in it, goes without.
 //
 // Scores of any size.  A score of 10^7 is rounded to whole numbers in fp32, and so would be x less a rounded maximum, or log2 s
 // beside it.  So the maximum is subtracted before anything else is done: with 16 bits m is one of the dot products as they are, and
@@ -240,6 +242,8 @@ struct Shape {
     // fp16 weights are 2^15 times as large as they need be (and so are results): what is below 2^-29 of the largest loses
     // bits, instead of what is below 2^-14.
     static constexpr float UP = std::is_same<Mma, __half>::value ? 15.0f : 0.0f, DOWN = std::is_same<Mma, __half>::value ? 0x1p-15f : 1.0f;
+    // What x' has besides log2 s, such that the sums of 8-bit caches are 2^12 times as large as they need be.
+    static constexpr float BESIDE = NARROW ? UP - 12.0f : 0.0f;
     static constexpr int STEPS = DP / 16;                   // of the first product
     static constexpr int HALVES = DP / 64;                  // of the second, 64 dimensions each
     static constexpr int PITCH = DP + 4;                    // of a row of partial results in shared memory, in floats
@@ -290,14 +294,16 @@ struct Running {
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) l[nt][c] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][c], d);
     }
-    // A row's frame, its sum, and eight dimensions, without the factor 2^UP.  (8-bit caches' sums do not have it.)
+    // A row's frame, its sum, and eight dimensions.  (The sum of a 16-bit cache without the factor 2^UP, of an 8-bit one with its own, and
+    // results to go with it.)
     __device__ __forceinline__ Frame frame(int nt, int c, float factor) const {
         return S::NARROW ? Frame{origin[nt][c], factor, m[nt][c] - S::UP} : Frame{0.0f, 0.0f, m[nt][c] * factor};
     }
     __device__ __forceinline__ float sum(int nt, int c) const { return S::NARROW ? l[nt][c] : l[nt][c] * S::DOWN; }
     __device__ __forceinline__ void eight(int h, int nt, int c, float (&y)[8]) const {
+        constexpr float BY = S::NARROW ? S::DOWN * 0x1p12f : S::DOWN;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = o[h][i / 2][nt][2 * (i & 1) + c] * S::DOWN;
+        for (int i = 0; i < 8; ++i) y[i] = o[h][i / 2][nt][2 * (i & 1) + c] * BY;
     }
 };
 
@@ -381,16 +387,18 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
     using S = Shape<KV, DP>;
     constexpr bool PART = ROWS == PART_OF_ROWS;
     using Mma = typename S::Mma;
-    float up[S::SUBS][2];                    // log2 of a value's scale, and UP
-    bool odd = false;                        // some scales are infinite or NaN
+    constexpr float LEAST = 0x1p-96f;
+    float up[S::SUBS][2];                    // log2 of a value's scale, and BESIDE
+    bool odd = false;                        // some scales are below LEAST, infinite or NaN
     if constexpr (S::NARROW) {
 #pragma unroll
         for (int s = 0; s < S::SUBS; ++s)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const float vs = scales[S::TILE + s * 16 + n + 8 * e];
-                up[s][e] = __log2f(vs >= 0x1p-80f && vs < -NEG_INFINITY ? vs : 0x1p-80f) + S::UP;
-                odd |= !(vs < -NEG_INFINITY);
+                const bool usual = vs >= LEAST && vs < -NEG_INFINITY;
+                up[s][e] = __log2f(usual ? vs : LEAST) + S::BESIDE;
+                odd |= !usual;
             }
         odd = __any_sync(0xFFFFFFFFu, odd);
     }
@@ -502,10 +510,17 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const float less = run.m[nt][c] - base[nt][c];
-                shrink[nt][c] = base[nt][c] > run.m[nt][c] ? power2(S::NARROW ? less : less * q.factor[nt][c]) : 1.0f;
+                const float less = (run.m[nt][c] - base[nt][c]) * (S::NARROW ? 1.0f : q.factor[nt][c]);
+                const bool more = base[nt][c] > run.m[nt][c];
+                shrink[nt][c] = more ? power2(less) : 1.0f;
                 run.m[nt][c] = base[nt][c];
-                run.l[nt][c] *= shrink[nt][c];
+                // (by halves: scales may differ by more than 2^126)
+                if constexpr (S::NARROW) {
+                    const float half = more ? power2(0.5f * less) : 1.0f;
+                    run.l[nt][c] = run.l[nt][c] * half * half;
+                } else {
+                    run.l[nt][c] *= shrink[nt][c];
+                }
             }
 #pragma unroll
             for (int h = 0; h < S::HALVES; ++h)
@@ -540,7 +555,10 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
                         y[c] = power2(S::NARROW ? z : fmaf(z, q.factor[nt][c], S::UP));
                         const float weight = S::NARROW ? power2(z - up[s][e]) : y[c];
                         run.l[nt][c] += weight;
-                        if (ODD && !(vs < -NEG_INFINITY) && (!PART || ((real >> at) & 1u))) y[c] = weight == 0.0f ? __uint_as_float(0x7FC00000u) : vs;
+                        if (ODD && vs < LEAST)
+                            y[c] *= vs * (1.0f / LEAST);
+                        else if (ODD && !(vs < -NEG_INFINITY) && (!PART || ((real >> at) & 1u)))
+                            y[c] = weight == 0.0f ? __uint_as_float(0x7FC00000u) : vs;
                     }
                     p[s][nt][e] = transpose8x8(pack<Mma>(y[0], y[1]));
                 }
@@ -662,6 +680,11 @@ struct Results {
     static __device__ __forceinline__ float weight(const Frame &f, float l, const Frame &top) {
         return f.near == NEG_INFINITY ? (l == l ? 0.0f : 1.0f) : power2(f.less(top));
     }
+    // The same for its sum, which may be so large that it counts beside a weight below fp32's range.
+    static __device__ __forceinline__ float weighed(const Frame &f, float l, const Frame &top) {
+        const float half = f.near == NEG_INFINITY ? (l == l ? 0.0f : 1.0f) : power2(0.5f * f.less(top));
+        return l * half * half;
+    }
 
     __device__ __forceinline__ int group_of(int t) const { return a.grouped ? t / a.group : t; }
 
@@ -739,10 +762,10 @@ attend_join_kernel(const __grid_constant__ CacheDev cache, const __grid_constant
         top = {__shfl_sync(0xFFFFFFFFu, top.origin, 0), __shfl_sync(0xFFFFFFFFu, top.factor, 0), __shfl_sync(0xFFFFFFFFu, top.near, 0)};
         if (m.less(top) > 0.0f) top = m;
         const float w = R::weight(at, st.w, top), old = R::weight(m, l, top);
-        float sum = st.w * w;
+        float sum = R::weighed(at, st.w, top);
 #pragma unroll
         for (int o = AHEAD / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        l = l * old + sum;
+        l = R::weighed(m, l, top) + sum;
         m = top;
 #pragma unroll
         for (int e = 0; e < PER; ++e) y[e] *= old;
@@ -765,7 +788,7 @@ attend_join_kernel(const __grid_constant__ CacheDev cache, const __grid_constant
         for (int w = 1; w < min(WARPS, (n + AHEAD - 1) / AHEAD); ++w) {
             const Frame mw{rows[w][DP], rows[w][DP + 1], rows[w][DP + 2]}, top = mw.less(m) > 0.0f ? mw : m;
             const float lw = rows[w][DP + 3], old = R::weight(m, l, top), by = R::weight(mw, lw, top);
-            m = top, l = l * old + lw * by;
+            l = R::weighed(m, l, top) + R::weighed(mw, lw, top), m = top;
 #pragma unroll
             for (int e = 0; e < PER; ++e) y[e] = y[e] * old + rows[w][lane * PER + e] * by;
         }
@@ -1040,8 +1063,9 @@ struct Attend : Results<DP> {
 #pragma unroll
             for (int s = 0; s < STREAMS; ++s) {
                 const float *of = reinterpret_cast<const float *>(base + s * WM * S::STAGES * S::STAGE) + in_warp * S::PITCH + d;
-                const float w = weight(Frame{st[s].x, st[s].y, st[s].z}, st[s].w, m);
-                l += st[s].w * w;
+                const Frame f{st[s].x, st[s].y, st[s].z};
+                const float w = weight(f, st[s].w, m);
+                l += R::weighed(f, st[s].w, m);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] += of[e] * w;
             }

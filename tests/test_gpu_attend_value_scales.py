@@ -28,8 +28,8 @@ def check_lse(s, lse, window=0, scale=None):
     scale = s.scale if scale is None else scale
     ones = torch.ones(s.v.shape, dtype=torch.float64)
     want, want_lse, mass, size = ref.attend(s.q, ref.held(s.k, s.ks), ones, s.table, s.seq, s.pos, scale, window)
-    # (every scale counts as 2^-80 at least: an exponent of 80 and a step of it)
-    _, tol = ref.tolerance(want, mass, size, (s.pos + 1).clamp(min=1), s.D, s.model, FP16, torch.tensor([2.0 ** -80]))
+    # (scales enter by their logarithms, no larger than 128)
+    _, tol = ref.tolerance(want, mass, size, (s.pos + 1).clamp(min=1), s.D, s.model, FP16, torch.tensor([2.0 ** -128]))
     empty = want_lse == -math.inf
     assert (lse[empty] == -math.inf).all()
     off = (lse.double() - want_lse)[~empty].abs()
@@ -104,3 +104,85 @@ def test_values_of_infinite_scale_alone(wg, held):
         out, lse = s.run(group=group)
         assert (out[..., 0::2] == math.inf).all() and (out[..., 1::2] == -math.inf).all()
         check_lse(s, lse)
+
+
+@pytest.mark.parametrize("held", [E4M3, INT8])
+@pytest.mark.parametrize("size", [-70, -85, -98])
+def test_values_as_small_as_are_written(wg, held, size):
+    """Vectors of about 2^size, written by the library: codes and scales as for any other."""
+    lens = [1, 40, 0, 700, 3000]
+    s = Setup(wg, lens, 8, 2, 64, held, BF16, seed=4)
+    slots = wg.SlotMap(1, s.n_blocks * 16)
+    slots.slot.copy_(torch.arange(s.n_blocks * 16))
+    g = ref.generator(size + 1000)
+    k, v = (torch.randn((s.n_blocks * 16, 2, 64), generator=g) for _ in range(2))
+    v = v * torch.exp2(size + 4 * torch.rand((s.n_blocks * 16, 2, 1), generator=g))
+    s.on_gpu()
+    s.cache.write(k.to(BF16).cuda(), v.to(BF16).cuda(), slots)
+    (s.k, s.ks), (s.v, s.vs) = (ref.codes_of(x.to(BF16).view(s.n_blocks, 16, 2, 64), held) for x in (k, v))
+    assert torch.equal(s.cache.value_scale.cpu(), s.vs) and (s.vs < 2.0 ** (size + 2)).all()
+    for group in (1, 5):
+        s.check(s.run(group=group))
+
+
+def lost(s):
+    """What fp16 weights may lose beside the largest.  A weight is exp(x[i] - lse) times the value's scale, divided by the largest of
+    the row and times 2^15.  Below 2^-14 it is off by up to half of fp16's smallest step, 2^-25, which is 2^-40 of the largest,
+    whatever it is itself, and that times the code in the result.  (It is seen in dimensions where the largest's code is 0.)"""
+    out = torch.zeros(s.q.shape, dtype=torch.float64)
+    keys = ref.held(s.k, s.ks)
+    G = s.Hq // s.H
+    for t in range(s.q.shape[0]):
+        p = torch.arange(int(s.pos[t]) + 1)
+        b = s.table[int(s.seq[t])].long()[p // 16]
+        for h in range(s.Hq if len(p) else 0):
+            weight = torch.softmax(keys[b, p % 16, h // G] @ s.q[t, h].double() * s.scale, 0) * s.vs[b, p % 16, h // G].double()
+            out[t, h] = 2.0 ** -40 * weight.max() * s.v[b, p % 16, h // G].double().abs().sum(0)
+    return out
+
+
+@pytest.mark.parametrize("held", [E4M3, INT8])
+@pytest.mark.parametrize("low,high", [(-100, -95), (-120, -110), (-110, 0), (-120, 110)])
+def test_value_scales_over_the_whole_range(wg, held, low, high):
+    for lens in ([1, 40, 0, 700, 3000], [1 + i % 70 for i in range(80)]):
+        s = Setup(wg, lens, 8, 2, 64, held, BF16, seed=5)
+        s.vs = torch.exp2(torch.randint(low, high + 1, s.vs.shape, generator=ref.generator(high)).float()) * s.vs.clamp(0.5, 2.0)
+        s.on_gpu()
+        want, want_lse, mass, size = s.want()
+        tol, tol_lse = ref.tolerance(want, mass, size, (s.pos + 1).clamp(min=1), 64, BF16, FP16, s.vs)
+        tol += lost(s)
+        for group in (1, 5):
+            out, lse = s.run(group=group)
+            off, some = (out.double() - want).abs(), s.lens > 0
+            assert (off <= tol).all(), ((off / tol).max().item(), int((off > tol).sum()))
+            assert ((lse.double() - want_lse)[some].abs() <= tol_lse[some]).all() and (lse[~some] == -math.inf).all()
+
+
+@pytest.mark.parametrize("held,largest", [(E4M3, 448.0), (INT8, 127.0)])
+def test_values_as_large_as_there_are(wg, held, largest):
+    """One vector of bf16's largest values among ordinary ones."""
+    lens = [1, 40, 0, 700, 3000]
+    s = Setup(wg, lens, 8, 2, 64, held, BF16, seed=6)
+    for i, n in enumerate(lens):
+        if n:
+            p = 2 * n // 3
+            b = int(s.table[i, p // 16])
+            top = torch.full((2, 64), torch.finfo(BF16).max) * torch.sign(torch.randn((2, 64), generator=ref.generator(i)))
+            s.v[b, p % 16], s.vs[b, p % 16] = ref.codes_of(top.to(BF16), held)
+    s.on_gpu()
+    want, want_lse, mass, size = s.want()
+    tol, tol_lse = ref.tolerance(want, mass, size, (s.pos + 1).clamp(min=1), 64, BF16, FP16, s.vs)
+    # beside a scale of 2^k the sum has no weights below 2^(k - 138) of the largest
+    keys, left_out = ref.held(s.k, s.ks), torch.zeros(5, 8, dtype=torch.float64)
+    for t, n in enumerate(lens):
+        p = torch.arange(n)
+        b = s.table[t].long()[p // 16]
+        for h in range(8 if n else 0):
+            w = torch.softmax(keys[b, p % 16, h // 4] @ s.q[t, h].double() * s.scale, 0)
+            left_out[t, h] = w[w < w.max() * 2.0 ** (math.log2(torch.finfo(BF16).max / largest) - 138)].sum()
+    assert left_out.max() < 2.0 ** -8
+    tol, tol_lse = tol + lost(s) + 2 * left_out[..., None] * mass, tol_lse + 2 * left_out
+    for group in (1, 5):
+        out, lse = s.run(group=group)
+        assert ((out.double() - want).abs() <= tol).all()
+        assert ((lse.double() - want_lse)[s.lens > 0].abs() <= tol_lse[s.lens > 0]).all()
