@@ -680,7 +680,7 @@ int32_t wg_kv_reorder(wg_kv_pool *pool, int32_t *table, int64_t table_stride, in
  * vector x and C the type's largest value (448, 127): scale = top / C and code[i] = x[i] * (C / top) rounded to the
  * nearest value of the type, ties to even, all in fp32; the value held is code * scale.  A vector whose `top` is below
  * 2^-100 is held as zeros with scale 1.  A vector with an infinity or a NaN has scale NaN and reads back as
- * NaN.  Scales that a caller writes himself are >= 0 or NaN; of values with scales below 2^-124, which wg_kv_write
+ * NaN.  Scales that a caller writes himself are >= 0 or NaN; of values with scales below 2^-124 or above 2^121, which wg_kv_write
  * does not write, wg_kv_attend loses bits. */
 enum {
     WG_KV_BF16 = 0,

@@ -24,6 +24,7 @@
 // For m, scales below 2^-96 count as that, which keeps l below 2^108 times the number of positions (all of them below that, and 2^20 of
 // them, are too much), and so do infinities and NaN: the rest of such a scale, or what it is, is put into p' where a tile has some, and
 // the sum, which has no values in it, goes without.
+// A vector that was written as zeros has the scale 1 and yet no part in the result: where one would raise the maximum it counts as 2^-96 too.
 //
 // Scores of any size.  A score of 10^7 is rounded to whole numbers in fp32, and so would be x less a rounded maximum, or log2 s
 // beside it.  So the maximum is subtracted before anything else is done: with 16 bits m is one of the dot products as they are, and
@@ -374,34 +375,47 @@ struct Queries {
     }
 };
 
+// Vectors of zeros with the scale 1 among a tile's values: bit 2 s + e for position 16 s + n + 8 e.
+template <typename KV, int DP>
+__device__ __forceinline__ uint32_t zeros_of_scale_1(uint32_t values, const float *scales) {
+    using S = Shape<KV, DP>;
+    const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
+    uint32_t ones = 0, some = 0;
+#pragma unroll
+    for (int i = 0; i < 2 * S::SUBS; ++i) {
+        const int r = n + 8 * i;
+        if (scales[S::TILE + r] == 1.0f) ones |= 1u << i;
+        uint32_t x = 0;
+#pragma unroll
+        for (int kk = 0; kk < S::CHUNKS / 4; ++kk) {
+            const uint4 v = load16(values + S::value_at(r, kk * 4 + j));
+            x |= v.x | v.y | v.z | v.w;
+        }
+        if (x & (std::is_same<KV, E4m3>::value ? 0x7F7F7F7Fu : 0xFFFFFFFFu)) some |= 1u << i;      // (-0 is 0)
+    }
+    some |= __shfl_xor_sync(0xFFFFFFFFu, some, 1);
+    some |= __shfl_xor_sync(0xFFFFFFFFu, some, 2);
+    return ones & ~some;
+}
+
 // A tile: keys at `keys`, values at `values` in shared memory; bit i of `real`: position i counts.  scales: TILE of keys,
 // then TILE of values.  ENDS: a row takes in the positions before its end only (in the tile); values have to be finite, for
 // those behind it get the weight 0.  PART: the positions that do not count may hold anything (otherwise zeros), and only rows whose
 // end is not 0 take them in; whatever the positions hold, the other rows stay as they are.
-// False: nothing was taken in, for an origin has moved (`moves`: how often, for this tile), and the tile has to be given once more.  (A
-// loop in here around the scores kept them apart from what follows: 64 x 16384 e4m3 315 us instead of 291.)
+//
+// 8 bits: a tile with a value's scale that is not usual, one where a vector of zeros might raise the maximum, and one for which an
+// origin has to move, are not taken in (false), but left to the CAREFUL form.  That one moves origins and does not take the tile in
+// either, up to twice (`moves`: how often so far).
 enum Rows { ALL_ROWS, ENDS, PART_OF_ROWS };
-template <typename KV, int DP, int NT, Rows ROWS>
+template <typename KV, int DP, int NT, Rows ROWS, bool CAREFUL>
 __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const Queries<KV, DP, NT> &q, uint32_t keys, uint32_t values,
-                                          const float *scales, uint32_t real, int n, int j, const int (&ends)[NT][2], int moves) {
+                                          const float *scales, uint32_t real, int n, int j, const int (&ends)[NT][2], int moves = 0) {
     using S = Shape<KV, DP>;
     constexpr bool PART = ROWS == PART_OF_ROWS;
     using Mma = typename S::Mma;
     constexpr float LEAST = 0x1p-96f;
     float up[S::SUBS][2];                    // log2 of a value's scale, and BESIDE
     bool odd = false;                        // some scales are below LEAST, infinite or NaN
-    if constexpr (S::NARROW) {
-#pragma unroll
-        for (int s = 0; s < S::SUBS; ++s)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float vs = scales[S::TILE + s * 16 + n + 8 * e];
-                const bool usual = vs >= LEAST && vs < -NEG_INFINITY;
-                up[s][e] = __log2f(usual ? vs : LEAST) + S::BESIDE;
-                odd |= !usual;
-            }
-        odd = __any_sync(0xFFFFFFFFu, odd);
-    }
     float x[S::SUBS][NT][4] = {};            // [2 e + c]: of position 16 s + n + 8 e
 #pragma unroll
     for (int kk = 0; kk < S::CHUNKS / 4; ++kk)
@@ -426,6 +440,17 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
                 }
             }
         }
+    if constexpr (S::NARROW) {
+#pragma unroll
+        for (int s = 0; s < S::SUBS; ++s)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float vs = scales[S::TILE + s * 16 + n + 8 * e];
+                const bool usual = vs >= LEAST && vs < -NEG_INFINITY;
+                up[s][e] = __log2f(usual ? vs : LEAST) + S::BESIDE;
+                odd |= !usual;
+            }
+    }
     if constexpr (S::NARROW) {
 #pragma unroll
         for (int s = 0; s < S::SUBS; ++s)
@@ -467,31 +492,75 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
                     if (s * 16 + n + 8 * (i >> 1) >= ends[nt][i & 1]) x[s][nt][i] = NEG_INFINITY;
     }
     // maxima: of x itself, which the factor (above 0) multiplies later; with scales of x' = factor x + up
+    if constexpr (S::NARROW) {
+#pragma unroll
+        for (int s = 0; s < S::SUBS; ++s)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[s][nt][i] = fmaf(x[s][nt][i], q.factor[nt][i & 1], up[s][i >> 1]);
+    }
     float base[NT][2], shrink[NT][2];
     bool grew = false, far = false;
+    const auto maxima = [&] {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            float m = run.m[nt][c];
+            for (int c = 0; c < 2; ++c) {
+                float m = run.m[nt][c];
+#pragma unroll
+                for (int s = 0; s < S::SUBS; ++s)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) m = fmaxf(m, x[s][nt][2 * e + c]);
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+                base[nt][c] = m;
+                grew |= m > run.m[nt][c];
+                far |= S::NARROW && m > run.m[nt][c] && fabsf(m) > 256.0f;
+            }
+    };
+    maxima();
+    if (__any_sync(0xFFFFFFFFu, grew || (!CAREFUL && odd))) {
+        bool zeros = false;                  // with the scale 1
+        if constexpr (S::NARROW) {
+            bool ones = false;
+#pragma unroll
+            for (int s = 0; s < S::SUBS; ++s) ones |= up[s][0] == S::BESIDE || up[s][1] == S::BESIDE;
+            if (__any_sync(0xFFFFFFFFu, ones)) {
+                const uint32_t which = zeros_of_scale_1<KV, DP>(values, scales);
+                zeros = which != 0;
+                if constexpr (CAREFUL) {
+#pragma unroll
+                    for (int s = 0; s < S::SUBS; ++s)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            if ((which >> (2 * s + e)) & 1u) {
+                                up[s][e] -= 96.0f;
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) x[s][nt][2 * e] -= 96.0f, x[s][nt][2 * e + 1] -= 96.0f;
+                            }
+                }
+            }
+        }
+        if constexpr (S::NARROW && !CAREFUL) {
+            odd = false;                     // (positions that do not count have no scale either)
 #pragma unroll
             for (int s = 0; s < S::SUBS; ++s)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float &y = x[s][nt][2 * e + c];
-                    if constexpr (S::NARROW) y = fmaf(y, q.factor[nt][c], up[s][e]);
-                    m = fmaxf(m, y);
+                    const int at = s * 16 + n + 8 * e;
+                    const float vs = scales[S::TILE + at];
+                    odd |= ((real >> at) & 1u) && !(vs >= LEAST && vs < -NEG_INFINITY);
                 }
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-            base[nt][c] = m;
-            grew |= m > run.m[nt][c];
-            far |= S::NARROW && m > run.m[nt][c] && fabsf(m) > 256.0f;
+            if (__any_sync(0xFFFFFFFFu, zeros || odd || far)) return false;
         }
-    if (__any_sync(0xFFFFFFFFu, grew)) {
+        if (CAREFUL && __any_sync(0xFFFFFFFFu, zeros)) {
+            far = false;
+            maxima();
+        }
         // x' of a few hundred has more bits behind the point than a weight: where there is more the origin follows.  (The second time
         // takes what the first one's rounding left.)
-        if (S::NARROW && moves < 2 && __any_sync(0xFFFFFFFFu, far)) {
+        if (CAREFUL && moves < 2 && __any_sync(0xFFFFFFFFu, far)) {
             bool moved = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -543,11 +612,11 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
 #pragma unroll
         for (int s = 0; s < S::SUBS; ++s)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int at = s * 16 + n + 8 * e;
-                const float vs = ODD ? scales[S::TILE + at] : 0.0f;
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
+                for (int e = 0; e < 2; ++e) {
+                    const int at = s * 16 + n + 8 * e;
+                    const float vs = ODD ? scales[S::TILE + at] : 0.0f;
                     float y[2];
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
@@ -562,9 +631,8 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
                     }
                     p[s][nt][e] = transpose8x8(pack<Mma>(y[0], y[1]));
                 }
-            }
     };
-    if (S::NARROW && odd)
+    if (CAREFUL && __any_sync(0xFFFFFFFFu, odd))
         weigh(std::true_type{});
     else
         weigh(std::false_type{});
@@ -618,6 +686,28 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
             }
         }
     return true;
+}
+
+// Called, and what it works on goes through local memory: in the loops it cost them registers and order.  (64 x 16384 int8 327 us instead
+// of 299, 32 x 8 beams int8 125 instead of 114, e4m3 106 instead of 94.)
+template <typename KV, int DP, int NT>
+struct Careful {
+    Running<Shape<KV, DP>, NT> run;
+    Queries<KV, DP, NT> q;
+    int ends[NT][2];
+};
+template <typename KV, int DP, int NT, Rows ROWS>
+__device__ __noinline__ void take_carefully(Careful<KV, DP, NT> &c, uint32_t keys, const float *scales, uint32_t real) {
+    using S = Shape<KV, DP>;
+    const int lane = threadIdx.x & 31;
+    Running<S, NT> run = c.run;
+    const Queries<KV, DP, NT> q = c.q;
+    int ends[NT][2], moves = 0;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) ends[nt][0] = c.ends[nt][0], ends[nt][1] = c.ends[nt][1];
+#pragma unroll 1
+    while (!take_tile<KV, DP, NT, ROWS, true>(run, q, keys, keys + S::PLANE, scales, real, lane >> 2, lane & 3, ends, moves)) ++moves;
+    c.run = run;
 }
 
 // ---- where things are ------------------------------------------------------------------------------------------
@@ -914,6 +1004,24 @@ struct Attend : Results<DP> {
         return !__any_sync(0xFFFFFFFFu, odd);
     }
 
+    // A tile, whatever is in it.
+    template <int ROWS_BY_8, Rows ROWS>
+    static __device__ __forceinline__ void take(Running<S, ROWS_BY_8> &run, Queries<KV, DP, ROWS_BY_8> &q, uint32_t keys, const float *scales, uint32_t real,
+                                                int n, int j, const int (&ends)[ROWS_BY_8][2]) {
+        if constexpr (!S::NARROW) {
+            take_tile<KV, DP, ROWS_BY_8, ROWS, false>(run, q, keys, keys + S::PLANE, scales, real, n, j, ends);
+        } else {
+            if (ROWS != PART_OF_ROWS)
+                if (take_tile<KV, DP, ROWS_BY_8, ROWS, false>(run, q, keys, keys + S::PLANE, scales, real, n, j, ends)) return;
+            Careful<KV, DP, ROWS_BY_8> c;
+            c.run = run, c.q = q;
+#pragma unroll
+            for (int nt = 0; nt < ROWS_BY_8; ++nt) c.ends[nt][0] = ends[nt][0], c.ends[nt][1] = ends[nt][1];
+            take_carefully<KV, DP, ROWS_BY_8, ROWS>(c, keys, scales, real);
+            run = c.run, q = c.q;
+        }
+    }
+
     // Units [u0, u1) of a pair.  Rows that nothing else belongs to are stored, others kept as partial results.
     __device__ __forceinline__ void segment(const Pair &pair, int64_t u0, int64_t u1) const {
         constexpr int STREAMS = ATTEND_WARPS / WM, STREAM = S::TILE * WM;
@@ -969,11 +1077,6 @@ struct Attend : Results<DP> {
             copy_tile(warp, (i + S::STAGES - 1) % S::STAGES, i + S::STAGES - 1 < mine, next, (uint32_t)position(i + S::STAGES - 1), pair.head, lane);
             next = block_at(i + S::STAGES);
             const int stage = i % S::STAGES;
-            int moves = 0;
-            const auto again = [&](bool taken, int &w) {      // the same tile once more where it was not taken in
-                moves = taken ? 0 : moves + 1;
-                w -= !taken;
-            };
 #pragma unroll 1
             for (int w = 0; w < WM; ++w) {
                 const int of = (stream * WM + w) * S::STAGES + stage;
@@ -981,17 +1084,20 @@ struct Attend : Results<DP> {
                 if (!ok) continue;
                 const uint32_t keys = shared_address(ring + of * S::STAGE);
                 const int at = from + (i * STREAMS + stream) * STREAM + w * S::TILE;
-                if (!GROUPED || at + S::TILE <= least) {
-                    again(take_tile<KV, DP, NTS, ALL_ROWS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in, moves), w);
-                    continue;
-                }
-                // rows that end within the tile, or before it
-                if (values_finite(keys + S::PLANE, scales + of * (2 * S::TILE) + S::TILE, lane)) {
+                const float *const its_scales = scales + of * (2 * S::TILE);
+                // all rows as one, where they do not end before the tile does, or its values are finite
+                const bool whole = !GROUPED || at + S::TILE <= least;
+                if (GROUPED) {
 #pragma unroll
                     for (int nt = 0; nt < NTS; ++nt)
 #pragma unroll
                         for (int c = 0; c < 2; ++c) in[nt][c] = ends[nt][c] - at;
-                    again(take_tile<KV, DP, NTS, ENDS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in, moves), w);
+                }
+                if (whole || values_finite(keys + S::PLANE, its_scales + S::TILE, lane)) {
+                    if (whole)
+                        take<NTS, ALL_ROWS>(run, q, keys, its_scales, ok, n, j, in);
+                    else
+                        take<NTS, ENDS>(run, q, keys, its_scales, ok, n, j, in);
                     continue;
                 }
                 // (an infinity or a NaN would reach them with the weight 0: the rows go by themselves)
@@ -1011,10 +1117,8 @@ struct Attend : Results<DP> {
                     for (int nt = 0; nt < NTS; ++nt)
 #pragma unroll
                         for (int c = 0; c < 2; ++c) in[nt][c] = min(ends[nt][c], at + S::TILE) == e;
-                    if (take_tile<KV, DP, NTS, PART_OF_ROWS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok & ((2u << (e - at - 1)) - 1u), n, j, in, moves))
-                        past = e, moves = 0;
-                    else
-                        ++moves;
+                    take<NTS, PART_OF_ROWS>(run, q, keys, its_scales, ok & ((2u << (e - at - 1)) - 1u), n, j, in);
+                    past = e;
                 }
             }
         }
@@ -1226,11 +1330,8 @@ struct Attend : Results<DP> {
             live = fetch(block, p, p_head);
             const int of = warp * S::STAGES + stage;
             const uint32_t ok = real[of], keys = shared_address(ring + of * S::STAGE);
-            if (ok) {
-                int moves = 0;
-#pragma unroll 1
-                while (!take_tile<KV, DP, NT, ALL_ROWS>(run, q, keys, keys + S::PLANE, scales + of * (2 * S::TILE), ok, n, j, in, moves)) ++moves;
-            }
+            const float *const its_scales = scales + of * (2 * S::TILE);
+            if (ok) take<NT, ALL_ROWS>(run, q, keys, its_scales, ok, n, j, in);
             if (++stage == S::STAGES) stage = 0;
             fresh = at.i == at.n - 1;
             if (fresh || u + 1 >= end) finish(run, q, at, u, begin, end, worker, sub, head_of(at.run), at.run % a.row_blocks * WARP_ROWS, n, j, lane);

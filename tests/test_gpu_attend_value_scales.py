@@ -186,3 +186,39 @@ def test_values_as_large_as_there_are(wg, held, largest):
         out, lse = s.run(group=group)
         assert ((out.double() - want).abs() <= tol).all()
         assert ((lse.double() - want_lse)[s.lens > 0].abs() <= tol_lse[s.lens > 0]).all()
+
+
+@pytest.mark.parametrize("held", [E4M3, INT8])
+@pytest.mark.parametrize("size", [1e-6, 1e-9, 2.0 ** -60])
+@pytest.mark.parametrize("lens", [[2, 40, 0, 700, 3000], [2 + i % 70 for i in range(80)]])
+def test_a_vector_of_zeros_has_no_part(wg, held, size, lens):
+    """Zeros are written with the scale 1.  One that nearly all of the weight lies on leaves the small ones beside it their bits; so do
+    minus zeros; and vectors whose scale happens to be 1 count as they are."""
+    for share in (None, same_tables(lens)):
+        s = Setup(wg, lens, 8, 2, 64, held, BF16, seed=7, share=share)
+        g = ref.generator(7)
+        slots = wg.SlotMap(1, s.n_blocks * 16)
+        slots.slot.copy_(torch.arange(s.n_blocks * 16))
+        k = torch.randn((s.n_blocks, 16, 2, 64), generator=g)
+        v = size * (1 + torch.rand((s.n_blocks, 16, 2, 64), generator=g)) * torch.sign(torch.randn((s.n_blocks, 16, 2, 64), generator=g))
+        for i, n in enumerate(lens):
+            for p in {n // 2, n - 1} if n else ():
+                k[s.table[i, p // 16], p % 16] = s.q[i].float().view(2, 4, 64).mean(1) * 3
+                v[s.table[i, p // 16], p % 16] = 0.0 if p == n - 1 else -0.0
+        s.on_gpu()
+        k, v = k.to(BF16), v.to(BF16)
+        s.cache.write(k.cuda().flatten(0, 1), v.cuda().flatten(0, 1), slots)
+        (s.k, s.ks), (s.v, s.vs) = ref.codes_of(k, held), ref.codes_of(v, held)
+        assert (s.vs == 1).any() and s.vs.min() < size
+        for group in (1, 5):
+            s.check(s.run(group=group))
+
+
+@pytest.mark.parametrize("held", [E4M3, INT8])
+def test_scales_of_one(wg, held):
+    for lens in ([1, 40, 0, 700, 3000], [1 + i % 70 for i in range(80)]):
+        s = Setup(wg, lens, 8, 2, 64, held, BF16, seed=8)
+        s.vs.fill_(1.0)
+        s.on_gpu()
+        for group in (1, 5):
+            s.check(s.run(group=group))
