@@ -155,22 +155,22 @@ attend_plan_kernel(const __grid_constant__ CacheDev cache, const __grid_constant
     const int cols = second > 0 ? (int)cache.block.quotient((uint32_t)(second - 1)) + 1 : 0;
     const int32_t *mine = a.table + (leader >= 0 ? seen[leader].s * a.stride : 0);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int c0 = 0; c0 < cols; c0 += 128) {
+    for (uint32_t c0 = 0; c0 < (uint32_t)cols; c0 += 128) {       // (up to 2^31 columns)
         int at = 0x7FFFFFFF;
         for (int m = warp; m < a.group; m += ATTEND_WARPS) {
             const Seen r = seen[m];
             if (r.end == 0 || r.s == seen[leader].s) continue;
-            const int mine_cols = (int)cache.block.quotient((uint32_t)(r.end - 1)) + 1;
+            const uint32_t mine_cols = cache.block.quotient((uint32_t)(r.end - 1)) + 1;
             const int32_t *theirs = a.table + r.s * a.stride;
             int32_t x[4], y[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int c = c0 + u * 32 + lane;
+                const uint32_t c = c0 + u * 32 + lane;
                 x[u] = c < mine_cols ? theirs[c] : 0, y[u] = c < mine_cols ? mine[c] : 0;
             }
 #pragma unroll
             for (int u = 3; u >= 0; --u)
-                if (x[u] != y[u]) at = min(at, c0 + u * 32 + lane);
+                if (x[u] != y[u]) at = min(at, (int)(c0 + u * 32 + lane));
         }
         if (at < 0x7FFFFFFF) atomicMin(&differs, at);
         if (__syncthreads_or(at < 0x7FFFFFFF)) break;
@@ -960,8 +960,9 @@ struct Attend : Results<DP> {
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    __device__ __forceinline__ int32_t entry(const int32_t *row, int pos, int to) const {   // anything but a block where there is none
-        return pos < to ? row[cache.block.quotient((uint32_t)pos)] : -1;
+    // Anything but a block where there is none.  (The last tile of a sequence of nearly 2^31 positions passes that: positions are unsigned.)
+    __device__ __forceinline__ int32_t entry(const int32_t *row, uint32_t pos, int to) const {
+        return pos < (uint32_t)to ? row[cache.block.quotient(pos)] : -1;
     }
     static __device__ __forceinline__ void wait_tile() { asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 2) : "memory"); }
 
@@ -1032,7 +1033,7 @@ struct Attend : Results<DP> {
         const int tiles = tiles_of(from, to, STREAM);                                // of all streams
         const int mine = tiles > stream ? (tiles - stream + STREAMS - 1) / STREAMS : 0;
         const int32_t *row = a.table + pair.seq * a.stride;
-        const auto position = [&](int i) { return from + (i * STREAMS + stream) * STREAM + wm * S::TILE + lane % S::TILE; };
+        const auto position = [&](int i) { return (uint32_t)from + (uint32_t)(i * STREAMS + stream) * STREAM + (uint32_t)(wm * S::TILE + lane % S::TILE); };
         const auto block_at = [&](int i) { return i < mine ? entry(row, position(i), to) : -1; };
         int32_t first_blocks[S::STAGES - 1];
 #pragma unroll
@@ -1059,7 +1060,7 @@ struct Attend : Results<DP> {
             typename Queries<KV, DP, NTS>::Raw raw;
             q.ask(raw, rows, cache.head_dim, j);
 #pragma unroll
-            for (int i = 0; i < S::STAGES - 1; ++i) copy_tile(warp, i, i < mine, first_blocks[i], (uint32_t)position(i), pair.head, lane);
+            for (int i = 0; i < S::STAGES - 1; ++i) copy_tile(warp, i, i < mine, first_blocks[i], position(i), pair.head, lane);
             q.take(raw, a.q_bf16, a.scale, j);
             if constexpr (GROUPED) {
 #pragma unroll
@@ -1074,7 +1075,7 @@ struct Attend : Results<DP> {
             wait_tile();
             stream_sync(stream);
             // (the tile that was used last is free: all warps of the stream are past it)
-            copy_tile(warp, (i + S::STAGES - 1) % S::STAGES, i + S::STAGES - 1 < mine, next, (uint32_t)position(i + S::STAGES - 1), pair.head, lane);
+            copy_tile(warp, (i + S::STAGES - 1) % S::STAGES, i + S::STAGES - 1 < mine, next, position(i + S::STAGES - 1), pair.head, lane);
             next = block_at(i + S::STAGES);
             const int stage = i % S::STAGES;
 #pragma unroll 1
@@ -1086,7 +1087,7 @@ struct Attend : Results<DP> {
                 const int at = from + (i * STREAMS + stream) * STREAM + w * S::TILE;
                 const float *const its_scales = scales + of * (2 * S::TILE);
                 // all rows as one, where they do not end before the tile does, or its values are finite
-                const bool whole = !GROUPED || at + S::TILE <= least;
+                const bool whole = !GROUPED || least - at >= S::TILE;
                 if (GROUPED) {
 #pragma unroll
                     for (int nt = 0; nt < NTS; ++nt)
@@ -1101,23 +1102,23 @@ struct Attend : Results<DP> {
                     continue;
                 }
                 // (an infinity or a NaN would reach them with the weight 0: the rows go by themselves)
-                int past = at;
+                int past = 0;
 #pragma unroll 1
                 while (true) {
-                    int e = 0x7FFFFFFF;
+                    int e = S::TILE + 1;
 #pragma unroll
                     for (int nt = 0; nt < NTS; ++nt)
 #pragma unroll
                         for (int c = 0; c < 2; ++c)
-                            if (min(ends[nt][c], at + S::TILE) > past) e = min(e, min(ends[nt][c], at + S::TILE));
+                            if (min(ends[nt][c] - at, S::TILE) > past) e = min(e, min(ends[nt][c] - at, S::TILE));
 #pragma unroll
                     for (int o = 16; o > 0; o >>= 1) e = min(e, __shfl_xor_sync(0xFFFFFFFFu, e, o));
-                    if (e == 0x7FFFFFFF) break;
+                    if (e > S::TILE) break;
 #pragma unroll
                     for (int nt = 0; nt < NTS; ++nt)
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) in[nt][c] = min(ends[nt][c], at + S::TILE) == e;
-                    take<NTS, PART_OF_ROWS>(run, q, keys, its_scales, ok & ((2u << (e - at - 1)) - 1u), n, j, in);
+                        for (int c = 0; c < 2; ++c) in[nt][c] = min(ends[nt][c] - at, S::TILE) == e;
+                    take<NTS, PART_OF_ROWS>(run, q, keys, its_scales, ok & ((2u << (e - 1)) - 1u), n, j, in);
                     past = e;
                 }
             }
@@ -1289,24 +1290,26 @@ struct Attend : Results<DP> {
             Q::ask(raw, rows, cache.head_dim, j);
         };
         ask(at);
-        const auto fetch = [&](int32_t &block, int &p, int &head) -> bool {    // the table's entry of the tile in front
+        const auto fetch = [&](int32_t &block, uint32_t &p, int &head) -> bool {    // the table's entry of the tile in front
             block = -1;
             if (ahead >= end) return false;
-            p = front.from + front.i * S::TILE + lane % S::TILE;
+            p = (uint32_t)front.from + (uint32_t)front.i * S::TILE + (uint32_t)lane % S::TILE;
             head = head_of(front.run);
             block = entry(front.row, p, front.end);
             step(front, ahead, runs);
             return true;
         };
         int32_t blocks[S::STAGES];
-        int pos[S::STAGES], heads[S::STAGES];
+        uint32_t pos[S::STAGES];
+        int heads[S::STAGES];
         bool lives[S::STAGES];
 #pragma unroll
         for (int i = 0; i < S::STAGES; ++i) lives[i] = fetch(blocks[i], pos[i], heads[i]);
 #pragma unroll
-        for (int i = 0; i < S::STAGES - 1; ++i) copy_tile(warp, i, lives[i], blocks[i], (uint32_t)pos[i], heads[i], lane);
+        for (int i = 0; i < S::STAGES - 1; ++i) copy_tile(warp, i, lives[i], blocks[i], pos[i], heads[i], lane);
         int32_t block = blocks[S::STAGES - 1];
-        int p = pos[S::STAGES - 1], p_head = heads[S::STAGES - 1];
+        uint32_t p = pos[S::STAGES - 1];
+        int p_head = heads[S::STAGES - 1];
         bool live = lives[S::STAGES - 1];
         Q q;
         Running<S, NT> run;
@@ -1326,7 +1329,7 @@ struct Attend : Results<DP> {
             }
             wait_tile();
             __syncwarp();
-            copy_tile(warp, stage == 0 ? S::STAGES - 1 : stage - 1, live, block, (uint32_t)p, p_head, lane);
+            copy_tile(warp, stage == 0 ? S::STAGES - 1 : stage - 1, live, block, p, p_head, lane);
             live = fetch(block, p, p_head);
             const int of = warp * S::STAGES + stage;
             const uint32_t ok = real[of], keys = shared_address(ring + of * S::STAGE);
