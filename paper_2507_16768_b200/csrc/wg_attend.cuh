@@ -1419,11 +1419,12 @@ attend_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ At
     for (int t0 = 0; t0 < a.n_tokens; t0 += ATTEND_THREADS) {
         const int t = t0 + (int)threadIdx.x;
         int64_t n = 0;
-        bool nothing = false, without = false;        // no row; no pairs
+        bool nothing = false, without = false, sees = false;       // of this block's: no row; no pairs
         if (t < a.n_tokens) {
             const Seen r = seen_by(a, cache, t);
             const bool mine = t % gridDim.x == blockIdx.x;
-            nothing = r.end == 0 && mine;
+            sees = r.end > 0;
+            nothing = !sees && mine;
             book.seq[t] = r.s, book.end[t] = r.end;
             book.from[t] = GROUPED ? max(r.first, a.shared[t / a.group]) : r.first;
             if (!GROUPED) book.to[t] = r.end;
@@ -1434,12 +1435,13 @@ attend_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ At
             without = mine && units == 0;
         }
         uint32_t empty = __ballot_sync(0xFFFFFFFFu, without);
+        const uint32_t seeing = __ballot_sync(0xFFFFFFFFu, sees);      // (a vote is no barrier: what others wrote is not read here)
         while (empty) {
-            const int i = t0 + warp * 32 + __ffs(empty) - 1;
+            const int bit = __ffs(empty) - 1, i = t0 + warp * 32 + bit;
             empty &= empty - 1;
             for (int c = lane; c < cache.n_heads * a.row_blocks; c += 32)
                 (SHARED_WARPS == 0 || GROUPED ? a.own_cuts : a.shared_cuts)[(int64_t)i * cache.n_heads * a.row_blocks + c] =
-                    make_int2(book.end[i] > 0 ? 0 : -1, 0);
+                    make_int2((seeing >> bit) & 1u ? 0 : -1, 0);
         }
         uint32_t which = __ballot_sync(0xFFFFFFFFu, nothing);
         while (which) {          // tokens without a row, by whole warps
