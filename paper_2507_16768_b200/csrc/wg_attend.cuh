@@ -332,8 +332,8 @@ struct Queries {
                 }
     }
     __device__ __forceinline__ void take(const Raw &raw, bool bf16, float scale, int j) {
-        // (2^-126 for 0: a score that stands for nothing stays -inf)
-        const float up = fmaxf(fabsf(scale), 0x1p-126f);
+        // (2^-149 for 0: a score that stands for nothing stays -inf, and any other is 0 to 10^-6)
+        const float up = fmaxf(fabsf(scale), 0x1p-149f);
         const uint32_t sign = scale < 0.0f ? 0x80008000u : 0u;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -369,7 +369,7 @@ struct Queries {
                     }
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
-                    factor[nt][c] = fmaxf(up * __uint_as_float(__shfl_sync(0xFFFFFFFFu, e, (2 * j + c) * 4) << 23), 0x1p-126f);
+                    factor[nt][c] = fminf(fmaxf(up * __uint_as_float(__shfl_sync(0xFFFFFFFFu, e, (2 * j + c) * 4) << 23), 0x1p-149f), 0x1.FFFFFEp127f);
             }
         }
     }

@@ -152,3 +152,45 @@ def test_scores_beyond_fp32(wg, n):
     assert (out[[1, 4]] == 0).all() and (lse[[1, 4]] == -math.inf).all()
     assert (out[2] == torch.tensor(n + 1.0).to(BF16)).all() and lse[2] == 0
     assert torch.isfinite(out[5]).all() and abs(lse[5].item() - math.log(n)) < 1e-5
+
+
+@pytest.mark.parametrize("held,size,scale", [(BF16, 2.0 ** 60, 0.0), (BF16, 2.0 ** 60, 1e-39), (BF16, 2.0 ** 60, -2e-38), (E4M3, 2.0 ** 60, 0.0), (INT8, 2.0 ** 60, 1e-38),
+                                             (INT8, 2.0 ** 60, -2e-38), (FP16, 2.0 ** 14, 0.0)])
+def test_scales_of_nothing(wg, held, size, scale):
+    """Dot products near the end of fp32's range times a scale of 0, or next to it."""
+    model = FP16 if held is FP16 else BF16
+    g = ref.generator(9)
+    q, k = torch.zeros((3, 4, D)), torch.zeros((3, 64, 1, D))
+    q[..., 0] = size * (1 + torch.arange(4) / 4)
+    k[..., 0] = size * torch.randn((3, 64, 1), generator=g)
+    v = torch.randn((3, 64, 1, D), generator=g)
+    if held in ref.LARGEST:
+        (k, ks), (v, vs) = ref.codes_of(k, held), ref.codes_of(v, held)
+    else:
+        k, v, ks, vs = k.to(held), v.to(held), None, None
+    put = lambda t: None if t is None else t.cuda()  # noqa: E731
+    cache, pool = wg.KvCache(*(put(t) for t in (k, v, ks, vs))), wg.KvPool(3, 64, 3)
+    tables = wg.KvTables(pool, torch.arange(3, dtype=torch.int32, device="cuda")[:, None].contiguous(), torch.full((3,), 60, dtype=torch.int32, device="cuda"))
+    out, lse = torch.empty((3, 4, D), dtype=model, device="cuda"), torch.empty((3, 4), device="cuda")
+    wg.Attend(3, 4, 1, D)(q.to(model).cuda(), cache, tables, out, scale=scale, lse=lse)
+    x = torch.einsum("srd,spd->srp", q.to(model).double(), ref.held(k, ks)[:, :60, 0]) * scale
+    values, w = ref.held(v, vs)[:, :60, 0], torch.softmax(x, 2)
+    mean, mass = w @ values, w @ values.abs()
+    # half a step of a weight and of the result; scores of some units, whose factors have at least 2^17 steps below fp32's normal range
+    assert ((out.cpu().double() - mean).abs() <= mean.abs() * ref.half_step(model) + mass * (ref.half_step(BF16 if held is BF16 else FP16) + 2.0 ** -14)).all()
+    assert ((lse.cpu().double() - torch.logsumexp(x, 2)).abs() <= 2.0 ** -14).all()
+
+
+@pytest.mark.parametrize("held", [E4M3, INT8])
+def test_keys_of_zeros_beside_the_largest_queries(wg, held):
+    """A query's size and the scale together are beyond fp32; its scores are 0."""
+    v = torch.randn((1, 16, 1, D), generator=ref.generator(10))
+    (k, ks), (v, vs) = ref.codes_of(torch.zeros((1, 16, 1, D)), held), ref.codes_of(v, held)
+    cache, pool = wg.KvCache(*(t.cuda() for t in (k, v, ks, vs))), wg.KvPool(1, 16, 1)
+    tables = wg.KvTables(pool, torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.full((1,), 16, dtype=torch.int32, device="cuda"))
+    out, lse = torch.empty((1, 4, D), dtype=BF16, device="cuda"), torch.empty((1, 4), device="cuda")
+    wg.Attend(1, 4, 1, D)(torch.full((1, 4, D), 2.0 ** 127, device="cuda").to(BF16), cache, tables, out, scale=64.0, lse=lse)
+    mean = ref.held(v, vs)[0, :, 0].mean(0)
+    mass = ref.held(v, vs)[0, :, 0].abs().mean(0)
+    assert ((out.cpu().double() - mean).abs() <= mean.abs() * 2.0 ** -8 + mass * (2.0 ** -11 + 2.0 ** -18)).all()
+    assert (lse.cpu().double() - math.log(16)).abs().max() < 1e-5
