@@ -423,11 +423,11 @@ int32_t wg_kv_write(const wg_kv_cache *cache, const void *k, int64_t k_stride, c
     if (!cache_ok(cache) || n_tokens < 0 || n_q_heads < 0 || n_q_heads > 65535) return WG_ERR_ARG;
     if (dtype != WG_DTYPE_BF16 && dtype != WG_DTYPE_FP16) return WG_ERR_ARG;
     if (cache->storage <= WG_KV_FP16 && (cache->storage == WG_KV_FP16) != (dtype == WG_DTYPE_FP16)) return WG_ERR_ARG;
-    if ((q != nullptr) != (q_out != nullptr) || (q != nullptr) != (n_q_heads > 0)) return WG_ERR_ARG;
     if (rope && (!rope->table || ((uintptr_t)rope->table & 15) || rope->n_pos < 1 || rope->rot_dim < 16 || rope->rot_dim % 16 ||
                  rope->rot_dim > cache->head_dim))
         return WG_ERR_ARG;
-    if (n_tokens == 0) return WG_OK;
+    if (n_tokens == 0) return WG_OK;                    // (arrays of nothing may have no address)
+    if ((q != nullptr) != (q_out != nullptr) || (q != nullptr) != (n_q_heads > 0)) return WG_ERR_ARG;
     const int64_t width = (int64_t)cache->n_heads * cache->head_dim, q_width = (int64_t)n_q_heads * cache->head_dim;
     if (!rows_ok(k, k_stride, width) || !rows_ok(v, v_stride, width) || !slot || (rope && !pos)) return WG_ERR_ARG;
     if (q && (!rows_ok(q, q_stride, q_width) || !rows_ok(q_out, q_out_stride, q_width))) return WG_ERR_ARG;
