@@ -447,8 +447,8 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
             for (int e = 0; e < 2; ++e) {
                 const float vs = scales[S::TILE + s * 16 + n + 8 * e];
                 const bool usual = vs >= LEAST && vs < -NEG_INFINITY;
-                up[s][e] = __log2f(usual ? vs : LEAST) + S::BESIDE;
-                odd |= !usual;
+                up[s][e] = __log2f(!CAREFUL || usual ? vs : LEAST) + S::BESIDE;
+                odd |= CAREFUL ? !usual : !(fabsf(up[s][e] - (S::BESIDE + 16.0f)) < 112.0f);      // (the border of 2^-96 is below all that is written)
             }
     }
     if constexpr (S::NARROW) {
@@ -501,7 +501,7 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
                 for (int i = 0; i < 4; ++i) x[s][nt][i] = fmaf(x[s][nt][i], q.factor[nt][i & 1], up[s][i >> 1]);
     }
     float base[NT][2], shrink[NT][2];
-    bool grew = false, far = false;
+    bool grew = false;
     const auto maxima = [&] {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -516,7 +516,6 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
                 for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
                 base[nt][c] = m;
                 grew |= m > run.m[nt][c];
-                far |= S::NARROW && m > run.m[nt][c] && fabsf(m) > 256.0f;
             }
     };
     maxima();
@@ -550,14 +549,19 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
                 for (int e = 0; e < 2; ++e) {
                     const int at = s * 16 + n + 8 * e;
                     const float vs = scales[S::TILE + at];
-                    odd |= ((real >> at) & 1u) && !(vs >= LEAST && vs < -NEG_INFINITY);
+                    if (!((real >> at) & 1u))
+                        up[s][e] = S::BESIDE;
+                    else
+                        odd |= !(vs > LEAST && vs < -NEG_INFINITY);
                 }
-            if (__any_sync(0xFFFFFFFFu, zeros || odd || far)) return false;
         }
-        if (CAREFUL && __any_sync(0xFFFFFFFFu, zeros)) {
-            far = false;
-            maxima();
-        }
+        if (CAREFUL && __any_sync(0xFFFFFFFFu, zeros)) maxima();
+        bool far = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) far |= S::NARROW && base[nt][c] > run.m[nt][c] && fabsf(base[nt][c]) > 256.0f;
+        if (S::NARROW && !CAREFUL && __any_sync(0xFFFFFFFFu, zeros || odd || far)) return false;
         // x' of a few hundred has more bits behind the point than a weight: where there is more the origin follows.  (The second time
         // takes what the first one's rounding left.)
         if (CAREFUL && moves < 2 && __any_sync(0xFFFFFFFFu, far)) {
@@ -1086,19 +1090,18 @@ struct Attend : Results<DP> {
                 const uint32_t keys = shared_address(ring + of * S::STAGE);
                 const int at = from + (i * STREAMS + stream) * STREAM + w * S::TILE;
                 const float *const its_scales = scales + of * (2 * S::TILE);
-                // all rows as one, where they do not end before the tile does, or its values are finite
                 const bool whole = !GROUPED || least - at >= S::TILE;
-                if (GROUPED) {
+                if (whole) {
+                    take<NTS, ALL_ROWS>(run, q, keys, its_scales, ok, n, j, in);
+                    continue;
+                }
+                // rows that end within the tile, or before it
+                if (values_finite(keys + S::PLANE, its_scales + S::TILE, lane)) {
 #pragma unroll
                     for (int nt = 0; nt < NTS; ++nt)
 #pragma unroll
                         for (int c = 0; c < 2; ++c) in[nt][c] = ends[nt][c] - at;
-                }
-                if (whole || values_finite(keys + S::PLANE, its_scales + S::TILE, lane)) {
-                    if (whole)
-                        take<NTS, ALL_ROWS>(run, q, keys, its_scales, ok, n, j, in);
-                    else
-                        take<NTS, ENDS>(run, q, keys, its_scales, ok, n, j, in);
+                    take<NTS, ENDS>(run, q, keys, its_scales, ok, n, j, in);
                     continue;
                 }
                 // (an infinity or a NaN would reach them with the weight 0: the rows go by themselves)
