@@ -21,7 +21,8 @@ int64_t part_row(int32_t head_dim) { return (head_dim <= 64 ? 64 : head_dim <= 1
 template <int DP, int WARPS>
 int32_t launch_join_by(const CacheDev &c, const AttendArgs &a, cudaStream_t st) {
     const dim3 grid((unsigned)((a.n_q_heads * WARPS + ATTEND_WARPS - 1) / ATTEND_WARPS), (unsigned)a.n_tokens);
-    WG_CUDA(launch_pdl(attend_join_kernel<DP, WARPS>, grid, dim3(ATTEND_THREADS), st, c, a));
+    const auto kernel = a.origins ? attend_join_kernel<DP, WARPS, true> : attend_join_kernel<DP, WARPS, false>;
+    WG_CUDA(launch_pdl(kernel, grid, dim3(ATTEND_THREADS), st, c, a));
     WG_LAUNCHED();
     return WG_OK;
 }

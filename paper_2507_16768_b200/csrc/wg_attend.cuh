@@ -96,7 +96,7 @@ struct AttendArgs {
     // how the kernel is cut out
     int32_t warp_rows, shared_rows_each;  // rows that a warp works for by itself, and those of a shared pair
     int32_t shared_row_blocks;    // 0: there are no pairs for whole blocks
-    int32_t grouped;
+    int32_t grouped, origins;
 };
 
 namespace {
@@ -259,11 +259,13 @@ struct Shape {
     static __device__ __forceinline__ int value_at(int r, int c) { return ((r * CHUNKS + c) ^ (r & 6)) * 16; }
 };
 
-// What results are relative to: 2^(origin factor + near), the largest exponent; near is -infinity where there is none.
+// What results are relative to: 2^(origin factor + near), the largest exponent; near is -infinity where there is none.  ORIGINS: they are not
+// all 0 (8-bit caches).
 struct Frame {
     float origin, factor, near;
     static __device__ __forceinline__ Frame none() { return {0.0f, 0.0f, NEG_INFINITY}; }
-    __device__ __forceinline__ float less(const Frame &f) const { return fmaf(origin - f.origin, factor, near - f.near); }
+    template <bool ORIGINS>
+    __device__ __forceinline__ float less(const Frame &f) const { return ORIGINS ? fmaf(origin - f.origin, factor, near - f.near) : near - f.near; }
     __device__ __forceinline__ float exponent() const { return fmaf(origin, factor, near); }
 };
 
@@ -771,12 +773,15 @@ struct Results {
         if (d == 0) *reinterpret_cast<float4 *>(row + DP) = make_float4(f.origin, f.factor, f.near, l);
     }
     // What a partial result counts beside frame `top`.  (Without a maximum its sum is 0, or NaN, which stays.)
+    template <bool ORIGINS>
     static __device__ __forceinline__ float weight(const Frame &f, float l, const Frame &top) {
-        return f.near == NEG_INFINITY ? (l == l ? 0.0f : 1.0f) : power2(f.less(top));
+        return f.near == NEG_INFINITY ? (l == l ? 0.0f : 1.0f) : power2(f.less<ORIGINS>(top));
     }
-    // The same for its sum, which may be so large that it counts beside a weight below fp32's range.
-    static __device__ __forceinline__ float weighed(const Frame &f, float l, const Frame &top) {
-        const float half = f.near == NEG_INFINITY ? (l == l ? 0.0f : 1.0f) : power2(0.5f * f.less(top));
+    // The same for its sum, which may be so large that it counts beside a weight below fp32's range (with origins, that is, scales).
+    template <bool ORIGINS>
+    static __device__ __forceinline__ float weighed(const Frame &f, float l, const Frame &top, float weight) {
+        if (!ORIGINS) return l * weight;
+        const float half = f.near == NEG_INFINITY ? (l == l ? 0.0f : 1.0f) : power2(0.5f * f.less<ORIGINS>(top));
         return l * half * half;
     }
 
@@ -798,7 +803,7 @@ struct Results {
 // and asked for all at once where they are not more than AHEAD.  Latencies: 2 to 5 us, of which a launch is one.  (In
 // the first kernel, by whichever warp is the last to be done with a token, the same took 6.5 us at the end of all others,
 // most of it on an atomic's way and back, and its registers cost the loops theirs.)
-template <int DP, int WARPS>
+template <int DP, int WARPS, bool ORIGINS>
 __global__ void __launch_bounds__(ATTEND_THREADS)
 attend_join_kernel(const __grid_constant__ CacheDev cache, const __grid_constant__ AttendArgs a) {
     attend_enter();
@@ -849,17 +854,24 @@ attend_join_kernel(const __grid_constant__ CacheDev cache, const __grid_constant
         Frame top = at;
 #pragma unroll
         for (int o = AHEAD / 2; o > 0; o >>= 1) {
+            if (!ORIGINS) {
+                top.near = fmaxf(top.near, __shfl_xor_sync(0xFFFFFFFFu, top.near, o));
+                continue;
+            }
             const Frame x{__shfl_xor_sync(0xFFFFFFFFu, top.origin, o), __shfl_xor_sync(0xFFFFFFFFu, top.factor, o), __shfl_xor_sync(0xFFFFFFFFu, top.near, o)};
-            if (x.less(top) > 0.0f) top = x;
+            if (x.less<ORIGINS>(top) > 0.0f) top = x;
         }
         // (frames that are equal up to rounding may have left lanes with different ones)
-        top = {__shfl_sync(0xFFFFFFFFu, top.origin, 0), __shfl_sync(0xFFFFFFFFu, top.factor, 0), __shfl_sync(0xFFFFFFFFu, top.near, 0)};
-        if (m.less(top) > 0.0f) top = m;
-        const float w = R::weight(at, st.w, top), old = R::weight(m, l, top);
-        float sum = R::weighed(at, st.w, top);
+        if (ORIGINS) top = {__shfl_sync(0xFFFFFFFFu, top.origin, 0), __shfl_sync(0xFFFFFFFFu, top.factor, 0), __shfl_sync(0xFFFFFFFFu, top.near, 0)};
+        if (!ORIGINS)
+            top.near = fmaxf(top.near, m.near);
+        else if (m.less<ORIGINS>(top) > 0.0f)
+            top = m;
+        const float w = R::template weight<ORIGINS>(at, st.w, top), old = R::template weight<ORIGINS>(m, l, top);
+        float sum = R::template weighed<ORIGINS>(at, st.w, top, w);
 #pragma unroll
         for (int o = AHEAD / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        l = R::weighed(m, l, top) + sum;
+        l = R::template weighed<ORIGINS>(m, l, top, old) + sum;
         m = top;
 #pragma unroll
         for (int e = 0; e < PER; ++e) y[e] *= old;
@@ -880,9 +892,9 @@ attend_join_kernel(const __grid_constant__ CacheDev cache, const __grid_constant
         __syncthreads();
         if (warp > 0) return;
         for (int w = 1; w < min(WARPS, (n + AHEAD - 1) / AHEAD); ++w) {
-            const Frame mw{rows[w][DP], rows[w][DP + 1], rows[w][DP + 2]}, top = mw.less(m) > 0.0f ? mw : m;
-            const float lw = rows[w][DP + 3], old = R::weight(m, l, top), by = R::weight(mw, lw, top);
-            l = R::weighed(m, l, top) + R::weighed(mw, lw, top), m = top;
+            const Frame mw{rows[w][DP], rows[w][DP + 1], rows[w][DP + 2]}, top = mw.less<ORIGINS>(m) > 0.0f ? mw : m;
+            const float lw = rows[w][DP + 3], old = R::template weight<ORIGINS>(m, l, top), by = R::template weight<ORIGINS>(mw, lw, top);
+            l = R::template weighed<ORIGINS>(m, l, top, old) + R::template weighed<ORIGINS>(mw, lw, top, by), m = top;
 #pragma unroll
             for (int e = 0; e < PER; ++e) y[e] = y[e] * old + rows[w][lane * PER + e] * by;
         }
@@ -895,7 +907,7 @@ attend_join_kernel(const __grid_constant__ CacheDev cache, const __grid_constant
 template <typename KV, int DP, int SHARED_WARPS, bool GROUPED, int NTS, int NT>
 struct Attend : Results<DP> {
     using R = Results<DP>;
-    using R::cache, R::a, R::PART_ROW, R::block_part, R::warp_part, R::kept, R::keep_row, R::weight, R::group_of;
+    using R::cache, R::a, R::PART_ROW, R::block_part, R::warp_part, R::kept, R::keep_row, R::group_of;
     using S = Shape<KV, DP>;
     static constexpr int WM = SHARED_WARPS == 0 ? 1 : SHARED_WARPS;
     static constexpr int WARP_ROWS = 8 * NT;
@@ -1166,14 +1178,14 @@ struct Attend : Results<DP> {
                 const float *of = reinterpret_cast<const float *>(base + s * WM * S::STAGES * S::STAGE);
                 st[s] = reinterpret_cast<const float4 *>(of + SHARED_ROWS * S::PITCH)[in_warp];
                 const Frame f{st[s].x, st[s].y, st[s].z};
-                if (f.less(m) > 0.0f) m = f;
+                if (f.less<S::NARROW>(m) > 0.0f) m = f;
             }
 #pragma unroll
             for (int s = 0; s < STREAMS; ++s) {
                 const float *of = reinterpret_cast<const float *>(base + s * WM * S::STAGES * S::STAGE) + in_warp * S::PITCH + d;
                 const Frame f{st[s].x, st[s].y, st[s].z};
-                const float w = weight(f, st[s].w, m);
-                l += R::weighed(f, st[s].w, m);
+                const float w = R::template weight<S::NARROW>(f, st[s].w, m);
+                l += R::template weighed<S::NARROW>(f, st[s].w, m, w);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] += of[e] * w;
             }

@@ -14,7 +14,7 @@ int32_t launch_attend_as(const CacheDev &c, AttendArgs a, int64_t most_tiles, cu
     static std::atomic<uint64_t> done{0};
     WG_CUDA(set_once(done, kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM));
     using A = Attend<KV, DP, SHARED_WARPS, GROUPED, NTS, NT>;
-    a.grouped = GROUPED, a.warp_rows = A::WARP_ROWS, a.shared_rows_each = A::ROWS;
+    a.grouped = GROUPED, a.origins = S::NARROW, a.warp_rows = A::WARP_ROWS, a.shared_rows_each = A::ROWS;
     a.shared_row_blocks = SHARED_WARPS == 0 ? 0 : GROUPED ? (a.group * a.rows + A::ROWS - 1) / A::ROWS : a.row_blocks;
     if (GROUPED) {
         WG_CUDA(launch_pdl(attend_plan_kernel, dim3((unsigned)a.n_groups), dim3(ATTEND_THREADS), st, c, a));
