@@ -759,15 +759,15 @@ int32_t wg_kv_read(const wg_kv_cache *cache, const int32_t *table, int64_t table
  * g = h / (n_q_heads / n_heads) and k[i], v[i] the values that the cache holds for head g at position i:
  *   x[i] = scale * (q . k[i]);  lse = log sum of exp(x[i]);  out = sum of exp(x[i] - lse) v[i]
  * in fp32, one rounding at the end; the weights exp(x[i] - max) enter the second product in the cache's 16-bit type (8-bit
- * caches: fp16).  Positions whose table entry is no block of the cache are passed over.  A token that sees nothing (no
+ * caches: fp16, times the scales of values; queries are fp16 there too, less a power of two).  Positions whose table entry is no block of the cache are passed over.  A token that sees nothing (no
  * row, all passed over, or all scores -inf) has out = 0, lse = -inf; a NaN or +inf among its scores makes them NaN.  Infinite and NaN
  * values (and scales of values) are in out, not in lse.
  * Nothing that a token does not see has an effect on it, NaN included.
  *
  * The work is dealt out evenly over the GPU by the lengths as they are, each long row to several blocks; their parts are
- * joined in the order of positions, so results do not depend on the order in which blocks run.  The lengths may change
- * between replays of a recorded call.  Made for one or a few tokens a sequence: every token of a long prompt would read all of
- * it again (wg_kv_read gives other attention kernels dense keys and values).
+ * joined in an order that the lengths decide (and, of what a group shares, its tables): results do not depend on the order in
+ * which blocks run.  The lengths may change between replays of a recorded call.  Made for one or a few tokens a sequence:
+ * every token of a long prompt would read all of it again (wg_kv_read gives other attention kernels dense keys and values).
  *
  * A wg_attend is scratch for up to max_tokens tokens a call; calls that share one are issued like calls that share a
  * wg_ctx: one at a time, on one stream or on streams ordered by events (recorded calls too).

@@ -28,7 +28,7 @@ int32_t launch_join_by(const CacheDev &c, const AttendArgs &a, cudaStream_t st) 
 }
 
 // A block per row where there are few rows, or few pairs, which then have many parts each; else a warp.  (32 x 4096 positions, 1024
-// rows: 76.9 us with blocks, 77.9 with warps; 128 x 128, 4096 rows: 28.1 and 22.3; 24 x 4 drafted tokens, 96 pairs: 32 and 39.)
+// rows: 74.8 us with blocks, 76.6 with warps; 128 x 128, 4096 rows: 26.5 and 22.7; 24 x 4 drafted tokens, 96 pairs: 28 and 31.)
 template <int DP>
 int32_t launch_join(const CacheDev &c, const AttendArgs &a, cudaStream_t st) {
     if ((int64_t)a.n_tokens * a.n_q_heads <= (int64_t)sm_count() * 8 || (int64_t)a.n_groups * c.n_heads <= sm_count())

@@ -5,7 +5,7 @@
 // units of a call, in order of tokens and heads, are dealt out in equal contiguous shares, whatever the lengths, to
 // warps that work by themselves, or, of pairs that several warps work on together (few pairs; positions that a group of tokens has in
 // common), to blocks.  A pair that was cut between shares is joined by a kernel that follows, from partial results in scratch,
-// always in the order of positions.
+// in an order that the lengths (and, of what a group shares, its tables) decide alone.
 //
 // A warp has a ring of tiles of its own, filled with cp.async, and the usual running maximum and sum: for x =
 // scale q.k and the maximum m so far, p = 2^(x - m), l = sum of p, o = sum of p v, all multiplied by 2^(m_old - m) when m
@@ -612,6 +612,8 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
             const float m = run.m[nt][c];
             base[nt][c] = m == NEG_INFINITY ? 0.0f : S::NARROW ? m - S::UP : m;
         }
+    // Weights go into the second product in its type: off by half a step of it (bf16 2^-8, fp16 2^-11; fp32 ones would take two products
+    // each), which the many positions that make up a row mostly even out.  The sum takes them as they were, so that it is exact to fp32.
     uint32_t p[S::SUBS][NT][2];
     const auto weigh = [&](auto some_odd) {
         constexpr bool ODD = decltype(some_odd)::value;
@@ -799,8 +801,8 @@ struct Results {
     }
 };
 
-// WARPS warps per row; those that were not cut are stored already.  A row's partial results are joined in the order of positions,
-// and asked for all at once where they are not more than AHEAD.  Latencies: 2 to 5 us, of which a launch is one.  (In
+// WARPS warps per row; those that were not cut are stored already.  A row's partial results are asked for AHEAD at a time and joined
+// in a fixed order: by eights, every WARPS-th eight by a warp, and then the warps.  Latencies: 2 to 5 us, of which a launch is one.  (In
 // the first kernel, by whichever warp is the last to be done with a token, the same took 6.5 us at the end of all others,
 // most of it on an atomic's way and back, and its registers cost the loops theirs.)
 template <int DP, int WARPS, bool ORIGINS>
@@ -1412,10 +1414,11 @@ __device__ __forceinline__ int64_t sums_before(int64_t n, int64_t &total, int64_
 }
 
 // What it measured (with the join behind it; from memory, 32 query and 8 key heads of 128): 32 tokens of 4096 positions, bf16: 75 us,
-// 5.9 TB/s, 0.90 of a copy's rate, of which the start to the first tile takes 6 us and the end 6; 64 of 16384, e4m3: 283 to 295 us,
-// 6.2 to 6.4 TB/s; one of 1000: 8.7 us; 32 x 8 beams of 1800 that share their prompts: 82 to 84 us, 3.5 TB/s.  The tensor pipe is
-// busy for 9 to 18 % of the time, and issue slots are taken to a quarter (16 bits) and to a half (8 bits: 647 instructions a tile).
-// Two blocks of four warps on an SM: 210 to 255 registers, three stages of 8 KB a warp.  Three blocks of 168 registers with two
+// 5.9 TB/s, 0.90 of a copy's rate, of which the start to the first tile takes 6 us and the end 6; 64 of 16384, e4m3: 284 to 297 us,
+// 6.1 to 6.4 TB/s (in long runs, at a lower clock, 305 to 330); one of 1000: 8.5 us; 32 x 8 beams of 1800 that share their prompts: 83 to 87 us, 3.4 TB/s.  The tensor pipe is
+// busy for 9 to 18 % of the time, and issue slots are taken to a quarter (16 bits) and to a half (8 bits: 680 instructions a tile).
+// Two blocks of four warps on an SM: 210 to 255 registers, three stages of 8 KB a warp.  With head sizes above 128 one block, and
+// registers do not suffice for groups, nor for more than 8 rows of a key head: 216 to 1824 bytes of a thread are spilled and loaded.  Three blocks of 168 registers with two
 // stages: 492 us instead of 283; tiles of 16 positions in 8-bit caches: 369.
 template <typename KV, int DP, int SHARED_WARPS, bool GROUPED, int NTS, int NT>
 __global__ void __launch_bounds__(ATTEND_THREADS, Shape<KV, DP>::BLOCKS)

@@ -32,8 +32,8 @@ template <typename KV, int DP>
 int32_t launch_attend_wide(const CacheDev &c, const AttendArgs &a, int64_t most_tiles, cudaStream_t st) {
     if (a.group == 1 && a.rows <= 16) {
         // Few (token, key head) pairs: a block works on one at a time, its warps side by side.  Many: every warp by itself.  (16-bit
-        // caches, 256 pairs of 4096 positions: 74.3 and 75.5 us; 512 of 500: 29.0 and 29.9; 64 of 500: 11.2 and 13.4.  8-bit ones,
-        // 128 pairs of 16384: 91 and 81; 64: 46.1 and 45.4.)
+        // caches, 256 pairs of 4096 positions: 74.6 and 75.2 us; 512 of 500: 28.6 and 29.7; 64 of 500: 9.7 and 13.2.  8-bit ones,
+        // 128 pairs of 16384: 93 and 83; 64: 46.2 and 45.8.)
         const bool few = (int64_t)a.n_tokens * c.n_heads < (Shape<KV, DP>::NARROW ? 128 : 4 * sm_count());
         if (a.rows <= 8)
             return few ? launch_attend_as<KV, DP, 1, false, 1, 1>(c, a, most_tiles, st) : launch_attend_as<KV, DP, 0, false, 1, 1>(c, a, most_tiles, st);
