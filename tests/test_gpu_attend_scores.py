@@ -3,6 +3,7 @@
 Queries and keys have one dimension that is not 0 and holds few bits, so that every dot product is exact in fp32.  Scores
 then differ by 0 or by so much that a row's result is the mean of the values at its largest score: a case of few roundings."""
 import math
+import sys
 
 import pytest
 import torch
@@ -194,3 +195,24 @@ def test_keys_of_zeros_beside_the_largest_queries(wg, held):
     mass = ref.held(v, vs)[0, :, 0].abs().mean(0)
     assert ((out.cpu().double() - mean).abs() <= mean.abs() * 2.0 ** -8 + mass * (2.0 ** -11 + 2.0 ** -18)).all()
     assert (lse.cpu().double() - math.log(16)).abs().max() < 1e-5
+
+
+@pytest.mark.parametrize("held,model", TYPES)
+@pytest.mark.parametrize("dim", [80, 128, 256])
+@pytest.mark.parametrize("rows", [4, 12, 20])
+def test_large_scores_at_other_head_sizes(wg, held, model, dim, rows, monkeypatch):
+    monkeypatch.setattr(sys.modules[__name__], "D", dim)
+    for share, n_keys in ((False, 8), (True, 8), (False, 1)):
+        s = Far(wg, [1, 40, 300, 1200], held, model, 1.2e7, 1, n_keys, rows, seed=dim, share=share)
+        s.check()
+        s.check(4)
+
+
+@pytest.mark.parametrize("held,model", [(BF16, BF16), (FP16, FP16), (E4M3, BF16), (INT8, FP16)])
+@pytest.mark.parametrize("window", [1, 16, 50])
+@pytest.mark.parametrize("new", [2, 5])
+def test_drafted_tokens_under_a_window(wg, held, model, window, new):
+    from test_gpu_attend import Setup
+    s = Setup(wg, [1, 0, 2, 17, 64, 130, 300], 8, 2, 64, held, model, seed=new, new=new).on_gpu()
+    for group in (1, new):
+        s.check(s.run(window=window, group=group), window)

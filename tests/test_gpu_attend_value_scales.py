@@ -222,3 +222,54 @@ def test_scales_of_one(wg, held):
         s.on_gpu()
         for group in (1, 5):
             s.check(s.run(group=group))
+
+
+def any_scales(s, seed):
+    """Scales of values from 2^-100 to 2^60, some 1, some of those with zeros; keys a hundred times as large in one sequence."""
+    g = ref.generator(seed)
+    s.vs = torch.exp2(torch.randint(-100, 61, s.vs.shape, generator=g).float()) * s.vs.clamp(0.5, 2.0)
+    s.vs[torch.rand(s.vs.shape, generator=g) < 0.3] = 1.0
+    s.v.view(torch.uint8)[(s.vs == 1) & (torch.rand(s.vs.shape, generator=g) < 0.5)] = 0
+    for c in range(s.table.shape[1]):
+        if s.table[3, c] >= 0:
+            s.ks[s.table[3, c]] *= 100.0
+
+
+@pytest.mark.parametrize("held,model", [(E4M3, BF16), (INT8, BF16)])
+@pytest.mark.parametrize("D", [80, 128, 256])
+@pytest.mark.parametrize("rows", [4, 12, 20])
+def test_unusual_tiles_at_other_head_sizes(wg, held, model, D, rows):
+    """Single tokens of few and of many sequences, drafted tokens, and beams that share a block."""
+    some = [1, 40, 0, 500, 90]
+    for lens, new, share in ((some, 1, None), ([1 + i % 70 for i in range(40)] * 2, 1, None), (some, 3, None), (some, 1, same_tables(some))):
+        s = Setup(wg, lens, 2 * rows, 2, D, held, model, seed=D, new=new, share=share)
+        any_scales(s, D + rows)
+        s.on_gpu()
+        few = torch.arange(0, s.q.shape[0], 1 if len(lens) == 5 else 11)
+        got = {group: s.run(group=group) for group in ((1,) if len(lens) > 5 else (1, 5, new))}
+        s.q, s.seq, s.pos = s.q[few], s.seq[few], s.pos[few]
+        want, want_lse, mass, size = s.want()
+        tol, tol_lse = ref.tolerance(want, mass, size, (s.pos + 1).clamp(min=1), D, model, FP16, s.vs)
+        tol = tol + lost(s)
+        seen = s.pos >= 0
+        for out, lse in got.values():
+            off = (out[few].double() - want).abs()
+            assert (off <= tol).all(), ((off / tol).max().item(), int((off > tol).sum()))
+            assert ((lse[few].double() - want_lse)[seen].abs() <= tol_lse[seen]).all() and (lse[few][~seen] == -math.inf).all()
+
+
+@pytest.mark.parametrize("held,model", [(E4M3, BF16), (INT8, FP16)])
+@pytest.mark.parametrize("D", [128, 256])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_values_without_a_number_at_other_head_sizes(wg, held, model, D, bad):
+    """Beams that share a block and end at different places before, at and behind one without a number."""
+    lens = [70, 75, 79, 72, 0, 40]
+    s = Setup(wg, lens, 8, 2, D, held, model, seed=33, share=same_tables(lens))
+    clean = Setup(wg, lens, 8, 2, D, held, model, seed=33, share=same_tables(lens)).on_gpu()
+    s.vs[int(s.table[2, 4]), 73 - 64] = bad
+    s.on_gpu()
+    for group in (1, 2, 6):
+        (out, lse), (want, want_lse) = s.run(group=group), clean.run(group=group)
+        assert torch.equal(out[[0, 3, 4, 5]], want[[0, 3, 4, 5]]) and torch.equal(lse[[0, 3, 4, 5]], want_lse[[0, 3, 4, 5]])
+        assert not torch.isfinite(out[[1, 2]]).any()
+        check_lse(s, lse)
