@@ -21,9 +21,9 @@
 // simply multiply p, which then might fall below fp16's range while it matters: with x' = x + log2 s and the maximum m taken
 // over x', p' = 2^(x' - m) is at most 1 and largest where the result comes from, and l is the sum of 2^(x - m), held 2^12 times as
 // large: beside a scale of 2^121, the largest that is written, it has weights down to 2^-17 of the largest, beside 2^100 down to 2^-38.
-// For m, scales below 2^-96 count as that, which keeps l below 2^108 times the number of positions (all of them below that, and 2^20 of
-// them, are too much), and so do infinities and NaN: the rest of such a scale, or what it is, is put into p' where a tile has some, and
-// the sum, which has no values in it, goes without.
+// For m, scales below 2^-96 count as that, which keeps l below 2^108 a position (where a lane's share of it passes 2^112, m is raised by 8),
+// and so do infinities and NaN: the rest of such a scale, or what it is, is put into p' where a tile has some, and the sum, which has no
+// values in it, goes without.
 // A vector that was written as zeros has the scale 1 and yet no part in the result: where one would raise the maximum it counts as 2^-96 too.
 //
 // Scores of any size.  A score of 10^7 is rounded to whole numbers in fp32, and so would be x less a rounded maximum, or log2 s
@@ -517,7 +517,7 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
                 base[nt][c] = m;
-                grew |= m > run.m[nt][c];
+                grew |= m > run.m[nt][c] || (S::NARROW && run.l[nt][c] > 0x1p112f);
             }
     };
     maxima();
@@ -580,6 +580,18 @@ __device__ __forceinline__ bool take_tile(Running<Shape<KV, DP>, NT> &run, const
                     }
                 }
             if (__any_sync(0xFFFFFFFFu, moved)) return false;
+        }
+        // (lanes of a row have shares of their own, but one maximum)
+        if constexpr (S::NARROW) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float l = run.l[nt][c];
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) l = fmaxf(l, __shfl_xor_sync(0xFFFFFFFFu, l, d));
+                    if (l > 0x1p112f) base[nt][c] += 8.0f;
+                }
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {

@@ -273,3 +273,35 @@ def test_values_without_a_number_at_other_head_sizes(wg, held, model, D, bad):
         assert torch.equal(out[[0, 3, 4, 5]], want[[0, 3, 4, 5]]) and torch.equal(lse[[0, 3, 4, 5]], want_lse[[0, 3, 4, 5]])
         assert not torch.isfinite(out[[1, 2]]).any()
         check_lse(s, lse)
+
+
+@pytest.mark.parametrize("held", [E4M3, INT8])
+@pytest.mark.parametrize("exponent", [None, -93, -99])
+@pytest.mark.parametrize("n", [1 << 17, (1 << 21) + 5, 1 << 27])
+def test_very_many_values_of_next_to_nothing(wg, held, exponent, n):
+    """Zeros (None) or vectors of about 2^exponent at every position, the same block over and over: the scores' sum counts them all."""
+    block, H, D, cols = 1 << 16, 1, 16, -(-n // (1 << 16))
+    g = ref.generator(12)
+    v = torch.zeros((block, H, D)) if exponent is None else torch.randn((block, H, D), generator=g) * 2.0 ** exponent
+    k = torch.zeros((block, H, D))
+    cache = wg.KvCache(*(torch.zeros((1, block, H, D), dtype=held, device="cuda") for _ in range(2)),
+                       *(torch.ones((1, block, H), device="cuda") for _ in range(2)))
+    slots = wg.SlotMap(1, block)
+    slots.slot.copy_(torch.arange(block))
+    cache.write(k.to(BF16).cuda(), v.to(BF16).cuda(), slots)
+    pool = wg.KvPool(1, block, 3)
+    lens = [n, 1000, 0]
+    tables = wg.KvTables(pool, torch.zeros((3, cols), dtype=torch.int32, device="cuda"), torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    q = torch.randn((3, 4, D), generator=g).to(BF16).cuda()
+    held_v = ref.held(*ref.codes_of(v.to(BF16), held))[:, 0]
+    attend = wg.Attend(3, 4, H, D)
+    for group in (1, 3):
+        out, lse = torch.full_like(q, 7.0), torch.full((3, 4), 7.0, device="cuda")
+        attend(q, cache, tables, out, lse=lse, group=group)
+        for s, m in enumerate(lens):
+            want = (held_v.sum(0) * (m // block) + held_v[:m % block].sum(0)) / max(m, 1)
+            mass = (held_v.abs().sum(0) * (m // block) + held_v[:m % block].abs().sum(0)) / max(m, 1)
+            # weights of 2^3 and less in fp16 of fp32 sums of some hundred thousand terms each
+            rel = ref.half_step(FP16) + 2.0 ** 18 * 2.0 ** -23 * (m > 1000) + 2.0 ** -13
+            assert ((out[s].cpu().double() - want).abs() <= want.abs() * 2.0 ** -8 + mass * rel + 2.0 ** -133).all()
+            assert ((lse[s].cpu().double() - (math.log(m) if m else -math.inf)).abs() <= 2.0 ** 18 * 2.0 ** -23).all() if m else (lse[s] == -math.inf).all()
